@@ -33,7 +33,8 @@
  *   - Tiles: [n x tile_elems] contiguous, each tile row-major over ALL the
  *     operand's labels in string order, with extent t_l for a promoted label
  *     and the full extent for a demoted one.  Inputs are fp32 or bf16 (raw
- *     bits, uint16).  Accumulation is fp32; W tiles are fp32, or bf16 bits
+ *     bits, uint16), or for a TRE_MXFP4 plan [n x tre_tile_bytes] of 4-bit
+ *     tiles in the layout given at tre_dtype.  Accumulation is fp32; W tiles are fp32, or bf16 bits
  *     rounded to nearest even from the fp32 sums when the plan was made with
  *     the w_bf16 option (tre_plan_info.w_dtype says which).  Tile arrays
  *     start on a 16-byte boundary (TRE_E_ARG otherwise).
@@ -68,7 +69,19 @@ typedef enum {
     TRE_E_STATE = 12      /* join result does not belong to this plan / workspace */
 } tre_status;
 
-typedef enum { TRE_F32 = 0, TRE_BF16 = 1 } tre_dtype;
+/* TRE_MXFP4: microscaled 4-bit floating point (the OCP MX format with E2M1
+ * elements).  32 values of the contracted index share a scale 2^e, stored as
+ * the byte e + 127, and each is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it, or
+ * its negative (codes 0 .. 7, sign in bit 3); scale byte 255: all 32 are NaN.
+ * A tile of R rows (the operand's labels that W keeps, in W's order, the ones
+ * both operands have first) and K contracted values (their labels in U's
+ * order) is
+ *     codes  [R][B][16 bytes]  value 2 i of a block in the low half of byte i
+ *     scales [R][B]
+ * with B blocks to a row: 1 for K <= 32, 2 for K <= 64, else 4 ceil(K / 128)
+ * (values past K are zero), padded to a multiple of 16 bytes.
+ * tre_mx_quantize writes such tiles, tre_tile_bytes gives their size. */
+typedef enum { TRE_F32 = 0, TRE_BF16 = 1, TRE_MXFP4 = 2 } tre_dtype;
 
 typedef struct tre_plan_s *tre_plan_t;
 
@@ -102,7 +115,7 @@ typedef struct {
     int32_t n_join;           /* promoted labels shared by U and V */
     int32_t kernel_class;     /* 0 = MFMA tile GEMM, 1 = vector (scale / GEMV / dot), 2 = MFMA GEMM with
                                  128x128 blocks and direct-to-LDS copies (bf16 with K a multiple of 64,
-                                 fp32 with K a multiple of 32) */
+                                 fp32 with K a multiple of 32), 3 = scaled MFMA on 4-bit tiles (TRE_MXFP4) */
     int64_t batch, m, n, k;   /* per-pair contraction: W[b,m,n] += sum_k U[b,m,k] V[b,k,n] */
     int64_t flops_per_pair;   /* 2 * batch * m * n * k */
     char key_labels[3][27];   /* promoted labels of U, V, W in key order (NUL-terminated) */
@@ -147,7 +160,7 @@ typedef struct {
     void *events[4];          /* library-owned while pending */
     int32_t contract_path;    /* out: the contraction launch tre_contract chose: 0 generic MFMA GEMM (64x64
                                  blocks), 1 vector class, 2 128x128 MFMA path, 3 the same as a paced
-                                 persistent grid, 4 the same with U-range units (partials summed after) */
+                                 persistent grid, 4 the same with U-range units (partials summed after), 5 4-bit tiles */
     int32_t join_path;        /* out (tre_join, tre_execute3): 0 driven by U (runs searched in V), 1 driven by V (runs
                                  searched in U), 2 driven by V with at most one U tuple each, 3 driven by V
                                  over a U holding every key (no search), 4 keyless one-tuple V with W keyed by
@@ -163,16 +176,25 @@ typedef struct {
  *   extent : host [26], indexed by letter - 'a'; >= 1 for used labels.
  *   tile   : host [26]; for a promoted label 1 <= t <= extent and extent % t == 0;
  *            ignored for demoted labels (their tile extent is the full extent).
- *   in_dtype : a tre_dtype value, TRE_F32 or TRE_BF16, for both inputs (passed
- *            as int32 so that any other value is a defined TRE_E_DTYPE);
- *            accumulation is fp32 and W is fp32 unless opt->w_bf16 asks for
- *            bf16 output.
+ *   in_dtype : a tre_dtype value, TRE_F32, TRE_BF16 or TRE_MXFP4, for both
+ *            inputs (passed as int32 so that any other value is a defined
+ *            TRE_E_DTYPE); accumulation is fp32 and W is fp32 unless
+ *            opt->w_bf16 asks for bf16 output (any TRE_MXFP4 plan takes it).
+ *            TRE_MXFP4: every label that is summed inside a tile (its tile
+ *            extent above 1) must be in both inputs, and an input's tile stay
+ *            below 2^31 bytes (TRE_E_SHAPE otherwise).  The products of 4-bit
+ *            values are exact, their sums fp32 on the matrix cores: sums and
+ *            products below 2^-126 in magnitude count as zero.
  *   opt    : host, may be NULL for defaults.
  *   out    : receives a host-owned, immutable plan; thread-safe to share. */
 tre_status tre_plan(const char *einsum, const char *upper, const int64_t *extent, const int32_t *tile,
                     int32_t in_dtype, const tre_options *opt, tre_plan_t *out);
 
 tre_status tre_plan_get_info(tre_plan_t plan, tre_plan_info *info);
+
+/* Bytes of one tile of operand 0 (U), 1 (V) or 2 (W) as the entry points take
+ * it (host only; -1 on a null plan or another operand). */
+int64_t tre_tile_bytes(tre_plan_t plan, int32_t operand);
 
 void tre_plan_destroy(tre_plan_t plan);
 
@@ -445,6 +467,79 @@ tre_status tre_execute3(const char *einsum, const char *upper, const int64_t *ex
  * address distinct positions (else the last writer is unspecified). */
 tre_status tre_tiles_from_entries(const int64_t *slot, const int64_t *offset, const void *value, int64_t n_entries,
                                   int32_t elem_bytes, void *tiles, int64_t n_tiles, int64_t tile_elems, void *stream);
+
+/* --- tiles in 4 bits ------------------------------------------------------ */
+
+/* tre_mx_quantize -- the tiles of operand 0 (U) or 1 (V) of a TRE_MXFP4 plan in
+ * 4 bits, laid out as the plan's contraction reads them: blocks of 32 run along
+ * the labels that the EinSum contracts, wherever these stand in the operand's
+ * string (so the transposed use of a matrix, as in a gradient, is its
+ * quantisation for another plan).
+ * With m the largest magnitude of a block, e = floor(log2 m) - 2, at least
+ * -127 (an m below 2^-125 or zero has that too), and a value x becomes the
+ * nearest of the eight magnitudes to |x| / 2^e, ties to the even code, at most
+ * 6, with x's sign.  A block with a NaN or an infinity gets scale byte 255.
+ *   tiles     : device [n x tile_elems] fp32 or bf16 (src_dtype TRE_F32 or
+ *               TRE_BF16), row-major over the operand's labels as for tre_plan.
+ *   mx_tiles  : device [n x tre_tile_bytes(plan, operand)], written whole.
+ * Both arrays 16-byte aligned and disjoint.  TRE_E_DTYPE for another plan or
+ * source type.  Asynchronous on the stream; no workspace, so it may be captured
+ * into a graph. */
+tre_status tre_mx_quantize(tre_plan_t plan, int32_t operand, const void *tiles, int32_t src_dtype, int64_t n,
+                           void *mx_tiles, void *stream);
+
+/* tre_mx_dequantize -- the reverse: tiles [n x tile_elems] in fp32 or bf16
+ * (dst_dtype; every value has at most two significant bits, so both are exact)
+ * from 4-bit tiles. */
+tre_status tre_mx_dequantize(tre_plan_t plan, int32_t operand, const void *mx_tiles, int64_t n, void *tiles,
+                             int32_t dst_dtype, void *stream);
+
+/* --- rows of a table by token --------------------------------------------- */
+
+/* tre_lookup -- out[t] = scale * table[id[t]]: the join of a list of tokens
+ * with a table that holds every key of its promoted label (Sec. 5), in one
+ * pass, each value rounded once.
+ *   table   : device [n_rows x row_elems] of table_dtype (TRE_F32, TRE_BF16), or
+ *             TRE_MXFP4: the n_rows / tile_rows tiles of tile_rows rows of
+ *             row_elems contracted values, row i in tile i / tile_rows, as
+ *             tre_mx_quantize lays out an operand whose only kept label is the
+ *             token's -- the tiles that a product with the same table reads.
+ *             (tile_rows is ignored for the other types.)
+ *   ids     : device [n_ids] int32 or int64 (id_bytes 4 or 8), in any order.  A
+ *             negative one stands for no token: its row of `out` is zero.  One
+ *             of n_rows or more reads nothing either, gives a zero row, and sets
+ *             `status`.
+ *   out     : device [n_ids x row_elems] of out_dtype (TRE_F32 or TRE_BF16).
+ *   status  : device int64 or NULL; set to TRE_E_KEYRANGE where an id is n_rows
+ *             or more, else left as it is.
+ * Arrays 16-byte aligned, `out` apart from the inputs.  At most 2^31 - 2 rows
+ * and ids, 2^30 elements (TRE_E_SHAPE).  Asynchronous on the stream; no
+ * workspace, so it may be captured into a graph. */
+tre_status tre_lookup(const void *table, int32_t table_dtype, int64_t n_rows, int64_t row_elems, int64_t tile_rows,
+                      const void *ids, int32_t id_bytes, int64_t n_ids, float scale, void *out, int32_t out_dtype,
+                      int64_t *status, void *stream);
+
+/* tre_lookup_grad -- the gradient of tre_lookup by its table: the rows of `grad`
+ * summed by token (the GROUP BY sum of Sec. 5),
+ *   table_grad[v] = scale * sum over t with id[t] = v of grad[t],
+ * the sums in fp32 in an order that the ids alone determine (no atomics on
+ * values: the same call gives the same bits), each result rounded once.
+ *   grad       : device [n_ids x row_elems] of grad_dtype (TRE_F32, TRE_BF16).
+ *   ids        : as for tre_lookup; negative ones add to no row, nor do those of
+ *                n_rows or more, which set `status`.
+ *   table_grad : device [n_rows x row_elems] of out_dtype (TRE_F32, TRE_BF16),
+ *                written whole, with zeros where no token falls; with
+ *                `accumulate` non-zero the sums are added to it instead and
+ *                rows without a token are left as they are.
+ *   ws, ws_bytes: device workspace, 256-byte aligned, at least
+ *                tre_lookup_grad_workspace_bytes(...) (0 on bad sizes); holds
+ *                nothing between calls.  Calls that overlap need one each.
+ * Arrays 16-byte aligned and disjoint.  Asynchronous on the stream; may be
+ * captured into a graph. */
+size_t tre_lookup_grad_workspace_bytes(int64_t n_ids, int64_t n_rows, int64_t row_elems);
+tre_status tre_lookup_grad(const void *grad, int32_t grad_dtype, const void *ids, int32_t id_bytes, int64_t n_ids,
+                           float scale, void *table_grad, int32_t out_dtype, int64_t n_rows, int64_t row_elems,
+                           int32_t accumulate, int64_t *status, void *ws, size_t ws_bytes, void *stream);
 
 /* --- errors -------------------------------------------------------------- */
 const char *tre_status_str(tre_status s);

@@ -33,6 +33,7 @@ int64_t blocks_per_unit(const Plan& p) {
         const int64_t bm = 32 * p.tile_m, bn = 32 * p.tile_n;
         return p.nB * ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
     }
+    if (p.kclass == KC_MX) return mx_blocks_per_unit(p);
     return (p.tile_elems[2] + 255) / 256;
 }
 
@@ -92,7 +93,7 @@ int32_t choose_pacing(const Plan& p, int64_t n_u, int64_t n_pairs, int64_t n_w, 
 // Workgroups one unit occupies: its output blocks (GEMM), or its threads /
 // 256 for the vector class (several small units share a workgroup).
 double unit_workgroups(const Plan& p) {
-    if (p.kclass == KC_GEMM) return double(blocks_per_unit(p));
+    if (p.kclass != KC_VEC) return double(blocks_per_unit(p));
     const int64_t threads = p.vec_dot ? p.tile_elems[2] * 16 : (p.tile_elems[2] + p.vec_ept - 1) / p.vec_ept;
     if (threads > 128) return double((threads + 255) / 256);
     int64_t t = 1;
@@ -117,7 +118,7 @@ int64_t choose_unit(const Plan& p, const Layout& L, int64_t n_pairs, int64_t n_w
         pu = p.opt.max_pairs_per_unit;
     } else if (p.kclass == KC_GEMM && !p.fast) {
         pu = tile_unit_pairs(p, n_pairs, n_w);
-    } else if (double(n_w) * uw >= kTargetWorkgroups || (p.kclass == KC_GEMM && double(n_w) * uw >= fill)) {
+    } else if (double(n_w) * uw >= kTargetWorkgroups || (p.kclass != KC_VEC && double(n_w) * uw >= fill)) {
         pu = std::max<int64_t>(n_pairs, 1);  // enough output blocks: one unit per key
     } else {
         pu = std::max<int64_t>(4, int64_t(std::ceil(double(n_pairs) * uw / kTargetWorkgroups)));
@@ -389,7 +390,7 @@ tre_status contract_enqueue(tre_plan_t plan, const tre_join_result* jr, int64_t 
         return dev_fail(e, "outputs");
     tm.mark(s);
     if (timing) {
-        timing->contract_path = pace ? 3 : R > 1 ? 4 : (p.kclass == KC_VEC ? 1 : p.fast ? 2 : 0);
+        timing->contract_path = pace ? 3 : R > 1 ? 4 : p.kclass == KC_VEC ? 1 : p.kclass == KC_MX ? 5 : p.fast ? 2 : 0;
         if (deferred) {
             if (ke.launched) {
                 timing->events[0] = reinterpret_cast<void*>(ke.start);
@@ -633,6 +634,133 @@ tre_status tre_scale_f32(const float* x, float* y, int64_t n, float scale, void*
     }
     hipError_t e = launch_scale(x, y, n, scale, reinterpret_cast<hipStream_t>(stream));
     return e == hipSuccess ? TRE_OK : dev_fail(e, "scale");
+}
+
+namespace {
+
+tre_status mx_args(tre_plan_t plan, int32_t operand, const void* tiles, int32_t dtype, int64_t n, const void* mx_tiles,
+                   const char* where) {
+    if (!plan || n < 0 || (operand != 0 && operand != 1) || (n > 0 && (!tiles || !mx_tiles))) {
+        set_error(std::string(where) + ": null plan or array, negative size or no such operand");
+        return TRE_E_ARG;
+    }
+    if (plan->p.dtype != TRE_MXFP4) {
+        set_error(std::string(where) + ": the plan's tiles are not TRE_MXFP4");
+        return TRE_E_DTYPE;
+    }
+    if (dtype != TRE_F32 && dtype != TRE_BF16) {
+        set_error(std::string(where) + ": unquantised tiles must be TRE_F32 or TRE_BF16");
+        return TRE_E_DTYPE;
+    }
+    if ((reinterpret_cast<uintptr_t>(tiles) | reinterpret_cast<uintptr_t>(mx_tiles)) & 15) {
+        set_error(std::string(where) + ": tile arrays must be 16-byte aligned");
+        return TRE_E_ARG;
+    }
+    if (n >= INT32_MAX) {
+        set_error(std::string(where) + ": more than 2^31 - 1 tiles");
+        return TRE_E_SHAPE;
+    }
+    return TRE_OK;
+}
+
+}  // namespace
+
+tre_status tre_mx_quantize(tre_plan_t plan, int32_t operand, const void* tiles, int32_t src_dtype, int64_t n,
+                           void* mx_tiles, void* stream) {
+    const tre_status st = mx_args(plan, operand, tiles, src_dtype, n, mx_tiles, "tre_mx_quantize");
+    if (st != TRE_OK || n == 0) return st;
+    const hipError_t e =
+        launch_mx_quantize(plan->p, operand, tiles, src_dtype, n, mx_tiles, reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TRE_OK : dev_fail(e, "mx_quantize");
+}
+
+tre_status tre_mx_dequantize(tre_plan_t plan, int32_t operand, const void* mx_tiles, int64_t n, void* tiles,
+                             int32_t dst_dtype, void* stream) {
+    const tre_status st = mx_args(plan, operand, tiles, dst_dtype, n, mx_tiles, "tre_mx_dequantize");
+    if (st != TRE_OK || n == 0) return st;
+    const hipError_t e =
+        launch_mx_dequantize(plan->p, operand, mx_tiles, n, tiles, dst_dtype, reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TRE_OK : dev_fail(e, "mx_dequantize");
+}
+
+namespace {
+
+// Sizes of a table that the row entry points take: offsets in bytes and the
+// launches' wavefronts stay within 63 bits.
+bool rows_ok(int64_t n_ids, int64_t n_rows, int64_t elems) {
+    return n_ids >= 0 && n_ids < INT32_MAX && n_rows >= 1 && n_rows < INT32_MAX && elems >= 1 && elems <= (int64_t(1) << 30);
+}
+
+}  // namespace
+
+tre_status tre_lookup(const void* table, int32_t table_dtype, int64_t n_rows, int64_t row_elems, int64_t tile_rows,
+                      const void* ids, int32_t id_bytes, int64_t n_ids, float scale, void* out, int32_t out_dtype,
+                      int64_t* status, void* stream) {
+    if (table_dtype != TRE_F32 && table_dtype != TRE_BF16 && table_dtype != TRE_MXFP4) {
+        set_error("tre_lookup: table_dtype must be TRE_F32, TRE_BF16 or TRE_MXFP4");
+        return TRE_E_DTYPE;
+    }
+    if (out_dtype != TRE_F32 && out_dtype != TRE_BF16) {
+        set_error("tre_lookup: out_dtype must be TRE_F32 or TRE_BF16");
+        return TRE_E_DTYPE;
+    }
+    const bool mx = table_dtype == TRE_MXFP4;
+    if (!rows_ok(n_ids, n_rows, row_elems) || (mx && (tile_rows < 1 || tile_rows > n_rows || n_rows % tile_rows))) {
+        set_error("tre_lookup: size out of range, or tile_rows does not divide n_rows");
+        return TRE_E_SHAPE;
+    }
+    if (mx && mx_tile_bytes(tile_rows, row_elems) > INT32_MAX) {
+        set_error("tre_lookup: 4-bit tile larger than 2^31 - 1 bytes");
+        return TRE_E_SHAPE;
+    }
+    if (n_ids == 0) return TRE_OK;
+    if (!table || !ids || !out || (id_bytes != 4 && id_bytes != 8)) {
+        set_error("tre_lookup: null array, or ids of neither 4 nor 8 bytes");
+        return TRE_E_ARG;
+    }
+    if ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(out)) & 15 ||
+        reinterpret_cast<uintptr_t>(ids) % size_t(id_bytes) || reinterpret_cast<uintptr_t>(status) % 8) {
+        set_error("tre_lookup: table and output must be 16-byte aligned, ids and status to their size");
+        return TRE_E_ARG;
+    }
+    const hipError_t e = launch_lookup(table, table_dtype, n_rows, row_elems, mx ? tile_rows : 1, ids, id_bytes, n_ids, scale,
+                                       out, out_dtype, status, reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TRE_OK : dev_fail(e, "lookup");
+}
+
+size_t tre_lookup_grad_workspace_bytes(int64_t n_ids, int64_t n_rows, int64_t row_elems) {
+    return rows_ok(n_ids, n_rows, row_elems) ? lookup_grad_ws_bytes(n_ids, n_rows, row_elems) : 0;
+}
+
+tre_status tre_lookup_grad(const void* grad, int32_t grad_dtype, const void* ids, int32_t id_bytes, int64_t n_ids,
+                           float scale, void* table_grad, int32_t out_dtype, int64_t n_rows, int64_t row_elems,
+                           int32_t accumulate, int64_t* status, void* ws, size_t ws_bytes, void* stream) {
+    if ((grad_dtype != TRE_F32 && grad_dtype != TRE_BF16) || (out_dtype != TRE_F32 && out_dtype != TRE_BF16)) {
+        set_error("tre_lookup_grad: grad_dtype and out_dtype must be TRE_F32 or TRE_BF16");
+        return TRE_E_DTYPE;
+    }
+    if (!rows_ok(n_ids, n_rows, row_elems)) {
+        set_error("tre_lookup_grad: size out of range");
+        return TRE_E_SHAPE;
+    }
+    if (!table_grad || !ws || (n_ids > 0 && (!grad || !ids)) || (id_bytes != 4 && id_bytes != 8)) {
+        set_error("tre_lookup_grad: null array, or ids of neither 4 nor 8 bytes");
+        return TRE_E_ARG;
+    }
+    if ((reinterpret_cast<uintptr_t>(grad) | reinterpret_cast<uintptr_t>(table_grad)) & 15 ||
+        reinterpret_cast<uintptr_t>(ids) % size_t(id_bytes) || reinterpret_cast<uintptr_t>(status) % 8 ||
+        reinterpret_cast<uintptr_t>(ws) % 256) {
+        set_error("tre_lookup_grad: grad and table_grad must be 16-byte, ws 256-byte aligned, ids and status to their size");
+        return TRE_E_ARG;
+    }
+    if (ws_bytes < lookup_grad_ws_bytes(n_ids, n_rows, row_elems)) {
+        set_error("tre_lookup_grad: workspace smaller than tre_lookup_grad_workspace_bytes");
+        return TRE_E_WORKSPACE;
+    }
+    const hipError_t e = launch_lookup_grad(grad, grad_dtype, ids, id_bytes, n_ids, scale, table_grad, out_dtype, n_rows,
+                                            row_elems, accumulate != 0, status, static_cast<char*>(ws),
+                                            reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TRE_OK : dev_fail(e, "lookup_grad");
 }
 
 size_t tre_stack_workspace_bytes(int64_t n) { return n < 0 ? 0 : stack_ws_bytes(n); }

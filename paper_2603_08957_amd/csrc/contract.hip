@@ -14,6 +14,7 @@
 // order / layout of the operand tiles is accepted.
 //   KC_GEMM: MFMA blocks (gemm_fast.hip, gemm_tile.hip).
 //   KC_VEC : one output element per thread, fp32 FMA (scale, GEMV, dot).
+//   KC_MX  : scaled MFMA on 4-bit tiles (mx.hip).
 #include "tre_internal.h"
 
 
@@ -808,6 +809,7 @@ namespace {
 // Whether the plan's contraction kernel reads offset table t.
 bool table_used(const Plan& p, int t) {
     if (p.kclass == KC_VEC) return t >= T_EU;
+    if (p.kclass == KC_MX) return (t == T_WM || t == T_WN) ? !p.tile_w_affine : t == T_WB && p.nB > 1;
     if (p.fast || t >= T_EU) return false;
     if (t == T_AM || t == T_AK || t == T_BN || t == T_BK)
         return p.tile_op[0].mode == TM_GATHER || p.tile_op[0].mode == TM_GATHER8;
@@ -881,7 +883,7 @@ hipError_t launch_units(const Plan& p, const Layout& L, char* ws, int64_t n_pair
         const bool with_tables = total > 0 && total <= kUnitsTableMax;
         if (total > kUnitsTableMax && (e = launch_tables(p, tables, s)) != hipSuccess) return e;
         k_units_small<<<1, kUnitsThreads, 0, s>>>(seg_start, n_w, std::max<int64_t>(p_unit, 1),
-                                                   !longest_first || p.kclass != KC_GEMM ? 0
+                                                   !longest_first || p.kclass == KC_VEC ? 0
                                                    // (units shorter than the average key: keys cut alike)
                                                    : !p.fast && p_unit * n_w < n_pairs   ? 2
                                                                                          : 1,
@@ -895,7 +897,7 @@ hipError_t launch_units(const Plan& p, const Layout& L, char* ws, int64_t n_pair
         k_key_units<<<blocks_for(n_w + 1), kThreads, 0, s>>>(seg_start, n_w, reinterpret_cast<Unit*>(ws + L.unit_desc),
                                                              hdr, dev_counts ? 1 : 0);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        if (longest_first && p.kclass == KC_GEMM && n_w <= kOrderMax) {
+        if (longest_first && p.kclass != KC_VEC && n_w <= kOrderMax) {
             k_order_units<<<1, kOrderBins, 0, s>>>(reinterpret_cast<Unit*>(ws + L.unit_desc), hdr);
             e = hipGetLastError();
         }
@@ -912,7 +914,7 @@ hipError_t launch_units(const Plan& p, const Layout& L, char* ws, int64_t n_pair
                                                           reinterpret_cast<int32_t*>(ws + L.split_list), hdr);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     // one workgroup per output block and unit: dispatch the longest first
-    if (longest_first && p.kclass == KC_GEMM && n_w + n_pairs / p_unit + 1 <= kOrderMax) {
+    if (longest_first && p.kclass != KC_VEC && n_w + n_pairs / p_unit + 1 <= kOrderMax) {
         k_order_units<<<1, kOrderBins, 0, s>>>(reinterpret_cast<Unit*>(ws + L.unit_desc), hdr);
         e = hipGetLastError();
     }
@@ -943,6 +945,7 @@ hipError_t launch_contract(const Plan& p, const Layout& L, char* ws, const void*
     if (p.kclass == KC_GEMM && p.fast)
         return launch_gemm_fast(p, L, ws, u_tiles, v_tiles, w_tiles, n_pairs, unit_bound, s);
     if (p.kclass == KC_GEMM) return launch_gemm_tile(p, L, ws, u_tiles, v_tiles, w_tiles, n_pairs, unit_bound, s);
+    if (p.kclass == KC_MX) return launch_mx(p, L, ws, u_tiles, v_tiles, w_tiles, n_pairs, unit_bound, s);
     // with vec_swap the kernel's first (vector) operand is V: the product is
     // symmetric, so only the roles of the pointers and tables change
     const bool sw = p.vec_swap;

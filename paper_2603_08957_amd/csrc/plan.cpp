@@ -117,6 +117,22 @@ static void push(Dims& d, int64_t size, int64_t stride) {
     d.n++;
 }
 
+// The same map with sizes of one left out and labels that lie side by side in
+// memory joined to one.
+static Dims merged(const Dims& d) {
+    Dims r;
+    for (int i = 0; i < d.n; i++) {
+        if (d.size[i] == 1) continue;
+        if (r.n > 0 && int64_t(r.stride[r.n - 1]) == int64_t(d.size[i]) * d.stride[i]) {
+            r.size[r.n - 1] *= d.size[i];
+            r.stride[r.n - 1] = d.stride[i];
+        } else {
+            push(r, d.size[i], d.stride[i]);
+        }
+    }
+    return r;
+}
+
 static std::vector<int32_t> host_table(const Dims& d) {
     std::vector<int32_t> t(size_t(d.count()));
     for (int64_t x = 0; x < d.count(); x++) {
@@ -252,10 +268,21 @@ static tre_status classify(Plan& p) {
     if (p.nK > (int64_t(1) << 30)) { set_error("contracted extent too large"); return TRE_E_SHAPE; }
 
     p.kclass = (p.nM >= 16 && p.nN >= 16 && p.nK >= 8) ? KC_GEMM : KC_VEC;
+    if (p.dtype == TRE_MXFP4) {
+        p.kclass = KC_MX;
+        if (prod(pul) * prod(pvl) != 1) {
+            set_error("4-bit tiles: a label summed inside a tile must be in both operands");
+            return TRE_E_SHAPE;
+        }
+        if (bl.size() + std::max(ml.size(), nl.size()) > kMaxDims) {
+            set_error("too many labels in the rows of a 4-bit tile");
+            return TRE_E_SHAPE;
+        }
+    }
     // GEMM output stores are coalesced along the kernel's N; when W's unit
     // stride label belongs to M, swap the operands so it becomes N.
     p.swap = false;
-    if (p.kclass == KC_GEMM) {
+    if (p.kclass != KC_VEC) {
         for (int i = p.nl[2] - 1; i >= 0; i--) {
             int l = p.lab[2][i];
             if (p.tsz[l] == 1) continue;
@@ -311,6 +338,32 @@ static tre_status classify(Plan& p) {
         off += (p.dims[t].count() + 63) / 64 * 64;
     }
     p.table_total = off;
+
+    if (p.kclass == KC_MX) {
+        for (int o = 0; o < 2; o++) {
+            Dims row;
+            for (int l : bl) push(row, p.tsz[l], stride_in(p, o, l));
+            for (int l : o == 0 ? ml : nl) push(row, p.tsz[l], stride_in(p, o, l));
+            p.mx_rows[o] = row.count();
+            p.mx_row[o] = merged(row);
+        }
+        Dims ku, kv;
+        for (int l : kl) {
+            push(ku, p.tsz[l], stride_in(p, 0, l));
+            push(kv, p.tsz[l], stride_in(p, 1, l));
+        }
+        p.mx_k[0] = merged(ku);
+        p.mx_k[1] = merged(kv);
+        p.mx_blocks = mx_row_blocks(p.nK);
+        for (int o = 0; o < 2; o++) {
+            p.mx_bytes[o] = mx_tile_bytes(p.mx_rows[o], p.nK);
+            if (p.mx_bytes[o] > INT32_MAX) { set_error("4-bit tile larger than 2^31 - 1 bytes"); return TRE_E_SHAPE; }
+        }
+        const Dims wm = merged(p.dims[T_WM]), wn = merged(p.dims[T_WN]);
+        p.tile_w_affine = wm.n <= 1 && wn.n <= 1 && (wn.n == 0 || wn.stride[0] == 1);
+        p.tile_w_sm = wm.n ? wm.stride[0] : 0;
+        return TRE_OK;
+    }
 
     // Vector class: EPT consecutive W elements per thread when U's offsets run
     // contiguously in aligned groups of EPT and V's either do too or stay
@@ -540,15 +593,15 @@ tre_status tre_plan(const char* einsum, const char* upper, const int64_t* extent
         return TRE_E_ARG;
     }
     *out = nullptr;
-    if (in_dtype != TRE_F32 && in_dtype != TRE_BF16) {
-        set_error("in_dtype must be TRE_F32 or TRE_BF16");
+    if (in_dtype != TRE_F32 && in_dtype != TRE_BF16 && in_dtype != TRE_MXFP4) {
+        set_error("in_dtype must be TRE_F32, TRE_BF16 or TRE_MXFP4");
         return TRE_E_DTYPE;
     }
     auto* h = new (std::nothrow) tre_plan_s();
     if (!h) return TRE_E_ARG;
     Plan& p = h->p;
     p.einsum = einsum;
-    p.dtype = in_dtype == TRE_BF16 ? TRE_BF16 : TRE_F32;
+    p.dtype = tre_dtype(in_dtype);
     p.opt.validate_keys = 1;
     if (opt) {
         p.opt = *opt;
@@ -582,7 +635,7 @@ tre_status tre_plan_get_info(tre_plan_t plan, tre_plan_info* info) {
         for (int a = 0; a < p.nk[o]; a++) info->key_labels[o][a] = char('a' + p.klab[o][a]);
     }
     info->n_join = p.n_join;
-    info->kernel_class = (p.kclass == KC_GEMM && p.fast) ? 2 : p.kclass;
+    info->kernel_class = p.kclass == KC_MX ? 3 : (p.kclass == KC_GEMM && p.fast) ? 2 : p.kclass;
     info->batch = p.nB;
     info->m = p.nM;
     info->n = p.nN;
@@ -594,6 +647,14 @@ tre_status tre_plan_get_info(tre_plan_t plan, tre_plan_info* info) {
     info->w_dtype = p.opt.w_bf16 ? TRE_BF16 : TRE_F32;
     info->join_outer = p.v_outer ? 1 : 0;
     return TRE_OK;
+}
+
+int64_t tre_tile_bytes(tre_plan_t plan, int32_t operand) {
+    if (!plan || operand < 0 || operand > 2) return -1;
+    const Plan& p = plan->p;
+    if (operand == 2) return p.tile_elems[2] * (p.opt.w_bf16 ? 2 : 4);
+    if (p.dtype == TRE_MXFP4) return p.mx_bytes[operand];
+    return p.tile_elems[operand] * (p.dtype == TRE_BF16 ? 2 : 4);
 }
 
 void tre_plan_destroy(tre_plan_t plan) { delete plan; }

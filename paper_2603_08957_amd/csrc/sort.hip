@@ -225,6 +225,13 @@ hipError_t radix_sort_u64(uint64_t* keys, uint32_t* vals, uint64_t* keys_alt, ui
                                          nullptr, s);
 }
 
+hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, uint32_t* vals_alt, int64_t n, int bits,
+                          int32_t* hist, int32_t* scan_tmp, hipStream_t s) {
+    if (bits > 32) return hipErrorInvalidValue;
+    return sort_impl<uint32_t, uint32_t>(keys, vals, keys_alt, vals_alt, n, nullptr, bits, hist, scan_tmp, nullptr,
+                                         nullptr, s);
+}
+
 hipError_t radix_sort_u64_pairs(uint64_t* keys, uint64_t* vals, uint64_t* keys_alt, uint64_t* vals_alt, int64_t n,
                                 const int64_t* dn, int bits, int32_t* hist, int32_t* scan_tmp, int32_t* split_hi,
                                 int32_t* split_lo, hipStream_t s) {

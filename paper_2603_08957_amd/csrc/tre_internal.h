@@ -71,7 +71,25 @@ struct Dims {
 //   of its non-contracted part; KU/KV map the contracted index.
 enum TableId { T_AM, T_AK, T_BK, T_BN, T_WM, T_WN, T_AB, T_BB, T_WB, T_EU, T_EV, T_KU, T_KV, T_COUNT };
 
-enum KernelClass { KC_GEMM = 0, KC_VEC = 1 };
+enum KernelClass { KC_GEMM = 0, KC_VEC = 1, KC_MX = 2 };
+
+// ----- tiles in microscaled 4-bit floating point (TRE_MXFP4) -----
+// A tile is [row][block] codes of 16 bytes (32 values of the contracted index,
+// the lower of two in a byte's low half), then [row][block] scale bytes.
+constexpr int kMxBlock = 32;
+constexpr int kMxNanScale = 255;
+
+// Blocks that a row of K values takes: one or two for up to 64 values, else
+// whole matrix instructions of four.  (Rows of one and two blocks share an
+// instruction with the next pairs; of other lengths the last instruction is
+// not filled anyway, and with rows of whole instructions every load of codes
+// is 16 bytes aligned and every load of scales 4.)  Values past K are zero.
+__host__ __device__ inline int64_t mx_row_blocks(int64_t K) {
+    return K <= kMxBlock ? 1 : K <= 2 * kMxBlock ? 2 : (K + 4 * kMxBlock - 1) / (4 * kMxBlock) * 4;
+}
+__host__ __device__ inline int64_t mx_tile_bytes(int64_t rows, int64_t K) {
+    return (rows * mx_row_blocks(K) * 17 + 15) / 16 * 16;
+}
 
 // How k_gemm_tile loads an operand (see gemm_tile.hip).
 enum TileMode { TM_GATHER = 0, TM_K_RUN = 1, TM_K_ODD = 2, TM_ROWS = 3, TM_GATHER8 = 4 };
@@ -133,6 +151,13 @@ struct Plan {
     bool fast = false;
     bool fast_a_rowfast = false, fast_b_rowfast = false;
     int64_t fast_lda = 0, fast_ldb = 0, fast_ldw = 0;
+    // 4-bit tiles (KC_MX), per operand U, V: rows (batch labels, then the
+    // operand's own) and contracted index over the unquantised tile, blocks of
+    // a row, bytes of a tile
+    Dims mx_row[2], mx_k[2];
+    int64_t mx_rows[2] = {0, 0};
+    int64_t mx_blocks = 0;
+    int64_t mx_bytes[2] = {0, 0};
     Dims dims[T_COUNT];
     int64_t table_off[T_COUNT] = {};
     int64_t table_total = 0;
@@ -190,6 +215,8 @@ int64_t radix_hist_elems(int64_t n);
 bool radix_result_in_alt(int64_t n, int bits);
 hipError_t radix_sort_u64(uint64_t* keys, uint32_t* vals, uint64_t* keys_alt, uint32_t* vals_alt, int64_t n,
                           int bits, int32_t* hist, int32_t* scan_tmp, hipStream_t s);
+hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, uint32_t* vals_alt, int64_t n, int bits,
+                          int32_t* hist, int32_t* scan_tmp, hipStream_t s);
 hipError_t radix_sort_u64_pairs(uint64_t* keys, uint64_t* vals, uint64_t* keys_alt, uint64_t* vals_alt, int64_t n,
                                 const int64_t* dn, int bits, int32_t* hist, int32_t* scan_tmp, int32_t* split_hi,
                                 int32_t* split_lo, hipStream_t s);
@@ -278,6 +305,25 @@ hipError_t launch_write_outputs(const Plan& p, const Layout& L, char* ws, int32_
                                 int64_t n_pairs, int64_t n_w, hipStream_t s, bool dev_counts = false,
                                 int64_t* counts = nullptr, float* reduce_into = nullptr, int64_t split_bound = 0);
 hipError_t launch_counts_set(int64_t n_pairs, int64_t n_w, int64_t status, int64_t* counts, hipStream_t s);
+
+// mx.hip: 4-bit tiles
+hipError_t launch_mx_quantize(const Plan& p, int op, const void* tiles, int src_dtype, int64_t n, void* mx_tiles,
+                              hipStream_t s);
+hipError_t launch_mx_dequantize(const Plan& p, int op, const void* mx_tiles, int64_t n, void* tiles, int dst_dtype,
+                                hipStream_t s);
+// workgroups that one unit takes
+int64_t mx_blocks_per_unit(const Plan& p);
+hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_tiles, const void* v_tiles, float* w_tiles,
+                     int64_t n_pairs, int64_t unit_bound, hipStream_t s);
+
+// rows.hip: rows of a table by token, and the table's gradient
+hipError_t launch_lookup(const void* table, int table_dtype, int64_t n_rows, int64_t elems, int64_t tile_rows,
+                         const void* ids, int id_bytes, int64_t n_ids, float scale, void* out, int out_dtype,
+                         int64_t* status, hipStream_t s);
+size_t lookup_grad_ws_bytes(int64_t n_ids, int64_t n_rows, int64_t elems);
+hipError_t launch_lookup_grad(const void* grad, int grad_dtype, const void* ids, int id_bytes, int64_t n_ids, float scale,
+                              void* out, int out_dtype, int64_t n_rows, int64_t elems, bool accumulate, int64_t* status,
+                              char* ws, hipStream_t s);
 
 // glue.hip
 hipError_t launch_cast_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t s);

@@ -24,7 +24,7 @@ STATUS = {
     11: "TRE_E_DEVICE", 12: "TRE_E_STATE",
 }
 STATUS_CODE = {v: k for k, v in STATUS.items()}
-DTYPE = {"f32": 0, "bf16": 1}
+DTYPE = {"f32": 0, "bf16": 1, "mxfp4": 2}
 
 # every symbol include/tre.h declares
 EXPORTS = [
@@ -34,6 +34,8 @@ EXPORTS = [
     "tre_tiles_from_entries", "tre_status_str", "tre_last_error", "tre_version",
     "tre_repartition_workspace_bytes", "tre_repartition", "tre_execute3_workspace_bytes", "tre_execute3",
     "tre_noalloc_scratch_bytes", "tre_execute_noalloc", "tre_output_bounds", "tre_execute_async",
+    "tre_tile_bytes", "tre_mx_quantize", "tre_mx_dequantize", "tre_lookup", "tre_lookup_grad_workspace_bytes",
+    "tre_lookup_grad",
 ]
 
 
@@ -71,7 +73,7 @@ class Timing(ctypes.Structure):
                 ("n_partials", ctypes.c_int64), ("events", ctypes.c_void_p * 4), ("contract_path", ctypes.c_int32),
                 ("join_path", ctypes.c_int32)]
 
-    PATHS = {0: "gemm", 1: "vec", 2: "gemm128", 3: "gemm128_paced", 4: "gemm128_u_ranges"}
+    PATHS = {0: "gemm", 1: "vec", 2: "gemm128", 3: "gemm128_paced", 4: "gemm128_u_ranges", 5: "mx"}
     JOIN_PATHS = {0: "u_driven", 1: "v_driven", 2: "v_driven_one_match", 3: "v_driven_dense", 4: "keyed_by_u",
                   5: "one_workgroup", 6: "u_driven_dense"}
 
@@ -130,6 +132,14 @@ def lib():
         L.tre_noalloc_scratch_bytes.argtypes = []
         L.tre_noalloc_scratch_bytes.restype = sz
         L.tre_execute_noalloc.argtypes = [P, P, i64, P, P, i64, P, P, P, i64, P, P, i64, P, P]
+        L.tre_tile_bytes.argtypes = [P, i32]
+        L.tre_tile_bytes.restype = i64
+        L.tre_mx_quantize.argtypes = [P, i32, P, i32, i64, P, P]
+        L.tre_mx_dequantize.argtypes = [P, i32, P, i64, P, i32, P]
+        L.tre_lookup.argtypes = [P, i32, i64, i64, i64, P, i32, i64, ctypes.c_float, P, i32, P, P]
+        L.tre_lookup_grad_workspace_bytes.argtypes = [i64, i64, i64]
+        L.tre_lookup_grad_workspace_bytes.restype = sz
+        L.tre_lookup_grad.argtypes = [P, i32, P, i32, i64, ctypes.c_float, P, i32, i64, i64, i32, P, P, sz, P]
         L.tre_status_str.restype = ctypes.c_char_p
         L.tre_last_error.restype = ctypes.c_char_p
         L.tre_version.restype = ctypes.c_char_p
@@ -183,7 +193,7 @@ class Plan:
         self.key_arity = list(info.key_arity)
         self.tile_elems = list(info.tile_elems)
         self.n_join = info.n_join
-        self.kernel_class = {0: "gemm", 1: "vec", 2: "gemm128"}[info.kernel_class]
+        self.kernel_class = {0: "gemm", 1: "vec", 2: "gemm128", 3: "mx"}[info.kernel_class]
         self.bmnk = (info.batch, info.m, info.n, info.k)
         self.flops_per_pair = info.flops_per_pair
         self.key_labels = [bytes(info.key_labels[o]).split(b"\0")[0].decode() for o in range(3)]
@@ -192,6 +202,8 @@ class Plan:
         self.v_needs_sort = bool(info.v_needs_sort)
         self.w_dtype = {0: "f32", 1: "bf16"}[info.w_dtype]
         self.join_outer = "v" if info.join_outer else "u"
+        # bytes of one tile of U, V and W as the calls take it
+        self.tile_bytes = [int(L.tre_tile_bytes(h, o)) for o in range(3)]
 
     @classmethod
     def from_spec(cls, spec: dict, **kw):
@@ -219,6 +231,22 @@ def alloc_workspace(nbytes: int, device="cuda"):
     return ws
 
 
+def _mx_operands(plan: Plan, u_tiles, v_tiles):
+    """4-bit tiles come as uint8 rows of the plan's tile size: anything else is
+    an array that was not quantised for this plan."""
+    import torch
+
+    if plan.dtype != "mxfp4":
+        return
+    for o, t in ((0, u_tiles), (1, v_tiles)):
+        if t is None:
+            continue
+        if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[1] != plan.tile_bytes[o] or not t.is_contiguous():
+            raise TreError(STATUS_CODE["TRE_E_SHAPE"], "tre.contract",
+                           f"operand {'uv'[o]} of an mxfp4 plan: contiguous uint8 [n, {plan.tile_bytes[o]}] wanted, "
+                           f"got {t.dtype} {tuple(t.shape)}")
+
+
 def join(plan: Plan, u_keys, n_u: int, v_keys, n_v: int, ws, stream=None, timing: Timing | None = None) -> JoinResult:
     jr = JoinResult()
     rc = lib().tre_join(plan.handle, _ptr(u_keys), n_u, _ptr(v_keys), n_v, _ptr(ws), ws.numel(), _stream(stream),
@@ -232,6 +260,7 @@ def join(plan: Plan, u_keys, n_u: int, v_keys, n_v: int, ws, stream=None, timing
 
 def contract(plan: Plan, jr: JoinResult, u_tiles, v_tiles, w_keys, w_tiles, pairs_out=None, stream=None,
              timing: Timing | None = None):
+    _mx_operands(plan, u_tiles, v_tiles)
     w_cap = w_tiles.shape[0] if w_tiles is not None else 0
     pair_cap = pairs_out.shape[0] if pairs_out is not None else 0
     rc = lib().tre_contract(plan.handle, ctypes.byref(jr), _ptr(u_tiles), _ptr(v_tiles), _ptr(w_keys), w_cap,
@@ -252,6 +281,7 @@ def execute(plan: Plan, u_keys, u_tiles, v_keys, v_tiles, w_keys, w_tiles, ws, p
     """tre_execute into caller-owned outputs and workspace (their row counts
     are the capacities): the join and the contraction in one call.  Returns
     (n_w, n_pairs); a TreError carries them when a capacity is short."""
+    _mx_operands(plan, u_tiles, v_tiles)
     n_u, n_v = int(u_tiles.shape[0]), int(v_tiles.shape[0])
     n_w, n_p = ctypes.c_int64(0), ctypes.c_int64(0)
     rc = lib().tre_execute(plan.handle, _ptr(u_keys), n_u, _ptr(u_tiles), _ptr(v_keys), n_v, _ptr(v_tiles),
@@ -281,6 +311,7 @@ def execute_async(plan: Plan, u_keys, u_tiles, v_keys, v_tiles, w_keys, w_tiles,
     counts ([pairs, keys, status, 0]) land in ``counts`` (device int64 [4]).
     ``n_u`` defaults to u_tiles' rows; ``n_u_dev`` (a device int64 tensor)
     holds U's actual count when n_u is only a bound."""
+    _mx_operands(plan, u_tiles, v_tiles)
     n_u = int(u_tiles.shape[0]) if n_u is None else int(n_u)
     n_v = int(v_tiles.shape[0])
     rc = lib().tre_execute_async(plan.handle, _ptr(u_keys), n_u, _ptr(n_u_dev), _ptr(u_tiles), _ptr(v_keys), n_v,
@@ -308,6 +339,7 @@ def einsum(plan: Plan, u_keys, u_tiles, v_keys, v_tiles, want_pairs: bool = Fals
     is grown and the join repeated once if the pair list does not fit."""
     import torch
 
+    _mx_operands(plan, u_tiles, v_tiles)
     n_u, n_v = int(u_tiles.shape[0]), int(v_tiles.shape[0])
     dev = u_tiles.device
     if ws is None:
@@ -335,6 +367,7 @@ def execute_noalloc(plan: Plan, u_keys, u_tiles, v_keys, v_tiles, w_keys, w_tile
     """tre_execute_noalloc: join + contract with the library's static device
     scratch as workspace; every output buffer is the caller's (their row
     counts are the capacities).  Returns (n_w, n_pairs)."""
+    _mx_operands(plan, u_tiles, v_tiles)
     n_u, n_v = int(u_tiles.shape[0]), int(v_tiles.shape[0])
     n_w, n_p = ctypes.c_int64(0), ctypes.c_int64(0)
     rc = lib().tre_execute_noalloc(plan.handle, _ptr(u_keys), n_u, _ptr(u_tiles), _ptr(v_keys), n_v, _ptr(v_tiles),
@@ -350,6 +383,201 @@ def execute_noalloc(plan: Plan, u_keys, u_tiles, v_keys, v_tiles, w_keys, w_tile
 
 def noalloc_scratch_bytes() -> int:
     return int(lib().tre_noalloc_scratch_bytes())
+
+
+# ------------------------------------------------ 4-bit tiles, rows by token
+
+def _value_type(t, where, what):
+    """0 / 1 for fp32 / bf16, of a tensor or a type."""
+    import torch
+
+    dt = getattr(t, "dtype", t)
+    if dt == torch.float32:
+        return 0
+    if dt == torch.bfloat16:
+        return 1
+    raise TreError(STATUS_CODE["TRE_E_DTYPE"], where, f"{what}: float32 or bfloat16 wanted, got {dt}")
+
+
+def _want(t, where, what, shape=None, dtype=None, device=None):
+    """A contiguous GPU tensor, of this shape, type and device where given."""
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"{what}: on {t.device}, wanted on {device or 'a GPU'}")
+    if dtype is not None and t.dtype != dtype:
+        raise TreError(STATUS_CODE["TRE_E_DTYPE"], where, f"{what}: {dtype} wanted, got {t.dtype}")
+    if (shape is not None and tuple(t.shape) != tuple(shape)) or not t.is_contiguous():
+        raise TreError(STATUS_CODE["TRE_E_SHAPE"], where,
+                       f"{what}: contiguous {tuple(shape) if shape is not None else 'tensor'} wanted, got {tuple(t.shape)}"
+                       f" with strides {tuple(t.stride())}")
+    return t
+
+
+def _on(device, stream):
+    """(a context with the tensors' device current, the stream to use there)."""
+    import torch
+
+    return torch.cuda.device(device), (stream if stream is not None else torch.cuda.current_stream(device))
+
+
+def _keep(stream, *tensors):
+    """Tensors made here for a stream other than the current one: their memory
+    must not be given out again before that stream is done with it."""
+    import torch
+
+    for t in tensors:
+        if stream != torch.cuda.current_stream(t.device):
+            t.record_stream(stream)
+
+
+def _operand(plan, operand, where):
+    if plan.dtype != "mxfp4":
+        raise TreError(STATUS_CODE["TRE_E_DTYPE"], where, f"the plan's tiles are {plan.dtype}, not mxfp4")
+    if operand not in ("u", "v"):
+        raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"operand 'u' or 'v' wanted, got {operand!r}")
+    return "uv".index(operand)
+
+
+def mx_quantize(plan: Plan, operand: str, tiles, out=None, stream=None):
+    """Tiles [n, tile_elems] (float32 or bfloat16) of the mxfp4 plan's operand
+    "u" or "v" in 4 bits (see tre_mx_quantize): uint8 [n, plan.tile_bytes],
+    which the plan's calls take."""
+    import torch
+
+    w = "tre.mx_quantize"
+    o = _operand(plan, operand, w)
+    dt = _value_type(tiles, w, "tiles")
+    n = int(tiles.shape[0]) if tiles.dim() else -1
+    _want(tiles, w, "tiles", (n, plan.tile_elems[o]))
+    dev, s = _on(tiles.device, stream)
+    with dev:
+        if out is None:
+            out = torch.empty((n, plan.tile_bytes[o]), dtype=torch.uint8, device=tiles.device)
+            _keep(s, out)
+        _want(out, w, "out", (n, plan.tile_bytes[o]), torch.uint8, tiles.device)
+        _check(lib().tre_mx_quantize(plan.handle, o, _ptr(tiles), dt, n, _ptr(out), _stream(s)), "tre_mx_quantize")
+    return out
+
+
+def mx_dequantize(plan: Plan, operand: str, mx_tiles, dtype=None, out=None, stream=None):
+    """The values of 4-bit tiles of the plan's operand "u" or "v" (see
+    tre_mx_dequantize): [n, tile_elems] in ``dtype`` (float32, the default, or
+    bfloat16; ``out``'s where that is given)."""
+    import torch
+
+    w = "tre.mx_dequantize"
+    o = _operand(plan, operand, w)
+    n = int(mx_tiles.shape[0]) if mx_tiles.dim() else -1
+    _want(mx_tiles, w, "mx_tiles", (n, plan.tile_bytes[o]), torch.uint8)
+    dev, s = _on(mx_tiles.device, stream)
+    with dev:
+        if out is None:
+            _value_type(dtype or torch.float32, w, "dtype")
+            out = torch.empty((n, plan.tile_elems[o]), dtype=dtype or torch.float32, device=mx_tiles.device)
+            _keep(s, out)
+        _want(out, w, "out", (n, plan.tile_elems[o]), dtype, mx_tiles.device)
+        _check(lib().tre_mx_dequantize(plan.handle, o, _ptr(mx_tiles), n, _ptr(out), _value_type(out, w, "out"),
+                                       _stream(s)), "tre_mx_dequantize")
+    return out
+
+
+def _ids(ids, where, device):
+    import torch
+
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TreError(STATUS_CODE["TRE_E_DTYPE"], where, f"ids: int32 or int64 wanted, got {ids.dtype}")
+    return _want(ids, where, "ids", device=device)
+
+
+def _status(status, where, device):
+    import torch
+
+    if status is not None:
+        _want(status, where, "status", (1,), torch.int64, device)
+    return status
+
+
+def lookup(table, ids, scale: float = 1.0, dtype=None, out=None, plan: Plan | None = None, operand: str = "u",
+           status=None, stream=None):
+    """Rows of a table by token, ids.shape + [row] (see tre_lookup):
+    scale * table[ids], zero where an id is negative.  ``table`` is [n_rows, row]
+    in float32 or bfloat16, or 4-bit tiles of an mxfp4 ``plan``'s operand, which
+    keeps one label, the token's, and contracts the row's.  ``dtype``: of the
+    result (the table's; float32 for 4-bit tiles).  ``status`` (int64 [1]) is
+    set to TRE_E_KEYRANGE where an id is n_rows or more; such rows are zero."""
+    import torch
+
+    w = "tre.lookup"
+    tile_rows = 1
+    if plan is not None:
+        o = _operand(plan, operand, w)
+        b, m, n, k = plan.bmnk
+        if b != 1:
+            raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, "the plan's operands share a label that W keeps in its tile")
+        tile_rows, elems, tdt = (m, n)[o], k, 2
+        n_tiles = int(table.shape[0]) if table.dim() else -1
+        _want(table, w, "table", (n_tiles, plan.tile_bytes[o]), torch.uint8)
+        n_rows = n_tiles * tile_rows
+    else:
+        tdt = _value_type(table, w, "table")
+        if table.dim() != 2:
+            raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"table: [rows, row] wanted, got {tuple(table.shape)}")
+        n_rows, elems = int(table.shape[0]), int(table.shape[1])
+        _want(table, w, "table")
+    _ids(ids, w, table.device)
+    _status(status, w, table.device)
+    shape = tuple(ids.shape) + (elems,)
+    dev, s = _on(table.device, stream)
+    with dev:
+        if out is None:
+            dtype = dtype or (torch.float32 if plan is not None else table.dtype)
+            _value_type(dtype, w, "dtype")
+            out = torch.empty(shape, dtype=dtype, device=table.device)
+            _keep(s, out)
+        _want(out, w, "out", shape, dtype, table.device)
+        _check(lib().tre_lookup(_ptr(table), tdt, n_rows, elems, tile_rows, _ptr(ids), ids.element_size(), ids.numel(),
+                                float(scale), _ptr(out), _value_type(out, w, "out"), _ptr(status), _stream(s)),
+               "tre_lookup")
+    return out
+
+
+def lookup_grad_workspace_bytes(n_ids: int, n_rows: int, row_elems: int) -> int:
+    return int(lib().tre_lookup_grad_workspace_bytes(int(n_ids), int(n_rows), int(row_elems)))
+
+
+def lookup_grad(grad, ids, n_rows: int, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False,
+                status=None, ws=None, stream=None):
+    """The gradient of `lookup` by its table, [n_rows, row] (see
+    tre_lookup_grad): scale times the rows of ``grad`` (ids.shape + [row],
+    float32 or bfloat16) summed by token in fp32.  ``dtype``: of the result
+    (float32); with ``accumulate`` the sums are added to ``out``."""
+    import torch
+
+    w = "tre.lookup_grad"
+    gdt = _value_type(grad, w, "grad")
+    _want(grad, w, "grad")
+    _ids(ids, w, grad.device)
+    if grad.dim() != ids.dim() + 1 or tuple(grad.shape[:-1]) != tuple(ids.shape):
+        raise TreError(STATUS_CODE["TRE_E_SHAPE"], w,
+                       f"grad: ids' shape {tuple(ids.shape)} and a row wanted, got {tuple(grad.shape)}")
+    if accumulate and out is None:
+        raise TreError(STATUS_CODE["TRE_E_ARG"], w, "accumulate needs out")
+    _status(status, w, grad.device)
+    n, elems = ids.numel(), int(grad.shape[-1])
+    dev, s = _on(grad.device, stream)
+    with dev:
+        if out is None:
+            _value_type(dtype or torch.float32, w, "dtype")
+            out = torch.empty((int(n_rows), elems), dtype=dtype or torch.float32, device=grad.device)
+            _keep(s, out)
+        _want(out, w, "out", (int(n_rows), elems), dtype, grad.device)
+        if ws is None:
+            ws = alloc_workspace(lookup_grad_workspace_bytes(n, n_rows, elems), grad.device)
+            _keep(s, ws)
+        _want(ws, w, "ws", device=grad.device)
+        _check(lib().tre_lookup_grad(_ptr(grad), gdt, _ptr(ids), ids.element_size(), n, float(scale), _ptr(out),
+                                     _value_type(out, w, "out"), int(n_rows), elems, int(accumulate), _ptr(status),
+                                     _ptr(ws), ws.numel() * ws.element_size(), _stream(s)), "tre_lookup_grad")
+    return out
 
 
 def cast_f32_bf16(x, out=None, stream=None):

@@ -1,0 +1,316 @@
+"""4-bit tiles on the GPU: quantising and reading back bit for bit against the
+oracle, and EinSums over them against float64.
+
+Sums: a product of two E2M1 values under their powers of two is exact in fp32,
+so only the additions round.  n additions in fp32 in any order are off by at
+most n 2^-24 of the sum of magnitudes (to first order); n is the contracted
+extent of all pairs of a key, padded to blocks, plus the partial sums.  A bf16
+result is rounded once more, by at most 2^-8 of its value.
+"""
+import itertools
+
+import numpy as np
+import pytest
+
+from oracle import microscaled as mx
+
+pytestmark = pytest.mark.gpu
+
+U32, UB16 = 2.0 ** -24, 2.0 ** -8
+
+
+def bf16(x):
+    import torch
+
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(torch.bfloat16)
+
+
+def special(rng, n, rows, k):
+    """Values over many powers of two, with every kind of block among them."""
+    x = rng.standard_normal((n, rows, k)) * np.exp2(rng.integers(-20, 20, (n, rows, 1)).astype(float))
+    x = x.astype(np.float32)
+    flat = x.reshape(-1, k)
+    grid = np.array([0, 0.25, 0.5, 0.75, 1, 1.25, 1.5, 1.75, 2, 2.5, 3, 3.5, 4, 5, 6, 7, 7.75, -0.25, -0.75, -5, -0.0], np.float32)
+    for i in range(0, flat.shape[0], 3):  # values on and beside the borders
+        flat[i] = rng.choice(grid, k) * np.float32(2.0 ** rng.integers(-30, 30))
+        flat[i] = np.nextafter(flat[i], rng.choice(np.array([-np.inf, np.inf], np.float32), k)) if i % 2 else flat[i]
+    picks = [0.0, 1e-45, 2.0 ** -130, 2.0 ** -126, 2.0 ** -124, 3.4e38, np.inf, -np.inf, np.nan]
+    for j, v in enumerate(picks):
+        if flat.shape[0] > j + 1:
+            if v == 0 or abs(v) < 1e-30:
+                flat[j + 1] = 0
+            flat[j + 1, k // 2] = v
+    return x
+
+
+FORMS = [  # (einsum, operand, the operand's labels in rows and contracted order are not its own order everywhere)
+    ("ik,jk->ij", 0), ("ik,jk->ij", 1), ("ki,jk->ij", 0), ("ik,kj->ij", 1), ("ik,kj->ji", 0),
+    ("bik,bjk->bij", 0), ("kib,bkj->ijb", 1), ("ikl,jlk->ij", 1), ("kil,jlk->ij", 0), ("aikc,ckj->jai", 0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("einsum,op", FORMS)
+@pytest.mark.parametrize("rows,k", [(1, 1), (3, 5), (16, 31), (17, 32), (5, 33), (64, 64), (7, 65), (33, 96), (128, 128),
+                                    (9, 130), (65, 257), (130, 100), (8, 1000)])
+def test_quantize_and_back(einsum, op, rows, k, dtype):
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    own, rl, kl = mx.roles(einsum, op)
+    sizes = {c: 1 for c in "abcijkl"}
+    # rows and k spread over the labels that stand for them
+    for labels, total in ((rl, rows), (kl, k)):
+        for c in labels[:-1]:
+            sizes[c] = 2
+        sizes[labels[-1]] = total
+    other = {c: 3 for c in einsum if c.isalpha() and c not in own}
+    plan = tre.Plan(einsum, "", {**{c: sizes[c] for c in own}, **other}, {}, "mxfp4")
+    rng = np.random.default_rng(rows * 1000 + k)
+    R, K = int(np.prod([sizes[c] for c in rl])), int(np.prod([sizes[c] for c in kl]))
+    n = 3
+    m = special(rng, n, R, K)
+    if dtype == "bf16":
+        m = bf16(m).float().numpy()
+    # into the operand's own order
+    t = m.reshape([n] + [sizes[c] for c in rl + kl]).transpose([0] + [1 + (rl + kl).index(c) for c in own])
+    t = np.ascontiguousarray(t).reshape(n, -1)
+    dev = (bf16(t) if dtype == "bf16" else torch.from_numpy(t)).cuda()
+    assert plan.tile_bytes[op] == mx.tile_bytes(R, K)
+    # written whole, and nothing behind it
+    buf = torch.full((n + 1, plan.tile_bytes[op]), 0xA5, dtype=torch.uint8, device="cuda")
+    q = tre.mx_quantize(plan, "uv"[op], dev, out=buf[:n])
+    codes, scales = mx.encode(mx.matrix(einsum, op, sizes, t.astype(np.float64)))
+    want = mx.pack(codes, scales)
+    used = 17 * R * mx.row_blocks(K)
+    got = buf.cpu().numpy()
+    # (codes of blocks that are not finite stand for nothing)
+    bad = np.repeat(scales.reshape(n, -1) == 255, 16, axis=1)
+    assert np.array_equal(got[:n, 16 * R * mx.row_blocks(K):used], want[:, 16 * R * mx.row_blocks(K):used]), "scales"
+    assert np.array_equal(np.where(bad, 0, got[:n, :bad.shape[1]]), np.where(bad, 0, want[:, :bad.shape[1]])), "codes"
+    assert np.all(got[n] == 0xA5)
+    ref = mx.values(einsum, op, sizes, t.astype(np.float64))
+    for dt in (torch.float32, torch.bfloat16):
+        out = torch.full((n + 1, plan.tile_elems[op]), -7.0, dtype=dt, device="cuda")
+        tre.mx_dequantize(plan, "uv"[op], q, out=out[:n])
+        v = out.double().cpu().numpy()
+        assert np.array_equal(v[:n], ref, equal_nan=True), dt
+        assert np.all(v[n] == -7.0)
+
+
+def relation(rng, labels, upper, ext, til, keep, dtype):
+    """(keys, tiles) of a random relation, float64 tiles already in the type."""
+    up = [c for c in labels if c in upper]
+    space = [range(ext[c] // til.get(c, 1)) for c in up]
+    keys = np.zeros((1, 0), np.int32)
+    if up:
+        keys = np.array([k for k in itertools.product(*space) if rng.random() < keep], np.int32).reshape(-1, len(up))
+    te = int(np.prod([til.get(c, 1) if c in upper else ext[c] for c in labels]))
+    t = rng.standard_normal((len(keys), te)) * np.exp2(rng.integers(-3, 4, (len(keys), 1)).astype(float))
+    t = t.astype(np.float32)
+    return keys, (bf16(t).float().numpy() if dtype == "bf16" else t)
+
+
+def run(orc, einsum, upper, ext, til, dtype="bf16", seed=0, keep=0.7, w_bf16=False, how="einsum", **opt):
+    """Quantise, run, compare with the oracle on the quantised values."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    rng = np.random.default_rng(seed)
+    la, lb = einsum.split("->")[0].split(",")
+    plan = tre.Plan(einsum, upper, ext, til, "mxfp4", w_bf16=w_bf16, **opt)
+    assert plan.kernel_class == "mx"
+    sizes = {c: til.get(c, 1) if c in upper else ext[c] for c in ext}
+    rel, dev = [], []
+    for o, lab in enumerate((la, lb)):
+        k, t = relation(rng, lab, upper, ext, til, keep, dtype)
+        x = (bf16(t) if dtype == "bf16" else torch.from_numpy(t)).cuda()
+        dev += [torch.from_numpy(k).cuda(), tre.mx_quantize(plan, "uv"[o], x)]
+        rel.append({"keys": k, "tiles": mx.values(einsum, o, sizes, t.astype(np.float64)).astype(np.float32), "dtype": "f32"})
+    ref = orc.run(orc.Plan(einsum, upper, ext, {c: til.get(c, 1) for c in ext}), *rel)
+    n_w, n_p = len(ref.wkeys), len(ref.pairs)
+    rw, dt = plan.key_arity[2], torch.bfloat16 if w_bf16 else torch.float32
+    if how == "einsum":
+        out = tre.einsum(plan, *dev, want_pairs=True, timing=True)
+        assert out.n_w == n_w and out.n_pairs == n_p
+        assert n_p == 0 or out.timing["contract_path"] == "mx"
+        assert np.array_equal(out.pairs.cpu().numpy().reshape(n_p, 2), ref.pairs.reshape(n_p, 2))
+        wk, wt = out.w_keys, out.w_tiles
+    else:
+        ws = tre.alloc_workspace(plan.workspace_bytes(dev[1].shape[0], dev[3].shape[0], max(n_p, 1) * 4))
+        _, kb, _ = tre.output_bounds(plan, dev[1].shape[0], dev[3].shape[0], ws.numel())
+        wk = torch.zeros((max(kb, 1), max(rw, 1)), dtype=torch.int32, device="cuda")
+        wt = torch.full((max(kb, 1), plan.tile_elems[2]), -3.0, dtype=dt, device="cuda")
+        if how == "async":
+            counts = torch.zeros(4, dtype=torch.int64, device="cuda")
+            tre.execute_async(plan, *dev, wk, wt, ws, counts)
+            assert counts.tolist() == [n_p, n_w, 0, 0]
+        elif how == "noalloc":
+            assert tre.execute_noalloc(plan, *dev, wk, wt) == (n_w, n_p)
+        else:
+            assert tre.execute(plan, *dev, wk, wt, ws) == (n_w, n_p)
+        # rows behind the last output tile stay as they were
+        assert torch.all(wt[n_w:] == -3.0)
+    if n_w == 0:
+        return plan
+    assert np.array_equal(wk[:n_w].cpu().numpy().reshape(n_w, -1)[:, :rw], ref.wkeys.reshape(n_w, -1))
+    got = wt[:n_w].double().cpu().numpy().reshape(ref.acc.shape)
+    most = max(n_p, 1)  # pairs of one key, at most
+    n = most * (32 * mx.row_blocks(plan.bmnk[3]) + 2)
+    tol = n * U32 * ref.mag
+    if w_bf16:
+        tol = tol * (1 + UB16) + UB16 * np.abs(ref.acc)
+    err = np.abs(got - ref.acc)
+    assert np.all(err <= tol), (err / np.maximum(ref.mag, 1e-300)).max()
+    # and nowhere near that in the norm: an fp32 sum of exact products
+    rel_norm = np.linalg.norm(got - ref.acc) / max(np.linalg.norm(ref.acc), 1e-300)
+    assert rel_norm <= (UB16 if w_bf16 else 1e-6), rel_norm
+    return plan
+
+
+PLANS = [  # einsum, promoted, extents, tiles
+    ("ik,jk->ij", "", {"i": 1, "j": 1, "k": 1}, {}),
+    ("ik,jk->ij", "", {"i": 17, "j": 70, "k": 100}, {}),
+    ("ik,jk->ji", "", {"i": 3, "j": 65, "k": 1000}, {}),                       # W's unit stride along U's rows
+    ("vd,nd->nv", "v", {"v": 1280, "n": 1, "d": 96}, {"v": 128}),               # a token's scores
+    ("vd,nd->nv", "v", {"v": 500, "n": 13, "d": 1000}, {"v": 50}),
+    ("vd,nd->nv", "v", {"v": 600, "n": 40, "d": 520}, {"v": 300}),
+    ("ij,jk->ik", "ij", {"i": 512, "j": 512, "k": 100}, {"i": 64, "j": 64}),
+    ("ij,jk->ik", "ij", {"i": 128, "j": 320, "k": 33}, {"i": 32, "j": 32}),     # one block a row: pairs share an instruction
+    ("ij,jk->ki", "jk", {"i": 40, "j": 200, "k": 200}, {"j": 20, "k": 20}),
+    ("ij,jk->ik", "ijk", {"i": 384, "j": 384, "k": 384}, {"i": 96, "j": 96, "k": 96}),
+    ("ij,jk->ik", "ijk", {"i": 512, "j": 512, "k": 512}, {"i": 128, "j": 128, "k": 128}),
+    ("ij,jk->ik", "ijk", {"i": 520, "j": 520, "k": 520}, {"i": 260, "j": 130, "k": 260}),
+    ("nv,nd->vd", "nv", {"n": 256, "v": 384, "d": 200}, {"n": 64, "v": 128}),   # a weight's gradient
+    ("bik,bkj->bij", "i", {"b": 3, "i": 96, "j": 50, "k": 40}, {"i": 24}),
+    ("bik,kjb->jbi", "k", {"b": 2, "i": 20, "j": 70, "k": 256}, {"k": 32}),
+    ("aikc,ckj->jai", "k", {"a": 2, "i": 11, "j": 9, "k": 96, "c": 3}, {"k": 24}),
+    ("ij,j->i", "ij", {"i": 60, "j": 80}, {"i": 20, "j": 16}),                  # a matrix and a vector
+    ("ij,ij->", "i", {"i": 40, "j": 70}, {"i": 8}),                             # one number
+    ("ix,jx->ijx", "", {"i": 5, "j": 6, "x": 7}, {}),                           # nothing contracted
+]
+
+
+@pytest.mark.parametrize("how", ["einsum", "async", "noalloc"])
+@pytest.mark.parametrize("case", range(len(PLANS)))
+def test_product(orc, case, how):
+    e, up, ext, til = PLANS[case]
+    run(orc, e, up, ext, til, "bf16", seed=case, how=how)
+
+
+@pytest.mark.parametrize("case", range(len(PLANS)))
+def test_product_bf16_out(orc, case):
+    e, up, ext, til = PLANS[case]
+    run(orc, e, up, ext, til, "f32", seed=100 + case, w_bf16=True, keep=1.0)
+
+
+@pytest.mark.parametrize("unit", [1, 2, 3, 7])
+def test_product_split_keys(orc, unit):
+    """Keys cut into units: partial tiles summed after, in fp32 and bf16."""
+    for i, (e, up, ext, til) in enumerate(PLANS):
+        if "j" in up or "n" in up and "v" in up:
+            run(orc, e, up, ext, til, "bf16", seed=200 + i, max_pairs_per_unit=unit)
+            run(orc, e, up, ext, til, "bf16", seed=300 + i, max_pairs_per_unit=unit, w_bf16=True, how="execute")
+
+
+def test_no_pairs(orc):
+    e, up, ext, til = PLANS[6]
+    for how in ("einsum", "async", "execute"):
+        run(orc, e, up, ext, til, keep=0.0, how=how)
+
+
+@pytest.mark.parametrize("m,n,k", [(256, 256, 128), (256, 256, 640), (300, 515, 384), (129, 255, 2048), (512, 384, 1024),
+                                   (1, 1000, 4096), (16, 260, 1500), (33, 129, 256), (64, 512, 64), (200, 200, 32)])
+def test_product_large_tiles(m, n, k):
+    """Tiles of several blocks, against float64 on the quantised values (read
+    back, which the tests above hold to the oracle)."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    g = torch.Generator(device="cuda").manual_seed(m + n + k)
+    for e, w_bf16 in (("ik,jk->ij", False), ("ik,jk->ji", True), ("ik,kj->ij", True)):
+        plan = tre.Plan(e, "i", {"i": 2 * m, "j": n, "k": k}, {"i": m}, "mxfp4", w_bf16=w_bf16)
+        u = torch.randn((2, m * k), generator=g, device="cuda")
+        v = torch.randn((1, n * k), generator=g, device="cuda")
+        uq, vq = tre.mx_quantize(plan, "u", u), tre.mx_quantize(plan, "v", v)
+        ud = tre.mx_dequantize(plan, "u", uq).double().view(2 * m, k)
+        vd = tre.mx_dequantize(plan, "v", vq).double()
+        vd = vd.view(k, n) if e.startswith("ik,kj") else vd.view(n, k).T
+        ref, mag = ud @ vd, ud.abs() @ vd.abs()
+        keys = torch.arange(2, dtype=torch.int32, device="cuda").reshape(2, 1)
+        out = tre.einsum(plan, keys, uq, None, vq).w_tiles.double()
+        out = out.view(2, n, m).transpose(1, 2).reshape(2 * m, n) if e.endswith("ji") else out.view(2 * m, n)
+        tol = (k + 128) * U32 * mag + (UB16 * ref.abs() if w_bf16 else 0)
+        assert bool(((out - ref).abs() <= tol).all())
+        if not w_bf16:
+            assert float((out - ref).norm() / ref.norm()) <= 1e-6
+
+
+def test_not_finite():
+    """A block that is not finite makes the sums that it enters NaN, and no others."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    for k in (20, 60, 100, 400):
+        plan = tre.Plan("ik,jk->ij", "", {"i": 40, "j": 50, "k": k}, {}, "mxfp4")
+        u = torch.randn((40, k), device="cuda")
+        v = torch.randn((50, k), device="cuda")
+        u[3, k // 2], u[39, 0], v[7, k - 1] = float("nan"), float("inf"), -float("inf")
+        w = tre.einsum(plan, None, tre.mx_quantize(plan, "u", u.view(1, -1)), None, tre.mx_quantize(plan, "v", v.view(1, -1)))
+        bad = torch.zeros((40, 50), dtype=torch.bool, device="cuda")
+        bad[3], bad[39], bad[:, 7] = True, True, True
+        assert torch.equal(w.w_tiles.view(40, 50).isnan(), bad)
+
+
+def test_same_bits_streams_and_graphs():
+    """Two calls give the same bits; on another stream and replayed from a graph
+    too, between eager calls that use the same workspace."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    n, c, t = 1024, 200, 64
+    plan = tre.Plan("ij,jk->ik", "ij", {"i": n, "j": n, "k": c}, {"i": t, "j": t}, "mxfp4", max_pairs_per_unit=3)
+    nb = n // t
+    keys = torch.cartesian_prod(torch.arange(nb), torch.arange(nb)).to(torch.int32).cuda()
+    bk = torch.arange(nb, dtype=torch.int32, device="cuda").reshape(nb, 1)
+    a = torch.randn((nb * nb, t * t), device="cuda").to(torch.bfloat16)
+    b = torch.randn((nb, t * c), device="cuda").to(torch.bfloat16)
+    ws = tre.alloc_workspace(plan.workspace_bytes(nb * nb, nb, nb * nb))
+    wk, wt = torch.zeros((nb, 1), dtype=torch.int32, device="cuda"), torch.zeros((nb, t * c), device="cuda")
+    counts = torch.zeros(4, dtype=torch.int64, device="cuda")
+    aq, bq = tre.mx_quantize(plan, "u", a), torch.zeros((nb, plan.tile_bytes[1]), dtype=torch.uint8, device="cuda")
+
+    def step():
+        tre.mx_quantize(plan, "v", b, out=bq)
+        tre.execute_async(plan, keys, aq, bk, bq, wk, wt, ws, counts)
+
+    step()
+    torch.cuda.synchronize()
+    first = wt.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    wt.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    out = tre.mx_quantize(plan, "v", b, stream=side)
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    assert torch.equal(wt, first) and torch.equal(out, bq)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        b.copy_(torch.randn_like(b.float()))
+        step()
+        torch.cuda.synchronize()
+        want = wt.clone()
+        wt.zero_()
+        bq.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(wt, want), i
