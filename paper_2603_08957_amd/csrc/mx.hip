@@ -7,6 +7,7 @@
 // v_mfma_scale_f32_16x16x128_f8f6f4 does for four blocks at a time: lane l
 // holds the 32 codes (16 bytes) and the scale byte of row l % 16, block l / 16,
 // of either operand, and element (4 (l / 16) + i, l % 16) of the sums.
+#include "lds_copy.h"
 #include "mx.h"
 #include "tre_internal.h"
 
@@ -141,6 +142,43 @@ struct MxArgs {
     float* partials;
 };
 
+// The sums of a wavefront's TM x TN tiles, whose first is at (m0, n0), to the
+// output or partial tile.
+template <int TM, int TN>
+__device__ inline void mx_store(const MxArgs& g, const Unit& u, int b, int m0, int n0, const f32x4 (&acc)[TM][TN]) {
+    const int lane = threadIdx.x & 63, r = lane & 15, gr = lane >> 4;
+    const int64_t base = (u.slot >= 0 ? int64_t(u.slot) : int64_t(u.seg)) * g.w_elems + (g.batched ? g.tWB[b] : 0);
+    const bool half = g.w_bf16 && u.slot < 0;
+    float* out = u.slot >= 0 ? g.partials : g.W;
+    int32_t col[TN];
+    bool in[TN];
+#pragma unroll
+    for (int j = 0; j < TN; j++) {
+        const int n = n0 + 16 * j + r;
+        in[j] = n < g.N;
+        col[j] = g.w_affine || !in[j] ? n : g.tWN[n];
+    }
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const int m = m0 + 16 * i + 4 * gr + e;
+            if (m >= g.M) continue;
+            const int64_t row = base + (g.w_affine ? m * g.w_sm : int64_t(g.tWM[m]));
+            if (half) {
+                uint16_t* at = reinterpret_cast<uint16_t*>(out) + row;
+#pragma unroll
+                for (int j = 0; j < TN; j++)
+                    if (in[j]) at[col[j]] = f32_to_bf16_rne(acc[i][j][e]);
+            } else {
+                float* at = out + row;
+#pragma unroll
+                for (int j = 0; j < TN; j++)
+                    if (in[j]) at[col[j]] = acc[i][j][e];
+            }
+        }
+}
+
 // Four wavefronts side by side along N, each with TM x TN tiles of 16 x 16.
 template <int TM, int TN>
 __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
@@ -194,30 +232,151 @@ __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
             for (int j = 0; j < TN; j++)
                 acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 0, sa[i], 0, sb[j]);
     }
-    const int64_t base = (u.slot >= 0 ? int64_t(u.slot) : int64_t(u.seg)) * g.w_elems + (g.batched ? g.tWB[b] : 0);
-    const bool half = g.w_bf16 && u.slot < 0;
-    float* out = u.slot >= 0 ? g.partials : g.W;
+    mx_store(g, u, b, m0, n0, acc);
+}
+
+// Rows of four blocks or more: 2 x 2 wavefronts, each with TM x TN tiles, read
+// their fragments from LDS.  A stage is four blocks of every row of one pair,
+// copied straight into LDS two stages ahead.
+//
+// A stage's codes are [row][4 blocks of 16 bytes], block k of row r in slot
+// k ^ ((r >> 1 ^ r >> 3) & 3): the eight or sixteen lanes that read together
+// then meet every bank once.  A row's four scale bytes are one dword; those of
+// a lane's TM (TN) rows, which lie 16 rows apart, are side by side.
+constexpr int kStages = 3;
+
+// An index list read by scalar loads: the compiler would take vector loads for
+// one that the copies' assembly might write, and wait for the copies with them.
+__device__ inline int32_t pair_index(const int32_t* list, int64_t i) {
+    typedef const __attribute__((address_space(4))) int32_t* constant;
+    return reinterpret_cast<constant>(reinterpret_cast<uintptr_t>(list))[i];
+}
+
+__device__ inline int mx_slot(int r, int k) { return k ^ ((r >> 1 ^ r >> 3) & 3); }
+
+template <int TM, int TN>
+constexpr int mx_stage_bytes() { return (32 * TM + 32 * TN) * 68; }
+
+template <int TM, int TN>
+__global__ __launch_bounds__(kThreads) void k_mx_lds(MxArgs g) {
+    extern __shared__ __align__(16) char lds[];
+    constexpr int BM = 32 * TM, BN = 32 * TN, ROWS = BM + BN, kStage = mx_stage_bytes<TM, TN>();
+    const int64_t unit = blockIdx.x / g.wg_blocks;
+    if (unit >= g.hdr->n_units) return;
+    const Unit u = g.units[unit];
+    int x = int(blockIdx.x - unit * g.wg_blocks);
+    const int nb = x % g.n_blocks;
+    x /= g.n_blocks;
+    const int mb = x % g.m_blocks, b = x / g.m_blocks;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, gr = lane >> 4;
+    const int wm = w >> 1, wn = w & 1;
+    const int steps = g.blocks / 4;  // stages of a pair
+
+    // this wavefront's copies of a stage: codes 16 rows at a time (A's rows,
+    // then B's), scales 64 at a time.  Rows past the last copy the last.
+    constexpr int NC = ROWS / 16 / 4, NS = (ROWS / 64 + 3) / 4;
+    static_assert(ROWS % 64 == 0, "a wavefront copies whole groups of rows");
+    auto row_of = [&](int row) {
+        return row < BM ? b * g.M + min(mb * BM + row, g.M - 1) : b * g.N + min(nb * BN + row - BM, g.N - 1);
+    };
+    uint32_t voff[NC], vsc[NS];
+#pragma unroll
+    for (int i = 0; i < NC; i++) {
+        const int row = (w + 4 * i) * 16 + (lane >> 2);
+        voff[i] = uint32_t(row_of(row) * g.blocks + mx_slot(row & 15, lane & 3)) * 16u;
+    }
+#pragma unroll
+    for (int i = 0; i < NS; i++) {
+        // position (half, r, tile) holds row 16 (tiles half + tile) + r
+        const int p = min((w + 4 * i) * 64, ROWS - 64) + lane;
+        const bool a = p < BM;
+        const int T = a ? TM : TN, q = a ? p : p - BM, half = q / (16 * T), rr = q % (16 * T) / T, t = q % T;
+        vsc[i] = uint32_t(row_of((a ? 0 : BM) + (half * T + t) * 16 + rr) * g.blocks);
+    }
+    const uint32_t lds0 = lds_address(lds);
+    const int64_t total = int64_t(u.p1 - u.p0) * steps;
+    // where the next stage to copy begins; the pair after its own is known
+    int64_t pair = u.p0;
+    int step = 0;
+    const uint8_t *at = g.A + pair_index(g.pa, pair) * g.a_bytes, *bt = g.B + pair_index(g.pb, pair) * g.b_bytes;
+    int64_t after = min(pair + 1, int64_t(u.p1) - 1);
+    int32_t a_next = pair_index(g.pa, after), b_next = pair_index(g.pb, after);
+    auto copy = [&](int slot) {
+        const uint32_t l = lds0 + uint32_t(slot) * kStage;
+#pragma unroll
+        for (int i = 0; i < NC; i++) {
+            const int rows = (w + 4 * i) * 16;
+            lds_copy16<false>(l + rows * 64, (rows < BM ? at : bt) + step * 64, voff[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NS; i++) {
+            const int p = (w + 4 * i) * 64;
+            if (p < ROWS) lds_copy4(l + ROWS * 64 + p * 4, (p < BM ? at + g.a_scales : bt + g.b_scales) + step * 4, vsc[i]);
+        }
+        if (++step == steps) {
+            step = 0;
+            at = g.A + a_next * g.a_bytes;
+            bt = g.B + b_next * g.b_bytes;
+            after = min(after + 1, int64_t(u.p1) - 1);
+            a_next = pair_index(g.pa, after);
+            b_next = pair_index(g.pb, after);
+        }
+    };
+    f32x4 acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; i++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int m = m0 + 16 * i + 4 * gr + e;
-            if (m >= g.M) continue;
-            const int64_t row = base + (g.w_affine ? m * g.w_sm : int64_t(g.tWM[m]));
-#pragma unroll
-            for (int j = 0; j < TN; j++) {
-                const int n = n0 + 16 * j + r;
-                if (n >= g.N) continue;
-                const int64_t o = row + (g.w_affine ? n : g.tWN[n]);
-                if (half) reinterpret_cast<uint16_t*>(out)[o] = f32_to_bf16_rne(acc[i][j][e]);
-                else out[o] = acc[i][j][e];
-            }
+        for (int j = 0; j < TN; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    copy(0);
+    if (total > 1) copy(1);
+    int now = 0;
+    for (int64_t s = 0; s < total; s++) {
+        // this stage's copies have landed once every wavefront has waited for
+        // its own (the next stage's may be in flight); the barrier also says
+        // that the stage before, whose place the copies below take, is read
+        if (s + 1 < total) {
+            if (ROWS / 64 == 4 * NS || w < ROWS / 64 % 4) lds_copy_wait<NC + NS>();
+            else lds_copy_wait<NC + NS - 1>();
+        } else {
+            lds_copy_wait<0>();
         }
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");  // no read of LDS moves up past it
+        const int then = now >= 1 ? now - 1 : now + 2;  // (now + 2) % 3
+        if (s + 2 < total) copy(then);
+        const char* l = lds + now * kStage;
+        now = now == 2 ? 0 : now + 1;
+        i32x8 fa[TM], fb[TN];
+        uint32_t sa[TM], sb[TN];
+        const int sl = mx_slot(r, gr) * 16;
+#pragma unroll
+        for (int i = 0; i < TM; i++) {
+            const uint4 c = *reinterpret_cast<const uint4*>(l + ((wm * TM + i) * 16 + r) * 64 + sl);
+            fa[i] = i32x8{int(c.x), int(c.y), int(c.z), int(c.w), 0, 0, 0, 0};
+            sa[i] = reinterpret_cast<const uint32_t*>(l + ROWS * 64)[wm * 16 * TM + r * TM + i] >> (8 * gr);
+        }
+#pragma unroll
+        for (int j = 0; j < TN; j++) {
+            const uint4 c = *reinterpret_cast<const uint4*>(l + (BM + (wn * TN + j) * 16 + r) * 64 + sl);
+            fb[j] = i32x8{int(c.x), int(c.y), int(c.z), int(c.w), 0, 0, 0, 0};
+            sb[j] = reinterpret_cast<const uint32_t*>(l + ROWS * 64)[BM + wn * 16 * TN + r * TN + j] >> (8 * gr);
+        }
+#pragma unroll
+        for (int j = 0; j < TN; j++)
+#pragma unroll
+            for (int i = 0; i < TM; i++)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 0, int(sa[i]), 0,
+                                                                             int(sb[j]));
+        lds_read_wait();
+    }
+    mx_store(g, u, b, mb * BM + wm * 16 * TM, nb * BN + wn * 16 * TN, acc);
 }
 
+// How a plan's tiles are cut among workgroups.
 struct MxShape {
     int64_t M, N;
-    int tm, tn;
+    bool lds;
+    int tm, tn;  // 16 x 16 tiles of a wavefront
     int64_t m_blocks, n_blocks;
 };
 
@@ -225,11 +384,43 @@ MxShape mx_shape(const Plan& p) {
     MxShape h;
     h.M = p.swap ? p.nN : p.nM;
     h.N = p.swap ? p.nM : p.nN;
+    h.lds = p.mx_blocks >= 4 && h.M > 32 && h.N > 32;
+    if (h.lds) {
+        // of 256, 128 or 64 rows the one that leaves the fewest places empty, the larger of two alike
+        auto cut = [](int64_t n) {
+            int best = 8;
+            for (int t : {4, 2})
+                if ((n + 32 * t - 1) / (32 * t) * t < (n + 32 * best - 1) / (32 * best) * best) best = t;
+            return best;
+        };
+        h.tm = cut(h.M);
+        h.tn = cut(h.N);
+        h.m_blocks = (h.M + 32 * h.tm - 1) / (32 * h.tm);
+        h.n_blocks = (h.N + 32 * h.tn - 1) / (32 * h.tn);
+        return h;
+    }
     h.tm = h.M > 32 ? 4 : h.M > 16 ? 2 : 1;
     h.tn = h.N > 64 ? 2 : 1;
     h.m_blocks = (h.M + 16 * h.tm - 1) / (16 * h.tm);
     h.n_blocks = (h.N + 64 * h.tn - 1) / (64 * h.tn);
     return h;
+}
+
+template <int TM, int TN>
+hipError_t run_lds(const MxArgs& g, dim3 grid, hipStream_t s) {
+    constexpr int bytes = kStages * mx_stage_bytes<TM, TN>();
+    // above 64 KB the kernel has to be told once per device (here: per call, a host-side note)
+    if (bytes > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_mx_lds<TM, TN>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
+    return launch_k(k_mx_lds<TM, TN>, grid, dim3{unsigned(kThreads)}, size_t(bytes), s, g);
+}
+
+template <int TM>
+hipError_t run_lds_n(int tn, const MxArgs& g, dim3 grid, hipStream_t s) {
+    return tn == 8 ? run_lds<TM, 8>(g, grid, s) : tn == 4 ? run_lds<TM, 4>(g, grid, s) : run_lds<TM, 2>(g, grid, s);
 }
 
 }  // namespace
@@ -301,6 +492,8 @@ hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_til
     g.W = w_tiles;
     g.partials = reinterpret_cast<float*>(ws + L.partials);
     const dim3 grid{unsigned(wg * unit_bound)}, block{unsigned(kThreads)};
+    if (h.lds)
+        return h.tm == 8 ? run_lds_n<8>(h.tn, g, grid, s) : h.tm == 4 ? run_lds_n<4>(h.tn, g, grid, s) : run_lds_n<2>(h.tn, g, grid, s);
     if (h.tm == 4)
         return h.tn == 2 ? launch_k(k_mx<4, 2>, grid, block, 0, s, g) : launch_k(k_mx<4, 1>, grid, block, 0, s, g);
     if (h.tm == 2)
