@@ -38,9 +38,22 @@ __device__ inline int64_t offset_of(const Dims& d, int64_t x) {
     return d.n ? o + x * d.stride[0] : 0;
 }
 
+// Division of x < 2^31 by d: with 2^(s - 1) < d <= 2^s and m = ceil(2^(31 + s) / d),
+// x m / 2^(31 + s) lies above x / d by less than x 2^-(31 + s) < 1 / d.
+struct Divisor {
+    uint32_t d = 1, m = 0, s = 0;
+    Divisor() = default;
+    explicit Divisor(int64_t by) : d(uint32_t(by)) {
+        while ((int64_t(1) << s) < by) s++;
+        if (s) m = uint32_t(((uint64_t(1) << (31 + s)) + d - 1) / d);
+    }
+    __device__ uint32_t of(uint32_t x) const { return s ? __umulhi(x, m) >> (s - 1) : x; }
+};
+
 // An operand's tiles before and after.
 struct MxTiles {
     Dims row, k;
+    Divisor tile, line;  // eights of a tile, of a row
     int64_t elems;      // of an unquantised tile
     int64_t rows, K;
     int64_t blocks;     // of a row
@@ -55,7 +68,20 @@ __device__ inline int scale_byte(uint32_t max_bits) {
     return max_bits >= 0x7f800000u ? kMxNanScale : max(int(max_bits >> 23) - 2, 0);
 }
 
-// A thread per block.
+// The codes of eight values under a scale byte.  (The conversion takes its
+// scale from the exponent field alone: a byte of 0 is 2^-127.)
+__device__ inline uint32_t codes8(const float* v, int sb) {
+    const float s = __uint_as_float(uint32_t(sb) << 23);
+    uint32_t q = 0;
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[0], v[1], s, 0);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[2], v[3], s, 1);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[4], v[5], s, 2);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[6], v[7], s, 3);
+    return sb == kMxNanScale ? 0u : q;
+}
+
+// ---- any layout: a thread per block
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxTiles g, const T* __restrict__ src, uint8_t* __restrict__ dst) {
     const int64_t b = int64_t(blockIdx.x) * kThreads + threadIdx.x;
@@ -71,18 +97,9 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxTiles g, const T* __
         m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
     }
     const int sb = scale_byte(m);
-    // (the conversion takes its scale from the exponent field alone: 0 is 2^-127)
-    const float s = __uint_as_float(uint32_t(sb) << 23);
-    uint32_t q[4] = {0, 0, 0, 0};
-    if (sb != kMxNanScale) {
+    uint32_t q[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q[i], v[8 * i], v[8 * i + 1], s, 0);
-            q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q[i], v[8 * i + 2], v[8 * i + 3], s, 1);
-            q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q[i], v[8 * i + 4], v[8 * i + 5], s, 2);
-            q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q[i], v[8 * i + 6], v[8 * i + 7], s, 3);
-        }
-    }
+    for (int i = 0; i < 4; i++) q[i] = codes8(v + 8 * i, sb);
     uint8_t* out = dst + t * g.bytes;
     *reinterpret_cast<uint4*>(out + x * 16) = make_uint4(q[0], q[1], q[2], q[3]);
     out[per * 16 + x] = uint8_t(sb);
@@ -107,6 +124,308 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantize(MxTiles g, const uin
         for (int j = 0; j < 8; j++) {
             const int64_t k = k0 + 8 * i + j;
             if (k < g.K) put(at + offset_of(g.k, k), v[j]);
+        }
+    }
+}
+
+// ---- the contracted index consecutive in the tile: a lane per eight values,
+// four to a block, so a wavefront's loads and stores are whole runs of the
+// row.  (A thread per block reads 64 bytes apart: 134 M bf16 values took 294 us
+// to quantise and 588 to read back.)
+
+constexpr int kRun = 4;  // eights of a thread, a workgroup's width apart, in flight together
+
+// Eight values of a row as they are loaded: rows begin on any element.
+typedef uint32_t u32x4_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+template <typename T>
+struct Eight;
+
+template <>
+struct Eight<uint16_t> {
+    uint32_t v[4];
+    __device__ void load(const uint16_t* p, int64_t n) {
+        if (n >= 8) {
+            const u32x4_2 a = *reinterpret_cast<const u32x4_2*>(p);
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[i] = a[i];
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            v[i] = (2 * i < n ? uint32_t(p[2 * i]) : 0u) | (2 * i + 1 < n ? uint32_t(p[2 * i + 1]) << 16 : 0u);
+    }
+    // the eight from k on of a row of K, a multiple of eight; zeros past it
+    __device__ void load_or_zero(const uint16_t* row, uint32_t k, uint32_t K) {
+        load(row + min(k, K - 8), 8);
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] = k < K ? v[i] : 0u;
+    }
+    // bits of the largest magnitude, as fp32
+    __device__ uint32_t top() const {
+        u16x2 m = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; i++) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[i] & 0x7fff7fffu));
+        return uint32_t(max(m[0], m[1])) << 16;
+    }
+    __device__ uint32_t codes(int sb) const {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        const float s = __uint_as_float(uint32_t(sb) << 23);
+        uint32_t q = 0;
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2, v[0]), s, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2, v[1]), s, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2, v[2]), s, 2);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2, v[3]), s, 3);
+        return sb == kMxNanScale ? 0u : q;
+    }
+};
+
+template <>
+struct Eight<float> {
+    float v[8];
+    __device__ void load(const float* p, int64_t n) {
+        if (n >= 8) {
+            const u32x4_4 a = *reinterpret_cast<const u32x4_4*>(p), b = *reinterpret_cast<const u32x4_4*>(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                v[i] = __uint_as_float(a[i]);
+                v[4 + i] = __uint_as_float(b[i]);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = i < n ? p[i] : 0.f;
+    }
+    __device__ void load_or_zero(const float* row, uint32_t k, uint32_t K) {
+        load(row + min(k, K - 8), 8);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = k < K ? v[i] : 0.f;
+    }
+    __device__ uint32_t top() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+        return m;
+    }
+    __device__ uint32_t codes(int sb) const { return codes8(v, sb); }
+};
+
+// the maximum over the four lanes of a quad
+__device__ inline uint32_t quad_max(uint32_t m) {
+    m = max(m, uint32_t(__builtin_amdgcn_mov_dpp(int(m), 0xB1, 0xf, 0xf, true)));  // lanes 1 0 3 2
+    return max(m, uint32_t(__builtin_amdgcn_mov_dpp(int(m), 0x4E, 0xf, 0xf, true)));  // lanes 2 3 0 1
+}
+
+// The eights of a workgroup: kRun * kThreads consecutive ones, g.line to a row
+// and g.tile to a tile, the first found in 64 bits and the others from it in 32.
+struct RunPos {
+    int64_t t0;
+    uint32_t w0;
+};
+__device__ inline RunPos run_pos(const MxTiles& g) {
+    const int64_t q = int64_t(blockIdx.x) * (kRun * kThreads), t = q / g.tile.d;
+    return RunPos{t, uint32_t(q - t * g.tile.d)};
+}
+
+// How a row's eights lie in the unquantised tile: one after the other through
+// the whole tile; whole, but rows begin anywhere or end in zeros; the last cut.
+enum RunKind { RUN_LINEAR, RUN_WHOLE, RUN_CUT };
+
+template <typename T, RunKind KIND>
+__global__ __launch_bounds__(kThreads) void k_mx_quantize_rows(MxTiles g, const T* __restrict__ src, uint8_t* __restrict__ dst) {
+    const RunPos p = run_pos(g);
+    const int64_t scales = g.rows * g.blocks * 16;
+    Eight<T> v[kRun];
+    uint32_t dt[kRun], w[kRun];  // tile after the first, eight in the tile
+    bool in[kRun];
+#pragma unroll
+    for (int i = 0; i < kRun; i++) {
+        const uint32_t x = p.w0 + i * kThreads + threadIdx.x;
+        dt[i] = g.tile.of(x);
+        w[i] = x - dt[i] * g.tile.d;
+        in[i] = p.t0 + dt[i] < g.n;
+        // (past the last tile: the first tile again, not written)
+        const T* at = src + (p.t0 + (in[i] ? dt[i] : 0)) * g.elems;
+        if constexpr (KIND == RUN_LINEAR) {
+            v[i].load(at + uint64_t(w[i]) * 8, 8);
+        } else {
+            const uint32_t r = g.line.of(w[i]), k = (w[i] - r * g.line.d) * 8;
+            at += g.row.n <= 1 ? int64_t(r) * g.row.stride[0] : offset_of(g.row, r);
+            if constexpr (KIND == RUN_WHOLE) v[i].load_or_zero(at, k, uint32_t(g.K));
+            else v[i].load(at + k, g.K - k);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kRun; i++) {
+        const int sb = scale_byte(quad_max(v[i].top()));
+        if (!in[i]) continue;
+        uint8_t* out = dst + (p.t0 + dt[i]) * g.bytes;
+        *reinterpret_cast<uint32_t*>(out + uint64_t(w[i]) * 4) = v[i].codes(sb);
+        if ((w[i] & 3) == 0) out[scales + w[i] / 4] = uint8_t(sb);
+    }
+}
+
+// (g.line: the eights of a row that reach into K; blocks past it are not read)
+template <typename T, bool CUT>
+__global__ __launch_bounds__(kThreads) void k_mx_dequantize_rows(MxTiles g, const uint8_t* __restrict__ src, T* __restrict__ dst) {
+    const RunPos p = run_pos(g);
+    const int64_t scales = g.rows * g.blocks * 16;
+    uint32_t q[kRun], dt[kRun], r[kRun], k[kRun];
+    int sb[kRun];
+    bool in[kRun];
+#pragma unroll
+    for (int i = 0; i < kRun; i++) {
+        const uint32_t x = p.w0 + i * kThreads + threadIdx.x;
+        dt[i] = g.tile.of(x);
+        const uint32_t w = x - dt[i] * g.tile.d;
+        in[i] = p.t0 + dt[i] < g.n;
+        r[i] = g.line.of(w);
+        k[i] = (w - r[i] * g.line.d) * 8;
+        const uint8_t* at = src + (p.t0 + (in[i] ? dt[i] : 0)) * g.bytes;
+        const uint32_t b = r[i] * uint32_t(g.blocks) + k[i] / kMxBlock;
+        q[i] = *reinterpret_cast<const uint32_t*>(at + uint64_t(b) * 16 + (k[i] % kMxBlock) / 2);
+        sb[i] = at[scales + b];
+    }
+#pragma unroll
+    for (int i = 0; i < kRun; i++) {
+        if (!in[i]) continue;
+        T* out = dst + (p.t0 + dt[i]) * g.elems + (g.row.n <= 1 ? int64_t(r[i]) * g.row.stride[0] : offset_of(g.row, r[i])) + k[i];
+        float v[8];
+        mx_values(q[i], sb[i], v);
+        if (!CUT || g.K - k[i] >= 8) {
+            if constexpr (sizeof(T) == 2) {
+                u32x4_2 a;
+#pragma unroll
+                for (int j = 0; j < 4; j++) a[j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]), 0x07060302u);
+                *reinterpret_cast<u32x4_2*>(out) = a;
+            } else {
+                u32x4_4 a, b;
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    a[j] = __float_as_uint(v[j]);
+                    b[j] = __float_as_uint(v[4 + j]);
+                }
+                *reinterpret_cast<u32x4_4*>(out) = a;
+                *reinterpret_cast<u32x4_4*>(out + 4) = b;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (k[i] + j < g.K) put(out + j, v[j]);
+        }
+    }
+}
+
+// ---- the rows consecutive in the tile (two or more: of one row the contracted
+// index is consecutive): a thread per block of one fp32 row or two bf16 rows,
+// so that lanes side by side read consecutive rows of one k.  The last of an
+// odd number of bf16 rows goes with the row before it once more.
+
+// A thread's tile, block and first row; g.line: lines (of R rows) of a tile,
+// g.tile: lines and blocks.
+struct ColPos {
+    int64_t t;
+    uint32_t kb, r;
+};
+template <int R>
+__device__ inline ColPos col_pos(const MxTiles& g) {
+    const int64_t x0 = int64_t(blockIdx.x) * kThreads, t0 = x0 / g.tile.d;
+    const uint32_t x = uint32_t(x0 - t0 * g.tile.d) + threadIdx.x, dt = g.tile.of(x), w = x - dt * g.tile.d;
+    ColPos p;
+    p.t = t0 + dt;
+    p.kb = g.line.of(w);
+    p.r = min((w - p.kb * g.line.d) * R, uint32_t(g.rows) - R);
+    return p;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_mx_quantize_cols(MxTiles g, const T* __restrict__ src, uint8_t* __restrict__ dst) {
+    constexpr int R = sizeof(T) == 2 ? 2 : 1;
+    typedef uint32_t u32_2 __attribute__((aligned(2)));
+    const ColPos p = col_pos<R>(g);
+    if (p.t >= g.n) return;
+    const int left = int(min(g.K - int64_t(p.kb) * kMxBlock, int64_t(kMxBlock)));  // below 1: a block of zeros
+    const int64_t sk = g.k.stride[0];
+    // k past the last reads the last (of a block past K: the tile's first) and counts as zero
+    const T* at = src + p.t * g.elems + (left > 0 ? int64_t(p.kb) * kMxBlock * sk : 0) + p.r;
+    uint32_t v[kMxBlock];  // bf16: both rows of a k
+#pragma unroll
+    for (int i = 0; i < kMxBlock; i++) {
+        v[i] = *reinterpret_cast<const u32_2*>(at);
+        if (i + 1 < left) at += sk;
+    }
+#pragma unroll
+    for (int i = 0; i < kMxBlock; i++) v[i] = i < left ? v[i] : 0u;
+    uint8_t* out = dst + p.t * g.bytes;
+    const int64_t b0 = int64_t(p.r) * g.blocks + p.kb, scales = g.rows * g.blocks * 16;
+    if constexpr (R == 1) {
+        uint32_t m = 0;
+        float f[kMxBlock];
+#pragma unroll
+        for (int i = 0; i < kMxBlock; i++) {
+            m = max(m, v[i] & 0x7fffffffu);
+            f[i] = __uint_as_float(v[i]);
+        }
+        const int sb = scale_byte(m);
+        *reinterpret_cast<uint4*>(out + b0 * 16) =
+            make_uint4(codes8(f, sb), codes8(f + 8, sb), codes8(f + 16, sb), codes8(f + 24, sb));
+        out[scales + b0] = uint8_t(sb);
+    } else {
+        u16x2 m = {0, 0};
+#pragma unroll
+        for (int i = 0; i < kMxBlock; i++) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[i] & 0x7fff7fffu));
+#pragma unroll
+        for (int h = 0; h < R; h++) {
+            const int sb = scale_byte(uint32_t(m[h]) << 16);
+            uint32_t q[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                Eight<uint16_t> e;
+#pragma unroll
+                for (int j = 0; j < 4; j++)  // the row's half of two k
+                    e.v[j] = __builtin_amdgcn_perm(v[8 * i + 2 * j + 1], v[8 * i + 2 * j], h ? 0x07060302u : 0x05040100u);
+                q[i] = e.codes(sb);
+            }
+            *reinterpret_cast<uint4*>(out + (b0 + h * g.blocks) * 16) = make_uint4(q[0], q[1], q[2], q[3]);
+            out[scales + b0 + h * g.blocks] = uint8_t(sb);
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_mx_dequantize_cols(MxTiles g, const uint8_t* __restrict__ src, T* __restrict__ dst) {
+    constexpr int R = sizeof(T) == 2 ? 2 : 1;
+    typedef uint32_t u32_2 __attribute__((aligned(2)));
+    const ColPos p = col_pos<R>(g);
+    if (p.t >= g.n) return;
+    const int left = int(min(g.K - int64_t(p.kb) * kMxBlock, int64_t(kMxBlock)));
+    const int64_t sk = g.k.stride[0];
+    T* at = dst + p.t * g.elems + int64_t(p.kb) * kMxBlock * sk + p.r;
+    const uint8_t* in = src + p.t * g.bytes;
+    const int64_t b0 = int64_t(p.r) * g.blocks + p.kb, scales = g.rows * g.blocks * 16;
+    uint4 c[R];
+    int sb[R];
+#pragma unroll
+    for (int h = 0; h < R; h++) {
+        c[h] = *reinterpret_cast<const uint4*>(in + (b0 + h * g.blocks) * 16);
+        sb[h] = in[scales + b0 + h * g.blocks];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        float v[R][8];
+#pragma unroll
+        for (int h = 0; h < R; h++) {
+            const uint32_t q[4] = {c[h].x, c[h].y, c[h].z, c[h].w};
+            mx_values(q[i], sb[h], v[h]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            if (8 * i + j >= left) return;
+            if constexpr (R == 1) put(at, v[0][j]);
+            else *reinterpret_cast<u32_2*>(at) = __builtin_amdgcn_perm(__float_as_uint(v[R - 1][j]), __float_as_uint(v[0][j]), 0x07060302u);
+            at += sk;
         }
     }
 }
@@ -425,28 +744,88 @@ hipError_t run_lds_n(int tn, const MxArgs& g, dim3 grid, hipStream_t s) {
 
 }  // namespace
 
+namespace {
+
+// How a tile is read or written: along its rows, across them, or element by element.
+enum MxWay { MX_ROWS, MX_COLS, MX_ANY };
+MxWay mx_way(const MxTiles& g) {
+    if (g.k.n == 0 || (g.k.n == 1 && g.k.stride[0] == 1)) return MX_ROWS;
+    if (g.k.n == 1 && g.row.n == 1 && g.row.stride[0] == 1) return MX_COLS;
+    return MX_ANY;
+}
+
+// Workgroups for `items` of `per` to a workgroup, 0 if they are too many.
+unsigned mx_grid(int64_t items, int64_t per) {
+    const int64_t b = (items + per - 1) / per;
+    return b > int64_t(0x7fffffff) ? 0u : unsigned(b);
+}
+
+// Threads to a tile across its rows, and where they stand.
+template <typename T>
+int64_t col_threads(MxTiles& g, int64_t blocks) {
+    constexpr int R = sizeof(T) == 2 ? 2 : 1;
+    const int64_t lines = (g.rows + R - 1) / R;
+    g.line = Divisor(lines);
+    g.tile = Divisor(lines * blocks);
+    return lines * blocks;
+}
+
+template <typename T>
+hipError_t quantize(MxTiles g, const T* src, uint8_t* dst, hipStream_t s) {
+    const MxWay way = mx_way(g);
+    if (way == MX_ROWS) {
+        g.line = Divisor(g.blocks * 4);
+        g.tile = Divisor(g.rows * g.blocks * 4);
+        const unsigned grid = mx_grid(g.n * g.rows * g.blocks * 4, kRun * kThreads);
+        if (!grid) return hipErrorInvalidConfiguration;
+        const bool side_by_side = g.row.n == 0 || (g.row.n == 1 && g.row.stride[0] == g.K);
+        if (side_by_side && g.K == g.blocks * kMxBlock) k_mx_quantize_rows<T, RUN_LINEAR><<<grid, kThreads, 0, s>>>(g, src, dst);
+        else if (g.K % 8 == 0) k_mx_quantize_rows<T, RUN_WHOLE><<<grid, kThreads, 0, s>>>(g, src, dst);
+        else k_mx_quantize_rows<T, RUN_CUT><<<grid, kThreads, 0, s>>>(g, src, dst);
+    } else {
+        const unsigned grid = mx_grid(g.n * (way == MX_COLS ? col_threads<T>(g, g.blocks) : g.rows * g.blocks), kThreads);
+        if (!grid) return hipErrorInvalidConfiguration;
+        if (way == MX_COLS) k_mx_quantize_cols<<<grid, kThreads, 0, s>>>(g, src, dst);
+        else k_mx_quantize<<<grid, kThreads, 0, s>>>(g, src, dst);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t dequantize(MxTiles g, const uint8_t* src, T* dst, hipStream_t s) {
+    const MxWay way = mx_way(g);
+    if (way == MX_ROWS) {
+        const int64_t line = (g.K + 7) / 8;
+        g.line = Divisor(line);
+        g.tile = Divisor(g.rows * line);
+        const unsigned grid = mx_grid(g.n * g.rows * line, kRun * kThreads);
+        if (!grid) return hipErrorInvalidConfiguration;
+        if (g.K % 8 == 0) k_mx_dequantize_rows<T, false><<<grid, kThreads, 0, s>>>(g, src, dst);
+        else k_mx_dequantize_rows<T, true><<<grid, kThreads, 0, s>>>(g, src, dst);
+    } else {
+        const unsigned grid = mx_grid(
+            g.n * (way == MX_COLS ? col_threads<T>(g, (g.K + kMxBlock - 1) / kMxBlock) : g.rows * g.blocks), kThreads);
+        if (!grid) return hipErrorInvalidConfiguration;
+        if (way == MX_COLS) k_mx_dequantize_cols<<<grid, kThreads, 0, s>>>(g, src, dst);
+        else k_mx_dequantize<<<grid, kThreads, 0, s>>>(g, src, dst);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
 hipError_t launch_mx_quantize(const Plan& p, int op, const void* tiles, int src_dtype, int64_t n, void* mx, hipStream_t s) {
     const MxTiles g = mx_tiles(p, op, n);
-    const int64_t grid = (n * g.rows * g.blocks + kThreads - 1) / kThreads;
-    if (grid > int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
     uint8_t* out = static_cast<uint8_t*>(mx);
-    if (src_dtype == TRE_BF16)
-        k_mx_quantize<<<unsigned(grid), kThreads, 0, s>>>(g, static_cast<const uint16_t*>(tiles), out);
-    else
-        k_mx_quantize<<<unsigned(grid), kThreads, 0, s>>>(g, static_cast<const float*>(tiles), out);
-    return hipGetLastError();
+    return src_dtype == TRE_BF16 ? quantize(g, static_cast<const uint16_t*>(tiles), out, s)
+                                 : quantize(g, static_cast<const float*>(tiles), out, s);
 }
 
 hipError_t launch_mx_dequantize(const Plan& p, int op, const void* mx, int64_t n, void* tiles, int dst_dtype, hipStream_t s) {
     const MxTiles g = mx_tiles(p, op, n);
-    const int64_t grid = (n * g.rows * g.blocks + kThreads - 1) / kThreads;
-    if (grid > int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
     const uint8_t* in = static_cast<const uint8_t*>(mx);
-    if (dst_dtype == TRE_BF16)
-        k_mx_dequantize<<<unsigned(grid), kThreads, 0, s>>>(g, in, static_cast<uint16_t*>(tiles));
-    else
-        k_mx_dequantize<<<unsigned(grid), kThreads, 0, s>>>(g, in, static_cast<float*>(tiles));
-    return hipGetLastError();
+    return dst_dtype == TRE_BF16 ? dequantize(g, in, static_cast<uint16_t*>(tiles), s)
+                                 : dequantize(g, in, static_cast<float*>(tiles), s);
 }
 
 int64_t mx_blocks_per_unit(const Plan& p) {
