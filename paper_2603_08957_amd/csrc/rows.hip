@@ -82,6 +82,21 @@ __device__ inline int64_t token(const void* ids, int id_bytes, int64_t t) {
     return id_bytes == 8 ? static_cast<const int64_t*>(ids)[t] : int64_t(static_cast<const int32_t*>(ids)[t]);
 }
 
+// How threads lie on rows: `lanes` (a power of two, at most a wavefront) side by
+// side on a row, each with some consecutive elements, `slices` such strips to a
+// row; a row of few elements then shares its wavefront with others.
+struct Strip {
+    int32_t shift;   // lanes = 1 << shift
+    int64_t slices;
+};
+Strip strip(int64_t elems, int per_lane) {
+    Strip p{0, 1};
+    while (p.shift < 6 && (int64_t(per_lane) << p.shift) < elems) p.shift++;
+    const int64_t w = int64_t(per_lane) << p.shift;
+    p.slices = (elems + w - 1) / w;
+    return p;
+}
+
 // ----------------------------------------------------------------- lookup
 
 struct LookupArgs {
@@ -90,7 +105,8 @@ struct LookupArgs {
     void* out;
     int64_t* status;
     int64_t n_rows, elems, n_ids;
-    int64_t slices;              // of a row
+    int64_t groups;              // of kStrips strips or rows
+    Strip strip;
     int64_t tile_rows, blocks;   // 4-bit tiles: rows of a tile, blocks of a row
     int64_t tile_bytes;
     float scale;
@@ -99,141 +115,285 @@ struct LookupArgs {
 
 struct Mx4 {};
 
-// A wavefront per row and slice.
-template <typename TI, typename TO>
+// Strips of a row (WIDE), or rows, that a thread has in flight together: a
+// wavefront that moves one strip lives too short for its launch (131,072 rows
+// of 4,096 bf16 values 406 us).
+constexpr int kStrips = 4;
+
+template <typename TI>
+__device__ inline void lookup_load(const LookupArgs& g, int64_t id, int64_t e, float (&v)[kLane]) {
+    if constexpr (std::is_same_v<TI, Mx4>) {
+        const int64_t tile = id / g.tile_rows, row = (id - tile * g.tile_rows) * g.blocks;
+        const uint8_t* at = static_cast<const uint8_t*>(g.table) + tile * g.tile_bytes;
+        const uint32_t q = *reinterpret_cast<const uint32_t*>(at + row * 16 + e / 2);
+        mx_values(q, at[g.tile_rows * g.blocks * 16 + row + e / kMxBlock], v);
+    } else {
+        load_run(static_cast<const TI*>(g.table) + id * g.elems, e, g.elems, v);
+    }
+}
+
+template <typename TI, typename TO, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
-    const int64_t x = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-    const int64_t t = x / g.slices;
-    if (t >= g.n_ids) return;
-    const int64_t e = (x - t * g.slices) * kSlice + (threadIdx.x & 63) * kLane;
-    const int64_t id = token(g.ids, g.id_bytes, t);
-    if (g.status && id >= g.n_rows && e == 0) *g.status = TRE_E_KEYRANGE;
-    if (e >= g.elems) return;
-    float v[kLane] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (id >= 0 && id < g.n_rows) {
-        if constexpr (std::is_same_v<TI, Mx4>) {
-            const int64_t tile = id / g.tile_rows, row = (id - tile * g.tile_rows) * g.blocks;
-            const uint8_t* at = static_cast<const uint8_t*>(g.table) + tile * g.tile_bytes;
-            const uint32_t q = *reinterpret_cast<const uint32_t*>(at + row * 16 + e / 2);
-            mx_values(q, at[g.tile_rows * g.blocks * 16 + row + e / kMxBlock], v);
-        } else {
-            load_run(static_cast<const TI*>(g.table) + id * g.elems, e, g.elems, v);
+    const int64_t x = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    const int lane = int(x & ((1 << g.strip.shift) - 1));
+    int64_t t[kStrips], e[kStrips];
+    float v[kStrips][kLane];
+    if constexpr (WIDE) {
+        // (a wavefront's row is the same for its lanes)
+        const int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t row = w / g.groups, s0 = (w - row * g.groups) * kStrips;
+        if (row >= g.n_ids) return;
+        const int64_t id = token(g.ids, g.id_bytes, row);
+        const bool in = id >= 0 && id < g.n_rows;
+        if (g.status && id >= g.n_rows && s0 == 0 && lane == 0) *g.status = TRE_E_KEYRANGE;
+#pragma unroll
+        for (int i = 0; i < kStrips; i++) {
+            t[i] = row;
+            e[i] = (s0 + i) * kSlice + lane * kLane;
+#pragma unroll
+            for (int j = 0; j < kLane; j++) v[i][j] = 0.f;
+            if (in && e[i] < g.elems) lookup_load<TI>(g, id, e[i], v[i]);
+        }
+    } else {
+        int64_t id[kStrips];
+        const int64_t r0 = (x >> g.strip.shift) * kStrips;
+#pragma unroll
+        for (int i = 0; i < kStrips; i++) {
+            t[i] = r0 + i;
+            e[i] = t[i] < g.n_ids ? lane * kLane : g.elems;
+            id[i] = t[i] < g.n_ids ? token(g.ids, g.id_bytes, t[i]) : -1;
+            if (g.status && id[i] >= g.n_rows && lane == 0) *g.status = TRE_E_KEYRANGE;
         }
 #pragma unroll
-        for (int i = 0; i < kLane; i++) v[i] *= g.scale;
+        for (int i = 0; i < kStrips; i++) {
+#pragma unroll
+            for (int j = 0; j < kLane; j++) v[i][j] = 0.f;
+            if (id[i] >= 0 && id[i] < g.n_rows && e[i] < g.elems) lookup_load<TI>(g, id[i], e[i], v[i]);
+        }
     }
-    store_run(static_cast<TO*>(g.out) + t * g.elems, e, g.elems, v);
+#pragma unroll
+    for (int i = 0; i < kStrips; i++) {
+        if (e[i] >= g.elems) continue;
+#pragma unroll
+        for (int j = 0; j < kLane; j++) v[i][j] *= g.scale;
+        store_run(static_cast<TO*>(g.out) + t[i] * g.elems, e[i], g.elems, v[i]);
+    }
 }
 
 // --------------------------------------------------------------- gradient
 
 // The tokens are sorted (stably, so those of a row stay in their order) and
-// cut into chunks of kChunk, each summed by its own workgroups; a token whose
-// run crosses a chunk's border leaves partial sums that a second launch adds
-// in chunk order.  The order of every sum follows from the tokens alone.
-constexpr int kChunk = 32;
+// cut into chunks, each summed by its own wavefronts; a token whose run crosses
+// a chunk's border leaves partial sums that a second launch adds in chunk
+// order.  The order of every sum follows from the tokens alone.
+//
+// Chunks are short where there are few of them to fill the chip.
+constexpr int64_t kShortChunks = 16384;  // up to so many tokens
+inline int chunk_of(int64_t n) { return n <= kShortChunks ? 8 : 32; }
+// Rows in flight together, and partial sums.
+constexpr int kBatch = 8;
 
 struct GradArgs {
     const uint32_t* keys;   // sorted; n_rows: no row
     const uint32_t* pos;
-    const uint32_t* bits;   // rows that occur
     const void* grad;
     void* out;
     float* part;            // [chunk][2][elems]: the sums of its first and last token
-    int64_t n_ids, n_rows, elems, slices, chunks;
+    int64_t n_ids, n_rows, elems, chunks;
+    int64_t sum_waves;      // the wavefronts after them zero rows
+    Strip strip, join_strip;
+    int64_t zero_slices;
     float scale;
-    int32_t accumulate;
+    int32_t accumulate, chunk;
 };
+
+__device__ inline uint32_t token_key(const void* ids, int id_bytes, int64_t t, int64_t n_rows, int64_t* status) {
+    const int64_t id = token(ids, id_bytes, t);
+    if (status && id >= n_rows) *status = TRE_E_KEYRANGE;
+    return uint32_t(id >= 0 && id < n_rows ? id : n_rows);
+}
 
 __global__ __launch_bounds__(kThreads) void k_grad_keys(const void* __restrict__ ids, int id_bytes, int64_t n,
                                                         int64_t n_rows, uint32_t* __restrict__ keys,
-                                                        uint32_t* __restrict__ pos, uint32_t* __restrict__ bits,
-                                                        int64_t* __restrict__ status) {
+                                                        uint32_t* __restrict__ pos, int64_t* __restrict__ status) {
     const int64_t t = int64_t(blockIdx.x) * kThreads + threadIdx.x;
     if (t >= n) return;
-    const int64_t id = token(ids, id_bytes, t);
-    const bool ok = id >= 0 && id < n_rows;
-    if (status && id >= n_rows) *status = TRE_E_KEYRANGE;
-    keys[t] = uint32_t(ok ? id : n_rows);
+    keys[t] = token_key(ids, id_bytes, t, n_rows, status);
     pos[t] = uint32_t(t);
-    if (ok && bits) atomicOr(&bits[id >> 5], 1u << (id & 31));
 }
 
-template <typename TO>
-__device__ inline void put_row(const GradArgs& g, int64_t row, int64_t e, const float (&acc)[kLane]) {
+// Few tokens are sorted in one launch: a workgroup counts, for its 64, the
+// tokens that go before them, each of its wavefronts among a quarter.
+constexpr int kRankMax = 8192;
+
+__global__ __launch_bounds__(kThreads) void k_grad_rank(const void* __restrict__ ids, int id_bytes, int n, int64_t n_rows,
+                                                        uint32_t* __restrict__ keys, uint32_t* __restrict__ pos,
+                                                        int64_t* __restrict__ status) {
+    __shared__ uint4 all[kRankMax / 4];
+    __shared__ int32_t part[kWaves][64];
+    uint32_t* flat = reinterpret_cast<uint32_t*>(all);
+    const int padded = (n + 4 * kWaves - 1) / (4 * kWaves) * (4 * kWaves);  // (after every token)
+    for (int t = threadIdx.x; t < padded; t += kThreads)
+        flat[t] = t < n ? token_key(ids, id_bytes, t, n_rows, blockIdx.x == 0 ? status : nullptr) : 0xffffffffu;
+    __syncthreads();
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i0 = blockIdx.x * 64, i = i0 + lane;
+    const uint32_t key = i < n ? flat[i] : 0u;
+    const int q0 = padded / 4 / kWaves * w, q1 = q0 + padded / 4 / kWaves;
+    int before = 0;
+    // quads before the workgroup's tokens (equal ones go before), its own, those after
+    const int a = min(max(i0 / 4, q0), q1), b = min(max(i0 / 4 + 16, q0), q1);
+#pragma unroll 4
+    for (int q = q0; q < a; q++) {
+        const uint4 k = all[q];
+        before += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+    }
+    for (int q = a; q < b; q++) {
+        const uint4 k = all[q];
+        before += (k.x < key || (k.x == key && 4 * q < i)) + (k.y < key || (k.y == key && 4 * q + 1 < i)) +
+                  (k.z < key || (k.z == key && 4 * q + 2 < i)) + (k.w < key || (k.w == key && 4 * q + 3 < i));
+    }
+#pragma unroll 4
+    for (int q = b; q < q1; q++) {
+        const uint4 k = all[q];
+        before += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+    }
+    part[w][lane] = before;
+    __syncthreads();
+    if (w == 0 && i < n) {
+        int at = 0;
+#pragma unroll
+        for (int j = 0; j < kWaves; j++) at += part[j][lane];
+        keys[at] = key;
+        pos[at] = uint32_t(i);
+    }
+}
+
+template <typename TO, int N>
+__device__ inline void put_row(const GradArgs& g, int64_t row, int64_t e, const float (&acc)[N]) {
     TO* at = static_cast<TO*>(g.out) + row * g.elems;
-    float v[kLane];
+    float v[N];
     if (g.accumulate) {
         load_run(at, e, g.elems, v);
 #pragma unroll
-        for (int i = 0; i < kLane; i++) v[i] += g.scale * acc[i];
+        for (int i = 0; i < N; i++) v[i] += g.scale * acc[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < kLane; i++) v[i] = g.scale * acc[i];
+        for (int i = 0; i < N; i++) v[i] = g.scale * acc[i];
     }
     store_run(at, e, g.elems, v);
 }
 
-// A wavefront per chunk and slice, then (not accumulating) one per row and
-// slice that zeroes the rows no token has.
-template <typename TI, typename TO>
+// Zeroes a strip of 64 rows, but for rows that a token has: every lane looks
+// one row up in the sorted keys.
+template <typename TO>
+__device__ inline void zero_rows(const GradArgs& g, int64_t w) {
+    const int lane = threadIdx.x & 63;
+    const int64_t r0 = w / g.zero_slices * 64, e = (w % g.zero_slices) * kSlice + lane * kLane;
+    const int64_t row = r0 + lane;
+    int64_t lo = 0, hi = g.n_ids;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (int64_t(g.keys[mid]) < row) lo = mid + 1;
+        else hi = mid;
+    }
+    const bool absent = row < g.n_rows && (lo == g.n_ids || int64_t(g.keys[lo]) != row);
+    const float zero[kLane] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (uint64_t m = __ballot(absent); m; m &= m - 1) {
+        const int64_t r = r0 + __ffsll((unsigned long long)m) - 1;
+        if (e < g.elems) store_run(static_cast<TO*>(g.out) + r * g.elems, e, g.elems, zero);
+    }
+}
+
+// A strip of a chunk; then, unless the sums are added to what is there, rows of
+// zeros.  WIDE: a wavefront to a strip.
+template <typename TI, typename TO, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_grad_sum(GradArgs g) {
-    const int64_t x = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-    const int64_t c = x / g.slices;
-    const int64_t e = (x - c * g.slices) * kSlice + (threadIdx.x & 63) * kLane;
-    if (e >= g.elems) return;
-    float acc[kLane] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (c >= g.chunks) {
-        const int64_t row = c - g.chunks;
-        if (g.accumulate || row >= g.n_rows || (g.bits[row >> 5] >> (row & 31)) & 1) return;
-        store_run(static_cast<TO*>(g.out) + row * g.elems, e, g.elems, acc);
+    const int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (w >= g.sum_waves) {
+        if (!g.accumulate && w - g.sum_waves < (g.n_rows + 63) / 64 * g.zero_slices) zero_rows<TO>(g, w - g.sum_waves);
         return;
     }
-    const int64_t i0 = c * kChunk, i1 = min(i0 + kChunk, g.n_ids);
+    const int64_t x = WIDE ? w : (w * 64 + (threadIdx.x & 63)) >> g.strip.shift;
+    const int64_t c = x / g.strip.slices;
+    const int lane = threadIdx.x & ((1 << g.strip.shift) - 1);
+    const int64_t e = ((x - c * g.strip.slices) << g.strip.shift) * kLane + lane * kLane;
+    if (c >= g.chunks || e >= g.elems) return;
+    const int64_t i0 = c * g.chunk, i1 = min(i0 + g.chunk, g.n_ids);
+    const int64_t none = g.n_rows;
     uint32_t key = g.keys[i0];
-    if (int64_t(key) >= g.n_rows) return;
+    if (int64_t(key) >= none) return;
+    float acc[kLane] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     bool first = i0 > 0 && g.keys[i0 - 1] == key;  // the run began in an earlier chunk
-    for (int64_t i = i0; i < i1; i++) {
-        const uint32_t k = g.keys[i];
-        if (k != key) {
-            if (first) store_run(g.part + 2 * c * g.elems, e, g.elems, acc);
-            else put_row<TO>(g, key, e, acc);
-            first = false;
+    for (int64_t ib = i0; ib < i1; ib += kBatch) {
+        uint32_t k[kBatch];
+        float v[kBatch][kLane];
 #pragma unroll
-            for (int j = 0; j < kLane; j++) acc[j] = 0.f;
-            key = k;
-            if (int64_t(key) >= g.n_rows) return;
+        for (int j = 0; j < kBatch; j++) {
+            const int64_t i = min(ib + j, i1 - 1);
+            k[j] = g.keys[i];
+            // (the row of a token that is none is there to be read too)
+            load_run(static_cast<const TI*>(g.grad) + int64_t(g.pos[i]) * g.elems, e, g.elems, v[j]);
         }
-        float v[kLane];
-        load_run(static_cast<const TI*>(g.grad) + int64_t(g.pos[i]) * g.elems, e, g.elems, v);
 #pragma unroll
-        for (int j = 0; j < kLane; j++) acc[j] += v[j];
+        for (int j = 0; j < kBatch; j++) {
+            if (ib + j >= i1) break;
+            if (k[j] != key) {
+                if (first) store_run(g.part + 2 * c * g.elems, e, g.elems, acc);
+                else put_row<TO>(g, key, e, acc);
+                first = false;
+#pragma unroll
+                for (int h = 0; h < kLane; h++) acc[h] = 0.f;
+                key = k[j];
+                if (int64_t(key) >= none) return;
+            }
+#pragma unroll
+            for (int h = 0; h < kLane; h++) acc[h] += v[j][h];
+        }
     }
     if (first) store_run(g.part + 2 * c * g.elems, e, g.elems, acc);
     else if (i1 < g.n_ids && g.keys[i1] == key) store_run(g.part + (2 * c + 1) * g.elems, e, g.elems, acc);
     else put_row<TO>(g, key, e, acc);
 }
 
-// A wavefront per chunk and slice: the run that begins in the chunk and goes
-// on past it.
+// A strip of the run that begins in a chunk and goes on past it.  (Few such runs
+// are long: short strips give them more wavefronts, and the partial sums are
+// read ahead of knowing whether they belong to the run.)
+constexpr int kJoinLane = 2;
+
 template <typename TO>
 __global__ __launch_bounds__(kThreads) void k_grad_join(GradArgs g) {
-    const int64_t x = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-    const int64_t c = x / g.slices;
-    const int64_t e = (x - c * g.slices) * kSlice + (threadIdx.x & 63) * kLane;
-    const int64_t i0 = c * kChunk, i1 = i0 + kChunk;
+    const int64_t x = (int64_t(blockIdx.x) * kThreads + threadIdx.x) >> g.join_strip.shift;
+    const int64_t c = x / g.join_strip.slices;
+    const int lane = threadIdx.x & ((1 << g.join_strip.shift) - 1);
+    const int64_t e = (((x - c * g.join_strip.slices) << g.join_strip.shift) + lane) * kJoinLane;
+    const int64_t i0 = c * g.chunk, i1 = i0 + g.chunk;
     if (i1 >= g.n_ids || e >= g.elems) return;
     const uint32_t key = g.keys[i1 - 1];
     if (int64_t(key) >= g.n_rows || g.keys[i1] != key) return;
     if (g.keys[i0] == key && i0 > 0 && g.keys[i0 - 1] == key) return;  // it began earlier
-    float acc[kLane], v[kLane];
-    load_run(g.part + (2 * c + 1) * g.elems, e, g.elems, acc);
-    for (int64_t d = c + 1; d < g.chunks && g.keys[d * kChunk] == key; d++) {
-        load_run(g.part + 2 * d * g.elems, e, g.elems, v);
+    const float* part = g.part + e;
+    const bool two = e + 1 < g.elems;
+    float a = part[(2 * c + 1) * g.elems], b = two ? part[(2 * c + 1) * g.elems + 1] : 0.f;
+    for (int64_t d = c + 1; d < g.chunks; d += kBatch) {
+        bool in[kBatch];
+        float va[kBatch], vb[kBatch];
 #pragma unroll
-        for (int j = 0; j < kLane; j++) acc[j] += v[j];
+        for (int j = 0; j < kBatch; j++) {
+            const int64_t at = min(d + j, g.chunks - 1);
+            in[j] = d + j < g.chunks && g.keys[at * g.chunk] == key;
+            va[j] = part[2 * at * g.elems];
+            vb[j] = two ? part[2 * at * g.elems + 1] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; j++) {
+            a += in[j] ? va[j] : 0.f;
+            b += in[j] ? vb[j] : 0.f;
+        }
+        if (!in[kBatch - 1]) break;  // (the run's chunks are consecutive)
     }
-    put_row<TO>(g, key, e, acc);
+    TO* out = static_cast<TO*>(g.out) + int64_t(key) * g.elems + e;
+    store1(out, g.accumulate ? load1(out) + g.scale * a : g.scale * a);
+    if (two) store1(out + 1, g.accumulate ? load1(out + 1) + g.scale * b : g.scale * b);
 }
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
@@ -245,10 +405,10 @@ int key_bits(int64_t n_rows) {
 }
 
 struct GradLayout {
-    size_t keys, keys_alt, pos, pos_alt, hist, tmp, bits, part, total;
+    size_t keys, keys_alt, pos, pos_alt, hist, tmp, part, total;
 };
 
-GradLayout grad_layout(int64_t n, int64_t n_rows, int64_t elems) {
+GradLayout grad_layout(int64_t n, int64_t elems) {
     GradLayout L{};
     size_t off = 0;
     auto take = [&](size_t b) {
@@ -256,25 +416,49 @@ GradLayout grad_layout(int64_t n, int64_t n_rows, int64_t elems) {
         off += align256(b);
         return o;
     };
-    const size_t m = size_t(std::max<int64_t>(n, 1));
+    const size_t m = size_t(std::max<int64_t>(n, 1)), c = size_t(chunk_of(n));
     L.keys = take(4 * m);
-    L.keys_alt = take(4 * m);
     L.pos = take(4 * m);
-    L.pos_alt = take(4 * m);
+    const size_t radix = n > kRankMax ? m : 0;
+    L.keys_alt = take(4 * radix);
+    L.pos_alt = take(4 * radix);
     const int64_t h = radix_hist_elems(int64_t(m));
-    L.hist = take(4 * size_t(h));
-    L.tmp = take(4 * scan_tmp_elems(h));
-    L.bits = take(4 * size_t((n_rows + 31) / 32));
-    L.part = take(8 * size_t((m + kChunk - 1) / kChunk) * size_t(elems));
+    L.hist = take(radix ? 4 * size_t(h) : 0);
+    L.tmp = take(radix ? 4 * scan_tmp_elems(h) : 0);
+    L.part = take(8 * ((m + c - 1) / c) * size_t(elems));
     L.total = off;
     return L;
 }
 
 unsigned wave_grid(int64_t waves) { return unsigned((waves + kWaves - 1) / kWaves); }
 
+template <typename TI, typename TO>
+hipError_t lookup(LookupArgs g, hipStream_t s) {
+    if (g.elems > kSlice) {
+        g.groups = (g.strip.slices + kStrips - 1) / kStrips;
+        const int64_t waves = g.n_ids * g.groups;
+        if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
+        k_lookup<TI, TO, true><<<wave_grid(waves), kThreads, 0, s>>>(g);
+    } else {
+        const int64_t threads = ((g.n_ids + kStrips - 1) / kStrips) << g.strip.shift;
+        k_lookup<TI, TO, false><<<wave_grid((threads + 63) / 64), kThreads, 0, s>>>(g);
+    }
+    return hipGetLastError();
+}
+
+template <typename TI, typename TO>
+hipError_t grad_sum(const GradArgs& g, unsigned grid, hipStream_t s) {
+    if (g.strip.shift == 6) k_grad_sum<TI, TO, true><<<grid, kThreads, 0, s>>>(g);
+    else k_grad_sum<TI, TO, false><<<grid, kThreads, 0, s>>>(g);
+    return hipGetLastError();
+}
+
 }  // namespace
 
-size_t lookup_grad_ws_bytes(int64_t n, int64_t n_rows, int64_t elems) { return grad_layout(n, n_rows, elems).total; }
+size_t lookup_grad_ws_bytes(int64_t n, int64_t n_rows, int64_t elems) {
+    (void)n_rows;
+    return grad_layout(n, elems).total;
+}
 
 hipError_t launch_lookup(const void* table, int table_dtype, int64_t n_rows, int64_t elems, int64_t tile_rows,
                          const void* ids, int id_bytes, int64_t n_ids, float scale, void* out, int out_dtype,
@@ -287,80 +471,72 @@ hipError_t launch_lookup(const void* table, int table_dtype, int64_t n_rows, int
     g.n_rows = n_rows;
     g.elems = elems;
     g.n_ids = n_ids;
-    g.slices = (elems + kSlice - 1) / kSlice;
+    g.strip = strip(elems, kLane);
     g.tile_rows = tile_rows;
     g.blocks = mx_row_blocks(elems);
     g.tile_bytes = mx_tile_bytes(tile_rows, elems);
     g.scale = scale;
     g.id_bytes = id_bytes;
-    const int64_t waves = n_ids * g.slices;
-    if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
-    const unsigned grid = wave_grid(waves);
     const bool half = out_dtype == TRE_BF16;
-    if (table_dtype == TRE_MXFP4) {
-        if (half) k_lookup<Mx4, uint16_t><<<grid, kThreads, 0, s>>>(g);
-        else k_lookup<Mx4, float><<<grid, kThreads, 0, s>>>(g);
-    } else if (table_dtype == TRE_BF16) {
-        if (half) k_lookup<uint16_t, uint16_t><<<grid, kThreads, 0, s>>>(g);
-        else k_lookup<uint16_t, float><<<grid, kThreads, 0, s>>>(g);
-    } else {
-        if (half) k_lookup<float, uint16_t><<<grid, kThreads, 0, s>>>(g);
-        else k_lookup<float, float><<<grid, kThreads, 0, s>>>(g);
-    }
-    return hipGetLastError();
+    if (table_dtype == TRE_MXFP4) return half ? lookup<Mx4, uint16_t>(g, s) : lookup<Mx4, float>(g, s);
+    if (table_dtype == TRE_BF16) return half ? lookup<uint16_t, uint16_t>(g, s) : lookup<uint16_t, float>(g, s);
+    return half ? lookup<float, uint16_t>(g, s) : lookup<float, float>(g, s);
 }
 
 hipError_t launch_lookup_grad(const void* grad, int grad_dtype, const void* ids, int id_bytes, int64_t n_ids, float scale,
                               void* out, int out_dtype, int64_t n_rows, int64_t elems, bool accumulate, int64_t* status,
                               char* ws, hipStream_t s) {
-    const GradLayout L = grad_layout(n_ids, n_rows, elems);
+    const GradLayout L = grad_layout(n_ids, elems);
     uint32_t* keys = reinterpret_cast<uint32_t*>(ws + L.keys);
     uint32_t* pos = reinterpret_cast<uint32_t*>(ws + L.pos);
-    uint32_t* keys2 = reinterpret_cast<uint32_t*>(ws + L.keys_alt);
-    uint32_t* pos2 = reinterpret_cast<uint32_t*>(ws + L.pos_alt);
-    uint32_t* bits = reinterpret_cast<uint32_t*>(ws + L.bits);
     hipError_t e;
-    if (!accumulate && (e = launch_fill_zero(bits, 4 * size_t((n_rows + 31) / 32), s)) != hipSuccess) return e;
-    const int kb = key_bits(n_rows);
-    if (n_ids > 0) {
+    if (n_ids > kRankMax) {
+        uint32_t* keys2 = reinterpret_cast<uint32_t*>(ws + L.keys_alt);
+        uint32_t* pos2 = reinterpret_cast<uint32_t*>(ws + L.pos_alt);
+        const int kb = key_bits(n_rows);
         k_grad_keys<<<unsigned((n_ids + kThreads - 1) / kThreads), kThreads, 0, s>>>(ids, id_bytes, n_ids, n_rows, keys, pos,
-                                                                                     accumulate ? nullptr : bits, status);
+                                                                                     status);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if ((e = radix_sort_u32(keys, pos, keys2, pos2, n_ids, kb, reinterpret_cast<int32_t*>(ws + L.hist),
                                 reinterpret_cast<int32_t*>(ws + L.tmp), s)) != hipSuccess)
             return e;
+        if (radix_result_in_alt(n_ids, kb)) {
+            keys = keys2;
+            pos = pos2;
+        }
+    } else if (n_ids > 0) {
+        k_grad_rank<<<unsigned((n_ids + 63) / 64), kThreads, 0, s>>>(ids, id_bytes, int(n_ids), n_rows, keys, pos, status);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    const bool alt = radix_result_in_alt(n_ids, kb);
     GradArgs g{};
-    g.keys = alt ? keys2 : keys;
-    g.pos = alt ? pos2 : pos;
-    g.bits = bits;
+    g.keys = keys;
+    g.pos = pos;
     g.grad = grad;
     g.out = out;
     g.part = reinterpret_cast<float*>(ws + L.part);
     g.n_ids = n_ids;
     g.n_rows = n_rows;
     g.elems = elems;
-    g.slices = (elems + kSlice - 1) / kSlice;
-    g.chunks = (n_ids + kChunk - 1) / kChunk;
+    g.chunk = chunk_of(n_ids);
+    g.chunks = (n_ids + g.chunk - 1) / g.chunk;
+    g.strip = strip(elems, kLane);
+    g.join_strip = strip(elems, kJoinLane);
+    g.zero_slices = (elems + kSlice - 1) / kSlice;
     g.scale = scale;
     g.accumulate = accumulate;
-    const int64_t waves = (g.chunks + (accumulate ? 0 : n_rows)) * g.slices;
+    g.sum_waves = ((g.chunks * g.strip.slices << g.strip.shift) + 63) / 64;
+    const int64_t waves = g.sum_waves + (accumulate ? 0 : (n_rows + 63) / 64 * g.zero_slices);
     if (waves == 0) return hipSuccess;
     if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
     const unsigned grid = wave_grid(waves);
     const bool half = out_dtype == TRE_BF16;
-    if (grad_dtype == TRE_BF16) {
-        if (half) k_grad_sum<uint16_t, uint16_t><<<grid, kThreads, 0, s>>>(g);
-        else k_grad_sum<uint16_t, float><<<grid, kThreads, 0, s>>>(g);
-    } else {
-        if (half) k_grad_sum<float, uint16_t><<<grid, kThreads, 0, s>>>(g);
-        else k_grad_sum<float, float><<<grid, kThreads, 0, s>>>(g);
-    }
-    if ((e = hipGetLastError()) != hipSuccess || g.chunks <= 1) return e;
-    const unsigned joins = wave_grid(g.chunks * g.slices);
-    if (half) k_grad_join<uint16_t><<<joins, kThreads, 0, s>>>(g);
-    else k_grad_join<float><<<joins, kThreads, 0, s>>>(g);
+    if (grad_dtype == TRE_BF16) e = half ? grad_sum<uint16_t, uint16_t>(g, grid, s) : grad_sum<uint16_t, float>(g, grid, s);
+    else e = half ? grad_sum<float, uint16_t>(g, grid, s) : grad_sum<float, float>(g, grid, s);
+    if (e != hipSuccess || g.chunks <= 1) return e;
+    const int64_t joins = ((g.chunks * g.join_strip.slices << g.join_strip.shift) + 63) / 64;
+    if (joins / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
+    if (half) k_grad_join<uint16_t><<<wave_grid(joins), kThreads, 0, s>>>(g);
+    else k_grad_join<float><<<wave_grid(joins), kThreads, 0, s>>>(g);
     return hipGetLastError();
 }
 
