@@ -107,8 +107,8 @@ def lookup_grad(grad: np.ndarray, ids: np.ndarray, n_rows: int, scale: float):
     """(gradient, sum of magnitudes), float64."""
     total = np.zeros((n_rows, grad.shape[-1]))
     mag = np.zeros_like(total)
-    for t, i in enumerate(ids.reshape(-1)):
-        if 0 <= i < n_rows:
-            total[i] += grad.reshape(-1, grad.shape[-1])[t]
-            mag[i] += np.abs(grad.reshape(-1, grad.shape[-1])[t])
+    flat, rows = ids.reshape(-1), grad.reshape(-1, grad.shape[-1])
+    ok = (flat >= 0) & (flat < n_rows)
+    np.add.at(total, flat[ok], rows[ok])
+    np.add.at(mag, flat[ok], np.abs(rows[ok]))
     return total * scale, mag * abs(scale)

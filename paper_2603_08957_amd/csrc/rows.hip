@@ -16,64 +16,89 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kLane = 8;              // elements of a row to a lane
-constexpr int kSlice = 64 * kLane;    // elements of a row to a wavefront
 
-// 16 bytes on any element boundary: rows of an odd number of elements begin
-// anywhere, and the wide access still costs less than one per element.
+// A lane moves E consecutive elements of a row with one access of 16 bytes in
+// the wider of the two types (eight where both sides have 16 bits, else four):
+// with eight fp32 values, two stores of 16 bytes 32 apart, 65,536 rows of
+// gradients took 25 us longer.  Rows of an odd number of elements begin
+// anywhere; a wide access off its alignment still costs less than narrow ones.
+template <typename TI, typename TO>
+constexpr int lane_elems() { return sizeof(TI) == 4 || sizeof(TO) == 4 ? 4 : 8; }
+
 typedef uint32_t u32x4_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
 
-__device__ inline void load8(const float* p, float (&v)[kLane]) {
-    const f32x4_4 a = *reinterpret_cast<const f32x4_4*>(p), b = *reinterpret_cast<const f32x4_4*>(p + 4);
+template <int E>
+__device__ inline void load_all(const float* p, float (&v)[E]) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        v[i] = a[i];
-        v[4 + i] = b[i];
+    for (int h = 0; h < E; h += 4) {
+        const f32x4_4 a = *reinterpret_cast<const f32x4_4*>(p + h);
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[h + i] = a[i];
     }
 }
-__device__ inline void load8(const uint16_t* p, float (&v)[kLane]) {
-    const u32x4_2 a = *reinterpret_cast<const u32x4_2*>(p);
+template <int E>
+__device__ inline void load_all(const uint16_t* p, float (&v)[E]) {
+    uint32_t a[E / 2];
+    if constexpr (E == 8) {
+        const u32x4_2 x = *reinterpret_cast<const u32x4_2*>(p);
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
+        for (int i = 0; i < 4; i++) a[i] = x[i];
+    } else {
+        const u32x2_2 x = *reinterpret_cast<const u32x2_2*>(p);
+        a[0] = x[0];
+        a[1] = x[1];
+    }
+#pragma unroll
+    for (int i = 0; i < E / 2; i++) {
         v[2 * i] = __uint_as_float(a[i] << 16);
         v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
     }
 }
-__device__ inline void store8(float* p, const float (&v)[kLane]) {
-    *reinterpret_cast<f32x4_4*>(p) = f32x4_4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4_4*>(p + 4) = f32x4_4{v[4], v[5], v[6], v[7]};
+// (ONCE: not kept in L2, where rows that are read again have their place)
+template <bool ONCE, typename V>
+__device__ inline void store_as(void* p, V v) {
+    if constexpr (ONCE) __builtin_nontemporal_store(v, static_cast<V*>(p));
+    else *static_cast<V*>(p) = v;
 }
-__device__ inline void store8(uint16_t* p, const float (&v)[kLane]) {
-    u32x4_2 a;
+template <bool ONCE, int E>
+__device__ inline void store_all(float* p, const float (&v)[E]) {
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int h = 0; h < E; h += 4) store_as<ONCE>(p + h, f32x4_4{v[h], v[h + 1], v[h + 2], v[h + 3]});
+}
+template <bool ONCE, int E>
+__device__ inline void store_all(uint16_t* p, const float (&v)[E]) {
+    uint32_t a[E / 2];
+#pragma unroll
+    for (int i = 0; i < E / 2; i++)
         a[i] = uint32_t(f32_to_bf16_rne(v[2 * i])) | (uint32_t(f32_to_bf16_rne(v[2 * i + 1])) << 16);
-    *reinterpret_cast<u32x4_2*>(p) = a;
+    if constexpr (E == 8) store_as<ONCE>(p, u32x4_2{a[0], a[1], a[2], a[3]});
+    else store_as<ONCE>(p, u32x2_2{a[0], a[1]});
 }
 __device__ inline float load1(const float* p) { return *p; }
 __device__ inline float load1(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }
 __device__ inline void store1(float* p, float v) { *p = v; }
 __device__ inline void store1(uint16_t* p, float v) { *p = f32_to_bf16_rne(v); }
 
-// The up to eight elements of a row from element e on.
-template <typename T>
-__device__ inline void load_run(const T* row, int64_t e, int64_t n, float (&v)[kLane]) {
-    if (e + kLane <= n) {
-        load8(row + e, v);
+// The up to E elements of a row from element e on.
+template <int E, typename T>
+__device__ inline void load_run(const T* row, int64_t e, int64_t n, float (&v)[E]) {
+    if (e + E <= n) {
+        load_all(row + e, v);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < kLane; i++) v[i] = e + i < n ? load1(row + e + i) : 0.f;
+    for (int i = 0; i < E; i++) v[i] = e + i < n ? load1(row + e + i) : 0.f;
 }
-template <typename T>
-__device__ inline void store_run(T* row, int64_t e, int64_t n, const float (&v)[kLane]) {
-    if (e + kLane <= n) {
-        store8(row + e, v);
+template <bool ONCE = false, int E, typename T>
+__device__ inline void store_run(T* row, int64_t e, int64_t n, const float (&v)[E]) {
+    if (e + E <= n) {
+        store_all<ONCE>(row + e, v);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < kLane; i++)
+    for (int i = 0; i < E; i++)
         if (e + i < n) store1(row + e + i, v[i]);
 }
 
@@ -120,13 +145,20 @@ struct Mx4 {};
 // of 4,096 bf16 values 406 us).
 constexpr int kStrips = 4;
 
-template <typename TI>
-__device__ inline void lookup_load(const LookupArgs& g, int64_t id, int64_t e, float (&v)[kLane]) {
+template <typename TI, int E>
+__device__ inline void lookup_load(const LookupArgs& g, int64_t id, int64_t e, float (&v)[E]) {
     if constexpr (std::is_same_v<TI, Mx4>) {
         const int64_t tile = id / g.tile_rows, row = (id - tile * g.tile_rows) * g.blocks;
         const uint8_t* at = static_cast<const uint8_t*>(g.table) + tile * g.tile_bytes;
-        const uint32_t q = *reinterpret_cast<const uint32_t*>(at + row * 16 + e / 2);
-        mx_values(q, at[g.tile_rows * g.blocks * 16 + row + e / kMxBlock], v);
+        const int sb = at[g.tile_rows * g.blocks * 16 + row + e / kMxBlock];
+        if constexpr (E == 8) {
+            mx_values(*reinterpret_cast<const uint32_t*>(at + row * 16 + e / 2), sb, v);
+        } else {
+            float w[8];
+            mx_values(*reinterpret_cast<const uint16_t*>(at + row * 16 + e / 2), sb, w);
+#pragma unroll
+            for (int i = 0; i < E; i++) v[i] = w[i];
+        }
     } else {
         load_run(static_cast<const TI*>(g.table) + id * g.elems, e, g.elems, v);
     }
@@ -134,10 +166,11 @@ __device__ inline void lookup_load(const LookupArgs& g, int64_t id, int64_t e, f
 
 template <typename TI, typename TO, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
+    constexpr int E = lane_elems<TI, TO>();
     const int64_t x = int64_t(blockIdx.x) * kThreads + threadIdx.x;
     const int lane = int(x & ((1 << g.strip.shift) - 1));
     int64_t t[kStrips], e[kStrips];
-    float v[kStrips][kLane];
+    float v[kStrips][E];
     if constexpr (WIDE) {
         // (a wavefront's row is the same for its lanes)
         const int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -149,9 +182,9 @@ __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
 #pragma unroll
         for (int i = 0; i < kStrips; i++) {
             t[i] = row;
-            e[i] = (s0 + i) * kSlice + lane * kLane;
+            e[i] = ((s0 + i) * 64 + lane) * E;
 #pragma unroll
-            for (int j = 0; j < kLane; j++) v[i][j] = 0.f;
+            for (int j = 0; j < E; j++) v[i][j] = 0.f;
             if (in && e[i] < g.elems) lookup_load<TI>(g, id, e[i], v[i]);
         }
     } else {
@@ -160,14 +193,14 @@ __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
 #pragma unroll
         for (int i = 0; i < kStrips; i++) {
             t[i] = r0 + i;
-            e[i] = t[i] < g.n_ids ? lane * kLane : g.elems;
+            e[i] = t[i] < g.n_ids ? lane * E : g.elems;
             id[i] = t[i] < g.n_ids ? token(g.ids, g.id_bytes, t[i]) : -1;
             if (g.status && id[i] >= g.n_rows && lane == 0) *g.status = TRE_E_KEYRANGE;
         }
 #pragma unroll
         for (int i = 0; i < kStrips; i++) {
 #pragma unroll
-            for (int j = 0; j < kLane; j++) v[i][j] = 0.f;
+            for (int j = 0; j < E; j++) v[i][j] = 0.f;
             if (id[i] >= 0 && id[i] < g.n_rows && e[i] < g.elems) lookup_load<TI>(g, id[i], e[i], v[i]);
         }
     }
@@ -175,8 +208,8 @@ __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
     for (int i = 0; i < kStrips; i++) {
         if (e[i] >= g.elems) continue;
 #pragma unroll
-        for (int j = 0; j < kLane; j++) v[i][j] *= g.scale;
-        store_run(static_cast<TO*>(g.out) + t[i] * g.elems, e[i], g.elems, v[i]);
+        for (int j = 0; j < E; j++) v[i][j] *= g.scale;
+        store_run<true>(static_cast<TO*>(g.out) + t[i] * g.elems, e[i], g.elems, v[i]);
     }
 }
 
@@ -184,14 +217,16 @@ __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
 
 // The tokens are sorted (stably, so those of a row stay in their order) and
 // cut into chunks, each summed by its own wavefronts; a token whose run crosses
-// a chunk's border leaves partial sums that a second launch adds in chunk
+// a chunk's border leaves partial sums that further launches add in chunk
 // order.  The order of every sum follows from the tokens alone.
 //
 // Chunks are short where there are few of them to fill the chip.
 constexpr int64_t kShortChunks = 16384;  // up to so many tokens
 inline int chunk_of(int64_t n) { return n <= kShortChunks ? 8 : 32; }
-// Rows in flight together, and partial sums.
-constexpr int kBatch = 8;
+// Rows in flight together.
+constexpr int kBatch = 4;
+// Wavefronts that zero rows: so many if there are four rows for each.
+constexpr int64_t kZeroWaves = 2048;
 
 struct GradArgs {
     const uint32_t* keys;   // sorted; n_rows: no row
@@ -200,11 +235,11 @@ struct GradArgs {
     void* out;
     float* part;            // [chunk][2][elems]: the sums of its first and last token
     int64_t n_ids, n_rows, elems, chunks;
-    int64_t sum_waves;      // the wavefronts after them zero rows
-    Strip strip, join_strip;
+    int64_t zero_waves;     // the first wavefronts zero rows
+    Strip strip;
     int64_t zero_slices;
     float scale;
-    int32_t accumulate, chunk;
+    int32_t accumulate, chunk, zero_rows;
 };
 
 __device__ inline uint32_t token_key(const void* ids, int id_bytes, int64_t t, int64_t n_rows, int64_t* status) {
@@ -280,15 +315,15 @@ __device__ inline void put_row(const GradArgs& g, int64_t row, int64_t e, const 
 #pragma unroll
         for (int i = 0; i < N; i++) v[i] = g.scale * acc[i];
     }
-    store_run(at, e, g.elems, v);
+    store_run<true>(at, e, g.elems, v);
 }
 
-// Zeroes a strip of 64 rows, but for rows that a token has: every lane looks
-// one row up in the sorted keys.
-template <typename TO>
+// Zeroes a strip of g.zero_rows rows (at most 64), but for rows that a token
+// has: every lane looks one row up in the sorted keys.
+template <typename TO, int E>
 __device__ inline void zero_rows(const GradArgs& g, int64_t w) {
     const int lane = threadIdx.x & 63;
-    const int64_t r0 = w / g.zero_slices * 64, e = (w % g.zero_slices) * kSlice + lane * kLane;
+    const int64_t r0 = w / g.zero_slices * g.zero_rows, e = ((w % g.zero_slices) * 64 + lane) * E;
     const int64_t row = r0 + lane;
     int64_t lo = 0, hi = g.n_ids;
     while (lo < hi) {
@@ -296,37 +331,43 @@ __device__ inline void zero_rows(const GradArgs& g, int64_t w) {
         if (int64_t(g.keys[mid]) < row) lo = mid + 1;
         else hi = mid;
     }
-    const bool absent = row < g.n_rows && (lo == g.n_ids || int64_t(g.keys[lo]) != row);
-    const float zero[kLane] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const bool absent = lane < g.zero_rows && row < g.n_rows && (lo == g.n_ids || int64_t(g.keys[lo]) != row);
+    float zero[E];
+#pragma unroll
+    for (int i = 0; i < E; i++) zero[i] = 0.f;
     for (uint64_t m = __ballot(absent); m; m &= m - 1) {
         const int64_t r = r0 + __ffsll((unsigned long long)m) - 1;
-        if (e < g.elems) store_run(static_cast<TO*>(g.out) + r * g.elems, e, g.elems, zero);
+        if (e < g.elems) store_run<true>(static_cast<TO*>(g.out) + r * g.elems, e, g.elems, zero);
     }
 }
 
-// A strip of a chunk; then, unless the sums are added to what is there, rows of
-// zeros.  WIDE: a wavefront to a strip.
+// Rows of zeros, unless the sums are added to what is there; then a strip of a
+// chunk.  WIDE: a wavefront to a strip.
 template <typename TI, typename TO, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_grad_sum(GradArgs g) {
-    const int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (w >= g.sum_waves) {
-        if (!g.accumulate && w - g.sum_waves < (g.n_rows + 63) / 64 * g.zero_slices) zero_rows<TO>(g, w - g.sum_waves);
+    constexpr int E = lane_elems<TI, TO>();
+    int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (w < g.zero_waves) {
+        zero_rows<TO, E>(g, w);
         return;
     }
+    w -= g.zero_waves;
     const int64_t x = WIDE ? w : (w * 64 + (threadIdx.x & 63)) >> g.strip.shift;
     const int64_t c = x / g.strip.slices;
     const int lane = threadIdx.x & ((1 << g.strip.shift) - 1);
-    const int64_t e = ((x - c * g.strip.slices) << g.strip.shift) * kLane + lane * kLane;
+    const int64_t e = (((x - c * g.strip.slices) << g.strip.shift) + lane) * E;
     if (c >= g.chunks || e >= g.elems) return;
     const int64_t i0 = c * g.chunk, i1 = min(i0 + g.chunk, g.n_ids);
     const int64_t none = g.n_rows;
     uint32_t key = g.keys[i0];
     if (int64_t(key) >= none) return;
-    float acc[kLane] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float acc[E];
+#pragma unroll
+    for (int h = 0; h < E; h++) acc[h] = 0.f;
     bool first = i0 > 0 && g.keys[i0 - 1] == key;  // the run began in an earlier chunk
     for (int64_t ib = i0; ib < i1; ib += kBatch) {
         uint32_t k[kBatch];
-        float v[kBatch][kLane];
+        float v[kBatch][E];
 #pragma unroll
         for (int j = 0; j < kBatch; j++) {
             const int64_t i = min(ib + j, i1 - 1);
@@ -342,12 +383,12 @@ __global__ __launch_bounds__(kThreads) void k_grad_sum(GradArgs g) {
                 else put_row<TO>(g, key, e, acc);
                 first = false;
 #pragma unroll
-                for (int h = 0; h < kLane; h++) acc[h] = 0.f;
+                for (int h = 0; h < E; h++) acc[h] = 0.f;
                 key = k[j];
                 if (int64_t(key) >= none) return;
             }
 #pragma unroll
-            for (int h = 0; h < kLane; h++) acc[h] += v[j][h];
+            for (int h = 0; h < E; h++) acc[h] += v[j][h];
         }
     }
     if (first) store_run(g.part + 2 * c * g.elems, e, g.elems, acc);
@@ -355,45 +396,94 @@ __global__ __launch_bounds__(kThreads) void k_grad_sum(GradArgs g) {
     else put_row<TO>(g, key, e, acc);
 }
 
-// A strip of the run that begins in a chunk and goes on past it.  (Few such runs
-// are long: short strips give them more wavefronts, and the partial sums are
-// read ahead of knowing whether they belong to the run.)
-constexpr int kJoinLane = 2;
+// One or two elements of a row from e on.
+__device__ inline void load_pair(const float* row, int64_t e, int64_t n, float (&v)[2]) {
+    v[0] = row[e];
+    v[1] = e + 1 < n ? row[e + 1] : 0.f;
+}
+__device__ inline void store_pair(float* row, int64_t e, int64_t n, const float (&v)[2]) {
+    row[e] = v[0];
+    if (e + 1 < n) row[e + 1] = v[1];
+}
+template <typename TO>
+__device__ inline void put_pair(const GradArgs& g, int64_t row, int64_t e, const float (&v)[2]) {
+    TO* at = static_cast<TO*>(g.out) + row * g.elems + e;
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+        if (e + i < g.elems) store1(at + i, g.accumulate ? load1(at + i) + g.scale * v[i] : g.scale * v[i]);
+}
+
+// The partial sums of kFan neighbouring chunks: those of a run that ends among
+// them are added to its row, the others to the two that the group leaves for
+// the next level, until one group holds all.  (One thread adding the partial
+// sums of a run to its end took 51 us for 65,536 tokens of which one is a
+// twentieth, and would take 15 times that if they were all alike.)
+//
+// A wavefront to a group and a strip of its rows.  Each lane looks at one
+// chunk's borders, and only the partial sums that are there are read.
+constexpr int kFan = 16, kJoinBatch = 16, kJoinLane = 2;
+
+struct JoinArgs {
+    const float* in;   // [chunk][2][elems]
+    float* out;        // [group][2][elems]
+    int64_t span;      // tokens of a chunk
+    int64_t chunks, groups, slices;
+};
 
 template <typename TO>
-__global__ __launch_bounds__(kThreads) void k_grad_join(GradArgs g) {
-    const int64_t x = (int64_t(blockIdx.x) * kThreads + threadIdx.x) >> g.join_strip.shift;
-    const int64_t c = x / g.join_strip.slices;
-    const int lane = threadIdx.x & ((1 << g.join_strip.shift) - 1);
-    const int64_t e = (((x - c * g.join_strip.slices) << g.join_strip.shift) + lane) * kJoinLane;
-    const int64_t i0 = c * g.chunk, i1 = i0 + g.chunk;
-    if (i1 >= g.n_ids || e >= g.elems) return;
-    const uint32_t key = g.keys[i1 - 1];
-    if (int64_t(key) >= g.n_rows || g.keys[i1] != key) return;
-    if (g.keys[i0] == key && i0 > 0 && g.keys[i0 - 1] == key) return;  // it began earlier
-    const float* part = g.part + e;
-    const bool two = e + 1 < g.elems;
-    float a = part[(2 * c + 1) * g.elems], b = two ? part[(2 * c + 1) * g.elems + 1] : 0.f;
-    for (int64_t d = c + 1; d < g.chunks; d += kBatch) {
-        bool in[kBatch];
-        float va[kBatch], vb[kBatch];
-#pragma unroll
-        for (int j = 0; j < kBatch; j++) {
-            const int64_t at = min(d + j, g.chunks - 1);
-            in[j] = d + j < g.chunks && g.keys[at * g.chunk] == key;
-            va[j] = part[2 * at * g.elems];
-            vb[j] = two ? part[2 * at * g.elems + 1] : 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < kBatch; j++) {
-            a += in[j] ? va[j] : 0.f;
-            b += in[j] ? vb[j] : 0.f;
-        }
-        if (!in[kBatch - 1]) break;  // (the run's chunks are consecutive)
+__global__ __launch_bounds__(kThreads) void k_grad_join(GradArgs g, JoinArgs a) {
+    const int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t group = w / a.slices;
+    if (group >= a.groups) return;
+    const int lane = threadIdx.x & 63;
+    const int64_t e = ((w - group * a.slices) * 64 + lane) * kJoinLane;
+    const int64_t c0 = group * kFan, c = c0 + lane;
+    const int count = int(min(int64_t(kFan), a.chunks - c0));
+    bool cont = false, more = false, whole = false;
+    uint32_t key = 0;
+    if (lane < count) {
+        const int64_t p0 = c * a.span, p1 = min(p0 + a.span, g.n_ids);
+        key = g.keys[p0];
+        const uint32_t before = g.keys[p0 > 0 ? p0 - 1 : 0], last = g.keys[p1 - 1], next = g.keys[p1 < g.n_ids ? p1 : p1 - 1];
+        cont = p0 > 0 && before == key && int64_t(key) < g.n_rows;            // its first run began earlier
+        more = p1 < g.n_ids && last == next && int64_t(last) < g.n_rows;      // its last run goes on
+        whole = cont && key == last;                                          // and is its first
     }
-    TO* out = static_cast<TO*>(g.out) + int64_t(key) * g.elems + e;
-    store1(out, g.accumulate ? load1(out) + g.scale * a : g.scale * a);
-    if (two) store1(out + 1, g.accumulate ? load1(out + 1) + g.scale * b : g.scale * b);
+    const uint64_t conts = __ballot(cont), goes = __ballot(more), wholes = __ballot(whole);
+    if (e >= g.elems) return;
+    float acc[kJoinLane] = {0.f, 0.f};
+    bool first = conts & 1;  // the run at hand began in an earlier group
+    for (uint64_t todo = conts | (goes & ~wholes); todo;) {
+        int at[kJoinBatch];
+        float v[kJoinBatch][2][kJoinLane];
+#pragma unroll
+        for (int j = 0; j < kJoinBatch; j++) {
+            at[j] = todo ? __ffsll((unsigned long long)todo) - 1 : -1;
+            todo &= todo - 1;
+            if (at[j] < 0) continue;
+            if (conts >> at[j] & 1) load_pair(a.in + 2 * (c0 + at[j]) * g.elems, e, g.elems, v[j][0]);
+            if ((goes & ~wholes) >> at[j] & 1) load_pair(a.in + (2 * (c0 + at[j]) + 1) * g.elems, e, g.elems, v[j][1]);
+        }
+#pragma unroll
+        for (int j = 0; j < kJoinBatch; j++) {
+            if (at[j] < 0) break;
+            const bool on = goes >> at[j] & 1, all = wholes >> at[j] & 1;
+            if (conts >> at[j] & 1) {
+#pragma unroll
+                for (int h = 0; h < kJoinLane; h++) acc[h] += v[j][0][h];
+                if (!(on && all)) {
+                    if (first) store_pair(a.out + 2 * group * g.elems, e, g.elems, acc);
+                    else put_pair<TO>(g, __builtin_amdgcn_readlane(key, at[j]), e, acc);
+                    first = false;
+                }
+            }
+            if (on && !all) {
+#pragma unroll
+                for (int h = 0; h < kJoinLane; h++) acc[h] = v[j][1][h];
+            }
+        }
+    }
+    if (goes >> (count - 1) & 1) store_pair(a.out + (2 * group + (first ? 0 : 1)) * g.elems, e, g.elems, acc);
 }
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
@@ -417,15 +507,18 @@ GradLayout grad_layout(int64_t n, int64_t elems) {
         return o;
     };
     const size_t m = size_t(std::max<int64_t>(n, 1)), c = size_t(chunk_of(n));
+    size_t chunks = 0;
     L.keys = take(4 * m);
     L.pos = take(4 * m);
     const size_t radix = n > kRankMax ? m : 0;
     L.keys_alt = take(4 * radix);
     L.pos_alt = take(4 * radix);
-    const int64_t h = radix_hist_elems(int64_t(m));
+    const int64_t h = radix_u32_hist_elems(int64_t(m));
     L.hist = take(radix ? 4 * size_t(h) : 0);
     L.tmp = take(radix ? 4 * scan_tmp_elems(h) : 0);
-    L.part = take(8 * ((m + c - 1) / c) * size_t(elems));
+    // two partial sums of a row for each chunk, of every level
+    for (size_t k = (m + c - 1) / c; k > 0; k = k > 1 ? (k + kFan - 1) / kFan : 0) chunks += k;
+    L.part = take(8 * chunks * size_t(elems));
     L.total = off;
     return L;
 }
@@ -434,7 +527,9 @@ unsigned wave_grid(int64_t waves) { return unsigned((waves + kWaves - 1) / kWave
 
 template <typename TI, typename TO>
 hipError_t lookup(LookupArgs g, hipStream_t s) {
-    if (g.elems > kSlice) {
+    constexpr int E = lane_elems<TI, TO>();
+    g.strip = strip(g.elems, E);
+    if (g.elems > 64 * E) {
         g.groups = (g.strip.slices + kStrips - 1) / kStrips;
         const int64_t waves = g.n_ids * g.groups;
         if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
@@ -447,7 +542,17 @@ hipError_t lookup(LookupArgs g, hipStream_t s) {
 }
 
 template <typename TI, typename TO>
-hipError_t grad_sum(const GradArgs& g, unsigned grid, hipStream_t s) {
+hipError_t grad_sum(GradArgs g, hipStream_t s) {
+    constexpr int E = lane_elems<TI, TO>();
+    g.strip = strip(g.elems, E);
+    g.zero_slices = (g.elems + 64 * E - 1) / (64 * E);
+    g.zero_rows = 64;
+    while (g.zero_rows > 4 && g.n_rows / g.zero_rows * g.zero_slices < kZeroWaves) g.zero_rows /= 2;
+    g.zero_waves = g.accumulate ? 0 : (g.n_rows + g.zero_rows - 1) / g.zero_rows * g.zero_slices;
+    const int64_t waves = g.zero_waves + ((g.chunks * g.strip.slices << g.strip.shift) + 63) / 64;
+    if (waves == 0) return hipSuccess;
+    if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
+    const unsigned grid = wave_grid(waves);
     if (g.strip.shift == 6) k_grad_sum<TI, TO, true><<<grid, kThreads, 0, s>>>(g);
     else k_grad_sum<TI, TO, false><<<grid, kThreads, 0, s>>>(g);
     return hipGetLastError();
@@ -471,7 +576,6 @@ hipError_t launch_lookup(const void* table, int table_dtype, int64_t n_rows, int
     g.n_rows = n_rows;
     g.elems = elems;
     g.n_ids = n_ids;
-    g.strip = strip(elems, kLane);
     g.tile_rows = tile_rows;
     g.blocks = mx_row_blocks(elems);
     g.tile_bytes = mx_tile_bytes(tile_rows, elems);
@@ -519,25 +623,29 @@ hipError_t launch_lookup_grad(const void* grad, int grad_dtype, const void* ids,
     g.elems = elems;
     g.chunk = chunk_of(n_ids);
     g.chunks = (n_ids + g.chunk - 1) / g.chunk;
-    g.strip = strip(elems, kLane);
-    g.join_strip = strip(elems, kJoinLane);
-    g.zero_slices = (elems + kSlice - 1) / kSlice;
     g.scale = scale;
     g.accumulate = accumulate;
-    g.sum_waves = ((g.chunks * g.strip.slices << g.strip.shift) + 63) / 64;
-    const int64_t waves = g.sum_waves + (accumulate ? 0 : (n_rows + 63) / 64 * g.zero_slices);
-    if (waves == 0) return hipSuccess;
-    if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
-    const unsigned grid = wave_grid(waves);
     const bool half = out_dtype == TRE_BF16;
-    if (grad_dtype == TRE_BF16) e = half ? grad_sum<uint16_t, uint16_t>(g, grid, s) : grad_sum<uint16_t, float>(g, grid, s);
-    else e = half ? grad_sum<float, uint16_t>(g, grid, s) : grad_sum<float, float>(g, grid, s);
-    if (e != hipSuccess || g.chunks <= 1) return e;
-    const int64_t joins = ((g.chunks * g.join_strip.slices << g.join_strip.shift) + 63) / 64;
-    if (joins / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
-    if (half) k_grad_join<uint16_t><<<wave_grid(joins), kThreads, 0, s>>>(g);
-    else k_grad_join<float><<<wave_grid(joins), kThreads, 0, s>>>(g);
-    return hipGetLastError();
+    if (grad_dtype == TRE_BF16) e = half ? grad_sum<uint16_t, uint16_t>(g, s) : grad_sum<uint16_t, float>(g, s);
+    else e = half ? grad_sum<float, uint16_t>(g, s) : grad_sum<float, float>(g, s);
+    if (e != hipSuccess) return e;
+    JoinArgs a{};
+    a.in = g.part;
+    a.span = g.chunk;
+    a.slices = (elems + 64 * kJoinLane - 1) / (64 * kJoinLane);
+    for (a.chunks = g.chunks; a.chunks > 1; a.chunks = a.groups) {
+        a.groups = (a.chunks + kFan - 1) / kFan;
+        float* out = const_cast<float*>(a.in) + 2 * a.chunks * elems;
+        a.out = out;
+        const int64_t waves = a.groups * a.slices;
+        if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
+        if (half) k_grad_join<uint16_t><<<wave_grid(waves), kThreads, 0, s>>>(g, a);
+        else k_grad_join<float><<<wave_grid(waves), kThreads, 0, s>>>(g, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        a.in = out;
+        a.span *= kFan;
+    }
+    return hipSuccess;
 }
 
 }  // namespace tre

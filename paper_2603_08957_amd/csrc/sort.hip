@@ -30,7 +30,6 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kIpt = 16;
 constexpr int kTile = kThreads * kIpt;  // 4096 items
-constexpr int kPerWave = kTile / kWaves;
 constexpr int kMaxBits = 8;
 constexpr int kRadix = 1 << kMaxBits;
 constexpr int kDpt = kRadix / kThreads;  // digits per thread in the prefix step
@@ -40,10 +39,11 @@ static_assert(kDpt >= 1 && kDpt * kThreads == kRadix, "radix must be a multiple 
 // memory (the grid is then sized for n, the capacity).
 __device__ inline int64_t item_count(int64_t n, const int64_t* dn) { return dn ? min(*dn, n) : n; }
 
-template <typename KT>
+template <typename KT, int kIpt>
 __global__ __launch_bounds__(kThreads) void k_digit_hist(const KT* __restrict__ keys, int64_t cap,
                                                          const int64_t* __restrict__ dn, int shift, int dbits,
                                                          int32_t* __restrict__ hist, int64_t n_tiles) {
+    constexpr int kTile = kThreads * kIpt;
     __shared__ int32_t cnt[kRadix];
     const int64_t n = item_count(cap, dn);
     const int radix = 1 << dbits;
@@ -68,13 +68,14 @@ __global__ __launch_bounds__(kThreads) void k_digit_hist(const KT* __restrict__ 
 // SPLIT (uint64 payloads only): write the payload's high and low halves to
 // two int32 arrays instead of vout.  KT: uint64 keys, or uint32 keys when
 // the sorted bits fit (less traffic per pass).
-template <typename KT, typename VT, bool SPLIT>
+template <typename KT, typename VT, bool SPLIT, int kIpt>
 __global__ __launch_bounds__(kThreads) void k_digit_scatter(const KT* __restrict__ kin, const VT* __restrict__ vin,
                                                             KT* __restrict__ kout, VT* __restrict__ vout,
                                                             int32_t* __restrict__ hi_out, int32_t* __restrict__ lo_out,
                                                             int64_t cap, const int64_t* __restrict__ dn, int shift,
                                                             int dbits, const int32_t* __restrict__ offs,
                                                             int64_t n_tiles) {
+    constexpr int kTile = kThreads * kIpt, kPerWave = kTile / kWaves;
     const int64_t n = item_count(cap, dn);
     if (int64_t(blockIdx.x) * kTile >= n) return;  // tiles past the count (their counts are 0)
     __shared__ KT skey[kTile];
@@ -187,25 +188,25 @@ __global__ __launch_bounds__(kThreads) void k_digit_scatter(const KT* __restrict
 
 int sort_passes(int bits) { return bits <= 0 ? 0 : (bits + kMaxBits - 1) / kMaxBits; }
 
-template <typename KT, typename VT>
+template <typename KT, typename VT, int IPT = kIpt>
 hipError_t sort_impl(KT* keys, VT* vals, KT* keys_alt, VT* vals_alt, int64_t n, const int64_t* dn, int bits,
                      int32_t* hist, int32_t* scan_tmp, int32_t* split_hi, int32_t* split_lo, hipStream_t s) {
     if (n <= 1 || bits <= 0) return hipSuccess;
-    const int64_t nt = (n + kTile - 1) / kTile;
+    const int64_t nt = (n + kThreads * IPT - 1) / (kThreads * IPT);
     const int passes = sort_passes(bits);
     const int dbits = (bits + passes - 1) / passes;
     KT *ki = keys, *ko = keys_alt;
     VT *vi = vals, *vo = vals_alt;
     for (int p = 0; p < passes; p++) {
         const int shift = dbits * p;
-        k_digit_hist<KT><<<dim3(unsigned(nt)), kThreads, 0, s>>>(ki, n, dn, shift, dbits, hist, nt);
+        k_digit_hist<KT, IPT><<<dim3(unsigned(nt)), kThreads, 0, s>>>(ki, n, dn, shift, dbits, hist, nt);
         hipError_t e = scan_exclusive_i32(hist, hist, (int64_t(1) << dbits) * nt, scan_tmp, s);
         if (e != hipSuccess) return e;
         if (split_hi && p == passes - 1)
-            k_digit_scatter<KT, VT, true><<<dim3(unsigned(nt)), kThreads, 0, s>>>(
+            k_digit_scatter<KT, VT, true, IPT><<<dim3(unsigned(nt)), kThreads, 0, s>>>(
                 ki, vi, ko, vo, split_hi, split_lo, n, dn, shift, dbits, hist, nt);
         else
-            k_digit_scatter<KT, VT, false><<<dim3(unsigned(nt)), kThreads, 0, s>>>(
+            k_digit_scatter<KT, VT, false, IPT><<<dim3(unsigned(nt)), kThreads, 0, s>>>(
                 ki, vi, ko, vo, nullptr, nullptr, n, dn, shift, dbits, hist, nt);
         std::swap(ki, ko);
         std::swap(vi, vo);
@@ -216,6 +217,13 @@ hipError_t sort_impl(KT* keys, VT* vals, KT* keys_alt, VT* vals_alt, int64_t n, 
 }  // namespace
 
 int64_t radix_hist_elems(int64_t n) { return int64_t(kRadix) * ((n + kTile - 1) / kTile) + 64; }
+
+// Tiles of 1,024 items while the count matrix of a pass is still scanned by one
+// workgroup: 65,536 items are 16 tiles of 4,096 for 256 CUs.
+static bool small_tiles(int64_t n) { return n <= 128 * 1024; }
+int64_t radix_u32_hist_elems(int64_t n) {
+    return small_tiles(n) ? int64_t(kRadix) * ((n + 1023) / 1024) + 64 : radix_hist_elems(n);
+}
 
 bool radix_result_in_alt(int64_t n, int bits) { return n > 1 && (sort_passes(bits) & 1); }
 
@@ -228,6 +236,9 @@ hipError_t radix_sort_u64(uint64_t* keys, uint32_t* vals, uint64_t* keys_alt, ui
 hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, uint32_t* vals_alt, int64_t n, int bits,
                           int32_t* hist, int32_t* scan_tmp, hipStream_t s) {
     if (bits > 32) return hipErrorInvalidValue;
+    if (small_tiles(n))
+        return sort_impl<uint32_t, uint32_t, 4>(keys, vals, keys_alt, vals_alt, n, nullptr, bits, hist, scan_tmp, nullptr,
+                                                nullptr, s);
     return sort_impl<uint32_t, uint32_t>(keys, vals, keys_alt, vals_alt, n, nullptr, bits, hist, scan_tmp, nullptr,
                                          nullptr, s);
 }

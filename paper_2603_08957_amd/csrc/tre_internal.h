@@ -215,6 +215,8 @@ int64_t radix_hist_elems(int64_t n);
 bool radix_result_in_alt(int64_t n, int bits);
 hipError_t radix_sort_u64(uint64_t* keys, uint32_t* vals, uint64_t* keys_alt, uint32_t* vals_alt, int64_t n,
                           int bits, int32_t* hist, int32_t* scan_tmp, hipStream_t s);
+// (hist: radix_u32_hist_elems(n) entries)
+int64_t radix_u32_hist_elems(int64_t n);
 hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, uint32_t* vals_alt, int64_t n, int bits,
                           int32_t* hist, int32_t* scan_tmp, hipStream_t s);
 hipError_t radix_sort_u64_pairs(uint64_t* keys, uint64_t* vals, uint64_t* keys_alt, uint64_t* vals_alt, int64_t n,

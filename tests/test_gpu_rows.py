@@ -121,10 +121,12 @@ def test_ids_out_of_range():
         assert torch.equal(tre.lookup(table, x), got) and torch.equal(tre.lookup_grad(g, x, 5), want)
 
 
-GRADS = [  # tokens, rows, row, kind: at and around the chunks of 32 and the sort's tiles of 4,096
+GRADS = [  # tokens, rows, row, kind: at and around the chunks of 8 and 32, their groups of 16, the sorts' tiles and limits
     (1, 1, 1, "one"), (1, 50, 9, "each"), (31, 5, 8, "zipf"), (32, 5, 33, "one"), (33, 40, 64, "one"), (64, 70, 7, "each"),
     (65, 3, 513, "padded"), (200, 10, 767, "none"), (500, 2000, 20, "zipf"), (1000, 100, 130, "padded"),
     (4096, 1000, 16, "zipf"), (4097, 300, 24, "one"), (9000, 70000, 8, "padded"), (20000, 50, 8, "zipf"),
+    (8192, 300, 6, "padded"), (8193, 9000, 6, "each"), (16384, 40, 10, "zipf"), (16385, 40, 10, "one"),
+    (300000, 9, 3, "zipf"), (140000, 3, 2, "one"),
 ]
 
 
