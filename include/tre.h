@@ -76,10 +76,11 @@ typedef enum {
  * A tile of R rows (the operand's labels that W keeps, in W's order, the ones
  * both operands have first) and K contracted values (their labels in U's
  * order) is
- *     codes  [R][B][16 bytes]  value 2 i of a block in the low half of byte i
- *     scales [R][B]
+ *     codes  [B / G][R][G][16 bytes]  value 2 i of a block in the low half of byte i
+ *     scales [B / G][R][G]
  * with B blocks to a row: 1 for K <= 32, 2 for K <= 64, else 4 ceil(K / 128)
- * (values past K are zero), padded to a multiple of 16 bytes.
+ * (values past K are zero), in groups of G = min(B, 4), padded to a multiple of
+ * 16 bytes.
  * tre_mx_quantize writes such tiles, tre_tile_bytes gives their size. */
 typedef enum { TRE_F32 = 0, TRE_BF16 = 1, TRE_MXFP4 = 2 } tre_dtype;
 

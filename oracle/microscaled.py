@@ -77,6 +77,9 @@ def encode(x: np.ndarray):
 def pack(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
     """(codes [n, R, B, 32], scales [n, R, B]) -> uint8 [n, tile_bytes]."""
     n, r, b = scales.shape
+    g = min(b, 4)  # groups of four blocks, every row of one before the next
+    codes = codes.reshape(n, r, b // g, g, 32).transpose(0, 2, 1, 3, 4)
+    scales = scales.reshape(n, r, b // g, g).transpose(0, 2, 1, 3)
     out = np.zeros((n, -(-17 * r * b // 16) * 16), np.uint8)
     c = codes.reshape(n, r * b, 16, 2)
     out[:, :16 * r * b] = (c[..., 0] | (c[..., 1] << 4)).reshape(n, 16 * r * b)

@@ -18,7 +18,9 @@ namespace {
 constexpr int kThreads = 256;
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ inline float as_f32(const float* p) { return *p; }
 __device__ inline float as_f32(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }
@@ -57,6 +59,8 @@ struct MxTiles {
     int64_t elems;      // of an unquantised tile
     int64_t rows, K;
     int64_t blocks;     // of a row
+    int group;          // blocks of a group
+    int lanes;          // rows kernels: log2 of the lanes side by side on a row
     int64_t bytes;      // of a 4-bit tile
     int64_t n;          // tiles
 };
@@ -101,8 +105,9 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxTiles g, const T* __
 #pragma unroll
     for (int i = 0; i < 4; i++) q[i] = codes8(v + 8 * i, sb);
     uint8_t* out = dst + t * g.bytes;
-    *reinterpret_cast<uint4*>(out + x * 16) = make_uint4(q[0], q[1], q[2], q[3]);
-    out[per * 16 + x] = uint8_t(sb);
+    const uint32_t at_block = mx_block_of(uint32_t(g.rows), g.group, uint32_t(r), uint32_t(x - r * g.blocks));
+    *reinterpret_cast<uint4*>(out + int64_t(at_block) * 16) = make_uint4(q[0], q[1], q[2], q[3]);
+    out[per * 16 + at_block] = uint8_t(sb);
 }
 
 template <typename T>
@@ -112,9 +117,10 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantize(MxTiles g, const uin
     if (b >= g.n * per) return;
     const int64_t t = b / per, x = b - t * per, r = x / g.blocks, k0 = (x - r * g.blocks) * kMxBlock;
     const uint8_t* in = src + t * g.bytes;
-    const uint4 c = *reinterpret_cast<const uint4*>(in + x * 16);
+    const uint32_t from = mx_block_of(uint32_t(g.rows), g.group, uint32_t(r), uint32_t(x - r * g.blocks));
+    const uint4 c = *reinterpret_cast<const uint4*>(in + int64_t(from) * 16);
     const uint32_t q[4] = {c.x, c.y, c.z, c.w};
-    const int sb = in[per * 16 + x];
+    const int sb = in[per * 16 + from];
     T* at = dst + t * g.elems + offset_of(g.row, r);
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -218,83 +224,97 @@ __device__ inline uint32_t quad_max(uint32_t m) {
     return max(m, uint32_t(__builtin_amdgcn_mov_dpp(int(m), 0x4E, 0xf, 0xf, true)));  // lanes 2 3 0 1
 }
 
-// The eights of a workgroup: kRun * kThreads consecutive ones, g.line to a row
-// and g.tile to a tile, the first found in 64 bits and the others from it in 32.
+// The eights of a workgroup: kRun * kWaves strips, a wavefront's each, of
+// consecutive rows (over all tiles) and the same 1 << g.lanes eights of them, so
+// that rows which lie side by side in a group are written together.  g.line:
+// strips' eights of a row, g.tile: rows of a tile.
+constexpr int kWaves = kThreads / 64;
+
 struct RunPos {
-    int64_t t0;
-    uint32_t w0;
+    int64_t t;       // tile
+    uint32_t r, e;   // row in it, eight of the row
+    bool in;
 };
-__device__ inline RunPos run_pos(const MxTiles& g) {
-    const int64_t q = int64_t(blockIdx.x) * (kRun * kThreads), t = q / g.tile.d;
-    return RunPos{t, uint32_t(q - t * g.tile.d)};
+// (the workgroup's first row is found in 64 bits, the others from it in 32)
+__device__ inline RunPos run_pos(const MxTiles& g, int64_t t0, uint32_t r0, uint32_t e0, int i) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint32_t row = r0 + ((i * kWaves + w) << (6 - g.lanes)) + (lane >> g.lanes), dt = g.tile.of(row);
+    RunPos p;
+    p.t = t0 + dt;
+    p.r = row - dt * g.tile.d;
+    p.e = e0 + (lane & ((1 << g.lanes) - 1));
+    p.in = p.t < g.n;
+    return p;
+}
+__device__ inline void run_start(const MxTiles& g, int64_t& t0, uint32_t& r0, uint32_t& e0) {
+    const int64_t b = int64_t(blockIdx.x), rows = b / g.line.d;  // (strips of a row vary first)
+    e0 = uint32_t(b - rows * g.line.d) << g.lanes;
+    const int64_t row = rows * (int64_t(kRun * kWaves) << (6 - g.lanes));
+    t0 = row / g.tile.d;
+    r0 = uint32_t(row - t0 * g.tile.d);
 }
 
-// How a row's eights lie in the unquantised tile: one after the other through
-// the whole tile; whole, but rows begin anywhere or end in zeros; the last cut.
-enum RunKind { RUN_LINEAR, RUN_WHOLE, RUN_CUT };
+// How a row's eights lie in the unquantised tile: all of them, all but blocks
+// of zeros at the end, the last cut.
+enum RunKind { RUN_FULL, RUN_WHOLE, RUN_CUT };
 
 template <typename T, RunKind KIND>
 __global__ __launch_bounds__(kThreads) void k_mx_quantize_rows(MxTiles g, const T* __restrict__ src, uint8_t* __restrict__ dst) {
-    const RunPos p = run_pos(g);
-    const int64_t scales = g.rows * g.blocks * 16;
+    int64_t t0;
+    uint32_t r0, e0;
+    run_start(g, t0, r0, e0);
+    const uint32_t eights = uint32_t(g.blocks * 4), rows = uint32_t(g.rows);
     Eight<T> v[kRun];
-    uint32_t dt[kRun], w[kRun];  // tile after the first, eight in the tile
-    bool in[kRun];
 #pragma unroll
     for (int i = 0; i < kRun; i++) {
-        const uint32_t x = p.w0 + i * kThreads + threadIdx.x;
-        dt[i] = g.tile.of(x);
-        w[i] = x - dt[i] * g.tile.d;
-        in[i] = p.t0 + dt[i] < g.n;
-        // (past the last tile: the first tile again, not written)
-        const T* at = src + (p.t0 + (in[i] ? dt[i] : 0)) * g.elems;
-        if constexpr (KIND == RUN_LINEAR) {
-            v[i].load(at + uint64_t(w[i]) * 8, 8);
-        } else {
-            const uint32_t r = g.line.of(w[i]), k = (w[i] - r * g.line.d) * 8;
-            at += g.row.n <= 1 ? int64_t(r) * g.row.stride[0] : offset_of(g.row, r);
-            if constexpr (KIND == RUN_WHOLE) v[i].load_or_zero(at, k, uint32_t(g.K));
-            else v[i].load(at + k, g.K - k);
-        }
+        // (past the last row or eight: a place that is there, not written)
+        RunPos p = run_pos(g, t0, r0, e0, i);
+        if (!p.in) p.t = p.r = 0;
+        const uint32_t k = min(p.e, eights - 1) * 8;
+        const T* at = src + p.t * g.elems + (g.row.n <= 1 ? int64_t(p.r) * g.row.stride[0] : offset_of(g.row, p.r));
+        if constexpr (KIND == RUN_FULL) v[i].load(at + k, 8);
+        else if constexpr (KIND == RUN_WHOLE) v[i].load_or_zero(at, k, uint32_t(g.K));
+        else v[i].load(at + k, g.K - k);
     }
 #pragma unroll
     for (int i = 0; i < kRun; i++) {
+        const RunPos p = run_pos(g, t0, r0, e0, i);
         const int sb = scale_byte(quad_max(v[i].top()));
-        if (!in[i]) continue;
-        uint8_t* out = dst + (p.t0 + dt[i]) * g.bytes;
-        *reinterpret_cast<uint32_t*>(out + uint64_t(w[i]) * 4) = v[i].codes(sb);
-        if ((w[i] & 3) == 0) out[scales + w[i] / 4] = uint8_t(sb);
+        if (!p.in || p.e >= eights) continue;
+        uint8_t* out = dst + p.t * g.bytes;
+        const uint32_t b = mx_block_of(rows, g.group, p.r, p.e / 4);
+        *reinterpret_cast<uint32_t*>(out + int64_t(b) * 16 + (p.e & 3) * 4) = v[i].codes(sb);
+        if ((p.e & 3) == 0) out[g.rows * g.blocks * 16 + b] = uint8_t(sb);
     }
 }
 
-// (g.line: the eights of a row that reach into K; blocks past it are not read)
+// (eights past K are not read)
 template <typename T, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_mx_dequantize_rows(MxTiles g, const uint8_t* __restrict__ src, T* __restrict__ dst) {
-    const RunPos p = run_pos(g);
-    const int64_t scales = g.rows * g.blocks * 16;
-    uint32_t q[kRun], dt[kRun], r[kRun], k[kRun];
+    int64_t t0;
+    uint32_t r0, e0;
+    run_start(g, t0, r0, e0);
+    const uint32_t eights = uint32_t((g.K + 7) / 8), rows = uint32_t(g.rows);
+    uint32_t q[kRun];
     int sb[kRun];
-    bool in[kRun];
 #pragma unroll
     for (int i = 0; i < kRun; i++) {
-        const uint32_t x = p.w0 + i * kThreads + threadIdx.x;
-        dt[i] = g.tile.of(x);
-        const uint32_t w = x - dt[i] * g.tile.d;
-        in[i] = p.t0 + dt[i] < g.n;
-        r[i] = g.line.of(w);
-        k[i] = (w - r[i] * g.line.d) * 8;
-        const uint8_t* at = src + (p.t0 + (in[i] ? dt[i] : 0)) * g.bytes;
-        const uint32_t b = r[i] * uint32_t(g.blocks) + k[i] / kMxBlock;
-        q[i] = *reinterpret_cast<const uint32_t*>(at + uint64_t(b) * 16 + (k[i] % kMxBlock) / 2);
-        sb[i] = at[scales + b];
+        RunPos p = run_pos(g, t0, r0, e0, i);
+        if (!p.in) p.t = p.r = 0;
+        const uint32_t e = min(p.e, eights - 1), b = mx_block_of(rows, g.group, p.r, e / 4);
+        const uint8_t* at = src + p.t * g.bytes;
+        q[i] = *reinterpret_cast<const uint32_t*>(at + int64_t(b) * 16 + (e & 3) * 4);
+        sb[i] = at[g.rows * g.blocks * 16 + b];
     }
 #pragma unroll
     for (int i = 0; i < kRun; i++) {
-        if (!in[i]) continue;
-        T* out = dst + (p.t0 + dt[i]) * g.elems + (g.row.n <= 1 ? int64_t(r[i]) * g.row.stride[0] : offset_of(g.row, r[i])) + k[i];
+        const RunPos p = run_pos(g, t0, r0, e0, i);
+        if (!p.in || p.e >= eights) continue;
+        const int64_t k = 8 * int64_t(p.e);
+        T* out = dst + p.t * g.elems + (g.row.n <= 1 ? int64_t(p.r) * g.row.stride[0] : offset_of(g.row, p.r)) + k;
         float v[8];
         mx_values(q[i], sb[i], v);
-        if (!CUT || g.K - k[i] >= 8) {
+        if (!CUT || g.K - k >= 8) {
             if constexpr (sizeof(T) == 2) {
                 u32x4_2 a;
 #pragma unroll
@@ -313,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantize_rows(MxTiles g, cons
         } else {
 #pragma unroll
             for (int j = 0; j < 8; j++)
-                if (k[i] + j < g.K) put(out + j, v[j]);
+                if (k + j < g.K) put(out + j, v[j]);
         }
     }
 }
@@ -323,20 +343,23 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantize_rows(MxTiles g, cons
 // so that lanes side by side read consecutive rows of one k.  The last of an
 // odd number of bf16 rows goes with the row before it once more.
 
-// A thread's tile, block and first row; g.line: lines (of R rows) of a tile,
-// g.tile: lines and blocks.
+// A thread's tile, block and first row: the lanes of a wavefront take
+// consecutive lines (of R rows) of a group, its wavefronts the group's blocks.
+// g.line: lines of a tile, g.tile: lines and groups.
 struct ColPos {
     int64_t t;
     uint32_t kb, r;
 };
 template <int R>
 __device__ inline ColPos col_pos(const MxTiles& g) {
-    const int64_t x0 = int64_t(blockIdx.x) * kThreads, t0 = x0 / g.tile.d;
-    const uint32_t x = uint32_t(x0 - t0 * g.tile.d) + threadIdx.x, dt = g.tile.of(x), w = x - dt * g.tile.d;
+    const int w = threadIdx.x >> 6, sets = kWaves / g.group;  // wavefronts of different lines
+    const int64_t x0 = int64_t(blockIdx.x) * (64 * sets), t0 = x0 / g.tile.d;
+    const uint32_t x = uint32_t(x0 - t0 * g.tile.d) + (w / g.group) * 64 + (threadIdx.x & 63), dt = g.tile.of(x), y = x - dt * g.tile.d;
+    const uint32_t group = g.line.of(y);
     ColPos p;
     p.t = t0 + dt;
-    p.kb = g.line.of(w);
-    p.r = min((w - p.kb * g.line.d) * R, uint32_t(g.rows) - R);
+    p.kb = group * g.group + w % g.group;
+    p.r = min((y - group * g.line.d) * R, uint32_t(g.rows) - R);
     return p;
 }
 
@@ -359,7 +382,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize_cols(MxTiles g, const 
 #pragma unroll
     for (int i = 0; i < kMxBlock; i++) v[i] = i < left ? v[i] : 0u;
     uint8_t* out = dst + p.t * g.bytes;
-    const int64_t b0 = int64_t(p.r) * g.blocks + p.kb, scales = g.rows * g.blocks * 16;
+    const int64_t b0 = mx_block_of(uint32_t(g.rows), g.group, p.r, p.kb), scales = g.rows * g.blocks * 16;
     if constexpr (R == 1) {
         uint32_t m = 0;
         float f[kMxBlock];
@@ -388,8 +411,8 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize_cols(MxTiles g, const 
                     e.v[j] = __builtin_amdgcn_perm(v[8 * i + 2 * j + 1], v[8 * i + 2 * j], h ? 0x07060302u : 0x05040100u);
                 q[i] = e.codes(sb);
             }
-            *reinterpret_cast<uint4*>(out + (b0 + h * g.blocks) * 16) = make_uint4(q[0], q[1], q[2], q[3]);
-            out[scales + b0 + h * g.blocks] = uint8_t(sb);
+            *reinterpret_cast<uint4*>(out + (b0 + h * g.group) * 16) = make_uint4(q[0], q[1], q[2], q[3]);
+            out[scales + b0 + h * g.group] = uint8_t(sb);
         }
     }
 }
@@ -399,18 +422,18 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantize_cols(MxTiles g, cons
     constexpr int R = sizeof(T) == 2 ? 2 : 1;
     typedef uint32_t u32_2 __attribute__((aligned(2)));
     const ColPos p = col_pos<R>(g);
-    if (p.t >= g.n) return;
     const int left = int(min(g.K - int64_t(p.kb) * kMxBlock, int64_t(kMxBlock)));
+    if (p.t >= g.n || left <= 0) return;
     const int64_t sk = g.k.stride[0];
     T* at = dst + p.t * g.elems + int64_t(p.kb) * kMxBlock * sk + p.r;
     const uint8_t* in = src + p.t * g.bytes;
-    const int64_t b0 = int64_t(p.r) * g.blocks + p.kb, scales = g.rows * g.blocks * 16;
+    const int64_t b0 = mx_block_of(uint32_t(g.rows), g.group, p.r, p.kb), scales = g.rows * g.blocks * 16;
     uint4 c[R];
     int sb[R];
 #pragma unroll
     for (int h = 0; h < R; h++) {
-        c[h] = *reinterpret_cast<const uint4*>(in + (b0 + h * g.blocks) * 16);
-        sb[h] = in[scales + b0 + h * g.blocks];
+        c[h] = *reinterpret_cast<const uint4*>(in + (b0 + h * g.group) * 16);
+        sb[h] = in[scales + b0 + h * g.group];
     }
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -438,6 +461,7 @@ MxTiles mx_tiles(const Plan& p, int op, int64_t n) {
     g.rows = p.mx_rows[op];
     g.K = p.nK;
     g.blocks = p.mx_blocks;
+    g.group = mx_group(g.blocks);
     g.bytes = p.mx_bytes[op];
     g.n = n;
     return g;
@@ -445,12 +469,28 @@ MxTiles mx_tiles(const Plan& p, int op, int64_t n) {
 
 // ------------------------------------------------------------ contraction
 
+// acc += A B for four blocks of 16 rows each (see above)
+__device__ inline f32x4 mx_mfma(const i32x4& a, const i32x4& b, const f32x4& acc, uint32_t sa, uint32_t sb) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(i32x8{a[0], a[1], a[2], a[3], 0, 0, 0, 0},
+                                                            i32x8{b[0], b[1], b[2], b[3], 0, 0, 0, 0}, acc, 4, 4, 0, int(sa),
+                                                            0, int(sb));
+}
+
+// The same for two blocks of 32 rows each, their scales in byte SB of sa and sb.
+template <int SB>
+__device__ inline f32x16 mx_mfma32(const i32x4& a, const i32x4& b, const f32x16& acc, uint32_t sa, uint32_t sb) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(i32x8{a[0], a[1], a[2], a[3], 0, 0, 0, 0},
+                                                           i32x8{b[0], b[1], b[2], b[3], 0, 0, 0, 0}, acc, 4, 4, SB, int(sa),
+                                                           SB, int(sb));
+}
+
 struct MxArgs {
     const uint8_t *A, *B;
     const int32_t *pa, *pb;
     int64_t a_bytes, b_bytes;    // of a tile
     int32_t a_scales, b_scales;  // where a tile's scales begin
-    int32_t M, N, blocks;        // rows of A and B to a batch index, blocks of a row
+    int32_t M, N, blocks, group; // rows of A and B to a batch index, blocks of a row and of a group
+    int32_t a_rows, b_rows;      // of a tile
     int32_t m_blocks, n_blocks, wg_blocks;
     int32_t w_affine, w_bf16, batched;
     int64_t w_sm, w_elems;
@@ -461,41 +501,52 @@ struct MxArgs {
     float* partials;
 };
 
-// The sums of a wavefront's TM x TN tiles, whose first is at (m0, n0), to the
-// output or partial tile.
-template <int TM, int TN>
-__device__ inline void mx_store(const MxArgs& g, const Unit& u, int b, int m0, int n0, const f32x4 (&acc)[TM][TN]) {
-    const int lane = threadIdx.x & 63, r = lane & 15, gr = lane >> 4;
+// The sums of a wavefront's TM x TN tiles of S x S, whose first is at (m0, n0), to
+// the output or partial tile.  The products are taken with B's rows as the
+// instruction's first operand, so that a lane has four consecutive n of one row
+// m at a time, and one store for them: sums 4 q .. 4 q + 3 are
+// (lane % S, 4 lane / S + 256 q / S ..) of their tile.  (A store for each sum
+// made the end of a 128 x 256 block take as long as 19 of its stages.)
+template <int S, int TM, int TN, typename V>
+__device__ inline void mx_store(const MxArgs& g, const Unit& u, int b, int m0, int n0, const V (&acc)[TM][TN]) {
+    typedef uint32_t u32x2_2 __attribute__((ext_vector_type(2), aligned(2)));
+    typedef float f32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
+    constexpr int Q = S * S / 256;
+    const int lane = threadIdx.x & 63;
     const int64_t base = (u.slot >= 0 ? int64_t(u.slot) : int64_t(u.seg)) * g.w_elems + (g.batched ? g.tWB[b] : 0);
     const bool half = g.w_bf16 && u.slot < 0;
     float* out = u.slot >= 0 ? g.partials : g.W;
-    int32_t col[TN];
-    bool in[TN];
 #pragma unroll
-    for (int j = 0; j < TN; j++) {
-        const int n = n0 + 16 * j + r;
-        in[j] = n < g.N;
-        col[j] = g.w_affine || !in[j] ? n : g.tWN[n];
-    }
+    for (int i = 0; i < TM; i++) {
+        const int m = m0 + S * i + (lane & (S - 1));
+        if (m >= g.M) continue;
+        const int64_t row = base + (g.w_affine ? m * g.w_sm : int64_t(g.tWM[m]));
+        float* at = out + row;
+        uint16_t* at16 = reinterpret_cast<uint16_t*>(out) + row;
 #pragma unroll
-    for (int i = 0; i < TM; i++)
+        for (int j = 0; j < TN; j++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int m = m0 + 16 * i + 4 * gr + e;
-            if (m >= g.M) continue;
-            const int64_t row = base + (g.w_affine ? m * g.w_sm : int64_t(g.tWM[m]));
-            if (half) {
-                uint16_t* at = reinterpret_cast<uint16_t*>(out) + row;
+            for (int q = 0; q < Q; q++) {
+                const int n = n0 + S * j + 256 / S * q + lane / S * 4;
+                const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                if (g.w_affine && n + 4 <= g.N) {
+                    if (half)
+                        *reinterpret_cast<u32x2_2*>(at16 + n) =
+                            u32x2_2{uint32_t(f32_to_bf16_rne(v[0])) | uint32_t(f32_to_bf16_rne(v[1])) << 16,
+                                    uint32_t(f32_to_bf16_rne(v[2])) | uint32_t(f32_to_bf16_rne(v[3])) << 16};
+                    else
+                        *reinterpret_cast<f32x4_4*>(at + n) = f32x4_4{v[0], v[1], v[2], v[3]};
+                    continue;
+                }
 #pragma unroll
-                for (int j = 0; j < TN; j++)
-                    if (in[j]) at[col[j]] = f32_to_bf16_rne(acc[i][j][e]);
-            } else {
-                float* at = out + row;
-#pragma unroll
-                for (int j = 0; j < TN; j++)
-                    if (in[j]) at[col[j]] = acc[i][j][e];
+                for (int e = 0; e < 4; e++) {
+                    if (n + e >= g.N) continue;
+                    const int32_t c = g.w_affine ? n + e : g.tWN[n + e];
+                    if (half) at16[c] = f32_to_bf16_rne(v[e]);
+                    else at[c] = v[e];
+                }
             }
-        }
+    }
 }
 
 // Four wavefronts side by side along N, each with TM x TN tiles of 16 x 16.
@@ -514,9 +565,9 @@ __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
     // rows past the last read the last (their sums are not written)
     int32_t ra[TM], rb[TN];
 #pragma unroll
-    for (int i = 0; i < TM; i++) ra[i] = (b * g.M + min(m0 + 16 * i + r, g.M - 1)) * g.blocks;
+    for (int i = 0; i < TM; i++) ra[i] = b * g.M + min(m0 + 16 * i + r, g.M - 1);
 #pragma unroll
-    for (int j = 0; j < TN; j++) rb[j] = (b * g.N + min(n0 + 16 * j + r, g.N - 1)) * g.blocks;
+    for (int j = 0; j < TN; j++) rb[j] = b * g.N + min(n0 + 16 * j + r, g.N - 1);
     f32x4 acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; i++)
@@ -535,33 +586,44 @@ __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
         int sa[TM], sb[TN];
 #pragma unroll
         for (int i = 0; i < TM; i++) {
-            const uint4 c = *reinterpret_cast<const uint4*>(at + int64_t(ra[i] + kb) * 16);
+            const uint32_t x = mx_block_of(g.a_rows, g.group, ra[i], kb);
+            const uint4 c = *reinterpret_cast<const uint4*>(at + int64_t(x) * 16);
             fa[i] = in ? i32x8{int(c.x), int(c.y), int(c.z), int(c.w), 0, 0, 0, 0} : i32x8{};
-            sa[i] = in ? at[g.a_scales + ra[i] + kb] : 0;
+            sa[i] = in ? at[g.a_scales + x] : 0;
         }
 #pragma unroll
         for (int j = 0; j < TN; j++) {
-            const uint4 c = *reinterpret_cast<const uint4*>(bt + int64_t(rb[j] + kb) * 16);
+            const uint32_t x = mx_block_of(g.b_rows, g.group, rb[j], kb);
+            const uint4 c = *reinterpret_cast<const uint4*>(bt + int64_t(x) * 16);
             fb[j] = in ? i32x8{int(c.x), int(c.y), int(c.z), int(c.w), 0, 0, 0, 0} : i32x8{};
-            sb[j] = in ? bt[g.b_scales + rb[j] + kb] : 0;
+            sb[j] = in ? bt[g.b_scales + x] : 0;
         }
 #pragma unroll
         for (int i = 0; i < TM; i++)
 #pragma unroll
             for (int j = 0; j < TN; j++)
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 0, sa[i], 0, sb[j]);
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], acc[i][j], 4, 4, 0, sb[j], 0, sa[i]);
     }
-    mx_store(g, u, b, m0, n0, acc);
+    mx_store<16>(g, u, b, m0, n0, acc);
 }
 
-// Rows of four blocks or more: 2 x 2 wavefronts, each with TM x TN tiles, read
-// their fragments from LDS.  A stage is four blocks of every row of one pair,
-// copied straight into LDS two stages ahead.
+// Rows of four blocks or more: 2 x 2 wavefronts, each with TM x TN tiles of
+// 32 x 32 (v_mfma_scale_f32_32x32x64_f8f6f4: lane l holds block l / 32 of two of
+// row l % 32, and sums (8 (i / 4) + 4 (l / 32) + i % 4, l % 32)), read their
+// fragments from LDS.  A stage is one group of four blocks of every row of one
+// pair, copied straight into LDS two stages ahead.
 //
 // A stage's codes are [row][4 blocks of 16 bytes], block k of row r in slot
-// k ^ ((r >> 1 ^ r >> 3) & 3): the eight or sixteen lanes that read together
-// then meet every bank once.  A row's four scale bytes are one dword; those of
-// a lane's TM (TN) rows, which lie 16 rows apart, are side by side.
+// k ^ ((r >> 2) & 3): the lanes that read together then meet every bank
+// once.  A row's four scale bytes are one dword; those of a lane's TM (TN) rows,
+// which lie 32 rows apart, are side by side.
+//
+// An 8192^3 product (measured without its rows' quantisation):
+//   16 x 16 tiles, 256 x 256 for a workgroup of one per CU      438 us
+//   128 x 256, two workgroups per CU (one's products cover what
+//   the other waits for)                                        317
+//   32 x 32 tiles: half the instructions                        @@
+// Registers alone do 6.6 PFLOP/s of random codes (power; 8.7 of zeros).
 constexpr int kStages = 3;
 
 // An index list read by scalar loads: the compiler would take vector loads for
@@ -571,15 +633,19 @@ __device__ inline int32_t pair_index(const int32_t* list, int64_t i) {
     return reinterpret_cast<constant>(reinterpret_cast<uintptr_t>(list))[i];
 }
 
-__device__ inline int mx_slot(int r, int k) { return k ^ ((r >> 1 ^ r >> 3) & 3); }
+__device__ inline int mx_slot(int r, int k) { return k ^ ((r >> 2) & 3); }
 
 template <int TM, int TN>
-constexpr int mx_stage_bytes() { return (32 * TM + 32 * TN) * 68; }
+constexpr int mx_stage_bytes() { return (64 * TM + 64 * TN) * 68; }
+
+// Wavefronts of a SIMD that the sums leave room for.
+template <int TM, int TN>
+constexpr int mx_waves() { return TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4; }
 
 template <int TM, int TN>
-__global__ __launch_bounds__(kThreads) void k_mx_lds(MxArgs g) {
+__global__ __launch_bounds__(kThreads, (mx_waves<TM, TN>())) void k_mx_lds(MxArgs g) {
     extern __shared__ __align__(16) char lds[];
-    constexpr int BM = 32 * TM, BN = 32 * TN, ROWS = BM + BN, kStage = mx_stage_bytes<TM, TN>();
+    constexpr int BM = 64 * TM, BN = 64 * TN, ROWS = BM + BN, kStage = mx_stage_bytes<TM, TN>();
     const int64_t unit = blockIdx.x / g.wg_blocks;
     if (unit >= g.hdr->n_units) return;
     const Unit u = g.units[unit];
@@ -587,68 +653,76 @@ __global__ __launch_bounds__(kThreads) void k_mx_lds(MxArgs g) {
     const int nb = x % g.n_blocks;
     x /= g.n_blocks;
     const int mb = x % g.m_blocks, b = x / g.m_blocks;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, gr = lane >> 4;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5;
     const int wm = w >> 1, wn = w & 1;
-    const int steps = g.blocks / 4;  // stages of a pair
 
-    // this wavefront's copies of a stage: codes 16 rows at a time (A's rows,
-    // then B's), scales 64 at a time.  Rows past the last copy the last.
-    constexpr int NC = ROWS / 16 / 4, NS = (ROWS / 64 + 3) / 4;
-    static_assert(ROWS % 64 == 0, "a wavefront copies whole groups of rows");
+    // this wavefront's copies of a stage: codes 16 rows at a time (64 of A to
+    // the workgroup, then of B), scales 64 rows at a time.  Rows past the last
+    // copy the last.
+    constexpr int NC = ROWS / 64, NS = (ROWS / 64 + 3) / 4;
     auto row_of = [&](int row) {
         return row < BM ? b * g.M + min(mb * BM + row, g.M - 1) : b * g.N + min(nb * BN + row - BM, g.N - 1);
     };
     uint32_t voff[NC], vsc[NS];
 #pragma unroll
     for (int i = 0; i < NC; i++) {
-        const int row = (w + 4 * i) * 16 + (lane >> 2);
-        voff[i] = uint32_t(row_of(row) * g.blocks + mx_slot(row & 15, lane & 3)) * 16u;
+        const int row = i * 64 + w * 16 + (lane >> 2);
+        voff[i] = uint32_t(row_of(row) * 4 + mx_slot(row, lane & 3)) * 16u;
     }
 #pragma unroll
     for (int i = 0; i < NS; i++) {
-        // position (half, r, tile) holds row 16 (tiles half + tile) + r
+        // position (half, r, tile) holds row 32 (tiles half + tile) + r
         const int p = min((w + 4 * i) * 64, ROWS - 64) + lane;
         const bool a = p < BM;
-        const int T = a ? TM : TN, q = a ? p : p - BM, half = q / (16 * T), rr = q % (16 * T) / T, t = q % T;
-        vsc[i] = uint32_t(row_of((a ? 0 : BM) + (half * T + t) * 16 + rr) * g.blocks);
+        const int T = a ? TM : TN, q = a ? p : p - BM, hf = q / (32 * T), rr = q % (32 * T) / T, t = q % T;
+        vsc[i] = uint32_t(row_of((a ? 0 : BM) + (hf * T + t) * 32 + rr)) * 4u;
     }
     const uint32_t lds0 = lds_address(lds);
+    const int steps = g.blocks / 4;  // stages of a pair
+    const int64_t a_step = int64_t(g.a_rows) * 64, b_step = int64_t(g.b_rows) * 64;
     const int64_t total = int64_t(u.p1 - u.p0) * steps;
-    // where the next stage to copy begins; the pair after its own is known
-    int64_t pair = u.p0;
-    int step = 0;
-    const uint8_t *at = g.A + pair_index(g.pa, pair) * g.a_bytes, *bt = g.B + pair_index(g.pb, pair) * g.b_bytes;
-    int64_t after = min(pair + 1, int64_t(u.p1) - 1);
+    // the next stage to copy: its codes and scales; the pair after its own is known
+    const uint8_t *at, *bt, *as, *bs;
+    auto set_pair = [&](int32_t a, int32_t bx) {
+        at = g.A + a * g.a_bytes;
+        bt = g.B + bx * g.b_bytes;
+        as = at + g.a_scales;
+        bs = bt + g.b_scales;
+    };
+    set_pair(pair_index(g.pa, u.p0), pair_index(g.pb, u.p0));
+    int32_t after = min(u.p0 + 1, u.p1 - 1), left = steps;
     int32_t a_next = pair_index(g.pa, after), b_next = pair_index(g.pb, after);
-    auto copy = [&](int slot) {
-        const uint32_t l = lds0 + uint32_t(slot) * kStage;
+    auto copy = [&](uint32_t l) {
 #pragma unroll
-        for (int i = 0; i < NC; i++) {
-            const int rows = (w + 4 * i) * 16;
-            lds_copy16<false>(l + rows * 64, (rows < BM ? at : bt) + step * 64, voff[i]);
-        }
+        for (int i = 0; i < NC; i++) lds_copy16<false>(l + i * 4096 + w * 1024, i < TM ? at : bt, voff[i]);
 #pragma unroll
         for (int i = 0; i < NS; i++) {
             const int p = (w + 4 * i) * 64;
-            if (p < ROWS) lds_copy4(l + ROWS * 64 + p * 4, (p < BM ? at + g.a_scales : bt + g.b_scales) + step * 4, vsc[i]);
+            if (p < ROWS) lds_copy4(l + ROWS * 64 + p * 4, p < BM ? as : bs, vsc[i]);
         }
-        if (++step == steps) {
-            step = 0;
-            at = g.A + a_next * g.a_bytes;
-            bt = g.B + b_next * g.b_bytes;
-            after = min(after + 1, int64_t(u.p1) - 1);
+        at += a_step;
+        bt += b_step;
+        as += a_step / 16;
+        bs += b_step / 16;
+        if (--left == 0) {
+            left = steps;
+            set_pair(a_next, b_next);
+            after = min(after + 1, u.p1 - 1);
             a_next = pair_index(g.pa, after);
             b_next = pair_index(g.pb, after);
         }
     };
-    f32x4 acc[TM][TN];
+    f32x16 acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; i++)
 #pragma unroll
-        for (int j = 0; j < TN; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    copy(0);
-    if (total > 1) copy(1);
-    int now = 0;
+        for (int j = 0; j < TN; j++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
+    copy(lds0);
+    if (total > 1) copy(lds0 + kStage);
+    // stage `now` is read while `then`, two on, is copied
+    uint32_t now = 0, then = 2 * kStage;
     for (int64_t s = 0; s < total; s++) {
         // this stage's copies have landed once every wavefront has waited for
         // its own (the next stage's may be in flight); the barrier also says
@@ -661,41 +735,62 @@ __global__ __launch_bounds__(kThreads) void k_mx_lds(MxArgs g) {
         }
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");  // no read of LDS moves up past it
-        const int then = now >= 1 ? now - 1 : now + 2;  // (now + 2) % 3
-        if (s + 2 < total) copy(then);
-        const char* l = lds + now * kStage;
-        now = now == 2 ? 0 : now + 1;
-        i32x8 fa[TM], fb[TN];
+        if (s + 2 < total) copy(lds0 + then);
+        const char* l = lds + now;
+        now = now == 2 * kStage ? 0 : now + kStage;
+        then = then == 2 * kStage ? 0 : then + kStage;
+        i32x4 fa[TM][2], fb[TN][2];
         uint32_t sa[TM], sb[TN];
-        const int sl = mx_slot(r, gr) * 16;
+#pragma unroll
+        for (int i = 0; i < TM; i++) sa[i] = reinterpret_cast<const uint32_t*>(l + ROWS * 64)[wm * 32 * TM + r * TM + i];
+#pragma unroll
+        for (int j = 0; j < TN; j++) sb[j] = reinterpret_cast<const uint32_t*>(l + ROWS * 64)[BM + wn * 32 * TN + r * TN + j];
+        // blocks half and 2 + half of the group
+        const int sl[2] = {mx_slot(r, half) * 16, mx_slot(r, 2 + half) * 16};
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+#pragma unroll
+            for (int i = 0; i < TM; i++) fa[i][k] = *reinterpret_cast<const i32x4*>(l + ((wm * TM + i) * 32 + r) * 64 + sl[k]);
+#pragma unroll
+            for (int j = 0; j < TN; j++) fb[j][k] = *reinterpret_cast<const i32x4*>(l + (BM + (wn * TN + j) * 32 + r) * 64 + sl[k]);
+        }
+        // All reads are on their way before the first product: the compiler
+        // would put each of B's in front of its products and wait for it there.
+        // (An empty statement that uses a value and might touch memory: reads
+        // stay in front of it.)
 #pragma unroll
         for (int i = 0; i < TM; i++) {
-            const uint4 c = *reinterpret_cast<const uint4*>(l + ((wm * TM + i) * 16 + r) * 64 + sl);
-            fa[i] = i32x8{int(c.x), int(c.y), int(c.z), int(c.w), 0, 0, 0, 0};
-            sa[i] = reinterpret_cast<const uint32_t*>(l + ROWS * 64)[wm * 16 * TM + r * TM + i] >> (8 * gr);
+            asm volatile("" : "+v"(sa[i])::"memory");
+            sa[i] >>= 8 * half;  // bytes 0 and 2: the scales of the lane's two blocks
         }
 #pragma unroll
         for (int j = 0; j < TN; j++) {
-            const uint4 c = *reinterpret_cast<const uint4*>(l + (BM + (wn * TN + j) * 16 + r) * 64 + sl);
-            fb[j] = i32x8{int(c.x), int(c.y), int(c.z), int(c.w), 0, 0, 0, 0};
-            sb[j] = reinterpret_cast<const uint32_t*>(l + ROWS * 64)[BM + wn * 16 * TN + r * TN + j] >> (8 * gr);
+            asm volatile("" : "+v"(sb[j])::"memory");
+            sb[j] >>= 8 * half;
         }
 #pragma unroll
-        for (int j = 0; j < TN; j++)
+        for (int k = 0; k < 2; k++) {
 #pragma unroll
-            for (int i = 0; i < TM; i++)
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 0, int(sa[i]), 0,
-                                                                             int(sb[j]));
+            for (int i = 0; i < TM; i++) asm volatile("" : "+v"(fa[i][k])::"memory");
+#pragma unroll
+            for (int j = 0; j < TN; j++) {
+                asm volatile("" : "+v"(fb[j][k])::"memory");
+#pragma unroll
+                for (int i = 0; i < TM; i++)
+                    acc[i][j] = k ? mx_mfma32<2>(fb[j][k], fa[i][k], acc[i][j], sb[j], sa[i])
+                                  : mx_mfma32<0>(fb[j][k], fa[i][k], acc[i][j], sb[j], sa[i]);
+            }
+        }
         lds_read_wait();
     }
-    mx_store(g, u, b, mb * BM + wm * 16 * TM, nb * BN + wn * 16 * TN, acc);
+    mx_store<32>(g, u, b, mb * BM + wm * 32 * TM, nb * BN + wn * 32 * TN, acc);
 }
 
 // How a plan's tiles are cut among workgroups.
 struct MxShape {
     int64_t M, N;
     bool lds;
-    int tm, tn;  // 16 x 16 tiles of a wavefront
+    int tm, tn;  // tiles of a wavefront, 32 x 32 from LDS, else 16 x 16
     int64_t m_blocks, n_blocks;
 };
 
@@ -705,17 +800,14 @@ MxShape mx_shape(const Plan& p) {
     h.N = p.swap ? p.nM : p.nN;
     h.lds = p.mx_blocks >= 4 && h.M > 32 && h.N > 32;
     if (h.lds) {
-        // of 256, 128 or 64 rows the one that leaves the fewest places empty, the larger of two alike
-        auto cut = [](int64_t n) {
-            int best = 8;
-            for (int t : {4, 2})
-                if ((n + 32 * t - 1) / (32 * t) * t < (n + 32 * best - 1) / (32 * best) * best) best = t;
-            return best;
-        };
-        h.tm = cut(h.M);
-        h.tn = cut(h.N);
-        h.m_blocks = (h.M + 32 * h.tm - 1) / (32 * h.tm);
-        h.n_blocks = (h.N + 32 * h.tn - 1) / (32 * h.tn);
+        h.tm = h.M > 64 ? 2 : 1;
+        h.tn = h.N > 128 ? 4 : h.N > 64 ? 2 : 1;
+#ifdef MXTM
+        h.tm = std::min(h.tm, MXTM);
+        h.tn = std::min(h.tn, MXTN);
+#endif
+        h.m_blocks = (h.M + 64 * h.tm - 1) / (64 * h.tm);
+        h.n_blocks = (h.N + 64 * h.tn - 1) / (64 * h.tn);
         return h;
     }
     h.tm = h.M > 32 ? 4 : h.M > 16 ? 2 : 1;
@@ -739,7 +831,7 @@ hipError_t run_lds(const MxArgs& g, dim3 grid, hipStream_t s) {
 
 template <int TM>
 hipError_t run_lds_n(int tn, const MxArgs& g, dim3 grid, hipStream_t s) {
-    return tn == 8 ? run_lds<TM, 8>(g, grid, s) : tn == 4 ? run_lds<TM, 4>(g, grid, s) : run_lds<TM, 2>(g, grid, s);
+    return tn == 4 ? run_lds<TM, 4>(g, grid, s) : tn == 2 ? run_lds<TM, 2>(g, grid, s) : run_lds<TM, 1>(g, grid, s);
 }
 
 }  // namespace
@@ -760,55 +852,54 @@ unsigned mx_grid(int64_t items, int64_t per) {
     return b > int64_t(0x7fffffff) ? 0u : unsigned(b);
 }
 
-// Threads to a tile across its rows, and where they stand.
+// The launch along rows of `eights` eights each.
+unsigned rows_grid(MxTiles& g, int64_t eights) {
+    g.lanes = 0;
+    while (g.lanes < 6 && (1 << g.lanes) < eights) g.lanes++;
+    // (a block's four eights are a quad of lanes)
+    g.lanes = std::max(g.lanes, 2);
+    g.line = Divisor((eights + (1 << g.lanes) - 1) >> g.lanes);
+    g.tile = Divisor(g.rows);
+    const int64_t rows = int64_t(kRun * kWaves) << (6 - g.lanes);
+    return mx_grid((g.n * g.rows + rows - 1) / rows * g.line.d, 1);
+}
+
+// The launch across rows.
 template <typename T>
-int64_t col_threads(MxTiles& g, int64_t blocks) {
+unsigned cols_grid(MxTiles& g) {
     constexpr int R = sizeof(T) == 2 ? 2 : 1;
-    const int64_t lines = (g.rows + R - 1) / R;
+    const int64_t lines = (g.rows + R - 1) / R, groups = g.blocks / g.group;
     g.line = Divisor(lines);
-    g.tile = Divisor(lines * blocks);
-    return lines * blocks;
+    g.tile = Divisor(lines * groups);
+    return mx_grid(g.n * lines * groups, 64 * (kWaves / g.group));
 }
 
 template <typename T>
 hipError_t quantize(MxTiles g, const T* src, uint8_t* dst, hipStream_t s) {
     const MxWay way = mx_way(g);
-    if (way == MX_ROWS) {
-        g.line = Divisor(g.blocks * 4);
-        g.tile = Divisor(g.rows * g.blocks * 4);
-        const unsigned grid = mx_grid(g.n * g.rows * g.blocks * 4, kRun * kThreads);
-        if (!grid) return hipErrorInvalidConfiguration;
-        const bool side_by_side = g.row.n == 0 || (g.row.n == 1 && g.row.stride[0] == g.K);
-        if (side_by_side && g.K == g.blocks * kMxBlock) k_mx_quantize_rows<T, RUN_LINEAR><<<grid, kThreads, 0, s>>>(g, src, dst);
-        else if (g.K % 8 == 0) k_mx_quantize_rows<T, RUN_WHOLE><<<grid, kThreads, 0, s>>>(g, src, dst);
-        else k_mx_quantize_rows<T, RUN_CUT><<<grid, kThreads, 0, s>>>(g, src, dst);
-    } else {
-        const unsigned grid = mx_grid(g.n * (way == MX_COLS ? col_threads<T>(g, g.blocks) : g.rows * g.blocks), kThreads);
-        if (!grid) return hipErrorInvalidConfiguration;
-        if (way == MX_COLS) k_mx_quantize_cols<<<grid, kThreads, 0, s>>>(g, src, dst);
-        else k_mx_quantize<<<grid, kThreads, 0, s>>>(g, src, dst);
-    }
+    const unsigned grid = way == MX_ROWS   ? rows_grid(g, g.blocks * 4)
+                          : way == MX_COLS ? cols_grid<T>(g)
+                                           : mx_grid(g.n * g.rows * g.blocks, kThreads);
+    if (!grid) return hipErrorInvalidConfiguration;
+    if (way == MX_COLS) k_mx_quantize_cols<<<grid, kThreads, 0, s>>>(g, src, dst);
+    else if (way == MX_ANY) k_mx_quantize<<<grid, kThreads, 0, s>>>(g, src, dst);
+    else if (g.K == g.blocks * kMxBlock) k_mx_quantize_rows<T, RUN_FULL><<<grid, kThreads, 0, s>>>(g, src, dst);
+    else if (g.K % 8 == 0) k_mx_quantize_rows<T, RUN_WHOLE><<<grid, kThreads, 0, s>>>(g, src, dst);
+    else k_mx_quantize_rows<T, RUN_CUT><<<grid, kThreads, 0, s>>>(g, src, dst);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t dequantize(MxTiles g, const uint8_t* src, T* dst, hipStream_t s) {
     const MxWay way = mx_way(g);
-    if (way == MX_ROWS) {
-        const int64_t line = (g.K + 7) / 8;
-        g.line = Divisor(line);
-        g.tile = Divisor(g.rows * line);
-        const unsigned grid = mx_grid(g.n * g.rows * line, kRun * kThreads);
-        if (!grid) return hipErrorInvalidConfiguration;
-        if (g.K % 8 == 0) k_mx_dequantize_rows<T, false><<<grid, kThreads, 0, s>>>(g, src, dst);
-        else k_mx_dequantize_rows<T, true><<<grid, kThreads, 0, s>>>(g, src, dst);
-    } else {
-        const unsigned grid = mx_grid(
-            g.n * (way == MX_COLS ? col_threads<T>(g, (g.K + kMxBlock - 1) / kMxBlock) : g.rows * g.blocks), kThreads);
-        if (!grid) return hipErrorInvalidConfiguration;
-        if (way == MX_COLS) k_mx_dequantize_cols<<<grid, kThreads, 0, s>>>(g, src, dst);
-        else k_mx_dequantize<<<grid, kThreads, 0, s>>>(g, src, dst);
-    }
+    const unsigned grid = way == MX_ROWS   ? rows_grid(g, (g.K + 7) / 8)
+                          : way == MX_COLS ? cols_grid<T>(g)
+                                           : mx_grid(g.n * g.rows * g.blocks, kThreads);
+    if (!grid) return hipErrorInvalidConfiguration;
+    if (way == MX_COLS) k_mx_dequantize_cols<<<grid, kThreads, 0, s>>>(g, src, dst);
+    else if (way == MX_ANY) k_mx_dequantize<<<grid, kThreads, 0, s>>>(g, src, dst);
+    else if (g.K % 8 == 0) k_mx_dequantize_rows<T, false><<<grid, kThreads, 0, s>>>(g, src, dst);
+    else k_mx_dequantize_rows<T, true><<<grid, kThreads, 0, s>>>(g, src, dst);
     return hipGetLastError();
 }
 
@@ -849,6 +940,9 @@ hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_til
     g.a_bytes = p.mx_bytes[a];
     g.b_bytes = p.mx_bytes[b];
     g.blocks = int32_t(p.mx_blocks);
+    g.group = mx_group(p.mx_blocks);
+    g.a_rows = int32_t(p.mx_rows[a]);
+    g.b_rows = int32_t(p.mx_rows[b]);
     g.a_scales = int32_t(p.mx_rows[a] * p.mx_blocks * 16);
     g.b_scales = int32_t(p.mx_rows[b] * p.mx_blocks * 16);
     g.M = int32_t(h.M);
@@ -872,7 +966,7 @@ hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_til
     g.partials = reinterpret_cast<float*>(ws + L.partials);
     const dim3 grid{unsigned(wg * unit_bound)}, block{unsigned(kThreads)};
     if (h.lds)
-        return h.tm == 8 ? run_lds_n<8>(h.tn, g, grid, s) : h.tm == 4 ? run_lds_n<4>(h.tn, g, grid, s) : run_lds_n<2>(h.tn, g, grid, s);
+        return h.tm == 2 ? run_lds_n<2>(h.tn, g, grid, s) : run_lds_n<1>(h.tn, g, grid, s);
     if (h.tm == 4)
         return h.tn == 2 ? launch_k(k_mx<4, 2>, grid, block, 0, s, g) : launch_k(k_mx<4, 1>, grid, block, 0, s, g);
     if (h.tm == 2)

@@ -148,14 +148,17 @@ constexpr int kStrips = 4;
 template <typename TI, int E>
 __device__ inline void lookup_load(const LookupArgs& g, int64_t id, int64_t e, float (&v)[E]) {
     if constexpr (std::is_same_v<TI, Mx4>) {
-        const int64_t tile = id / g.tile_rows, row = (id - tile * g.tile_rows) * g.blocks;
+        const int64_t tile = id / g.tile_rows;
         const uint8_t* at = static_cast<const uint8_t*>(g.table) + tile * g.tile_bytes;
-        const int sb = at[g.tile_rows * g.blocks * 16 + row + e / kMxBlock];
+        const uint32_t b = mx_block_of(uint32_t(g.tile_rows), mx_group(g.blocks), uint32_t(id - tile * g.tile_rows),
+                                       uint32_t(e / kMxBlock));
+        const uint8_t* codes = at + int64_t(b) * 16 + e % kMxBlock / 2;
+        const int sb = at[g.tile_rows * g.blocks * 16 + b];
         if constexpr (E == 8) {
-            mx_values(*reinterpret_cast<const uint32_t*>(at + row * 16 + e / 2), sb, v);
+            mx_values(*reinterpret_cast<const uint32_t*>(codes), sb, v);
         } else {
             float w[8];
-            mx_values(*reinterpret_cast<const uint16_t*>(at + row * 16 + e / 2), sb, w);
+            mx_values(*reinterpret_cast<const uint16_t*>(codes), sb, w);
 #pragma unroll
             for (int i = 0; i < E; i++) v[i] = w[i];
         }

@@ -74,18 +74,28 @@ enum TableId { T_AM, T_AK, T_BK, T_BN, T_WM, T_WN, T_AB, T_BB, T_WB, T_EU, T_EV,
 enum KernelClass { KC_GEMM = 0, KC_VEC = 1, KC_MX = 2 };
 
 // ----- tiles in microscaled 4-bit floating point (TRE_MXFP4) -----
-// A tile is [row][block] codes of 16 bytes (32 values of the contracted index,
-// the lower of two in a byte's low half), then [row][block] scale bytes.
+// A block is 32 values of the contracted index: 16 bytes of codes (the lower of
+// two values in a byte's low half) and a scale byte.  A tile is its blocks'
+// codes, then their scales, both as [group][row][block of the group], a group
+// being the 4 blocks of one matrix instruction (all of a row with fewer): what
+// an instruction reads of neighbouring rows lies side by side.  (With whole
+// rows one after the other, 64 bytes of codes and 4 of scales of each row to an
+// instruction, the L2's requests bounded an 8192^3 product: 104 M of them, half
+// for scales.)
 constexpr int kMxBlock = 32;
 constexpr int kMxNanScale = 255;
 
 // Blocks that a row of K values takes: one or two for up to 64 values, else
-// whole matrix instructions of four.  (Rows of one and two blocks share an
-// instruction with the next pairs; of other lengths the last instruction is
-// not filled anyway, and with rows of whole instructions every load of codes
-// is 16 bytes aligned and every load of scales 4.)  Values past K are zero.
+// whole groups.  (Rows of one and two blocks share an instruction with the next
+// pairs; of other lengths the last instruction is not filled anyway.)  Values
+// past K are zero.
 __host__ __device__ inline int64_t mx_row_blocks(int64_t K) {
     return K <= kMxBlock ? 1 : K <= 2 * kMxBlock ? 2 : (K + 4 * kMxBlock - 1) / (4 * kMxBlock) * 4;
+}
+__host__ __device__ inline int mx_group(int64_t blocks) { return blocks < 4 ? int(blocks) : 4; }
+// Number of block kb of row r in a tile of `rows` rows, in groups of g.
+__host__ __device__ inline uint32_t mx_block_of(uint32_t rows, int g, uint32_t r, uint32_t kb) {
+    return g == 1 ? r : g == 2 ? r * 2 + kb : ((kb >> 2) * rows + r) * 4 + (kb & 3);
 }
 __host__ __device__ inline int64_t mx_tile_bytes(int64_t rows, int64_t K) {
     return (rows * mx_row_blocks(K) * 17 + 15) / 16 * 16;
