@@ -33,7 +33,6 @@ int64_t blocks_per_unit(const Plan& p) {
         const int64_t bm = 32 * p.tile_m, bn = 32 * p.tile_n;
         return p.nB * ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
     }
-    if (p.kclass == KC_MX) return mx_blocks_per_unit(p);
     return (p.tile_elems[2] + 255) / 256;
 }
 
@@ -93,7 +92,7 @@ int32_t choose_pacing(const Plan& p, int64_t n_u, int64_t n_pairs, int64_t n_w, 
 // Workgroups one unit occupies: its output blocks (GEMM), or its threads /
 // 256 for the vector class (several small units share a workgroup).
 double unit_workgroups(const Plan& p) {
-    if (p.kclass != KC_VEC) return double(blocks_per_unit(p));
+    if (p.kclass == KC_GEMM) return double(blocks_per_unit(p));
     const int64_t threads = p.vec_dot ? p.tile_elems[2] * 16 : (p.tile_elems[2] + p.vec_ept - 1) / p.vec_ept;
     if (threads > 128) return double((threads + 255) / 256);
     int64_t t = 1;
@@ -118,7 +117,9 @@ int64_t choose_unit(const Plan& p, const Layout& L, int64_t n_pairs, int64_t n_w
         pu = p.opt.max_pairs_per_unit;
     } else if (p.kclass == KC_GEMM && !p.fast) {
         pu = tile_unit_pairs(p, n_pairs, n_w);
-    } else if (double(n_w) * uw >= kTargetWorkgroups || (p.kclass != KC_VEC && double(n_w) * uw >= fill)) {
+    } else if (p.kclass == KC_MX) {
+        pu = mx_unit_pairs(p, n_pairs, n_w);
+    } else if (double(n_w) * uw >= kTargetWorkgroups || (p.kclass == KC_GEMM && double(n_w) * uw >= fill)) {
         pu = std::max<int64_t>(n_pairs, 1);  // enough output blocks: one unit per key
     } else {
         pu = std::max<int64_t>(4, int64_t(std::ceil(double(n_pairs) * uw / kTargetWorkgroups)));
@@ -347,21 +348,23 @@ tre_status contract_enqueue(tre_plan_t plan, const tre_join_result* jr, int64_t 
     // (no key holds more than n_pairs - n_w + 1 pairs, or more than the labels
     // that W does not keep have values: nothing to cut)
     if ((!dev && p_unit > n_pairs - n_w) || p_unit >= p.key_pairs_max) p_unit = n_pairs;
+    // (a key to a unit, as the join left them)
+    const bool whole_keys = p.kclass == KC_MX && !one_pair_keys && p_unit >= n_pairs && mx_whole_keys(p, n_pairs, n_w);
     hipError_t e;
     // (launch_units writes the tile offset tables itself)
     if (R > 1) {
         if ((e = launch_tables(p, reinterpret_cast<int32_t*>(w + L.tables), s)) != hipSuccess)
             return dev_fail(e, "tables");
         e = launch_range_units(p, L, w, n_w, jr->n_u, R, s);
-    } else if (one_pair_keys) {
-        // the join wrote the units
+    } else if (one_pair_keys || whole_keys) {
+        // the join wrote the units, or the kernel takes its segments
         e = launch_tables(p, reinterpret_cast<int32_t*>(w + L.tables), s);
     } else {
         e = launch_units(p, L, w, n_pairs, n_w, p_unit, !pace, s, dev);
     }
     if (e != hipSuccess) return dev_fail(e, "units");
     tm.mark(s);
-    const int64_t unit_bound = R > 1 ? int64_t(R) * n_w : n_w + n_pairs / p_unit + 1;
+    const int64_t unit_bound = R > 1 ? int64_t(R) * n_w : whole_keys ? n_w : n_w + n_pairs / p_unit + 1;
     if (pace) {
         // one unit per key; every workgroup of the grid is resident at once
         const int64_t n_wg = std::min(n_w, slots);
@@ -372,7 +375,7 @@ tre_status contract_enqueue(tre_plan_t plan, const tre_join_result* jr, int64_t 
         e = launch_gemm_paced(p, L, w, u_tiles, v_tiles, w_tiles, n_pairs, n_wg, pace, s);
     } else {
         if (ke.start && ke.stop) t_kernel_events = &ke;
-        e = launch_contract(p, L, w, u_tiles, v_tiles, w_tiles, n_pairs, n_w, unit_bound, s);
+        e = launch_contract(p, L, w, u_tiles, v_tiles, w_tiles, n_pairs, n_w, unit_bound, whole_keys, s);
     }
     t_kernel_events = nullptr;
     if (e != hipSuccess) return dev_fail(e, "contract");
@@ -406,7 +409,7 @@ tre_status contract_enqueue(tre_plan_t plan, const tre_join_result* jr, int64_t 
         }
         WsHeader h{};
         if (!deferred && hipMemcpy(&h, w + L.hdr, sizeof(h), hipMemcpyDeviceToHost) == hipSuccess) {
-            timing->n_units = h.n_units;
+            timing->n_units = whole_keys ? n_w : h.n_units;
             timing->n_split_segments = h.n_split;
             timing->n_partials = h.n_parts;
         }

@@ -933,7 +933,7 @@ hipError_t launch_range_units(const Plan& p, const Layout& L, char* ws, int64_t 
 }
 
 hipError_t launch_contract(const Plan& p, const Layout& L, char* ws, const void* u_tiles, const void* v_tiles,
-                           float* w_tiles, int64_t n_pairs, int64_t n_w, int64_t unit_bound, hipStream_t s) {
+                           float* w_tiles, int64_t n_pairs, int64_t n_w, int64_t unit_bound, bool whole_keys, hipStream_t s) {
     (void)n_w;
     if (unit_bound <= 0) return hipSuccess;
     const int32_t* tb = reinterpret_cast<const int32_t*>(ws + L.tables);
@@ -945,7 +945,7 @@ hipError_t launch_contract(const Plan& p, const Layout& L, char* ws, const void*
     if (p.kclass == KC_GEMM && p.fast)
         return launch_gemm_fast(p, L, ws, u_tiles, v_tiles, w_tiles, n_pairs, unit_bound, s);
     if (p.kclass == KC_GEMM) return launch_gemm_tile(p, L, ws, u_tiles, v_tiles, w_tiles, n_pairs, unit_bound, s);
-    if (p.kclass == KC_MX) return launch_mx(p, L, ws, u_tiles, v_tiles, w_tiles, n_pairs, unit_bound, s);
+    if (p.kclass == KC_MX) return launch_mx(p, L, ws, u_tiles, v_tiles, w_tiles, n_pairs, unit_bound, whole_keys, s);
     // with vec_swap the kernel's first (vector) operand is V: the product is
     // symmetric, so only the roles of the pointers and tables change
     const bool sw = p.vec_swap;

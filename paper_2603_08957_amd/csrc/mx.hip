@@ -343,6 +343,12 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantize_rows(MxTiles g, cons
 // so that lanes side by side read consecutive rows of one k.  The last of an
 // odd number of bf16 rows goes with the row before it once more.
 
+#ifndef DT
+#define DT 100.0
+#endif
+#ifndef UU
+#define UU 4
+#endif
 // A thread's tile, block and first row: the lanes of a wavefront take
 // consecutive lines (of R rows) of a group, its wavefronts the group's blocks.
 // g.line: lines of a tile, g.tile: lines and groups.
@@ -493,13 +499,21 @@ struct MxArgs {
     int32_t a_rows, b_rows;      // of a tile
     int32_t m_blocks, n_blocks, wg_blocks;
     int32_t w_affine, w_bf16, batched;
-    int64_t w_sm, w_elems;
+    int32_t waves_n;             // k_mx: wavefronts of a workgroup side by side along N
+    int64_t w_sm, w_sn, w_elems; // affine: W(m, n) at m w_sm + n w_sn
     const int32_t *tWM, *tWN, *tWB;
     const Unit* units;
+    const int32_t* seg_start;    // not null: a unit to a key, its pairs from here
     const WsHeader* hdr;
     float* W;
     float* partials;
 };
+
+__device__ inline bool mx_unit(const MxArgs& g, int64_t unit, Unit& u) {
+    if (unit >= (g.seg_start ? g.hdr->n_w : g.hdr->n_units)) return false;
+    u = g.seg_start ? Unit{int32_t(unit), g.seg_start[unit], g.seg_start[unit + 1], -1} : g.units[unit];
+    return true;
+}
 
 // The sums of a wavefront's TM x TN tiles of S x S, whose first is at (m0, n0), to
 // the output or partial tile.  The products are taken with B's rows as the
@@ -529,7 +543,7 @@ __device__ inline void mx_store(const MxArgs& g, const Unit& u, int b, int m0, i
             for (int q = 0; q < Q; q++) {
                 const int n = n0 + S * j + 256 / S * q + lane / S * 4;
                 const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                if (g.w_affine && n + 4 <= g.N) {
+                if (g.w_affine && g.w_sn == 1 && n + 4 <= g.N) {
                     if (half)
                         *reinterpret_cast<u32x2_2*>(at16 + n) =
                             u32x2_2{uint32_t(f32_to_bf16_rne(v[0])) | uint32_t(f32_to_bf16_rne(v[1])) << 16,
@@ -541,7 +555,7 @@ __device__ inline void mx_store(const MxArgs& g, const Unit& u, int b, int m0, i
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     if (n + e >= g.N) continue;
-                    const int32_t c = g.w_affine ? n + e : g.tWN[n + e];
+                    const int64_t c = g.w_affine ? (n + e) * g.w_sn : int64_t(g.tWN[n + e]);
                     if (half) at16[c] = f32_to_bf16_rne(v[e]);
                     else at[c] = v[e];
                 }
@@ -549,62 +563,142 @@ __device__ inline void mx_store(const MxArgs& g, const Unit& u, int b, int m0, i
     }
 }
 
-// Four wavefronts side by side along N, each with TM x TN tiles of 16 x 16.
-template <int TM, int TN>
+// An index list read by scalar loads: the compiler would take vector loads for
+// one that the copies' assembly might write, and wait for the copies with them.
+__device__ inline int32_t pair_index(const int32_t* list, int64_t i) {
+    typedef const __attribute__((address_space(4))) int32_t* constant;
+    return reinterpret_cast<constant>(reinterpret_cast<uintptr_t>(list))[i];
+}
+
+// Few rows on one side (M), or rows of one or two blocks: a wavefront has TM x TN
+// tiles of 16 x 16 and reads its fragments from memory, a batch of steps (of
+// four blocks) ahead of the one it multiplies.  g.waves_n wavefronts of a
+// workgroup lie side by side along N; the others take every other step of the
+// same tiles, and the first of them adds their sums in order.
+//
+// What bounds it is how much is on its way: one token against 32,768 rows of
+// 4,096 values (71 MB) took @@ us with one step at a time.
+//
+// SHORT: rows of one or two blocks; a step is then the rows of four or two
+// pairs, each lane's its own.
+template <int TM, int TN, int U, bool SHORT>
 __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
+    __shared__ f32x4 sums[kWaves][TM * TN][64];
     const int64_t unit = blockIdx.x / g.wg_blocks;
-    if (unit >= g.hdr->n_units) return;
-    const Unit u = g.units[unit];
+    Unit u;
+    if (!mx_unit(g, unit, u)) return;
     int x = int(blockIdx.x - unit * g.wg_blocks);
     const int nb = x % g.n_blocks;
     x /= g.n_blocks;
     const int mb = x % g.m_blocks, b = x / g.m_blocks;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = lane & 15, gr = lane >> 4;
-    const int m0 = mb * 16 * TM, n0 = (nb * 4 + w) * 16 * TN;
-    if (n0 >= g.N) return;
-    // rows past the last read the last (their sums are not written)
-    int32_t ra[TM], rb[TN];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, gr = lane >> 4;
+    const int wn = w % g.waves_n, wk = w / g.waves_n, deep = kWaves / g.waves_n;
+    const int m0 = mb * 16 * TM, n0 = (nb * g.waves_n + wn) * 16 * TN;
+    // a lane's rows: past the last they are the last (their sums are not written)
+    const int per_row = SHORT ? g.blocks : 4;
+    uint32_t ra[TM], rb[TN];
 #pragma unroll
-    for (int i = 0; i < TM; i++) ra[i] = b * g.M + min(m0 + 16 * i + r, g.M - 1);
+    for (int i = 0; i < TM; i++) ra[i] = uint32_t(b * g.M + min(m0 + 16 * i + r, g.M - 1)) * per_row + (SHORT ? gr & (per_row - 1) : gr);
 #pragma unroll
-    for (int j = 0; j < TN; j++) rb[j] = b * g.N + min(n0 + 16 * j + r, g.N - 1);
+    for (int j = 0; j < TN; j++) rb[j] = uint32_t(b * g.N + min(n0 + 16 * j + r, g.N - 1)) * per_row + (SHORT ? gr & (per_row - 1) : gr);
     f32x4 acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; i++)
 #pragma unroll
         for (int j = 0; j < TN; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // the unit's blocks one pair after the other, four to an instruction
-    const int64_t total = int64_t(u.p1 - u.p0) * g.blocks;
-    for (int64_t q0 = 0; q0 < total; q0 += 4) {
-        const int64_t q = q0 + gr;
-        const bool in = q < total;
-        const int64_t pair = in ? q / g.blocks : 0;
-        const int kb = in ? int(q - pair * g.blocks) : 0;
-        const uint8_t* at = g.A + g.pa[u.p0 + pair] * g.a_bytes;
-        const uint8_t* bt = g.B + g.pb[u.p0 + pair] * g.b_bytes;
-        i32x8 fa[TM], fb[TN];
-        int sa[TM], sb[TN];
+    const int n_pairs = u.p1 - u.p0;
+    const int steps = SHORT ? 1 : g.blocks / 4;                 // of a pair
+    const int shift = SHORT ? 2 - (g.blocks >> 1) : 0;          // pairs of a step: 1 << shift
+    const int64_t total = SHORT ? (int64_t(n_pairs) + (1 << shift) - 1) >> shift : int64_t(n_pairs) * steps;
+    struct Batch {
+        i32x4 a[U][TM], b[U][TN];
+        uint32_t sa[U][TM], sb[U][TN];
+    };
+    // The batch's steps s, s + deep, ...: past the last one, the last again.
+    auto load = [&](Batch& v, int64_t s) {
+        int64_t ia[U], ib[U];
+        int kk[U];
 #pragma unroll
-        for (int i = 0; i < TM; i++) {
-            const uint32_t x = mx_block_of(g.a_rows, g.group, ra[i], kb);
-            const uint4 c = *reinterpret_cast<const uint4*>(at + int64_t(x) * 16);
-            fa[i] = in ? i32x8{int(c.x), int(c.y), int(c.z), int(c.w), 0, 0, 0, 0} : i32x8{};
-            sa[i] = in ? at[g.a_scales + x] : 0;
+        for (int i = 0; i < U; i++) {
+            const int64_t at = min(s + int64_t(i) * deep, total - 1);
+            if constexpr (SHORT) {
+                const int64_t p = u.p0 + min((at << shift) + (gr >> (2 - shift)), int64_t(n_pairs) - 1);
+                ia[i] = g.pa[p];
+                ib[i] = g.pb[p];
+                kk[i] = 0;
+            } else {
+                const int p = int(at / steps);
+                ia[i] = pair_index(g.pa, u.p0 + p);
+                ib[i] = pair_index(g.pb, u.p0 + p);
+                kk[i] = int(at - int64_t(p) * steps);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < TN; j++) {
-            const uint32_t x = mx_block_of(g.b_rows, g.group, rb[j], kb);
-            const uint4 c = *reinterpret_cast<const uint4*>(bt + int64_t(x) * 16);
-            fb[j] = in ? i32x8{int(c.x), int(c.y), int(c.z), int(c.w), 0, 0, 0, 0} : i32x8{};
-            sb[j] = in ? bt[g.b_scales + x] : 0;
+        for (int i = 0; i < U; i++) {
+            const uint8_t* at = g.A + ia[i] * g.a_bytes + int64_t(kk[i]) * g.a_rows * 64;
+            const uint8_t* bt = g.B + ib[i] * g.b_bytes + int64_t(kk[i]) * g.b_rows * 64;
+            const uint8_t* as = g.A + ia[i] * g.a_bytes + g.a_scales + int64_t(kk[i]) * g.a_rows * 4;
+            const uint8_t* bs = g.B + ib[i] * g.b_bytes + g.b_scales + int64_t(kk[i]) * g.b_rows * 4;
+#pragma unroll
+            for (int h = 0; h < TM; h++) {
+                v.a[i][h] = *reinterpret_cast<const i32x4*>(at + ra[h] * 16);
+                v.sa[i][h] = as[ra[h]];
+            }
+#pragma unroll
+            for (int h = 0; h < TN; h++) {
+                v.b[i][h] = *reinterpret_cast<const i32x4*>(bt + rb[h] * 16);
+                v.sb[i][h] = bs[rb[h]];
+            }
         }
+    };
+    auto multiply = [&](Batch& v, int64_t s) {
+#pragma unroll
+        for (int i = 0; i < U; i++) {
+            const int64_t at = s + int64_t(i) * deep;
+            if (at >= total) break;
+            if constexpr (SHORT) {
+                // (a pair past the last: zeros under a scale that is a number)
+                const bool in = (at << shift) + (gr >> (2 - shift)) < n_pairs;
+#pragma unroll
+                for (int h = 0; h < TM; h++) {
+                    v.a[i][h] = in ? v.a[i][h] : i32x4{0, 0, 0, 0};
+                    v.sa[i][h] = in ? v.sa[i][h] : 0;
+                }
+#pragma unroll
+                for (int h = 0; h < TN; h++) v.sb[i][h] = in ? v.sb[i][h] : 0;
+            }
+#pragma unroll
+            for (int h = 0; h < TM; h++)
+#pragma unroll
+                for (int j = 0; j < TN; j++) acc[h][j] = mx_mfma(v.b[i][j], v.a[i][h], acc[h][j], v.sb[i][j], v.sa[i][h]);
+        }
+    };
+    if (n0 < g.N) {
+        Batch x0, x1;
+        const int64_t stride = int64_t(U) * deep;
+        int64_t s = wk;
+        if (s < total) load(x0, s);
+        for (; s < total; s += 2 * stride) {
+            if (s + stride < total) load(x1, s + stride);
+            multiply(x0, s);
+            if (s + 2 * stride < total) load(x0, s + 2 * stride);
+            if (s + stride < total) multiply(x1, s + stride);
+        }
+    }
+    if (deep > 1) {
 #pragma unroll
         for (int i = 0; i < TM; i++)
 #pragma unroll
-            for (int j = 0; j < TN; j++)
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], acc[i][j], 4, 4, 0, sb[j], 0, sa[i]);
+            for (int j = 0; j < TN; j++) sums[w][i * TN + j][lane] = acc[i][j];
+        __syncthreads();
+        if (wk > 0) return;
+        for (int d = 1; d < deep; d++)
+#pragma unroll
+            for (int i = 0; i < TM; i++)
+#pragma unroll
+                for (int j = 0; j < TN; j++) acc[i][j] += sums[d * g.waves_n + wn][i * TN + j][lane];
     }
-    mx_store<16>(g, u, b, m0, n0, acc);
+    if (n0 < g.N) mx_store<16>(g, u, b, m0, n0, acc);
 }
 
 // Rows of four blocks or more: 2 x 2 wavefronts, each with TM x TN tiles of
@@ -626,13 +720,6 @@ __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
 // Registers alone do 6.6 PFLOP/s of random codes (power; 8.7 of zeros).
 constexpr int kStages = 3;
 
-// An index list read by scalar loads: the compiler would take vector loads for
-// one that the copies' assembly might write, and wait for the copies with them.
-__device__ inline int32_t pair_index(const int32_t* list, int64_t i) {
-    typedef const __attribute__((address_space(4))) int32_t* constant;
-    return reinterpret_cast<constant>(reinterpret_cast<uintptr_t>(list))[i];
-}
-
 __device__ inline int mx_slot(int r, int k) { return k ^ ((r >> 2) & 3); }
 
 template <int TM, int TN>
@@ -647,8 +734,8 @@ __global__ __launch_bounds__(kThreads, (mx_waves<TM, TN>())) void k_mx_lds(MxArg
     extern __shared__ __align__(16) char lds[];
     constexpr int BM = 64 * TM, BN = 64 * TN, ROWS = BM + BN, kStage = mx_stage_bytes<TM, TN>();
     const int64_t unit = blockIdx.x / g.wg_blocks;
-    if (unit >= g.hdr->n_units) return;
-    const Unit u = g.units[unit];
+    Unit u;
+    if (!mx_unit(g, unit, u)) return;
     int x = int(blockIdx.x - unit * g.wg_blocks);
     const int nb = x % g.n_blocks;
     x /= g.n_blocks;
@@ -792,30 +879,65 @@ struct MxShape {
     bool lds;
     int tm, tn;  // tiles of a wavefront, 32 x 32 from LDS, else 16 x 16
     int64_t m_blocks, n_blocks;
+    bool turned = false;   // k_mx: A and B exchanged
+    int waves_n = 1;
 };
 
-MxShape mx_shape(const Plan& p) {
+// The blocks that k_mx_lds is built for and what they take, in microseconds:
+// `step` for a stage with every place on the chip taken, and `ends` for a
+// workgroup's start and stores, from 8192 x 8192 outputs of 16 and 64 stages.
+// (64 x 128 took 1.24 a stage, more than the same turned: not built.)
+struct MxKind {
+    int tm, tn, slots;
+    double step, ends;
+};
+constexpr MxKind kMxKinds[] = {
+    {2, 4, 512, 0.99, 11.8}, {2, 2, 768, 0.77, 8.9}, {2, 1, 1024, 0.73, 4.9}, {1, 4, 512, 0.67, 7.5}, {1, 1, 1536, 0.67, 3.3},
+};
+// A stage is no shorter than this, however few workgroups there are.
+constexpr double kMxStep = 0.4;
+
+double mx_rounds(double groups, int slots, double steps, double step, double ends) {
+    const double whole = std::floor(groups / slots), rest = groups / slots - whole;
+    return whole * (steps * step + ends) + (rest > 0 ? steps * std::max(kMxStep, step * rest) + ends : 0);
+}
+
+// The cut for `units` units of `steps` steps each, and its time.
+MxShape mx_shape(const Plan& p, double units, double steps, double* time = nullptr) {
     MxShape h;
     h.M = p.swap ? p.nN : p.nM;
     h.N = p.swap ? p.nM : p.nN;
     h.lds = p.mx_blocks >= 4 && h.M > 32 && h.N > 32;
+    double best = 0;
     if (h.lds) {
-        h.tm = h.M > 64 ? 2 : 1;
-        h.tn = h.N > 128 ? 4 : h.N > 64 ? 2 : 1;
-#ifdef MXTM
-        h.tm = std::min(h.tm, MXTM);
-        h.tn = std::min(h.tn, MXTN);
-#endif
-        h.m_blocks = (h.M + 64 * h.tm - 1) / (64 * h.tm);
-        h.n_blocks = (h.N + 64 * h.tn - 1) / (64 * h.tn);
+        for (const MxKind& k : kMxKinds) {
+            const int64_t mb = (h.M + 64 * k.tm - 1) / (64 * k.tm), nb = (h.N + 64 * k.tn - 1) / (64 * k.tn);
+            const double t = mx_rounds(units * double(p.nB * mb * nb), k.slots, steps, k.step, k.ends);
+            if (best > 0 && t >= best) continue;
+            best = t;
+            h.tm = k.tm;
+            h.tn = k.tn;
+            h.m_blocks = mb;
+            h.n_blocks = nb;
+        }
+        if (time) *time = best;
         return h;
     }
-    h.tm = h.M > 32 ? 4 : h.M > 16 ? 2 : 1;
-    h.tn = h.N > 64 ? 2 : 1;
+    // the longer side along N
+    h.turned = h.M > h.N;
+    if (h.turned) std::swap(h.M, h.N);
+    h.tm = h.M > 16 ? 2 : 1;
+    h.tn = h.N > 16 ? 2 : 1;
+    h.waves_n = h.N > 32 * h.tn ? 4 : h.N > 16 * h.tn ? 2 : 1;
     h.m_blocks = (h.M + 16 * h.tm - 1) / (16 * h.tm);
-    h.n_blocks = (h.N + 64 * h.tn - 1) / (64 * h.tn);
+    h.n_blocks = (h.N + 16 * h.tn * h.waves_n - 1) / (16 * h.tn * h.waves_n);
+    // (a step of a wavefront about 0.4 us, a workgroup's start and end 5)
+    if (time) *time = mx_rounds(units * double(p.nB * h.m_blocks * h.n_blocks), 512, std::ceil(steps * h.waves_n / kWaves), 0.4, 5.0);
     return h;
 }
+
+// Matrix instructions that a pair takes along its contracted index.
+double mx_steps(const Plan& p) { return double(p.mx_blocks) / 4; }
 
 template <int TM, int TN>
 hipError_t run_lds(const MxArgs& g, dim3 grid, hipStream_t s) {
@@ -829,9 +951,17 @@ hipError_t run_lds(const MxArgs& g, dim3 grid, hipStream_t s) {
     return launch_k(k_mx_lds<TM, TN>, grid, dim3{unsigned(kThreads)}, size_t(bytes), s, g);
 }
 
+template <int TM, int TN, int U>
+hipError_t run_mx(bool few, const MxArgs& g, dim3 grid, hipStream_t s) {
+    return few ? launch_k(k_mx<TM, TN, U / 2, true>, grid, dim3{unsigned(kThreads)}, 0, s, g)
+               : launch_k(k_mx<TM, TN, U, false>, grid, dim3{unsigned(kThreads)}, 0, s, g);
+}
+
 template <int TM>
 hipError_t run_lds_n(int tn, const MxArgs& g, dim3 grid, hipStream_t s) {
-    return tn == 4 ? run_lds<TM, 4>(g, grid, s) : tn == 2 ? run_lds<TM, 2>(g, grid, s) : run_lds<TM, 1>(g, grid, s);
+    if constexpr (TM == 2)
+        if (tn == 2) return run_lds<TM, 2>(g, grid, s);
+    return tn == 4 ? run_lds<TM, 4>(g, grid, s) : run_lds<TM, 1>(g, grid, s);
 }
 
 }  // namespace
@@ -919,16 +1049,38 @@ hipError_t launch_mx_dequantize(const Plan& p, int op, const void* mx, int64_t n
                                  : dequantize(g, in, static_cast<float*>(tiles), s);
 }
 
-int64_t mx_blocks_per_unit(const Plan& p) {
-    const MxShape h = mx_shape(p);
-    return p.nB * h.m_blocks * h.n_blocks;
+// Unit length: keys are cut where that shortens the launch by more than the
+// partial tiles cost (written and read once, at about 4 TB/s, and a launch).
+int64_t mx_unit_pairs(const Plan& p, int64_t n_pairs, int64_t n_w) {
+    const double len = double(n_pairs) / double(std::max<int64_t>(n_w, 1));
+    int64_t unit = std::max<int64_t>(n_pairs, 1);
+    double best = 0;
+    for (int c = 1; c <= 64 && c <= len; c++) {
+        const double pairs = std::ceil(len / c);
+        double t;
+        mx_shape(p, double(n_w) * c, std::ceil(pairs * mx_steps(p)), &t);
+        if (c > 1) t += 6.0 + double(n_w) * c * double(p.tile_elems[2]) * 8.0 / 4e6;
+        if (c > 1 && t >= 0.95 * best) continue;
+        best = t;
+        if (c > 1) unit = int64_t(pairs);
+    }
+    return unit;
+}
+
+// Whether a launch of one unit per key reads the join's segments instead of a
+// unit table, which takes a launch of 8 us to write: that one gives the longest
+// keys first, which keys of one length, or work of few rounds, do not need.
+bool mx_whole_keys(const Plan& p, int64_t n_pairs, int64_t n_w) {
+    if (p.n_join == 0 || n_pairs <= n_w) return true;
+    double t;
+    mx_shape(p, double(n_w), std::ceil(double(n_pairs) / double(std::max<int64_t>(n_w, 1)) * mx_steps(p)), &t);
+    return t <= DT;
 }
 
 hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_tiles, const void* v_tiles, float* w_tiles,
-                     int64_t n_pairs, int64_t unit_bound, hipStream_t s) {
-    (void)n_pairs;
-    const MxShape h = mx_shape(p);
-    const int a = p.swap ? 1 : 0, b = 1 - a;
+                     int64_t n_pairs, int64_t unit_bound, bool whole_keys, hipStream_t s) {
+    const MxShape h = mx_shape(p, double(unit_bound), std::ceil(double(n_pairs) / double(unit_bound) * mx_steps(p)));
+    const int a = p.swap != h.turned ? 1 : 0, b = 1 - a;
     const int32_t* tb = reinterpret_cast<const int32_t*>(ws + L.tables);
     const int32_t* pairs[2] = {reinterpret_cast<const int32_t*>(ws + L.pu), reinterpret_cast<const int32_t*>(ws + L.pv)};
     const void* tiles[2] = {u_tiles, v_tiles};
@@ -953,25 +1105,27 @@ hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_til
     if (wg > int64_t(0x7fffffff) || wg * unit_bound > int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
     g.wg_blocks = int32_t(wg);
     g.w_affine = p.tile_w_affine;
-    g.w_sm = p.tile_w_sm;
+    g.w_sm = h.turned ? 1 : p.tile_w_sm;
+    g.w_sn = h.turned ? p.tile_w_sm : 1;
+    g.waves_n = h.waves_n;
     g.w_bf16 = p.opt.w_bf16;
     g.batched = p.nB > 1;
     g.w_elems = p.tile_elems[2];
-    g.tWM = tb + p.table_off[T_WM];
-    g.tWN = tb + p.table_off[T_WN];
+    g.tWM = tb + p.table_off[h.turned ? T_WN : T_WM];
+    g.tWN = tb + p.table_off[h.turned ? T_WM : T_WN];
     g.tWB = tb + p.table_off[T_WB];
     g.units = reinterpret_cast<const Unit*>(ws + L.unit_desc);
+    g.seg_start = whole_keys ? reinterpret_cast<const int32_t*>(ws + L.seg_start) : nullptr;
     g.hdr = reinterpret_cast<const WsHeader*>(ws + L.hdr);
     g.W = w_tiles;
     g.partials = reinterpret_cast<float*>(ws + L.partials);
-    const dim3 grid{unsigned(wg * unit_bound)}, block{unsigned(kThreads)};
+    const dim3 grid{unsigned(wg * unit_bound)};
     if (h.lds)
         return h.tm == 2 ? run_lds_n<2>(h.tn, g, grid, s) : run_lds_n<1>(h.tn, g, grid, s);
-    if (h.tm == 4)
-        return h.tn == 2 ? launch_k(k_mx<4, 2>, grid, block, 0, s, g) : launch_k(k_mx<4, 1>, grid, block, 0, s, g);
+    const bool few = p.mx_blocks < 4;
     if (h.tm == 2)
-        return h.tn == 2 ? launch_k(k_mx<2, 2>, grid, block, 0, s, g) : launch_k(k_mx<2, 1>, grid, block, 0, s, g);
-    return h.tn == 2 ? launch_k(k_mx<1, 2>, grid, block, 0, s, g) : launch_k(k_mx<1, 1>, grid, block, 0, s, g);
+        return h.tn == 2 ? run_mx<2, 2, 4>(few, g, grid, s) : run_mx<2, 1, 4>(few, g, grid, s);
+    return h.tn == 2 ? run_mx<1, 2, UU>(few, g, grid, s) : run_mx<1, 1, UU>(few, g, grid, s);
 }
 
 }  // namespace tre

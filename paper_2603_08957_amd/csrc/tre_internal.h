@@ -297,7 +297,7 @@ hipError_t launch_units(const Plan& p, const Layout& L, char* ws, int64_t n_pair
 hipError_t launch_range_units(const Plan& p, const Layout& L, char* ws, int64_t n_w, int64_t n_u, int32_t R,
                               hipStream_t s);
 hipError_t launch_contract(const Plan& p, const Layout& L, char* ws, const void* u_tiles, const void* v_tiles,
-                           float* w_tiles, int64_t n_pairs, int64_t n_w, int64_t unit_bound, hipStream_t s);
+                           float* w_tiles, int64_t n_pairs, int64_t n_w, int64_t unit_bound, bool whole_keys, hipStream_t s);
 // gemm_tile.hip: the GEMM class outside the 128x128 path.  tile_unit_pairs:
 // the unit length for n_pairs pairs of n_w keys.
 int64_t tile_unit_pairs(const Plan& p, int64_t n_pairs, int64_t n_w);
@@ -323,10 +323,12 @@ hipError_t launch_mx_quantize(const Plan& p, int op, const void* tiles, int src_
                               hipStream_t s);
 hipError_t launch_mx_dequantize(const Plan& p, int op, const void* mx_tiles, int64_t n, void* tiles, int dst_dtype,
                                 hipStream_t s);
-// workgroups that one unit takes
-int64_t mx_blocks_per_unit(const Plan& p);
+// the unit length for n_pairs pairs of n_w keys, and whether a launch of one
+// unit per key takes the join's segments in place of a unit table
+int64_t mx_unit_pairs(const Plan& p, int64_t n_pairs, int64_t n_w);
+bool mx_whole_keys(const Plan& p, int64_t n_pairs, int64_t n_w);
 hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_tiles, const void* v_tiles, float* w_tiles,
-                     int64_t n_pairs, int64_t unit_bound, hipStream_t s);
+                     int64_t n_pairs, int64_t unit_bound, bool whole_keys, hipStream_t s);
 
 // rows.hip: rows of a table by token, and the table's gradient
 hipError_t launch_lookup(const void* table, int table_dtype, int64_t n_rows, int64_t elems, int64_t tile_rows,
