@@ -383,7 +383,7 @@ tre_status contract_enqueue(tre_plan_t plan, const tre_join_result* jr, int64_t 
     // units as long as the average key or longer: outliers are cut, and their
     // partial tiles summed on the way of the outputs
     const bool outliers =
-        p.kclass == KC_GEMM && !p.fast && R <= 1 && p_unit < n_pairs && p_unit * n_w >= n_pairs;
+        p.kclass != KC_VEC && !p.fast && R <= 1 && p_unit < n_pairs && p_unit * n_w >= n_pairs;
     const int64_t split_bound = R > 1 ? n_w : std::min<int64_t>(n_w, n_pairs / (p_unit + 1) + 1);
     if ((R > 1 || p_unit < n_pairs) && !outliers) {
         if ((e = launch_reduce(p, L, w, w_tiles, split_bound, s)) != hipSuccess) return dev_fail(e, "reduce");

@@ -343,12 +343,6 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantize_rows(MxTiles g, cons
 // so that lanes side by side read consecutive rows of one k.  The last of an
 // odd number of bf16 rows goes with the row before it once more.
 
-#ifndef DT
-#define DT 100.0
-#endif
-#ifndef UU
-#define UU 4
-#endif
 // A thread's tile, block and first row: the lanes of a wavefront take
 // consecutive lines (of R rows) of a group, its wavefronts the group's blocks.
 // g.line: lines of a tile, g.tile: lines and groups.
@@ -895,7 +889,7 @@ constexpr MxKind kMxKinds[] = {
     {2, 4, 512, 0.99, 11.8}, {2, 2, 768, 0.77, 8.9}, {2, 1, 1024, 0.73, 4.9}, {1, 4, 512, 0.67, 7.5}, {1, 1, 1536, 0.67, 3.3},
 };
 // A stage is no shorter than this, however few workgroups there are.
-constexpr double kMxStep = 0.4;
+constexpr double kMxStep = 0.4, kMxAlone = 60;
 
 double mx_rounds(double groups, int slots, double steps, double step, double ends) {
     const double whole = std::floor(groups / slots), rest = groups / slots - whole;
@@ -1062,19 +1056,31 @@ int64_t mx_unit_pairs(const Plan& p, int64_t n_pairs, int64_t n_w) {
         if (c > 1) t += 6.0 + double(n_w) * c * double(p.tile_elems[2]) * 8.0 / 4e6;
         if (c > 1 && t >= 0.95 * best) continue;
         best = t;
-        if (c > 1) unit = int64_t(pairs);
+        if (c > 1) {
+            unit = int64_t(pairs);
+            continue;
+        }
+        // One key far longer than the others would be alone at the end: where
+        // the labels allow one of more than kMxAlone, units end there (or at
+        // the launch's own time, or twice the average).  Below that the unit
+        // table and the partial sums' look in the outputs cost more (10 us)
+        // than they save in most launches.
+        const double step = kMxStep * mx_steps(p), most = std::max(kMxAlone, t);
+        if (double(p.key_pairs_max) * step > most) unit = std::min(unit, int64_t(std::ceil(std::max(most / step, 2 * len))));
     }
     return unit;
 }
 
 // Whether a launch of one unit per key reads the join's segments instead of a
 // unit table, which takes a launch of 8 us to write: that one gives the longest
-// keys first, which keys of one length, or work of few rounds, do not need.
+// keys first, which keys of one length, or work of few rounds, do not need
+// (128 keys of 5 to 13 pairs of 128 x 1024 outputs: 52 us without, 62 with).
+constexpr double kMxTable = 100;
 bool mx_whole_keys(const Plan& p, int64_t n_pairs, int64_t n_w) {
     if (p.n_join == 0 || n_pairs <= n_w) return true;
     double t;
     mx_shape(p, double(n_w), std::ceil(double(n_pairs) / double(std::max<int64_t>(n_w, 1)) * mx_steps(p)), &t);
-    return t <= DT;
+    return t <= kMxTable;
 }
 
 hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_tiles, const void* v_tiles, float* w_tiles,
@@ -1125,7 +1131,7 @@ hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_til
     const bool few = p.mx_blocks < 4;
     if (h.tm == 2)
         return h.tn == 2 ? run_mx<2, 2, 4>(few, g, grid, s) : run_mx<2, 1, 4>(few, g, grid, s);
-    return h.tn == 2 ? run_mx<1, 2, UU>(few, g, grid, s) : run_mx<1, 1, UU>(few, g, grid, s);
+    return h.tn == 2 ? run_mx<1, 2, 4>(few, g, grid, s) : run_mx<1, 1, 4>(few, g, grid, s);
 }
 
 }  // namespace tre

@@ -405,28 +405,41 @@ def _want(t, where, what, shape=None, dtype=None, device=None):
         raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"{what}: on {t.device}, wanted on {device or 'a GPU'}")
     if dtype is not None and t.dtype != dtype:
         raise TreError(STATUS_CODE["TRE_E_DTYPE"], where, f"{what}: {dtype} wanted, got {t.dtype}")
-    if (shape is not None and tuple(t.shape) != tuple(shape)) or not t.is_contiguous():
+    if (shape is not None and t.shape != shape) or not t.is_contiguous():
         raise TreError(STATUS_CODE["TRE_E_SHAPE"], where,
                        f"{what}: contiguous {tuple(shape) if shape is not None else 'tensor'} wanted, got {tuple(t.shape)}"
                        f" with strides {tuple(t.stride())}")
     return t
 
 
-def _on(device, stream):
-    """(a context with the tensors' device current, the stream to use there)."""
-    import torch
+class _Here:
+    """The device of a call's tensors made current for it (nothing where it is
+    already: that check costs a tenth of the context), and its stream: the
+    caller's, else the device's current one."""
 
-    return torch.cuda.device(device), (stream if stream is not None else torch.cuda.current_stream(device))
+    def __init__(self, device, stream):
+        import torch
 
+        self.given = stream is not None
+        self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+        self.stream = stream if self.given else torch.cuda.current_stream(device)
+        self.ptr = ctypes.c_void_p(self.stream.cuda_stream)
 
-def _keep(stream, *tensors):
-    """Tensors made here for a stream other than the current one: their memory
-    must not be given out again before that stream is done with it."""
-    import torch
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self
 
-    for t in tensors:
-        if stream != torch.cuda.current_stream(t.device):
-            t.record_stream(stream)
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+    def keep(self, t):
+        """A tensor made here for a stream other than the current one: its
+        memory must not be given out again before that stream is done with it."""
+        if self.given:
+            t.record_stream(self.stream)
+        return t
 
 
 def _operand(plan, operand, where):
@@ -448,13 +461,12 @@ def mx_quantize(plan: Plan, operand: str, tiles, out=None, stream=None):
     dt = _value_type(tiles, w, "tiles")
     n = int(tiles.shape[0]) if tiles.dim() else -1
     _want(tiles, w, "tiles", (n, plan.tile_elems[o]))
-    dev, s = _on(tiles.device, stream)
-    with dev:
+    with _Here(tiles.device, stream) as here:
         if out is None:
-            out = torch.empty((n, plan.tile_bytes[o]), dtype=torch.uint8, device=tiles.device)
-            _keep(s, out)
-        _want(out, w, "out", (n, plan.tile_bytes[o]), torch.uint8, tiles.device)
-        _check(lib().tre_mx_quantize(plan.handle, o, _ptr(tiles), dt, n, _ptr(out), _stream(s)), "tre_mx_quantize")
+            out = here.keep(torch.empty((n, plan.tile_bytes[o]), dtype=torch.uint8, device=tiles.device))
+        else:
+            _want(out, w, "out", (n, plan.tile_bytes[o]), torch.uint8, tiles.device)
+        _check(lib().tre_mx_quantize(plan.handle, o, _ptr(tiles), dt, n, _ptr(out), here.ptr), "tre_mx_quantize")
     return out
 
 
@@ -468,15 +480,13 @@ def mx_dequantize(plan: Plan, operand: str, mx_tiles, dtype=None, out=None, stre
     o = _operand(plan, operand, w)
     n = int(mx_tiles.shape[0]) if mx_tiles.dim() else -1
     _want(mx_tiles, w, "mx_tiles", (n, plan.tile_bytes[o]), torch.uint8)
-    dev, s = _on(mx_tiles.device, stream)
-    with dev:
+    dt = _value_type(out if out is not None else dtype or torch.float32, w, "out")
+    with _Here(mx_tiles.device, stream) as here:
         if out is None:
-            _value_type(dtype or torch.float32, w, "dtype")
-            out = torch.empty((n, plan.tile_elems[o]), dtype=dtype or torch.float32, device=mx_tiles.device)
-            _keep(s, out)
-        _want(out, w, "out", (n, plan.tile_elems[o]), dtype, mx_tiles.device)
-        _check(lib().tre_mx_dequantize(plan.handle, o, _ptr(mx_tiles), n, _ptr(out), _value_type(out, w, "out"),
-                                       _stream(s)), "tre_mx_dequantize")
+            out = here.keep(torch.empty((n, plan.tile_elems[o]), dtype=dtype or torch.float32, device=mx_tiles.device))
+        else:
+            _want(out, w, "out", (n, plan.tile_elems[o]), dtype, mx_tiles.device)
+        _check(lib().tre_mx_dequantize(plan.handle, o, _ptr(mx_tiles), n, _ptr(out), dt, here.ptr), "tre_mx_dequantize")
     return out
 
 
@@ -526,17 +536,15 @@ def lookup(table, ids, scale: float = 1.0, dtype=None, out=None, plan: Plan | No
     _ids(ids, w, table.device)
     _status(status, w, table.device)
     shape = tuple(ids.shape) + (elems,)
-    dev, s = _on(table.device, stream)
-    with dev:
+    dtype = dtype or (out.dtype if out is not None else torch.float32 if plan is not None else table.dtype)
+    odt = _value_type(dtype, w, "out")
+    with _Here(table.device, stream) as here:
         if out is None:
-            dtype = dtype or (torch.float32 if plan is not None else table.dtype)
-            _value_type(dtype, w, "dtype")
-            out = torch.empty(shape, dtype=dtype, device=table.device)
-            _keep(s, out)
-        _want(out, w, "out", shape, dtype, table.device)
+            out = here.keep(torch.empty(shape, dtype=dtype, device=table.device))
+        else:
+            _want(out, w, "out", shape, dtype, table.device)
         _check(lib().tre_lookup(_ptr(table), tdt, n_rows, elems, tile_rows, _ptr(ids), ids.element_size(), ids.numel(),
-                                float(scale), _ptr(out), _value_type(out, w, "out"), _ptr(status), _stream(s)),
-               "tre_lookup")
+                                float(scale), _ptr(out), odt, _ptr(status), here.ptr), "tre_lookup")
     return out
 
 
@@ -562,21 +570,21 @@ def lookup_grad(grad, ids, n_rows: int, scale: float = 1.0, dtype=None, out=None
     if accumulate and out is None:
         raise TreError(STATUS_CODE["TRE_E_ARG"], w, "accumulate needs out")
     _status(status, w, grad.device)
-    n, elems = ids.numel(), int(grad.shape[-1])
-    dev, s = _on(grad.device, stream)
-    with dev:
+    n, elems, n_rows = ids.numel(), int(grad.shape[-1]), int(n_rows)
+    dtype = dtype or (out.dtype if out is not None else torch.float32)
+    odt = _value_type(dtype, w, "out")
+    with _Here(grad.device, stream) as here:
         if out is None:
-            _value_type(dtype or torch.float32, w, "dtype")
-            out = torch.empty((int(n_rows), elems), dtype=dtype or torch.float32, device=grad.device)
-            _keep(s, out)
-        _want(out, w, "out", (int(n_rows), elems), dtype, grad.device)
+            out = here.keep(torch.empty((n_rows, elems), dtype=dtype, device=grad.device))
+        else:
+            _want(out, w, "out", (n_rows, elems), dtype, grad.device)
         if ws is None:
-            ws = alloc_workspace(lookup_grad_workspace_bytes(n, n_rows, elems), grad.device)
-            _keep(s, ws)
-        _want(ws, w, "ws", device=grad.device)
-        _check(lib().tre_lookup_grad(_ptr(grad), gdt, _ptr(ids), ids.element_size(), n, float(scale), _ptr(out),
-                                     _value_type(out, w, "out"), int(n_rows), elems, int(accumulate), _ptr(status),
-                                     _ptr(ws), ws.numel() * ws.element_size(), _stream(s)), "tre_lookup_grad")
+            ws = here.keep(alloc_workspace(lookup_grad_workspace_bytes(n, n_rows, elems), grad.device))
+        else:
+            _want(ws, w, "ws", device=grad.device)
+        _check(lib().tre_lookup_grad(_ptr(grad), gdt, _ptr(ids), ids.element_size(), n, float(scale), _ptr(out), odt, n_rows,
+                                     elems, int(accumulate), _ptr(status), _ptr(ws), ws.numel() * ws.element_size(),
+                                     here.ptr), "tre_lookup_grad")
     return out
 
 

@@ -314,3 +314,45 @@ def test_same_bits_streams_and_graphs():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(wt, want), i
+
+
+@pytest.mark.parametrize("t,how", [(16, "execute"), (64, "async"), (96, "execute")])
+def test_one_long_key(t, how):
+    """One key with nearly all pairs, the others with one or none: it is cut and
+    its partial tiles summed, with no unit far longer than the launch."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    nb, long = 6000, 5000
+    plan = tre.Plan("ij,jk->ik", "ij", {"i": nb * t, "j": nb * t, "k": t}, {"i": t, "j": t}, "mxfp4", w_bf16=t == 96)
+    g = torch.Generator(device="cuda").manual_seed(t)
+    keys = torch.cat([torch.stack([torch.full((long,), 7), torch.arange(long) + 500], 1),
+                      torch.stack([torch.arange(8, 408), torch.arange(8, 408)], 1)]).to(torch.int32).cuda()
+    a = torch.randn((keys.shape[0], t * t), generator=g, device="cuda")
+    b = torch.randn((nb, t * t), generator=g, device="cuda")
+    bk = torch.arange(nb, dtype=torch.int32, device="cuda").reshape(nb, 1)
+    aq, bq = tre.mx_quantize(plan, "u", a), tre.mx_quantize(plan, "v", b)
+    ws = tre.alloc_workspace(plan.workspace_bytes(keys.shape[0], nb, keys.shape[0]))
+    n_w = 401
+    wk = torch.zeros((keys.shape[0], 1), dtype=torch.int32, device="cuda")
+    wt = torch.zeros((keys.shape[0], t * t), dtype=torch.bfloat16 if t == 96 else torch.float32, device="cuda")
+    if how == "async":
+        counts = torch.zeros(4, dtype=torch.int64, device="cuda")
+        tre.execute_async(plan, keys, aq, bk, bq, wk, wt, ws, counts)
+        assert counts.tolist() == [keys.shape[0], n_w, 0, 0]
+    else:
+        tm = tre.Timing()
+        assert tre.execute(plan, keys, aq, bk, bq, wk, wt, ws, timing=tm) == (n_w, keys.shape[0])
+        assert tm.n_split_segments == 1 and tm.n_partials > 4
+    ad = tre.mx_dequantize(plan, "u", aq).double().view(-1, t, t)
+    bd = tre.mx_dequantize(plan, "v", bq).double().view(-1, t, t)[keys[:, 1].long()].contiguous()
+    ref, mag = torch.bmm(ad, bd), torch.bmm(ad.abs(), bd.abs())
+    ref = torch.cat([ref[:long].sum(0, keepdim=True), ref[long:]])
+    mag = torch.cat([mag[:long].sum(0, keepdim=True), mag[long:]])
+    got = wt[:n_w].double().view(n_w, t, t)
+    n = torch.ones((n_w, 1, 1), device="cuda", dtype=torch.float64)
+    n[0] = long
+    tol = (n * (32 * mx.row_blocks(t) + 2)) * U32 * mag + (UB16 * ref.abs() if t == 96 else 0)
+    assert bool(((got - ref).abs() <= tol).all())
+    assert float((got - ref).norm() / ref.norm()) <= (UB16 if t == 96 else 1e-6)
