@@ -424,13 +424,16 @@ __device__ inline void put_pair(const GradArgs& g, int64_t row, int64_t e, const
 //
 // A wavefront to a group and a strip of its rows.  Each lane looks at one
 // chunk's borders, and only the partial sums that are there are read.
-constexpr int kFan = 16, kJoinBatch = 16, kJoinLane = 2;
+// Up to 64 chunks are joined at once.
+constexpr int kFan = 16, kFanLast = 64, kJoinBatch = 16, kJoinLane = 2;
+inline int fan_of(int64_t chunks) { return chunks <= kFanLast ? kFanLast : kFan; }
 
 struct JoinArgs {
     const float* in;   // [chunk][2][elems]
     float* out;        // [group][2][elems]
     int64_t span;      // tokens of a chunk
     int64_t chunks, groups, slices;
+    int32_t fan;
 };
 
 template <typename TO>
@@ -440,8 +443,8 @@ __global__ __launch_bounds__(kThreads) void k_grad_join(GradArgs g, JoinArgs a) 
     if (group >= a.groups) return;
     const int lane = threadIdx.x & 63;
     const int64_t e = ((w - group * a.slices) * 64 + lane) * kJoinLane;
-    const int64_t c0 = group * kFan, c = c0 + lane;
-    const int count = int(min(int64_t(kFan), a.chunks - c0));
+    const int64_t c0 = group * a.fan, c = c0 + lane;
+    const int count = int(min(int64_t(a.fan), a.chunks - c0));
     bool cont = false, more = false, whole = false;
     uint32_t key = 0;
     if (lane < count) {
@@ -520,7 +523,8 @@ GradLayout grad_layout(int64_t n, int64_t elems) {
     L.hist = take(radix ? 4 * size_t(h) : 0);
     L.tmp = take(radix ? 4 * scan_tmp_elems(h) : 0);
     // two partial sums of a row for each chunk, of every level
-    for (size_t k = (m + c - 1) / c; k > 0; k = k > 1 ? (k + kFan - 1) / kFan : 0) chunks += k;
+    for (size_t k = (m + c - 1) / c; k > 0; k = k > 1 ? (k + size_t(fan_of(int64_t(k))) - 1) / size_t(fan_of(int64_t(k))) : 0)
+        chunks += k;
     L.part = take(8 * chunks * size_t(elems));
     L.total = off;
     return L;
@@ -637,7 +641,8 @@ hipError_t launch_lookup_grad(const void* grad, int grad_dtype, const void* ids,
     a.span = g.chunk;
     a.slices = (elems + 64 * kJoinLane - 1) / (64 * kJoinLane);
     for (a.chunks = g.chunks; a.chunks > 1; a.chunks = a.groups) {
-        a.groups = (a.chunks + kFan - 1) / kFan;
+        a.fan = fan_of(a.chunks);
+        a.groups = (a.chunks + a.fan - 1) / a.fan;
         float* out = const_cast<float*>(a.in) + 2 * a.chunks * elems;
         a.out = out;
         const int64_t waves = a.groups * a.slices;
@@ -646,7 +651,7 @@ hipError_t launch_lookup_grad(const void* grad, int grad_dtype, const void* ids,
         else k_grad_join<float><<<wave_grid(waves), kThreads, 0, s>>>(g, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         a.in = out;
-        a.span *= kFan;
+        a.span *= a.fan;
     }
     return hipSuccess;
 }
