@@ -11,6 +11,9 @@
 #include "mx.h"
 #include "tre_internal.h"
 
+#include <atomic>
+#include <cmath>
+
 namespace tre {
 
 namespace {
@@ -936,11 +939,19 @@ double mx_steps(const Plan& p) { return double(p.mx_blocks) / 4; }
 template <int TM, int TN>
 hipError_t run_lds(const MxArgs& g, dim3 grid, hipStream_t s) {
     constexpr int bytes = kStages * mx_stage_bytes<TM, TN>();
-    // above 64 KB the kernel has to be told once per device (here: per call, a host-side note)
+    // above 64 KB a kernel has to be allowed it, once per device
     if (bytes > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_mx_lds<TM, TN>),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        static std::atomic<uint64_t> allowed{0};
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;
+        const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+        if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_mx_lds<TM, TN>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                    bytes);
+            if (e != hipSuccess) return e;
+            allowed.fetch_or(bit, std::memory_order_relaxed);
+        }
     }
     return launch_k(k_mx_lds<TM, TN>, grid, dim3{unsigned(kThreads)}, size_t(bytes), s, g);
 }

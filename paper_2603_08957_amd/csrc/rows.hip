@@ -261,22 +261,24 @@ __global__ __launch_bounds__(kThreads) void k_grad_keys(const void* __restrict__
 }
 
 // Few tokens are sorted in one launch: a workgroup counts, for its 64, the
-// tokens that go before them, each of its wavefronts among a quarter.
-constexpr int kRankMax = 8192;
+// tokens that go before them, each of its wavefronts among a part of them.
+// (Four wavefronts took 30 us for 6,300 tokens, most of it to read them.)
+constexpr int kRankMax = 8192, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
 
-__global__ __launch_bounds__(kThreads) void k_grad_rank(const void* __restrict__ ids, int id_bytes, int n, int64_t n_rows,
+__global__ __launch_bounds__(kRankThreads) void k_grad_rank(const void* __restrict__ ids, int id_bytes, int n, int64_t n_rows,
                                                         uint32_t* __restrict__ keys, uint32_t* __restrict__ pos,
                                                         int64_t* __restrict__ status) {
     __shared__ uint4 all[kRankMax / 4];
-    __shared__ int32_t part[kWaves][64];
+    __shared__ int32_t part[kRankWaves][64];
     uint32_t* flat = reinterpret_cast<uint32_t*>(all);
-    const int padded = (n + 4 * kWaves - 1) / (4 * kWaves) * (4 * kWaves);  // (after every token)
-    for (int t = threadIdx.x; t < padded; t += kThreads)
+    const int padded = (n + 4 * kRankWaves - 1) / (4 * kRankWaves) * (4 * kRankWaves);  // (after every token)
+#pragma unroll 4
+    for (int t = threadIdx.x; t < padded; t += kRankThreads)
         flat[t] = t < n ? token_key(ids, id_bytes, t, n_rows, blockIdx.x == 0 ? status : nullptr) : 0xffffffffu;
     __syncthreads();
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i0 = blockIdx.x * 64, i = i0 + lane;
     const uint32_t key = i < n ? flat[i] : 0u;
-    const int q0 = padded / 4 / kWaves * w, q1 = q0 + padded / 4 / kWaves;
+    const int q0 = padded / 4 / kRankWaves * w, q1 = q0 + padded / 4 / kRankWaves;
     int before = 0;
     // quads before the workgroup's tokens (equal ones go before), its own, those after
     const int a = min(max(i0 / 4, q0), q1), b = min(max(i0 / 4 + 16, q0), q1);
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_rank(const void* __restrict__
     if (w == 0 && i < n) {
         int at = 0;
 #pragma unroll
-        for (int j = 0; j < kWaves; j++) at += part[j][lane];
+        for (int j = 0; j < kRankWaves; j++) at += part[j][lane];
         keys[at] = key;
         pos[at] = uint32_t(i);
     }
@@ -616,7 +618,7 @@ hipError_t launch_lookup_grad(const void* grad, int grad_dtype, const void* ids,
             pos = pos2;
         }
     } else if (n_ids > 0) {
-        k_grad_rank<<<unsigned((n_ids + 63) / 64), kThreads, 0, s>>>(ids, id_bytes, int(n_ids), n_rows, keys, pos, status);
+        k_grad_rank<<<unsigned((n_ids + 63) / 64), kRankThreads, 0, s>>>(ids, id_bytes, int(n_ids), n_rows, keys, pos, status);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     GradArgs g{};

@@ -159,11 +159,17 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
-def _stream(stream=None):
+def _stream(stream=None, device=None):
+    """The hipStream_t of a torch stream, or of the (current) device's current
+    one, whose handle torch gives without making a stream object (3 us less)."""
     import torch
 
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
+        return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    return ctypes.c_void_p(raw(torch.cuda.current_device() if device is None else device.index))
 
 
 class Plan:
@@ -420,10 +426,9 @@ class _Here:
     def __init__(self, device, stream):
         import torch
 
-        self.given = stream is not None
+        self.stream = stream
         self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
-        self.stream = stream if self.given else torch.cuda.current_stream(device)
-        self.ptr = ctypes.c_void_p(self.stream.cuda_stream)
+        self.ptr = _stream(stream, device)
 
     def __enter__(self):
         if self.guard is not None:
@@ -437,7 +442,7 @@ class _Here:
     def keep(self, t):
         """A tensor made here for a stream other than the current one: its
         memory must not be given out again before that stream is done with it."""
-        if self.given:
+        if self.stream is not None:
             t.record_stream(self.stream)
         return t
 
