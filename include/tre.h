@@ -499,7 +499,7 @@ tre_status tre_mx_dequantize(tre_plan_t plan, int32_t operand, const void *mx_ti
 
 /* tre_lookup -- out[t] = scale * table[id[t]]: the join of a list of tokens
  * with a table that holds every key of its promoted label (Sec. 5), in one
- * pass, each value rounded once.
+ * pass: the product in fp32, rounded to the output's type.
  *   table   : device [n_rows x row_elems] of table_dtype (TRE_F32, TRE_BF16), or
  *             TRE_MXFP4: the n_rows / tile_rows tiles of tile_rows rows of
  *             row_elems contracted values, row i in tile i / tile_rows, as
@@ -523,8 +523,9 @@ tre_status tre_lookup(const void *table, int32_t table_dtype, int64_t n_rows, in
 /* tre_lookup_grad -- the gradient of tre_lookup by its table: the rows of `grad`
  * summed by token (the GROUP BY sum of Sec. 5),
  *   table_grad[v] = scale * sum over t with id[t] = v of grad[t],
- * the sums in fp32 in an order that the ids alone determine (no atomics on
- * values: the same call gives the same bits), each result rounded once.
+ * the sums in fp32 in an order that the ids alone determine (no atomics: the
+ * same call gives the same bits), times the scale in fp32, rounded to the
+ * output's type.
  *   grad       : device [n_ids x row_elems] of grad_dtype (TRE_F32, TRE_BF16).
  *   ids        : as for tre_lookup; negative ones add to no row, nor do those of
  *                n_rows or more, which set `status`.

@@ -574,7 +574,8 @@ __device__ inline int32_t pair_index(const int32_t* list, int64_t i) {
 // same tiles, and the first of them adds their sums in order.
 //
 // What bounds it is how much is on its way: one token against 32,768 rows of
-// 4,096 values (71 MB) took @@ us with one step at a time.
+// 4,096 values (71 MB) took 36 us a step at a time and takes 15 (4.6 TB/s) with
+// batches of four in two tiles of 16 rows; of eight, or in one tile, 17 to 19.
 //
 // SHORT: rows of one or two blocks; a step is then the rows of four or two
 // pairs, each lane's its own.
@@ -709,12 +710,22 @@ __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
 // once.  A row's four scale bytes are one dword; those of a lane's TM (TN) rows,
 // which lie 32 rows apart, are side by side.
 //
-// An 8192^3 product (measured without its rows' quantisation):
-//   16 x 16 tiles, 256 x 256 for a workgroup of one per CU      438 us
-//   128 x 256, two workgroups per CU (one's products cover what
-//   the other waits for)                                        317
-//   32 x 32 tiles: half the instructions                        @@
-// Registers alone do 6.6 PFLOP/s of random codes (power; 8.7 of zeros).
+// A call of an 8192^3 product took, with its rows' quantisation and the join
+// (60 us of it, then 50):
+//   256 x 256 for the only workgroup of a CU, 16 x 16 tiles        533 us
+//   128 x 256, two workgroups per CU: one's products cover what the
+//   other waits for                                                503
+//   tiles in groups of four blocks: a third of the L2's requests   385
+//   all reads of a stage on their way before its first product     377
+//   four sums to a store                                           340
+//   no unit table                                                  325
+// The kernel is then at 285 to 300 us, 3.7 to 3.85 PFLOP/s (a stage 0.99 us for
+// two workgroups, their starts and ends 12 us each).  With no copies in the loop
+// 16 x 16 tiles took 240; registers alone do 6.6 PFLOP/s of random codes (power;
+// 8.7 of zeros), so the wavefronts' waits for LDS and each other bound it.  A
+// raised priority around the products, the copies issued after the reads, and
+// other slots (the bank conflicts' third of the LDS time) changed it by 2% or
+// less.
 constexpr int kStages = 3;
 
 __device__ inline int mx_slot(int r, int k) { return k ^ ((r >> 2) & 3); }

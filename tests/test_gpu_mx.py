@@ -356,3 +356,35 @@ def test_one_long_key(t, how):
     tol = (n * (32 * mx.row_blocks(t) + 2)) * U32 * mag + (UB16 * ref.abs() if t == 96 else 0)
     assert bool(((got - ref).abs() <= tol).all())
     assert float((got - ref).norm() / ref.norm()) <= (UB16 if t == 96 else 1e-6)
+
+
+def test_far_offsets():
+    """Tiles past 2^31 elements and 2^32 bytes, in and out."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    n, r, k = 40000, 256, 1024
+    plan = tre.Plan("ik,jk->ij", "i", {"i": n * r, "j": 16, "k": k}, {"i": r}, "mxfp4")
+    far = [0, 12345, 30839, 30840, n - 1]
+    q = torch.zeros((n, plan.tile_bytes[0]), dtype=torch.uint8, device="cuda")  # 5.6 GB; zero codes, scale 2^-127
+    x = torch.randn((len(far), r * k), device="cuda")
+    q[far] = tre.mx_quantize(plan, "u", x)
+    v = tre.mx_quantize(plan, "v", torch.randn((1, 16 * k), device="cuda"))
+    keys = torch.arange(n, dtype=torch.int32, device="cuda").reshape(n, 1)
+    w = tre.einsum(plan, keys, q, None, v).w_tiles
+    xd = tre.mx_dequantize(plan, "u", q[far].contiguous()).double().view(-1, k)
+    vd = tre.mx_dequantize(plan, "v", v).double().view(16, k)
+    ref, mag = xd @ vd.T, xd.abs() @ vd.abs().T
+    assert bool(((w[far].double().view(-1, 16) - ref).abs() <= (k + 2) * U32 * mag).all())
+    w[far] = 0
+    assert not bool(w.any())
+    del w, keys
+    m = 20500  # 5.4 G values of bf16: 10.7 GB
+    tiles = torch.zeros((m, r * k), dtype=torch.bfloat16, device="cuda")
+    tiles[m - 1] = x[0].to(torch.bfloat16)
+    tre.mx_quantize(plan, "u", tiles, out=q[:m])
+    assert torch.equal(q[m - 1], tre.mx_quantize(plan, "u", tiles[m - 1:].contiguous())[0])
+    back = tre.mx_dequantize(plan, "u", q[:m], out=tiles)
+    assert torch.equal(back[m - 1], tre.mx_dequantize(plan, "u", q[m - 1:m].contiguous(), dtype=torch.bfloat16)[0])
+    assert not bool(back[:m - 1].any())

@@ -235,14 +235,15 @@ def test_refused_on_the_gpu():
     refused("TRE_E_SHAPE", tre.mx_quantize, plan, "v", g[:2].T.contiguous())
 
 
-def test_streams_and_graphs():
+@pytest.mark.parametrize("n", [60, 5000, 20000])  # one chunk's groups, tokens ranked, tokens sorted by digits
+def test_streams_and_graphs(n):
     """On another stream, and replayed from a graph between eager calls that
     share its workspace."""
     import torch
 
     import paper_2603_08957_amd as tre
 
-    n, vocab, d = 5000, 700, 40
+    vocab, d = 700, 40
     ids = torch.randint(-1, vocab, (n,), device="cuda")
     g = torch.randn((n, d), device="cuda")
     table = torch.randn((vocab, d), device="cuda")
