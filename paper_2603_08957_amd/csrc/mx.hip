@@ -492,7 +492,7 @@ struct MxArgs {
     const int32_t *pa, *pb;
     int64_t a_bytes, b_bytes;    // of a tile
     int32_t a_scales, b_scales;  // where a tile's scales begin
-    int32_t M, N, blocks, group; // rows of A and B to a batch index, blocks of a row and of a group
+    int32_t M, N, blocks;        // rows of A and B to a batch index, blocks of a row
     int32_t a_rows, b_rows;      // of a tile
     int32_t m_blocks, n_blocks, wg_blocks;
     int32_t w_affine, w_bf16, batched;
@@ -1120,7 +1120,6 @@ hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_til
     g.a_bytes = p.mx_bytes[a];
     g.b_bytes = p.mx_bytes[b];
     g.blocks = int32_t(p.mx_blocks);
-    g.group = mx_group(p.mx_blocks);
     g.a_rows = int32_t(p.mx_rows[a]);
     g.b_rows = int32_t(p.mx_rows[b]);
     g.a_scales = int32_t(p.mx_rows[a] * p.mx_blocks * 16);

@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
     const int64_t x = int64_t(blockIdx.x) * kThreads + threadIdx.x;
     const int lane = int(x & ((1 << g.strip.shift) - 1));
     int64_t t[kStrips], e[kStrips];
-    float v[kStrips][E];
+    float v[kStrips][E], scale[kStrips];  // 0 for no token: its row is zero under any scale
     if constexpr (WIDE) {
         // (a wavefront's row is the same for its lanes)
         const int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -186,6 +186,7 @@ __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
         for (int i = 0; i < kStrips; i++) {
             t[i] = row;
             e[i] = ((s0 + i) * 64 + lane) * E;
+            scale[i] = in ? g.scale : 0.f;
 #pragma unroll
             for (int j = 0; j < E; j++) v[i][j] = 0.f;
             if (in && e[i] < g.elems) lookup_load<TI>(g, id, e[i], v[i]);
@@ -204,14 +205,16 @@ __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
         for (int i = 0; i < kStrips; i++) {
 #pragma unroll
             for (int j = 0; j < E; j++) v[i][j] = 0.f;
-            if (id[i] >= 0 && id[i] < g.n_rows && e[i] < g.elems) lookup_load<TI>(g, id[i], e[i], v[i]);
+            const bool in = id[i] >= 0 && id[i] < g.n_rows;
+            scale[i] = in ? g.scale : 0.f;
+            if (in && e[i] < g.elems) lookup_load<TI>(g, id[i], e[i], v[i]);
         }
     }
 #pragma unroll
     for (int i = 0; i < kStrips; i++) {
         if (e[i] >= g.elems) continue;
 #pragma unroll
-        for (int j = 0; j < E; j++) v[i][j] *= g.scale;
+        for (int j = 0; j < E; j++) v[i][j] *= scale[i];
         store_run<true>(static_cast<TO*>(g.out) + t[i] * g.elems, e[i], g.elems, v[i]);
     }
 }

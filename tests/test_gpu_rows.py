@@ -130,6 +130,29 @@ GRADS = [  # tokens, rows, row, kind: at and around the chunks of 8 and 32, thei
 ]
 
 
+@pytest.mark.parametrize("scale", [-2.0, float("inf"), float("nan")])
+@pytest.mark.parametrize("d", [24, 1200])
+def test_rows_of_no_token_under_any_scale(d, scale):
+    """Such rows are +0, whatever the others become."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    rng = np.random.default_rng(d)
+    table = torch.from_numpy(1 + rng.random((9, d)).astype(np.float32)).cuda()
+    ids = torch.tensor([3, -1, 8, 0, -7, 2, -1], device="cuda")
+    plan = tre.Plan("vd,td->vt", "v", {"v": 9, "d": d, "t": 16}, {"v": 3}, dtype="mxfp4")
+    q = tre.mx_quantize(plan, "u", table.view(3, 3 * d))
+    for got, rows in ((tre.lookup(table, ids, scale=scale), table),
+                      (tre.lookup(table.bfloat16(), ids, scale=scale, dtype=torch.float32), table.bfloat16().float()),
+                      (tre.lookup(q, ids, scale=scale, plan=plan), tre.mx_dequantize(plan, "u", q).view(9, d))):
+        v, none = got.cpu().numpy(), (ids < 0).cpu().numpy()
+        assert np.all(v[none].view(np.uint32) == 0)
+        np.testing.assert_array_equal(v[~none], (rows[ids[~torch.from_numpy(none).cuda()]] * scale).cpu().numpy())
+    grad = tre.lookup_grad(tre.lookup(table, ids), ids, 9, scale=scale).cpu().numpy()
+    assert np.all(grad[[1, 4, 5, 6, 7]].view(np.uint32) == 0)
+
+
 @pytest.mark.parametrize("gdt", ["f32", "bf16"])
 @pytest.mark.parametrize("odt", ["f32", "bf16"])
 @pytest.mark.parametrize("n,vocab,d,kind", GRADS)
