@@ -263,28 +263,30 @@ __global__ __launch_bounds__(kThreads) void k_grad_keys(const void* __restrict__
     pos[t] = uint32_t(t);
 }
 
-// Few tokens are sorted in one launch: a workgroup counts, for its 64, the
-// tokens that go before them, each of its wavefronts among a part of them.
-// (Four wavefronts took 30 us for 6,300 tokens, most of it to read them.)
-constexpr int kRankMax = 8192, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
+// Few tokens are sorted in one launch: a workgroup counts, for its 16, the
+// tokens that go before them, 16 threads to a part of the list.  (Four
+// wavefronts for 64 tokens took 30 us for 6,300 of them, sixteen 13; with 16
+// tokens to a workgroup a gradient of 5,900 takes 38.5 us in all, with 32 39.4,
+// with 64 41, and one of 8,192 54, 56 and 58.)
+constexpr int kRankMax = 8192, kRankThreads = 1024, kRankTokens = 16, kRankParts = kRankThreads / kRankTokens;
 
 __global__ __launch_bounds__(kRankThreads) void k_grad_rank(const void* __restrict__ ids, int id_bytes, int n, int64_t n_rows,
                                                         uint32_t* __restrict__ keys, uint32_t* __restrict__ pos,
                                                         int64_t* __restrict__ status) {
     __shared__ uint4 all[kRankMax / 4];
-    __shared__ int32_t part[kRankWaves][64];
+    __shared__ int32_t part[kRankParts][kRankTokens];
     uint32_t* flat = reinterpret_cast<uint32_t*>(all);
-    const int padded = (n + 4 * kRankWaves - 1) / (4 * kRankWaves) * (4 * kRankWaves);  // (after every token)
+    const int padded = (n + 4 * kRankParts - 1) / (4 * kRankParts) * (4 * kRankParts);  // (after every token)
 #pragma unroll 4
     for (int t = threadIdx.x; t < padded; t += kRankThreads)
         flat[t] = t < n ? token_key(ids, id_bytes, t, n_rows, blockIdx.x == 0 ? status : nullptr) : 0xffffffffu;
     __syncthreads();
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i0 = blockIdx.x * 64, i = i0 + lane;
+    const int own = threadIdx.x % kRankTokens, p = threadIdx.x / kRankTokens, i0 = blockIdx.x * kRankTokens, i = i0 + own;
     const uint32_t key = i < n ? flat[i] : 0u;
-    const int q0 = padded / 4 / kRankWaves * w, q1 = q0 + padded / 4 / kRankWaves;
+    const int q0 = padded / 4 / kRankParts * p, q1 = q0 + padded / 4 / kRankParts;
     int before = 0;
     // quads before the workgroup's tokens (equal ones go before), its own, those after
-    const int a = min(max(i0 / 4, q0), q1), b = min(max(i0 / 4 + 16, q0), q1);
+    const int a = min(max(i0 / 4, q0), q1), b = min(max((i0 + kRankTokens) / 4, q0), q1);
 #pragma unroll 4
     for (int q = q0; q < a; q++) {
         const uint4 k = all[q];
@@ -300,12 +302,12 @@ __global__ __launch_bounds__(kRankThreads) void k_grad_rank(const void* __restri
         const uint4 k = all[q];
         before += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
     }
-    part[w][lane] = before;
+    part[p][own] = before;
     __syncthreads();
-    if (w == 0 && i < n) {
+    if (p == 0 && i < n) {
         int at = 0;
 #pragma unroll
-        for (int j = 0; j < kRankWaves; j++) at += part[j][lane];
+        for (int j = 0; j < kRankParts; j++) at += part[j][own];
         keys[at] = key;
         pos[at] = uint32_t(i);
     }
@@ -621,7 +623,8 @@ hipError_t launch_lookup_grad(const void* grad, int grad_dtype, const void* ids,
             pos = pos2;
         }
     } else if (n_ids > 0) {
-        k_grad_rank<<<unsigned((n_ids + 63) / 64), kRankThreads, 0, s>>>(ids, id_bytes, int(n_ids), n_rows, keys, pos, status);
+        const unsigned grid = unsigned((n_ids + kRankTokens - 1) / kRankTokens);
+        k_grad_rank<<<grid, kRankThreads, 0, s>>>(ids, id_bytes, int(n_ids), n_rows, keys, pos, status);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     GradArgs g{};
