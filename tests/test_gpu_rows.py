@@ -191,6 +191,27 @@ def test_lookup_grad(n, vocab, d, kind, gdt, odt):
     assert torch.equal(out[torch.from_numpy(c[:, 0] == 0).cuda()], base[torch.from_numpy(c[:, 0] == 0).cuda()])
 
 
+@pytest.mark.parametrize("odt", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,d", [(1, 1), (300, 1), (130, 37), (1000, 64), (70, 8193), (9, 20000), (5000, 3), (200, 1001)])
+def test_zero_rows(vocab, d, odt):
+    """Every row without a token is zero, none behind the last is touched."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    T = types()
+    rng = np.random.default_rng(vocab + d)
+    for n in (0, 1, vocab // 2, vocab):
+        ids = torch.from_numpy(rng.integers(0, vocab, n)).cuda()
+        grad = torch.ones((n, d), device="cuda")
+        buf = torch.full((vocab + 1, d), float("nan"), dtype=T[odt], device="cuda")
+        buf[vocab] = -7.0
+        tre.lookup_grad(grad, ids, vocab, out=buf[:vocab])
+        want = torch.bincount(ids.cpu(), minlength=vocab).float()[:, None].expand(vocab, d)
+        assert torch.equal(buf[:vocab].float().cpu(), want)  # counts below 256: exact in bf16
+        assert torch.all(buf[vocab] == -7.0)
+
+
 def test_lookup_grad_by_differences():
     """The gradient of sum(g * lookup(E)) by differences: with small whole
     numbers and a scale of 2 every step is exact."""
