@@ -506,10 +506,13 @@ struct MxArgs {
     float* partials;
 };
 
+// (Keys out of order, which an asynchronous call reports in its counts, can
+// leave segments that end where they begin or before: no pair of theirs is
+// looked at.)
 __device__ inline bool mx_unit(const MxArgs& g, int64_t unit, Unit& u) {
     if (unit >= (g.seg_start ? g.hdr->n_w : g.hdr->n_units)) return false;
     u = g.seg_start ? Unit{int32_t(unit), g.seg_start[unit], g.seg_start[unit + 1], -1} : g.units[unit];
-    return true;
+    return u.p1 > u.p0;
 }
 
 // The sums of a wavefront's TM x TN tiles of S x S, whose first is at (m0, n0), to

@@ -388,3 +388,36 @@ def test_far_offsets():
     back = tre.mx_dequantize(plan, "u", q[:m], out=tiles)
     assert torch.equal(back[m - 1], tre.mx_dequantize(plan, "u", q[m - 1:m].contiguous(), dtype=torch.bfloat16)[0])
     assert not bool(back[:m - 1].any())
+
+
+@pytest.mark.parametrize("t", [64, 24])  # fragments from LDS, and straight from memory
+def test_keys_out_of_order_async(t):
+    """Keys that are not sorted leave output keys whose pairs end before they
+    begin: the call says so in its counts, and reads and writes nothing of
+    theirs.  Keys in order then give their sums in the same buffers."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    nb, k = 8, 128
+    # (the join in several launches: the one-workgroup one leaves no such segments)
+    plan = tre.Plan("ij,jk->ik", "ij", {"i": nb * t, "j": nb * k, "k": t}, {"i": t, "j": k}, "mxfp4", small_join=-1)
+    g = torch.Generator(device="cuda").manual_seed(t)
+    keys = torch.cartesian_prod(torch.arange(nb), torch.arange(nb)).to(torch.int32).cuda()
+    bk = torch.arange(nb, dtype=torch.int32, device="cuda").reshape(nb, 1)
+    u = tre.mx_quantize(plan, "u", torch.randn((nb * nb, t * k), generator=g, device="cuda"))
+    v = tre.mx_quantize(plan, "v", torch.randn((nb, k * t), generator=g, device="cuda"))
+    ws = tre.alloc_workspace(plan.workspace_bytes(nb * nb, nb, nb * nb))
+    wk = torch.zeros((nb + 1, 1), dtype=torch.int32, device="cuda")
+    wt = torch.full((nb + 1, t * t), -3.0, device="cuda")
+    counts = torch.zeros(4, dtype=torch.int64, device="cuda")
+    tre.execute_async(plan, keys.flip(0).contiguous(), u, bk, v, wk[:nb], wt[:nb], ws, counts)
+    assert counts[2].item() == tre.tre.STATUS_CODE["TRE_E_UNSORTED"]
+    assert torch.all(wt[nb] == -3.0) and wk[nb].item() == 0
+    tre.execute_async(plan, keys, u, bk, v, wk[:nb], wt[:nb], ws, counts)
+    assert counts.tolist() == [nb * nb, nb, 0, 0]
+    ud = tre.mx_dequantize(plan, "u", u).double().view(nb, nb, t, k).transpose(1, 2).reshape(nb * t, nb * k)
+    vd = tre.mx_dequantize(plan, "v", v).double().view(nb * k, t)
+    ref, mag = ud @ vd, ud.abs() @ vd.abs()
+    assert bool(((wt[:nb].double().view(nb * t, t) - ref).abs() <= (nb * k + 2) * U32 * mag).all())
+    assert torch.all(wt[nb] == -3.0)
