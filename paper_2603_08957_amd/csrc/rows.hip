@@ -432,14 +432,15 @@ __global__ __launch_bounds__(kThreads) void k_grad_sum(GradArgs g) {
     else put_row<TO>(g, key, e, acc);
 }
 
-// One or two elements of a row from e on.
+// The up to two elements of a row from e on (past its end, its last one again).
 __device__ inline void load_pair(const float* row, int64_t e, int64_t n, float (&v)[2]) {
-    v[0] = row[e];
-    v[1] = e + 1 < n ? row[e + 1] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; i++) v[i] = row[min(e + i, n - 1)];
 }
 __device__ inline void store_pair(float* row, int64_t e, int64_t n, const float (&v)[2]) {
-    row[e] = v[0];
-    if (e + 1 < n) row[e + 1] = v[1];
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+        if (e + i < n) row[e + i] = v[i];
 }
 template <typename TO>
 __device__ inline void put_pair(const GradArgs& g, int64_t row, int64_t e, const float (&v)[2]) {
@@ -489,7 +490,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_join(GradArgs g, JoinArgs a) 
         whole = cont && key == last;                                          // and is its first
     }
     const uint64_t conts = __ballot(cont), goes = __ballot(more), wholes = __ballot(whole);
-    if (e >= g.elems) return;
+    // (Lanes past the row's end stay: the keys that they hold are read below.)
     float acc[kJoinLane] = {0.f, 0.f};
     bool first = conts & 1;  // the run at hand began in an earlier group
     for (uint64_t todo = conts | (goes & ~wholes); todo;) {

@@ -389,3 +389,24 @@ def test_training_step_of_a_tied_table():
     _, m2 = mx.lookup_grad(dxm, ids_h, vocab, 3.0)
     dwr, dwm = gn @ xn, np.abs(gn) @ np.abs(xn)
     near(de.double().cpu().numpy(), dwr + e1, dwm + m1 + m2, vocab + 2 * n + 140)
+
+
+@pytest.mark.parametrize("d", [1, 2, 3, 63, 127, 129, 250])
+@pytest.mark.parametrize("n", [8 * 40, 8 * 64, 32 * 600])
+def test_runs_that_end_in_every_chunk(n, d):
+    """Each chunk of tokens ends one run and begins the next, so that every lane
+    of the wavefront that joins partial sums holds the key of a row, those past
+    the row's end too.  Whole numbers: every sum is exact."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    chunk = 8 if n <= 16384 else 32
+    ids = (torch.arange(n) + chunk // 2) // chunk  # runs of a chunk's length, half a chunk off
+    vocab = int(ids[-1]) + 1
+    g = torch.randint(-8, 9, (n, d), generator=torch.Generator().manual_seed(n + d)).float()
+    want = torch.zeros((vocab, d)).index_add_(0, ids, g) * 2
+    assert torch.equal(tre.lookup_grad(g.cuda(), ids.cuda(), vocab, scale=2.0).cpu(), want)
+    out = torch.ones((vocab, d), device="cuda")
+    tre.lookup_grad(g.cuda(), ids.cuda(), vocab, scale=2.0, out=out, accumulate=True)
+    assert torch.equal(out.cpu(), want + 1)
