@@ -426,7 +426,7 @@ class _Here:
     def __init__(self, device, stream):
         import torch
 
-        self.stream = stream
+        self.device, self.stream = device, stream
         self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
         self.ptr = _stream(stream, device)
 
@@ -439,11 +439,20 @@ class _Here:
         if self.guard is not None:
             self.guard.__exit__(*exc)
 
-    def keep(self, t):
-        """A tensor made here for a stream other than the current one: its
-        memory must not be given out again before that stream is done with it."""
-        if self.stream is not None:
-            t.record_stream(self.stream)
+    def buffer(self, make, result=True):
+        """The tensor that ``make()`` allocates, out of the memory of the stream
+        that will use it: a block that the current stream has just given back may
+        still be in use by what is queued there, which a caller's stream does not
+        wait for.  A result is the current stream's too: its memory is not given
+        out again before what that stream does with it is done."""
+        import torch
+
+        if self.stream is None:
+            return make()
+        with torch.cuda.stream(self.stream):
+            t = make()
+        if result:
+            t.record_stream(torch.cuda.current_stream(self.device))
         return t
 
 
@@ -468,7 +477,7 @@ def mx_quantize(plan: Plan, operand: str, tiles, out=None, stream=None):
     _want(tiles, w, "tiles", (n, plan.tile_elems[o]))
     with _Here(tiles.device, stream) as here:
         if out is None:
-            out = here.keep(torch.empty((n, plan.tile_bytes[o]), dtype=torch.uint8, device=tiles.device))
+            out = here.buffer(lambda: torch.empty((n, plan.tile_bytes[o]), dtype=torch.uint8, device=tiles.device))
         else:
             _want(out, w, "out", (n, plan.tile_bytes[o]), torch.uint8, tiles.device)
         _check(lib().tre_mx_quantize(plan.handle, o, _ptr(tiles), dt, n, _ptr(out), here.ptr), "tre_mx_quantize")
@@ -488,7 +497,8 @@ def mx_dequantize(plan: Plan, operand: str, mx_tiles, dtype=None, out=None, stre
     dt = _value_type(out if out is not None else dtype or torch.float32, w, "out")
     with _Here(mx_tiles.device, stream) as here:
         if out is None:
-            out = here.keep(torch.empty((n, plan.tile_elems[o]), dtype=dtype or torch.float32, device=mx_tiles.device))
+            out = here.buffer(lambda: torch.empty((n, plan.tile_elems[o]), dtype=dtype or torch.float32,
+                                                  device=mx_tiles.device))
         else:
             _want(out, w, "out", (n, plan.tile_elems[o]), dtype, mx_tiles.device)
         _check(lib().tre_mx_dequantize(plan.handle, o, _ptr(mx_tiles), n, _ptr(out), dt, here.ptr), "tre_mx_dequantize")
@@ -545,7 +555,7 @@ def lookup(table, ids, scale: float = 1.0, dtype=None, out=None, plan: Plan | No
     odt = _value_type(dtype, w, "out")
     with _Here(table.device, stream) as here:
         if out is None:
-            out = here.keep(torch.empty(shape, dtype=dtype, device=table.device))
+            out = here.buffer(lambda: torch.empty(shape, dtype=dtype, device=table.device))
         else:
             _want(out, w, "out", shape, dtype, table.device)
         _check(lib().tre_lookup(_ptr(table), tdt, n_rows, elems, tile_rows, _ptr(ids), ids.element_size(), ids.numel(),
@@ -580,11 +590,12 @@ def lookup_grad(grad, ids, n_rows: int, scale: float = 1.0, dtype=None, out=None
     odt = _value_type(dtype, w, "out")
     with _Here(grad.device, stream) as here:
         if out is None:
-            out = here.keep(torch.empty((n_rows, elems), dtype=dtype, device=grad.device))
+            out = here.buffer(lambda: torch.empty((n_rows, elems), dtype=dtype, device=grad.device))
         else:
             _want(out, w, "out", (n_rows, elems), dtype, grad.device)
         if ws is None:
-            ws = here.keep(alloc_workspace(lookup_grad_workspace_bytes(n, n_rows, elems), grad.device))
+            ws = here.buffer(lambda: alloc_workspace(lookup_grad_workspace_bytes(n, n_rows, elems), grad.device),
+                             result=False)
         else:
             _want(ws, w, "ws", device=grad.device)
         _check(lib().tre_lookup_grad(_ptr(grad), gdt, _ptr(ids), ids.element_size(), n, float(scale), _ptr(out), odt, n_rows,
