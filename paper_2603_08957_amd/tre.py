@@ -172,6 +172,23 @@ def _stream(stream=None, device=None):
     return ctypes.c_void_p(raw(torch.cuda.current_device() if device is None else device.index))
 
 
+def _buffer(stream, device, make, result=True):
+    """The tensor that ``make()`` allocates, out of the memory of the stream that
+    will use it: a block that the current stream has just given back may still
+    be in use by what is queued there, which a caller's stream does not wait
+    for.  A result is the current stream's too: its memory is not given out
+    again before what that stream does with it is done."""
+    import torch
+
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        t = make()
+    if result:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 class Plan:
     """A parsed, classified binary EinSum (host object, see tre_plan)."""
 
@@ -350,21 +367,22 @@ def einsum(plan: Plan, u_keys, u_tiles, v_keys, v_tiles, want_pairs: bool = Fals
     dev = u_tiles.device
     if ws is None:
         hint = pair_hint if pair_hint is not None else max(n_u, n_v, 1) * 2
-        ws = alloc_workspace(plan.workspace_bytes(n_u, n_v, hint), dev)
+        ws = _buffer(stream, dev, lambda: alloc_workspace(plan.workspace_bytes(n_u, n_v, hint), dev))
     tm = Timing() if timing else None
     try:
         jr = join(plan, u_keys, n_u, v_keys, n_v, ws, stream, tm)
     except TreError as e:
         if e.code != 10 or e.join_result.n_pairs <= 0:
             raise
-        ws = alloc_workspace(plan.workspace_bytes(n_u, n_v, int(e.join_result.n_pairs)), dev)
+        need = int(e.join_result.n_pairs)
+        ws = _buffer(stream, dev, lambda: alloc_workspace(plan.workspace_bytes(n_u, n_v, need), dev))
         jr = join(plan, u_keys, n_u, v_keys, n_v, ws, stream, tm)
     n_w, n_p = int(jr.n_w), int(jr.n_pairs)
     rw = plan.key_arity[2]
-    w_keys = torch.empty((n_w, rw), dtype=torch.int32, device=dev)
-    w_tiles = torch.empty((n_w, plan.tile_elems[2]), dtype=torch.bfloat16 if plan.w_bf16 else torch.float32,
-                          device=dev)
-    pairs = torch.empty((n_p, 2), dtype=torch.int32, device=dev) if want_pairs else None
+    w_keys = _buffer(stream, dev, lambda: torch.empty((n_w, rw), dtype=torch.int32, device=dev))
+    w_tiles = _buffer(stream, dev, lambda: torch.empty((n_w, plan.tile_elems[2]),
+                                                       dtype=torch.bfloat16 if plan.w_bf16 else torch.float32, device=dev))
+    pairs = _buffer(stream, dev, lambda: torch.empty((n_p, 2), dtype=torch.int32, device=dev)) if want_pairs else None
     contract(plan, jr, u_tiles, v_tiles, w_keys if rw > 0 else None, w_tiles, pairs, stream, tm)
     return Output(w_keys, w_tiles, pairs, n_p, n_w, tm.as_dict() if tm is not None else None, ws)
 
@@ -440,20 +458,7 @@ class _Here:
             self.guard.__exit__(*exc)
 
     def buffer(self, make, result=True):
-        """The tensor that ``make()`` allocates, out of the memory of the stream
-        that will use it: a block that the current stream has just given back may
-        still be in use by what is queued there, which a caller's stream does not
-        wait for.  A result is the current stream's too: its memory is not given
-        out again before what that stream does with it is done."""
-        import torch
-
-        if self.stream is None:
-            return make()
-        with torch.cuda.stream(self.stream):
-            t = make()
-        if result:
-            t.record_stream(torch.cuda.current_stream(self.device))
-        return t
+        return _buffer(self.stream, self.device, make, result)
 
 
 def _operand(plan, operand, where):
@@ -607,7 +612,9 @@ def lookup_grad(grad, ids, n_rows: int, scale: float = 1.0, dtype=None, out=None
 def cast_f32_bf16(x, out=None, stream=None):
     import torch
 
-    y = out if out is not None else torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+    y = out
+    if y is None:
+        y = _buffer(stream, x.device, lambda: torch.empty(x.shape, dtype=torch.bfloat16, device=x.device))
     _check(lib().tre_cast_f32_bf16(_ptr(x), _ptr(y), x.numel(), _stream(stream)), "tre_cast_f32_bf16")
     return y
 
@@ -616,7 +623,7 @@ def scale_f32(x, scale: float, out=None, stream=None):
     """out = scale * x (fp32, elementwise; out may be x)."""
     import torch
 
-    y = out if out is not None else torch.empty_like(x)
+    y = out if out is not None else _buffer(stream, x.device, lambda: torch.empty_like(x))
     _check(lib().tre_scale_f32(_ptr(x), _ptr(y), x.numel(), float(scale), _stream(stream)), "tre_scale_f32")
     return y
 
@@ -628,10 +635,11 @@ def stack_rows(keys, tiles, group: int, stream=None):
     n = int(keys.shape[0])
     row = int(tiles.numel() // max(n, 1)) if n else int(tiles.shape[1])
     eb = tiles.element_size()
-    ws = alloc_workspace(int(lib().tre_stack_workspace_bytes(n)), tiles.device)
+    dev = tiles.device
+    ws = _buffer(stream, dev, lambda: alloc_workspace(int(lib().tre_stack_workspace_bytes(n)), dev), result=False)
     cap = n
-    out_keys = torch.empty((cap, 1), dtype=torch.int32, device=tiles.device)
-    out_tiles = torch.empty((cap, group * row), dtype=tiles.dtype, device=tiles.device)
+    out_keys = _buffer(stream, dev, lambda: torch.empty((cap, 1), dtype=torch.int32, device=dev))
+    out_tiles = _buffer(stream, dev, lambda: torch.empty((cap, group * row), dtype=tiles.dtype, device=dev))
     n_out = ctypes.c_int64(0)
     rc = lib().tre_stack_rows(_ptr(keys), n, _ptr(tiles), row, group, eb, _ptr(out_keys), _ptr(out_tiles), cap,
                               ctypes.byref(n_out), _ptr(ws), ws.numel(), _stream(stream))
@@ -668,7 +676,8 @@ def repartition(labels: str, upper_in: str, upper_out: str, extents: dict, tiles
         rc = lib().tre_repartition(*args, tiles.element_size(), _ptr(keys), n, _ptr(tiles), None, None, 0,
                                    ctypes.byref(n_out), None, 0, _stream(stream))
         _check(rc if rc else STATUS_CODE["TRE_E_ARG"], "tre_repartition")
-    ws = alloc_workspace(wsb, tiles.device)
+    dev = tiles.device
+    ws = _buffer(stream, dev, lambda: alloc_workspace(wsb, dev), result=False)
     te_in = te_out = 1
     grid = cover = 1
     for c in labels:
@@ -681,7 +690,7 @@ def repartition(labels: str, upper_in: str, upper_out: str, extents: dict, tiles
             cover *= min(e // to, (ti - 1) // to + 2)
     if in_place:
         cap = (n * te_in) // max(te_out, 1)
-        out_keys = torch.empty((max(cap, 1), len(upper_out)), dtype=torch.int32, device=tiles.device)
+        out_keys = _buffer(stream, dev, lambda: torch.empty((max(cap, 1), len(upper_out)), dtype=torch.int32, device=dev))
         rc = lib().tre_repartition(*args, tiles.element_size(), _ptr(keys), n, _ptr(tiles), _ptr(out_keys),
                                    _ptr(tiles), cap, ctypes.byref(n_out), _ptr(ws), ws.numel(), _stream(stream))
         _check(rc, "tre_repartition")
@@ -693,8 +702,8 @@ def repartition(labels: str, upper_in: str, upper_out: str, extents: dict, tiles
     esz = tiles.element_size()
     cap = bound if bound * te_out * esz <= max(2 * n * te_in * esz, 1 << 26) else 0
     while True:
-        out_keys = torch.empty((max(cap, 1), len(upper_out)), dtype=torch.int32, device=tiles.device)
-        out_tiles = torch.empty((max(cap, 1), te_out), dtype=tiles.dtype, device=tiles.device)
+        out_keys = _buffer(stream, dev, lambda: torch.empty((max(cap, 1), len(upper_out)), dtype=torch.int32, device=dev))
+        out_tiles = _buffer(stream, dev, lambda: torch.empty((max(cap, 1), te_out), dtype=tiles.dtype, device=dev))
         rc = lib().tre_repartition(*args, tiles.element_size(), _ptr(keys), n, _ptr(tiles), _ptr(out_keys),
                                    _ptr(out_tiles), cap, ctypes.byref(n_out), _ptr(ws), ws.numel(), _stream(stream))
         if rc == STATUS_CODE["TRE_E_CAPACITY"] and n_out.value > cap:
@@ -709,7 +718,8 @@ def tiles_from_entries(slot, offset, values, n_tiles: int, tile_elems: int, stre
     """Dense tiles [n_tiles, tile_elems] (dtype of ``values``) from scalar entries."""
     import torch
 
-    tiles = torch.empty((n_tiles, tile_elems), dtype=values.dtype, device=values.device)
+    tiles = _buffer(stream, values.device,
+                    lambda: torch.empty((n_tiles, tile_elems), dtype=values.dtype, device=values.device))
     rc = lib().tre_tiles_from_entries(_ptr(slot), _ptr(offset), _ptr(values), int(values.numel()),
                                       values.element_size(), _ptr(tiles), n_tiles, tile_elems, _stream(stream))
     _check(rc, "tre_tiles_from_entries")
@@ -763,10 +773,13 @@ class Einsum3:
         if n_u > self.n_u_max:
             raise ValueError(f"n_u {n_u} above the workspace sizing {self.n_u_max}")
         dev = u_tiles.device
+        if stream is not None:
+            self.ws.record_stream(stream)
         if out is None:
             cap = min(n_u, self.w_key_space)
-            out = (torch.empty((max(cap, 1), self.w_arity), dtype=torch.int32, device=dev),
-                   torch.empty((max(cap, 1), self.w_tile_elems), dtype=torch.float32, device=dev))
+            out = (_buffer(stream, dev, lambda: torch.empty((max(cap, 1), self.w_arity), dtype=torch.int32, device=dev)),
+                   _buffer(stream, dev, lambda: torch.empty((max(cap, 1), self.w_tile_elems), dtype=torch.float32,
+                                                            device=dev)))
             cap_given = cap
         else:
             cap_given = int(out[1].shape[0])
@@ -784,7 +797,12 @@ def execute3(einsum: str, upper: str, extents: dict, tiles: dict, u_keys, u_tile
              stream=None, timing: bool = False):
     """One-shot tre_execute3 with a fresh workspace; returns (w_keys, w_tiles,
     n_triples[, timing dict])."""
-    op = Einsum3(einsum, upper, extents, tiles, int(u_tiles.shape[0]), u_tiles.device)
+    import contextlib
+
+    import torch
+
+    with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():  # its workspace is that stream's
+        op = Einsum3(einsum, upper, extents, tiles, int(u_tiles.shape[0]), u_tiles.device)
     tm = Timing() if timing else None
     wk, wt, nt = op(u_keys, u_tiles, v_keys, v_tiles, x_keys, x_tiles, stream, tm)
     return (wk, wt, nt, tm.as_dict()) if timing else (wk, wt, nt)
