@@ -255,8 +255,9 @@ def alloc_workspace(nbytes: int, device="cuda"):
 
 
 def _mx_operands(plan: Plan, u_tiles, v_tiles):
-    """4-bit tiles come as uint8 rows of the plan's tile size: anything else is
-    an array that was not quantised for this plan."""
+    """4-bit tiles come as uint8 rows of the plan's tile size, on the GPU that the
+    call runs on (the current one): anything else is an array that was not
+    quantised for this plan, or not for here."""
     import torch
 
     if plan.dtype != "mxfp4":
@@ -268,6 +269,9 @@ def _mx_operands(plan: Plan, u_tiles, v_tiles):
             raise TreError(STATUS_CODE["TRE_E_SHAPE"], "tre.contract",
                            f"operand {'uv'[o]} of an mxfp4 plan: contiguous uint8 [n, {plan.tile_bytes[o]}] wanted, "
                            f"got {t.dtype} {tuple(t.shape)}")
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise TreError(STATUS_CODE["TRE_E_ARG"], "tre.contract",
+                           f"operand {'uv'[o]} of an mxfp4 plan: on {t.device}, wanted on the current GPU")
 
 
 def join(plan: Plan, u_keys, n_u: int, v_keys, n_v: int, ws, stream=None, timing: Timing | None = None) -> JoinResult:

@@ -421,3 +421,21 @@ def test_keys_out_of_order_async(t):
     ref, mag = ud @ vd, ud.abs() @ vd.abs()
     assert bool(((wt[:nb].double().view(nb * t, t) - ref).abs() <= (nb * k + 2) * U32 * mag).all())
     assert torch.all(wt[nb] == -3.0)
+
+
+def test_einsum_refuses_tiles_off_the_current_gpu(monkeypatch):
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    plan = tre.Plan("ik,jk->ij", "", {"i": 4, "j": 5, "k": 40}, {}, "mxfp4")
+    u, v = tre.mx_quantize(plan, "u", torch.ones((1, 160), device="cuda")), tre.mx_quantize(plan, "v", torch.ones((1, 200), device="cuda"))
+    assert torch.all(tre.einsum(plan, None, u, None, v).w_tiles == 40)
+    for a, b in ((u.cpu(), v), (u, v.cpu())):
+        with pytest.raises(tre.TreError) as e:
+            tre.einsum(plan, None, a, None, b)
+        assert e.value.status == "TRE_E_ARG"
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: u.device.index + 1)
+    with pytest.raises(tre.TreError) as e:
+        tre.einsum(plan, None, u, None, v)
+    assert e.value.status == "TRE_E_ARG"

@@ -136,3 +136,20 @@ def test_binding_refuses(tre):
     u = torch.zeros(2, 28)
     refused(tre, "TRE_E_SHAPE", tre.contract, p, tre.JoinResult(), u, u, None, u)
     refused(tre, "TRE_E_SHAPE", tre.einsum, p, None, u, None, u)
+
+
+@pytest.mark.parametrize("where", ["cpu", "meta"])
+def test_einsum_refuses_tiles_that_are_not_on_the_gpu(tre, where):
+    """Tiles of the right shape and type, but not on a GPU: no entry point that
+    takes them hands their addresses on."""
+    import torch
+
+    p = tre.Plan("nd,vd->nv", "", {"n": 3, "v": 5, "d": 7}, {}, "mxfp4")
+    u, v = (torch.zeros((1, b), dtype=torch.uint8, device=where) for b in p.tile_bytes[:2])
+    w, counts = torch.zeros((1, 15)), torch.zeros(4, dtype=torch.int64)
+    ws = torch.zeros(p.workspace_bytes(1, 1, 1), dtype=torch.uint8)
+    refused(tre, "TRE_E_ARG", tre.einsum, p, None, u, None, v)
+    refused(tre, "TRE_E_ARG", tre.execute, p, None, u, None, v, None, w, ws)
+    refused(tre, "TRE_E_ARG", tre.execute_async, p, None, u, None, v, None, w, ws, counts)
+    refused(tre, "TRE_E_ARG", tre.execute_noalloc, p, None, u, None, v, None, w)
+    refused(tre, "TRE_E_ARG", tre.contract, p, tre.JoinResult(), u, v, None, w)
