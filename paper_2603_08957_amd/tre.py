@@ -445,9 +445,11 @@ class _Here:
     already: that check costs a tenth of the context), and its stream: the
     caller's, else the device's current one."""
 
-    def __init__(self, device, stream):
+    def __init__(self, device, stream, where):
         import torch
 
+        if stream is not None and stream.device != device:
+            raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"stream: on {stream.device}, the tensors on {device}")
         self.device, self.stream = device, stream
         self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
         self.ptr = _stream(stream, device)
@@ -484,7 +486,7 @@ def mx_quantize(plan: Plan, operand: str, tiles, out=None, stream=None):
     dt = _value_type(tiles, w, "tiles")
     n = int(tiles.shape[0]) if tiles.dim() else -1
     _want(tiles, w, "tiles", (n, plan.tile_elems[o]))
-    with _Here(tiles.device, stream) as here:
+    with _Here(tiles.device, stream, w) as here:
         if out is None:
             out = here.buffer(lambda: torch.empty((n, plan.tile_bytes[o]), dtype=torch.uint8, device=tiles.device))
         else:
@@ -504,7 +506,7 @@ def mx_dequantize(plan: Plan, operand: str, mx_tiles, dtype=None, out=None, stre
     n = int(mx_tiles.shape[0]) if mx_tiles.dim() else -1
     _want(mx_tiles, w, "mx_tiles", (n, plan.tile_bytes[o]), torch.uint8)
     dt = _value_type(out if out is not None else dtype or torch.float32, w, "out")
-    with _Here(mx_tiles.device, stream) as here:
+    with _Here(mx_tiles.device, stream, w) as here:
         if out is None:
             out = here.buffer(lambda: torch.empty((n, plan.tile_elems[o]), dtype=dtype or torch.float32,
                                                   device=mx_tiles.device))
@@ -562,7 +564,7 @@ def lookup(table, ids, scale: float = 1.0, dtype=None, out=None, plan: Plan | No
     shape = tuple(ids.shape) + (elems,)
     dtype = dtype or (out.dtype if out is not None else torch.float32 if plan is not None else table.dtype)
     odt = _value_type(dtype, w, "out")
-    with _Here(table.device, stream) as here:
+    with _Here(table.device, stream, w) as here:
         if out is None:
             out = here.buffer(lambda: torch.empty(shape, dtype=dtype, device=table.device))
         else:
@@ -597,7 +599,7 @@ def lookup_grad(grad, ids, n_rows: int, scale: float = 1.0, dtype=None, out=None
     n, elems, n_rows = ids.numel(), int(grad.shape[-1]), int(n_rows)
     dtype = dtype or (out.dtype if out is not None else torch.float32)
     odt = _value_type(dtype, w, "out")
-    with _Here(grad.device, stream) as here:
+    with _Here(grad.device, stream, w) as here:
         if out is None:
             out = here.buffer(lambda: torch.empty((n_rows, elems), dtype=dtype, device=grad.device))
         else:

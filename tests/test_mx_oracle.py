@@ -153,3 +153,12 @@ def test_einsum_refuses_tiles_that_are_not_on_the_gpu(tre, where):
     refused(tre, "TRE_E_ARG", tre.execute_async, p, None, u, None, v, None, w, ws, counts)
     refused(tre, "TRE_E_ARG", tre.execute_noalloc, p, None, u, None, v, None, w)
     refused(tre, "TRE_E_ARG", tre.contract, p, tre.JoinResult(), u, v, None, w)
+
+
+def test_streams_of_another_gpu_refused(tre):
+    import torch
+
+    class Stream:
+        device, cuda_stream = torch.device("cuda", 1), 0
+
+    refused(tre, "TRE_E_ARG", tre.tre._Here, torch.device("cuda", 0), Stream(), "tre.lookup")
