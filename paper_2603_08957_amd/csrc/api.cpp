@@ -409,9 +409,10 @@ tre_status contract_enqueue(tre_plan_t plan, const tre_join_result* jr, int64_t 
         }
         WsHeader h{};
         if (!deferred && hipMemcpy(&h, w + L.hdr, sizeof(h), hipMemcpyDeviceToHost) == hipSuccess) {
-            timing->n_units = whole_keys ? n_w : h.n_units;
-            timing->n_split_segments = h.n_split;
-            timing->n_partials = h.n_parts;
+            // (without a unit table nobody has written its counts)
+            timing->n_units = whole_keys ? h.n_w : h.n_units;
+            timing->n_split_segments = whole_keys ? 0 : h.n_split;
+            timing->n_partials = whole_keys ? 0 : h.n_parts;
         }
     }
     return TRE_OK;

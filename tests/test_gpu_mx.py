@@ -439,3 +439,25 @@ def test_einsum_refuses_tiles_off_the_current_gpu(monkeypatch):
     with pytest.raises(tre.TreError) as e:
         tre.einsum(plan, None, u, None, v)
     assert e.value.status == "TRE_E_ARG"
+
+
+@pytest.mark.parametrize("small_join", [0, -1])
+def test_timing_of_whole_keys(small_join):
+    """A call that cuts no key counts none as cut, whatever its workspace held."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    nb, t = 12, 64
+    plan = tre.Plan("ij,jk->ik", "ij", {"i": nb * t, "j": nb * t, "k": t}, {"i": t, "j": t}, "mxfp4", small_join=small_join)
+    keys = torch.cartesian_prod(torch.arange(nb), torch.arange(nb)).to(torch.int32).cuda()
+    bk = torch.arange(nb, dtype=torch.int32, device="cuda").reshape(nb, 1)
+    u = tre.mx_quantize(plan, "u", torch.randn((nb * nb, t * t), device="cuda"))
+    v = tre.mx_quantize(plan, "v", torch.randn((nb, t * t), device="cuda"))
+    ws = tre.alloc_workspace(plan.workspace_bytes(nb * nb, nb, nb * nb))
+    wk, wt = torch.zeros((nb, 1), dtype=torch.int32, device="cuda"), torch.zeros((nb, t * t), device="cuda")
+    for fill in (0, 0x33):
+        ws.fill_(fill)
+        tm = tre.Timing()
+        assert tre.execute(plan, keys, u, bk, v, wk, wt, ws, timing=tm) == (nb, nb * nb)
+        assert (tm.n_units, tm.n_split_segments, tm.n_partials) == (nb, 0, 0)
