@@ -225,6 +225,10 @@ class Plan:
         self.v_needs_sort = bool(info.v_needs_sort)
         self.w_dtype = {0: "f32", 1: "bf16"}[info.w_dtype]
         self.join_outer = "v" if info.join_outer else "u"
+        # whether U's and V's tuples are rows of a table: W keeps one of its labels, and no other is promoted
+        ins, w = einsum.replace(" ", "").split("->")
+        kept = [[c for c in lab if c in w] for lab in ins.split(",")]
+        self.token_keyed = [len(k) == 1 and self.key_labels[o] in ("", k[0]) for o, k in enumerate(kept)]
         # bytes of one tile of U, V and W as the calls take it
         self.tile_bytes = [int(L.tre_tile_bytes(h, o)) for o in range(3)]
 
@@ -549,6 +553,10 @@ def lookup(table, ids, scale: float = 1.0, dtype=None, out=None, plan: Plan | No
         b, m, n, k = plan.bmnk
         if b != 1:
             raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, "the plan's operands share a label that W keeps in its tile")
+        if not plan.token_keyed[o]:
+            raise TreError(STATUS_CODE["TRE_E_SHAPE"], w,
+                           f"operand {operand!r} of {plan.einsum!r} ({plan.upper!r} promoted): one label that W keeps, the "
+                           "token's, and the others whole in the tile wanted")
         tile_rows, elems, tdt = (m, n)[o], k, 2
         n_tiles = int(table.shape[0]) if table.dim() else -1
         _want(table, w, "table", (n_tiles, plan.tile_bytes[o]), torch.uint8)

@@ -162,3 +162,37 @@ def test_streams_of_another_gpu_refused(tre):
         device, cuda_stream = torch.device("cuda", 1), 0
 
     refused(tre, "TRE_E_ARG", tre.tre._Here, torch.device("cuda", 0), Stream(), "tre.lookup")
+
+
+@pytest.mark.parametrize("einsum,upper,tiles,operand", [
+    ("vd,nd->nv", "vd", {"v": 4, "d": 32}, "u"),      # rows in pieces, a tile of each
+    ("vd,nd->nv", "d", {"d": 32}, "u"),
+    ("nd,dv->nv", "dv", {"v": 4, "d": 32}, "v"),
+    ("vpd,nd->nvp", "v", {"v": 4}, "u"),              # two labels for the token
+    ("vpd,nd->nvp", "vp", {"v": 4, "p": 1}, "u"),
+    ("vpd,nd->nv", "vp", {"v": 4, "p": 1}, "u"),      # a promoted label that neither side has
+    ("d,nd->n", "", {}, "u"),                         # none
+])
+def test_lookup_refuses_plans_of_other_tables(tre, einsum, upper, tiles, operand):
+    """A table's key is the token alone: what else a plan promotes, or keeps,
+    would give pieces of rows, or rows in another order."""
+    import torch
+
+    p = tre.Plan(einsum, upper, {"v": 8, "d": 64, "n": 3, "p": 1 if "nvp" not in einsum else 2}, tiles, "mxfp4")
+    o = "uv".index(operand)
+    t = torch.zeros((2, p.tile_bytes[o]), dtype=torch.uint8)
+    ids = torch.zeros(3, dtype=torch.int64)
+    refused(tre, "TRE_E_SHAPE", tre.lookup, t, ids, plan=p, operand=operand)
+
+
+@pytest.mark.parametrize("einsum,upper,tiles,operand", [
+    ("vd,nd->nv", "v", {"v": 4}, "u"), ("vd,nd->nv", "", {}, "u"), ("nd,dv->nv", "v", {"v": 2}, "v"),
+    ("vd,nd->nv", "vn", {"v": 4, "n": 1}, "u"), ("vdc,ncd->nv", "v", {"v": 4}, "u"),
+])
+def test_lookup_takes_plans_of_tables(tre, einsum, upper, tiles, operand):
+    """Plans that a lookup takes get as far as the tensors' place."""
+    import torch
+
+    p = tre.Plan(einsum, upper, {"v": 8, "d": 64, "n": 3, "c": 2}, tiles, "mxfp4")
+    t = torch.zeros((2, p.tile_bytes["uv".index(operand)]), dtype=torch.uint8)
+    refused(tre, "TRE_E_ARG", tre.lookup, t, torch.zeros(3, dtype=torch.int64), plan=p, operand=operand)
