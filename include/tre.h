@@ -155,6 +155,8 @@ typedef struct {
     float total_ms;
     int32_t deferred;         /* in */
     int32_t pending;          /* out: events recorded, not yet read */
+    int32_t contract_block;   /* out (contract_path 5): rows << 16 | columns of the outputs that a workgroup takes; 0 for
+                                 the other paths */
     int64_t n_units;
     int64_t n_split_segments;
     int64_t n_partials;       /* partial tiles written by units of split segments */

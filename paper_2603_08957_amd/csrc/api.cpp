@@ -394,6 +394,7 @@ tre_status contract_enqueue(tre_plan_t plan, const tre_join_result* jr, int64_t 
     tm.mark(s);
     if (timing) {
         timing->contract_path = pace ? 3 : R > 1 ? 4 : p.kclass == KC_VEC ? 1 : p.kclass == KC_MX ? 5 : p.fast ? 2 : 0;
+        timing->contract_block = p.kclass == KC_MX ? mx_block(p, n_pairs, unit_bound) : 0;
         if (deferred) {
             if (ke.launched) {
                 timing->events[0] = reinterpret_cast<void*>(ke.start);

@@ -1108,9 +1108,23 @@ bool mx_whole_keys(const Plan& p, int64_t n_pairs, int64_t n_w) {
     return t <= kMxTable;
 }
 
+namespace {
+
+MxShape launch_shape(const Plan& p, int64_t n_pairs, int64_t unit_bound) {
+    return mx_shape(p, double(unit_bound), std::ceil(double(n_pairs) / double(unit_bound) * mx_steps(p)));
+}
+
+}  // namespace
+
+int32_t mx_block(const Plan& p, int64_t n_pairs, int64_t unit_bound) {
+    const MxShape h = launch_shape(p, n_pairs, unit_bound);
+    const int rows = h.lds ? 64 * h.tm : 16 * h.tm, cols = h.lds ? 64 * h.tn : 16 * h.tn * h.waves_n;
+    return rows << 16 | cols;
+}
+
 hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_tiles, const void* v_tiles, float* w_tiles,
                      int64_t n_pairs, int64_t unit_bound, bool whole_keys, hipStream_t s) {
-    const MxShape h = mx_shape(p, double(unit_bound), std::ceil(double(n_pairs) / double(unit_bound) * mx_steps(p)));
+    const MxShape h = launch_shape(p, n_pairs, unit_bound);
     const int a = p.swap != h.turned ? 1 : 0, b = 1 - a;
     const int32_t* tb = reinterpret_cast<const int32_t*>(ws + L.tables);
     const int32_t* pairs[2] = {reinterpret_cast<const int32_t*>(ws + L.pu), reinterpret_cast<const int32_t*>(ws + L.pv)};

@@ -327,6 +327,8 @@ hipError_t launch_mx_dequantize(const Plan& p, int op, const void* mx_tiles, int
 // unit per key takes the join's segments in place of a unit table
 int64_t mx_unit_pairs(const Plan& p, int64_t n_pairs, int64_t n_w);
 bool mx_whole_keys(const Plan& p, int64_t n_pairs, int64_t n_w);
+// tre_timing.contract_block of launch_mx
+int32_t mx_block(const Plan& p, int64_t n_pairs, int64_t unit_bound);
 hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_tiles, const void* v_tiles, float* w_tiles,
                      int64_t n_pairs, int64_t unit_bound, bool whole_keys, hipStream_t s);
 

@@ -69,7 +69,7 @@ class JoinResult(ctypes.Structure):
 class Timing(ctypes.Structure):
     _fields_ = [("join_ms", ctypes.c_float), ("units_ms", ctypes.c_float), ("contract_ms", ctypes.c_float),
                 ("reduce_ms", ctypes.c_float), ("total_ms", ctypes.c_float), ("deferred", ctypes.c_int32),
-                ("pending", ctypes.c_int32), ("n_units", ctypes.c_int64), ("n_split_segments", ctypes.c_int64),
+                ("pending", ctypes.c_int32), ("contract_block", ctypes.c_int32), ("n_units", ctypes.c_int64), ("n_split_segments", ctypes.c_int64),
                 ("n_partials", ctypes.c_int64), ("events", ctypes.c_void_p * 4), ("contract_path", ctypes.c_int32),
                 ("join_path", ctypes.c_int32)]
 
@@ -86,6 +86,7 @@ class Timing(ctypes.Structure):
         d = {k: getattr(self, k) for k, _ in self._fields_ if k not in ("events", "deferred", "pending")}
         d["contract_path"] = self.PATHS.get(self.contract_path, self.contract_path)
         d["join_path"] = self.JOIN_PATHS.get(self.join_path, self.join_path)
+        d["contract_block"] = (self.contract_block >> 16, self.contract_block & 0xffff)
         return d
 
 
