@@ -364,7 +364,11 @@ tre_status contract_enqueue(tre_plan_t plan, const tre_join_result* jr, int64_t 
     }
     if (e != hipSuccess) return dev_fail(e, "units");
     tm.mark(s);
-    const int64_t unit_bound = R > 1 ? int64_t(R) * n_w : whole_keys ? n_w : n_w + n_pairs / p_unit + 1;
+    // (4-bit tiles take the block of outputs and the grid from it: of whole keys
+    // there are n_w units, no more)
+    const int64_t unit_bound = R > 1                                      ? int64_t(R) * n_w
+                               : p.kclass == KC_MX && p_unit >= n_pairs ? n_w
+                                                                        : n_w + n_pairs / p_unit + 1;
     if (pace) {
         // one unit per key; every workgroup of the grid is resident at once
         const int64_t n_wg = std::min(n_w, slots);

@@ -149,7 +149,7 @@ def test_batches(m, n, a, b, groups, want, w_bf16):
 
 
 SPARSE = [  # rows and columns of a tile (columns and rows in `across`), keys, pairs of a key on average, longest unit (0: whole keys), block
-    (66, 193, 395, 9, 0, (128, 256)), (131, 65, 259, 7, 0, (128, 128)), (65, 65, 388, 12, 0, (128, 64)),
+    (66, 193, 395, 9, 0, (128, 256)), (66, 193, 2560, 12, 0, (128, 256)), (131, 65, 259, 7, 0, (128, 128)), (65, 65, 388, 12, 0, (128, 64)),
     (33, 200, 386, 7, 0, (64, 256)), (40, 40, 30, 3, 0, (64, 64)),
     (65, 194, 161, 12, 7, (128, 256)), (66, 68, 192, 12, 7, (128, 128)), (66, 65, 124, 12, 5, (128, 64)),
     (33, 198, 120, 12, 5, (64, 256)), (40, 40, 30, 12, 2, (64, 64)),
@@ -191,3 +191,24 @@ def test_sparse_rows(m, n, keys, avg, unit, want, form):
     terms = torch.tensor(counts, device="cuda").double().mul_(32 * mx.row_blocks(k) + 2).view(keys, 1)
     order = lambda z: (z.transpose(1, 2) if form == "across" else z).reshape(keys, -1)  # noqa: E731
     near(wt, order(ref), order(mag), terms, w_bf16)
+
+
+@pytest.mark.parametrize("upper", ["", "n"])
+@pytest.mark.parametrize("m,n,k,want", [(2048, 2048, 8192, (128, 64)), (1500, 1700, 900, (64, 64)), (4000, 3900, 260, (128, 64)),
+                                        (2900, 3000, 700, (128, 128)), (3000, 5000, 1000, (128, 256))])
+def test_one_product(m, n, k, want, upper):
+    """A product of two whole matrices is one unit, and of two tiles against one
+    two: the block follows that count."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    g = torch.Generator(device="cuda").manual_seed(m + n)
+    parts = 2 if upper else 1
+    plan = tre.Plan("nd,vd->nv", upper, {"n": m, "v": n, "d": k}, {"n": m // parts}, "mxfp4")
+    uq, ud = values(plan, parts, (m // parts, k), "u", g)
+    vq, vd = values(plan, 1, (n, k), "v", g)
+    _, wt, tm = call(plan, range_keys(2) if upper else None, uq, None, vq, parts, parts)
+    assert tm.n_units == parts and block(tm) == want
+    x, y = ud.view(m, k), vd.view(n, k)
+    near(wt.view(m, n), x @ y.T, x.abs() @ y.abs().T, 32 * mx.row_blocks(k) + 2, False)
