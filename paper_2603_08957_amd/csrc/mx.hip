@@ -1167,8 +1167,8 @@ hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_til
     if (h.lds)
         return h.tm == 2 ? run_lds_n<2>(h.tn, g, grid, s) : run_lds_n<1>(h.tn, g, grid, s);
     const bool few = p.mx_blocks < 4;
-    if (h.tm == 2)
-        return h.tn == 2 ? run_mx<2, 2, 4>(few, g, grid, s) : run_mx<2, 1, 4>(few, g, grid, s);
+    // (of two rows of tiles there are two columns too: the longer side is N)
+    if (h.tm == 2) return run_mx<2, 2, 4>(few, g, grid, s);
     return h.tn == 2 ? run_mx<1, 2, 4>(few, g, grid, s) : run_mx<1, 1, 4>(few, g, grid, s);
 }
 
