@@ -91,7 +91,7 @@ __device__ inline uint32_t codes8(const float* v, int sb) {
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxTiles g, const T* __restrict__ src, uint8_t* __restrict__ dst) {
-    const int64_t b = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    const int64_t b = block_index() * kThreads + threadIdx.x;
     const int64_t per = g.rows * g.blocks;
     if (b >= g.n * per) return;
     const int64_t t = b / per, x = b - t * per, r = x / g.blocks, k0 = (x - r * g.blocks) * kMxBlock;
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxTiles g, const T* __
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_mx_dequantize(MxTiles g, const uint8_t* __restrict__ src, T* __restrict__ dst) {
-    const int64_t b = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    const int64_t b = block_index() * kThreads + threadIdx.x;
     const int64_t per = g.rows * g.blocks;
     if (b >= g.n * per) return;
     const int64_t t = b / per, x = b - t * per, r = x / g.blocks, k0 = (x - r * g.blocks) * kMxBlock;
@@ -250,7 +250,7 @@ __device__ inline RunPos run_pos(const MxTiles& g, int64_t t0, uint32_t r0, uint
     return p;
 }
 __device__ inline void run_start(const MxTiles& g, int64_t& t0, uint32_t& r0, uint32_t& e0) {
-    const int64_t b = int64_t(blockIdx.x), rows = b / g.line.d;  // (strips of a row vary first)
+    const int64_t b = block_index(), rows = b / g.line.d;  // (strips of a row vary first)
     e0 = uint32_t(b - rows * g.line.d) << g.lanes;
     const int64_t row = rows * (int64_t(kRun * kWaves) << (6 - g.lanes));
     t0 = row / g.tile.d;
@@ -356,7 +356,7 @@ struct ColPos {
 template <int R>
 __device__ inline ColPos col_pos(const MxTiles& g) {
     const int w = threadIdx.x >> 6, sets = kWaves / g.group;  // wavefronts of different lines
-    const int64_t x0 = int64_t(blockIdx.x) * (64 * sets), t0 = x0 / g.tile.d;
+    const int64_t x0 = block_index() * (64 * sets), t0 = x0 / g.tile.d;
     const uint32_t x = uint32_t(x0 - t0 * g.tile.d) + (w / g.group) * 64 + (threadIdx.x & 63), dt = g.tile.of(x), y = x - dt * g.tile.d;
     const uint32_t group = g.line.of(y);
     ColPos p;
@@ -585,10 +585,10 @@ __device__ inline int32_t pair_index(const int32_t* list, int64_t i) {
 template <int TM, int TN, int U, bool SHORT>
 __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
     __shared__ f32x4 sums[kWaves][TM * TN][64];
-    const int64_t unit = blockIdx.x / g.wg_blocks;
+    const uint32_t wg = uint32_t(block_index()), unit = wg / uint32_t(g.wg_blocks);
     Unit u;
     if (!mx_unit(g, unit, u)) return;
-    int x = int(blockIdx.x - unit * g.wg_blocks);
+    int x = int(wg - unit * g.wg_blocks);
     const int nb = x % g.n_blocks;
     x /= g.n_blocks;
     const int mb = x % g.m_blocks, b = x / g.m_blocks;
@@ -744,10 +744,10 @@ template <int TM, int TN>
 __global__ __launch_bounds__(kThreads, (mx_waves<TM, TN>())) void k_mx_lds(MxArgs g) {
     extern __shared__ __align__(16) char lds[];
     constexpr int BM = 64 * TM, BN = 64 * TN, ROWS = BM + BN, kStage = mx_stage_bytes<TM, TN>();
-    const int64_t unit = blockIdx.x / g.wg_blocks;
+    const uint32_t wg = uint32_t(block_index()), unit = wg / uint32_t(g.wg_blocks);
     Unit u;
     if (!mx_unit(g, unit, u)) return;
-    int x = int(blockIdx.x - unit * g.wg_blocks);
+    int x = int(wg - unit * g.wg_blocks);
     const int nb = x % g.n_blocks;
     x /= g.n_blocks;
     const int mb = x % g.m_blocks, b = x / g.m_blocks;
@@ -995,14 +995,11 @@ MxWay mx_way(const MxTiles& g) {
     return MX_ANY;
 }
 
-// Workgroups for `items` of `per` to a workgroup, 0 if they are too many.
-unsigned mx_grid(int64_t items, int64_t per) {
-    const int64_t b = (items + per - 1) / per;
-    return b > int64_t(0x7fffffff) ? 0u : unsigned(b);
-}
+// Workgroups for `items` of `per` to a workgroup.
+dim3 mx_grid(int64_t items, int64_t per) { return grid_of((items + per - 1) / per); }
 
 // The launch along rows of `eights` eights each.
-unsigned rows_grid(MxTiles& g, int64_t eights) {
+dim3 rows_grid(MxTiles& g, int64_t eights) {
     g.lanes = 0;
     while (g.lanes < 6 && (1 << g.lanes) < eights) g.lanes++;
     // (a block's four eights are a quad of lanes)
@@ -1015,7 +1012,7 @@ unsigned rows_grid(MxTiles& g, int64_t eights) {
 
 // The launch across rows.
 template <typename T>
-unsigned cols_grid(MxTiles& g) {
+dim3 cols_grid(MxTiles& g) {
     constexpr int R = sizeof(T) == 2 ? 2 : 1;
     const int64_t lines = (g.rows + R - 1) / R, groups = g.blocks / g.group;
     g.line = Divisor(lines);
@@ -1026,10 +1023,9 @@ unsigned cols_grid(MxTiles& g) {
 template <typename T>
 hipError_t quantize(MxTiles g, const T* src, uint8_t* dst, hipStream_t s) {
     const MxWay way = mx_way(g);
-    const unsigned grid = way == MX_ROWS   ? rows_grid(g, g.blocks * 4)
+    const dim3 grid = way == MX_ROWS   ? rows_grid(g, g.blocks * 4)
                           : way == MX_COLS ? cols_grid<T>(g)
                                            : mx_grid(g.n * g.rows * g.blocks, kThreads);
-    if (!grid) return hipErrorInvalidConfiguration;
     if (way == MX_COLS) k_mx_quantize_cols<<<grid, kThreads, 0, s>>>(g, src, dst);
     else if (way == MX_ANY) k_mx_quantize<<<grid, kThreads, 0, s>>>(g, src, dst);
     else if (g.K == g.blocks * kMxBlock) k_mx_quantize_rows<T, RUN_FULL><<<grid, kThreads, 0, s>>>(g, src, dst);
@@ -1041,10 +1037,9 @@ hipError_t quantize(MxTiles g, const T* src, uint8_t* dst, hipStream_t s) {
 template <typename T>
 hipError_t dequantize(MxTiles g, const uint8_t* src, T* dst, hipStream_t s) {
     const MxWay way = mx_way(g);
-    const unsigned grid = way == MX_ROWS   ? rows_grid(g, (g.K + 7) / 8)
+    const dim3 grid = way == MX_ROWS   ? rows_grid(g, (g.K + 7) / 8)
                           : way == MX_COLS ? cols_grid<T>(g)
                                            : mx_grid(g.n * g.rows * g.blocks, kThreads);
-    if (!grid) return hipErrorInvalidConfiguration;
     if (way == MX_COLS) k_mx_dequantize_cols<<<grid, kThreads, 0, s>>>(g, src, dst);
     else if (way == MX_ANY) k_mx_dequantize<<<grid, kThreads, 0, s>>>(g, src, dst);
     else if (g.K % 8 == 0) k_mx_dequantize_rows<T, false><<<grid, kThreads, 0, s>>>(g, src, dst);
@@ -1163,7 +1158,7 @@ hipError_t launch_mx(const Plan& p, const Layout& L, char* ws, const void* u_til
     g.hdr = reinterpret_cast<const WsHeader*>(ws + L.hdr);
     g.W = w_tiles;
     g.partials = reinterpret_cast<float*>(ws + L.partials);
-    const dim3 grid{unsigned(wg * unit_bound)};
+    const dim3 grid = grid_of(wg * unit_bound);
     if (h.lds)
         return h.tm == 2 ? run_lds_n<2>(h.tn, g, grid, s) : run_lds_n<1>(h.tn, g, grid, s);
     const bool few = p.mx_blocks < 4;

@@ -170,13 +170,13 @@ __device__ inline void lookup_load(const LookupArgs& g, int64_t id, int64_t e, f
 template <typename TI, typename TO, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_lookup(LookupArgs g) {
     constexpr int E = lane_elems<TI, TO>();
-    const int64_t x = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    const int64_t x = block_index() * kThreads + threadIdx.x;
     const int lane = int(x & ((1 << g.strip.shift) - 1));
     int64_t t[kStrips], e[kStrips];
     float v[kStrips][E], scale[kStrips];  // 0 for no token: its row is zero under any scale
     if constexpr (WIDE) {
         // (a wavefront's row is the same for its lanes)
-        const int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t w = block_index() * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int64_t row = w / g.groups, s0 = (w - row * g.groups) * kStrips;
         if (row >= g.n_ids) return;
         const int64_t id = token(g.ids, g.id_bytes, row);
@@ -382,7 +382,7 @@ __device__ inline void zero_rows(const GradArgs& g, int64_t w) {
 template <typename TI, typename TO, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_grad_sum(GradArgs g) {
     constexpr int E = lane_elems<TI, TO>();
-    int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t w = block_index() * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (w < g.zero_waves) {
         zero_rows<TO>(g, w);
         return;
@@ -472,7 +472,7 @@ struct JoinArgs {
 
 template <typename TO>
 __global__ __launch_bounds__(kThreads) void k_grad_join(GradArgs g, JoinArgs a) {
-    const int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t w = block_index() * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t group = w / a.slices;
     if (group >= a.groups) return;
     const int lane = threadIdx.x & 63;
@@ -564,7 +564,7 @@ GradLayout grad_layout(int64_t n, int64_t elems) {
     return L;
 }
 
-unsigned wave_grid(int64_t waves) { return unsigned((waves + kWaves - 1) / kWaves); }
+dim3 wave_grid(int64_t waves) { return grid_of((waves + kWaves - 1) / kWaves); }
 
 template <typename TI, typename TO>
 hipError_t lookup(LookupArgs g, hipStream_t s) {
@@ -573,7 +573,6 @@ hipError_t lookup(LookupArgs g, hipStream_t s) {
     if (g.elems > 64 * E) {
         g.groups = (g.strip.slices + kStrips - 1) / kStrips;
         const int64_t waves = g.n_ids * g.groups;
-        if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
         k_lookup<TI, TO, true><<<wave_grid(waves), kThreads, 0, s>>>(g);
     } else {
         const int64_t threads = ((g.n_ids + kStrips - 1) / kStrips) << g.strip.shift;
@@ -592,8 +591,7 @@ hipError_t grad_sum(GradArgs g, hipStream_t s) {
     g.zero_waves = g.accumulate ? 0 : (g.n_rows + g.zero_rows - 1) / g.zero_rows * g.zero_slices;
     const int64_t waves = g.zero_waves + ((g.chunks * g.strip.slices << g.strip.shift) + 63) / 64;
     if (waves == 0) return hipSuccess;
-    if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
-    const unsigned grid = wave_grid(waves);
+    const dim3 grid = wave_grid(waves);
     if (g.strip.shift == 6) k_grad_sum<TI, TO, true><<<grid, kThreads, 0, s>>>(g);
     else k_grad_sum<TI, TO, false><<<grid, kThreads, 0, s>>>(g);
     return hipGetLastError();
@@ -681,7 +679,6 @@ hipError_t launch_lookup_grad(const void* grad, int grad_dtype, const void* ids,
         float* out = const_cast<float*>(a.in) + 2 * a.chunks * elems;
         a.out = out;
         const int64_t waves = a.groups * a.slices;
-        if (waves / kWaves >= int64_t(0x7fffffff)) return hipErrorInvalidConfiguration;
         if (half) k_grad_join<uint16_t><<<wave_grid(waves), kThreads, 0, s>>>(g, a);
         else k_grad_join<float><<<wave_grid(waves), kThreads, 0, s>>>(g, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;

@@ -382,6 +382,17 @@ struct same_type {
     using type = T;
 };
 
+// A launch of any number of workgroups of up to 256 threads.  One dimension
+// holds fewer than 2^32 threads; beyond, workgroups are missing, without an
+// error.  Kernels launched so take block_index() for their workgroup's number,
+// which may pass `blocks` by less than the grid's height.
+constexpr int64_t kMaxGridWidth = int64_t(1) << 23;
+inline dim3 grid_of(int64_t blocks) {
+    const int64_t y = (blocks + kMaxGridWidth - 1) / kMaxGridWidth;
+    return y <= 1 ? dim3{unsigned(blocks)} : dim3{unsigned((blocks + y - 1) / y), unsigned(y)};
+}
+__device__ inline int64_t block_index() { return int64_t(blockIdx.y) * gridDim.x + blockIdx.x; }
+
 // Launch `kernel` (<<<>>> semantics); with t_kernel_events set, through
 // hipExtLaunchKernel with its start / stop events.
 template <typename... KArgs>
