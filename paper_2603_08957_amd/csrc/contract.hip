@@ -998,6 +998,7 @@ hipError_t launch_contract(const Plan& p, const Layout& L, char* ws, const void*
 hipError_t launch_reduce(const Plan& p, const Layout& L, char* ws, float* w_tiles, int64_t split_bound,
                          hipStream_t s) {
     if (split_bound <= 0) return hipSuccess;
+    if (!grid_fits(split_bound, kThreads)) return hipErrorInvalidConfiguration;
     const unsigned gy = unsigned(std::min<int64_t>(reduce_blocks(p.tile_elems[2]), 65535));
     k_reduce<<<dim3(unsigned(split_bound), gy), kThreads, 0, s>>>(reduction(p, L, ws, w_tiles),
                                                                   reinterpret_cast<const WsHeader*>(ws + L.hdr));

@@ -393,11 +393,15 @@ inline dim3 grid_of(int64_t blocks) {
 }
 __device__ inline int64_t block_index() { return int64_t(blockIdx.y) * gridDim.x + blockIdx.x; }
 
+// Whether one dimension of a launch holds `blocks` workgroups of `threads`.
+inline bool grid_fits(int64_t blocks, int64_t threads) { return blocks * threads <= int64_t(0xffffffffll); }
+
 // Launch `kernel` (<<<>>> semantics); with t_kernel_events set, through
 // hipExtLaunchKernel with its start / stop events.
 template <typename... KArgs>
 inline hipError_t launch_k(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t shmem, hipStream_t s,
                            typename same_type<KArgs>::type... args) {
+    if (!grid_fits(grid.x, block.x)) return hipErrorInvalidConfiguration;
     KernelEvents* ke = t_kernel_events;
     if (!ke) {
         kernel<<<grid, block, shmem, s>>>(args...);

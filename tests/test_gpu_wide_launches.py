@@ -1,6 +1,7 @@
-"""Calls of the 4-bit tile and row entry points with more than 2^32 threads,
-which one dimension of a launch does not hold: results past that point are
-those of the same rows in a small call."""
+"""Calls that take more than 2^32 threads, which one dimension of a launch does
+not hold.  Those of the 4-bit tile and row entry points give, past that point,
+the results of the same rows in a small call; contractions of the other types,
+which have one dimension, say that they cannot."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +66,23 @@ def test_quantize_and_back(labels, k, dtype):
     tre.mx_dequantize(plan, "u", q, out=x)
     for at in range(0, n, step):
         assert torch.equal(x[at:at + step], tre.mx_dequantize(plan, "u", q[at:at + step], dtype=x.dtype)), at
+
+
+def test_contractions_of_other_types_refuse():
+    """Above 2^24 keys of a workgroup each."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    d = 130
+    v = torch.randn((1, d), device="cuda")
+    for keys in ((1 << 24) - 10, 1 << 24):
+        plan = tre.Plan("id,d->id", "i", {"i": keys, "d": d}, {"i": 1})
+        uk = torch.arange(keys, dtype=torch.int32, device="cuda").reshape(keys, 1)
+        u = torch.ones((keys, d), device="cuda")
+        if keys < 1 << 24:
+            assert torch.equal(tre.einsum(plan, uk, u, None, v).w_tiles, v.expand(keys, d))
+            continue
+        with pytest.raises(tre.TreError) as e:
+            tre.einsum(plan, uk, u, None, v)
+        assert e.value.status == "TRE_E_DEVICE"
