@@ -458,3 +458,41 @@ def test_buffers_of_a_callers_stream():
             torch.empty_like(want).view(torch.uint8).fill_(0x55)
         torch.cuda.synchronize()
         assert torch.equal(copy, want), name
+
+
+@pytest.mark.parametrize("odt", ["f32", "bf16"])
+@pytest.mark.parametrize("gdt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,d,kind", [
+    (16384, 40, 10, "one"), (16385, 40, 10, "one"), (16385, 40, 130, "zipf"), (33000, 5, 3, "zipf"), (140000, 3, 2, "one"),
+    (140000, 3, 257, "zipf"), (300000, 9, 3, "zipf"), (300000, 9, 5, "padded"), (600000, 4, 1, "one"),
+])
+def test_long_runs_exactly(n, vocab, d, kind, gdt, odt):
+    """Runs of one token over many chunks and their groups, of whole numbers whose
+    sums fp32 holds exactly in any order (up to 4 n < 2^24): no row of a run may
+    be missing or counted twice.  A bf16 result is the sum rounded once."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    assert 4 * n < 1 << 24
+    T = types()
+    rng = np.random.default_rng(n + d)
+    ids = tokens(rng, n, vocab, kind)
+    whole = rng.integers(-2, 3, (n, d))
+    total = np.zeros((vocab, d), np.int64)
+    np.add.at(total, ids[ids >= 0], whole[ids >= 0])
+    grad = torch.from_numpy(whole.astype(np.float32)).to(T[gdt]).cuda()
+    want = torch.from_numpy(2.0 * total).float().to(T[odt])
+    dev = torch.from_numpy(ids).cuda()
+    got = tre.lookup_grad(grad, dev, vocab, scale=2.0, dtype=T[odt])
+    assert torch.equal(got.cpu(), want)
+    # added to whole numbers that are there
+    base = torch.from_numpy(rng.integers(-2, 3, (vocab, d)).astype(np.float32)).to(T[odt])
+    out = base.cuda()
+    tre.lookup_grad(grad, dev, vocab, scale=2.0, out=out, accumulate=True)
+    there = torch.from_numpy((ids[ids >= 0][None, :] == np.arange(vocab)[:, None]).any(1))[:, None]
+    assert torch.equal(out.cpu(), torch.where(there, (base.double() + torch.from_numpy(2.0 * total)).float().to(T[odt]), base))
+    # all ones: the number of a row's tokens
+    ones = torch.ones((n, d), dtype=T[gdt], device="cuda")
+    count = torch.bincount(torch.from_numpy(ids[ids >= 0]), minlength=vocab).float()[:, None].expand(vocab, d)
+    assert torch.equal(tre.lookup_grad(ones, dev, vocab).cpu(), count)
