@@ -461,3 +461,37 @@ def test_timing_of_whole_keys(small_join):
         tm = tre.Timing()
         assert tre.execute(plan, keys, u, bk, v, wk, wt, ws, timing=tm) == (nb, nb * nb)
         assert (tm.n_units, tm.n_split_segments, tm.n_partials) == (nb, 0, 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("einsum,op", FORMS)
+@pytest.mark.parametrize("rows,k", [(16, 1), (33, 1), (1, 40), (2, 3), (3, 2), (2, 64), (300, 4)])
+def test_quantize_thin_tiles(einsum, op, rows, k, dtype):
+    """One value to a row, one or two rows, rows longer than their contracted index."""
+    test_quantize_and_back(einsum, op, rows, k, dtype)
+
+
+def test_count_of_tiles_on_the_device():
+    """U's tuple count known on the device alone: tiles past it are neither read
+    as operands nor written."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    most, t, k, n = 40, 70, 200, 90
+    plan = tre.Plan("vd,nd->nv", "v", {"v": most * t, "n": n, "d": k}, {"v": t}, "mxfp4")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    u = tre.mx_quantize(plan, "u", torch.randn((most, t * k), generator=g, device="cuda"))
+    v = tre.mx_quantize(plan, "v", torch.randn((1, n * k), generator=g, device="cuda"))
+    uk = torch.arange(most, dtype=torch.int32, device="cuda").reshape(most, 1)
+    want = tre.einsum(plan, uk, u, None, v).w_tiles
+    ws = tre.alloc_workspace(plan.workspace_bytes(most, 1, most))
+    counts = torch.zeros(4, dtype=torch.int64, device="cuda")
+    for here in (0, 1, 17, most):
+        wk = torch.full((most, 1), -9, dtype=torch.int32, device="cuda")
+        wt = torch.full((most, n * t), -3.0, device="cuda")
+        tre.execute_async(plan, uk, u, None, v, wk, wt, ws, counts, n_u=most,
+                          n_u_dev=torch.tensor([here], dtype=torch.int64, device="cuda"))
+        assert counts.tolist() == [here, here, 0, 0]
+        assert torch.equal(wt[:here], want[:here]) and torch.equal(wk[:here], uk[:here])
+        assert torch.all(wt[here:] == -3.0) and torch.all(wk[here:] == -9)

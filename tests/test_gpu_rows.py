@@ -496,3 +496,55 @@ def test_long_runs_exactly(n, vocab, d, kind, gdt, odt):
     ones = torch.ones((n, d), dtype=T[gdt], device="cuda")
     count = torch.bincount(torch.from_numpy(ids[ids >= 0]), minlength=vocab).float()[:, None].expand(vocab, d)
     assert torch.equal(tre.lookup_grad(ones, dev, vocab).cpu(), count)
+
+
+@pytest.mark.parametrize("n", [8192, 9000, 140000])  # ranked; sorted in small tiles and in large ones
+def test_many_ids_out_of_range(n):
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    vocab, d = 300, 5
+    g = torch.Generator().manual_seed(n)
+    ids = torch.randint(-2, vocab, (n,), generator=g)
+    ids[::97] = vocab
+    ids[5::89] = 2 ** 40 + 3  # its low half is a row's number
+    ids[7::83] = -2 ** 40 + 3
+    grad = torch.randint(-2, 3, (n, d), generator=g).float()
+    ok = (ids >= 0) & (ids < vocab)
+    want = torch.zeros((vocab, d)).index_add_(0, ids[ok], grad[ok])
+    status = torch.zeros(1, dtype=torch.int64, device="cuda")
+    assert torch.equal(tre.lookup_grad(grad.cuda(), ids.cuda(), vocab, status=status).cpu(), want)
+    assert status.item() == tre.tre.STATUS_CODE["TRE_E_KEYRANGE"]
+    table = torch.randn((vocab, d), generator=g)
+    status.zero_()
+    rows = tre.lookup(table.cuda(), ids.cuda(), status=status).cpu()
+    assert status.item() == tre.tre.STATUS_CODE["TRE_E_KEYRANGE"]
+    assert torch.equal(rows, torch.where(ok[:, None], table[ids.clamp(0, vocab - 1)], torch.zeros(())))
+
+
+@pytest.mark.parametrize("n", [7, 60, 5000, 20000])
+@pytest.mark.parametrize("gdt", ["f32", "bf16"])
+def test_values_of_no_token_do_not_count(n, gdt):
+    """NaN and infinities in the gradient's rows of no token, and in table rows
+    that no token names, reach nothing."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    vocab, d = 50, 37
+    g = torch.Generator().manual_seed(n)
+    ids = torch.randint(0, vocab - 1, (n,), generator=g)
+    ids[::3] = -1
+    ids[1::7] = vocab + 4
+    grad = torch.randint(-2, 3, (n, d), generator=g).float()
+    ok = (ids >= 0) & (ids < vocab)
+    want = torch.zeros((vocab, d)).index_add_(0, ids[ok], grad[ok])
+    grad[~ok] = float("nan")
+    grad[0] = float("inf")
+    assert torch.equal(tre.lookup_grad(grad.to(types()[gdt]).cuda(), ids.cuda(), vocab).cpu(), want)
+    table = torch.ones((vocab, d)) * 2
+    table[vocab - 1] = float("nan")
+    table = table.to(types()[gdt]).cuda()
+    rows = tre.lookup(table, ids.cuda(), dtype=torch.float32).cpu()
+    assert torch.equal(rows, torch.where(ok, 2.0, 0.0)[:, None].expand(n, d))
