@@ -252,6 +252,8 @@ tre_status tre_join_keys(tre_plan_t plan, const tre_join_result *join, int32_t *
  *             plan was made with w_bf16.
  *   pairs_out : device [pair_cap x 2] int32 (u, v) or NULL.
  * TRE_E_CAPACITY if w_cap < n_w or (pairs_out and pair_cap < n_pairs).
+ * TRE_E_DEVICE if the tiles are fp32 or bf16 and the keys, each with its blocks
+ * of outputs, take 2^24 workgroups or more.
  * Asynchronous on the stream unless timing is non-NULL and not deferred. */
 tre_status tre_contract(tre_plan_t plan, const tre_join_result *jr, const void *u_tiles, const void *v_tiles,
                         int32_t *w_keys, int64_t w_cap, void *w_tiles, int32_t *pairs_out, int64_t pair_cap,

@@ -87,7 +87,9 @@ __device__ inline uint32_t codes8(const float* v, int sb) {
     return sb == kMxNanScale ? 0u : q;
 }
 
-// ---- any layout: a thread per block
+// ---- any layout: a thread per block, its values found one by one (134 M bf16
+// values whose contracted labels are not side by side 380 us to quantise and 650
+// to read back; the kernels below take 67 and 53)
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxTiles g, const T* __restrict__ src, uint8_t* __restrict__ dst) {
@@ -581,7 +583,8 @@ __device__ inline int32_t pair_index(const int32_t* list, int64_t i) {
 // batches of four in two tiles of 16 rows; of eight, or in one tile, 17 to 19.
 //
 // SHORT: rows of one or two blocks; a step is then the rows of four or two
-// pairs, each lane's its own.
+// pairs, each lane's its own.  (5% dense blocks of 64 in 8,192 x 8,192 times 512
+// columns: 14 us; of 32 in 4,096 x 4,096: 6.7.)
 template <int TM, int TN, int U, bool SHORT>
 __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
     __shared__ f32x4 sums[kWaves][TM * TN][64];
@@ -722,8 +725,9 @@ __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
 //   all reads of a stage on their way before its first product     377
 //   four sums to a store                                           340
 //   no unit table                                                  325
-// The kernel is then at 285 to 300 us, 3.7 to 3.85 PFLOP/s (a stage 0.99 us for
-// two workgroups, their starts and ends 12 us each).  With no copies in the loop
+// The kernel is then at 299 to 308 us, 3.57 to 3.68 PFLOP/s, on two cards (348
+// on one whose clock had come down; a stage 0.99 us for two workgroups, their
+// starts and ends 12 us each).  With no copies in the loop
 // 16 x 16 tiles took 240; registers alone do 6.6 PFLOP/s of random codes (power;
 // 8.7 of zeros), so the wavefronts' waits for LDS and each other bound it.  A
 // raised priority around the products, the copies issued after the reads, and
@@ -897,7 +901,9 @@ struct MxShape {
 // The blocks that k_mx_lds is built for and what they take, in microseconds:
 // `step` for a stage with every place on the chip taken, and `ends` for a
 // workgroup's start and stores, from 8192 x 8192 outputs of 16 and 64 stages.
-// (64 x 128 took 1.24 a stage, more than the same turned: not built.)
+// (64 x 128 took 1.24 a stage, more than the same turned: not built.)  Of short
+// keys that is too little: 128 keys of 128 x 1024 outputs and seven stages on
+// average are 19 us by it, and 26 to 28 measured.
 struct MxKind {
     int tm, tn, slots;
     double step, ends;
@@ -905,7 +911,9 @@ struct MxKind {
 constexpr MxKind kMxKinds[] = {
     {2, 4, 512, 0.99, 11.8}, {2, 2, 768, 0.77, 8.9}, {2, 1, 1024, 0.73, 4.9}, {1, 4, 512, 0.67, 7.5}, {1, 1, 1536, 0.67, 3.3},
 };
-// A stage is no shorter than this, however few workgroups there are.
+// A stage is taken to be no shorter than kMxStep, however few workgroups there
+// are (of 64 x 64 outputs it measures 0.25 us with up to 64 of them on the chip,
+// 0.34 with 512).
 constexpr double kMxStep = 0.4, kMxAlone = 60;
 
 double mx_rounds(double groups, int slots, double steps, double step, double ends) {

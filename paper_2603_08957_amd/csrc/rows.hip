@@ -335,7 +335,8 @@ __device__ inline void put_row(const GradArgs& g, int64_t row, int64_t e, const 
 // Zeroes elements begin to end of the output: whole 128-byte lines but for the
 // first and last.  (A strip of each row for itself leaves a broken line at every
 // strip's end where rows are not of whole lines: 46,492 rows of 998 fp32 values
-// took 56 us, of 1,001 bf16 values 33.)
+// took 56 us, of 1,001 bf16 values 33; with one token's gradient they take 36 and
+// 19 now.)
 template <typename TO>
 __device__ inline void zero_span(TO* out, int64_t begin, int64_t end) {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
