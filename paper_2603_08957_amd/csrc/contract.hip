@@ -157,6 +157,15 @@ __global__ __launch_bounds__(kOrderBins) void k_order_units(Unit* __restrict__ u
 // into units of one length, where the workgroups that run together then read
 // the same range of U's tiles (a key's pairs are in U order) and share them in
 // L2 (320 keys cut in 7 over 8 MB of U tiles: 3.3 GB fetched in key order).
+// Keys that an asynchronous call contracts: the join's count, at most the bound
+// that grids and tables are sized for, and none after a key error.  Pairs of
+// keys out of order are not grouped, a key's segment may then end before it
+// begins or reach over those of others, and units cut from it would not fit the
+// table.
+__device__ inline int64_t contracted_keys(const WsHeader* hdr, int64_t bound) {
+    return (hdr->err_u | hdr->err_v) ? 0 : min(bound, hdr->n_w);
+}
+
 constexpr int kUnitsThreads = kOrderBins;
 constexpr int kUnitsPer = kOrderMax / kUnitsThreads;
 constexpr int64_t kUnitsTableMax = 16384;
@@ -176,7 +185,7 @@ __global__ __launch_bounds__(kUnitsThreads) void k_units_small(const int32_t* __
     __shared__ int32_t wsum[kUnitsThreads / 64];
     __shared__ int32_t key_uo[kOrderMax + 1], key_po[kOrderMax], key_a[kOrderMax + 1];
     const int t = threadIdx.x;
-    if (dev_nw) n_w = min(n_w, hdr->n_w);  // n_w is then a bound; the key count is the join's
+    if (dev_nw) n_w = contracted_keys(hdr, n_w);  // n_w is then a bound; the key count is the join's
     if (tables) {
         // the table shapes through LDS: read from the kernel arguments with
         // dynamic indices they would be one dependent scalar load each
@@ -850,7 +859,7 @@ hipError_t launch_tables(const Plan& p, int32_t* tables, hipStream_t s) {
 __global__ void k_key_units(const int32_t* __restrict__ seg_start, int64_t n_w, Unit* __restrict__ units,
                             WsHeader* hdr, int dev_nw) {
     const int64_t s = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
-    if (dev_nw) n_w = min(n_w, hdr->n_w);
+    if (dev_nw) n_w = contracted_keys(hdr, n_w);
     if (s > n_w) return;
     if (s == n_w) {
         hdr->n_units = int32_t(n_w);

@@ -509,10 +509,12 @@ struct MxArgs {
 };
 
 // (Keys out of order, which an asynchronous call reports in its counts, can
-// leave segments that end where they begin or before: no pair of theirs is
-// looked at.)
+// leave segments that end before they begin or reach over others: none of them
+// is a unit.)
 __device__ inline bool mx_unit(const MxArgs& g, int64_t unit, Unit& u) {
-    if (unit >= (g.seg_start ? g.hdr->n_w : g.hdr->n_units)) return false;
+    const int32_t err = g.hdr->err_u | g.hdr->err_v;
+    const int64_t n_w = g.hdr->n_w, n_units = g.hdr->n_units;
+    if (unit >= (g.seg_start ? err ? 0 : n_w : n_units)) return false;
     u = g.seg_start ? Unit{int32_t(unit), g.seg_start[unit], g.seg_start[unit + 1], -1} : g.units[unit];
     return u.p1 > u.p0;
 }
