@@ -87,6 +87,15 @@ __device__ inline uint32_t codes8(const float* v, int sb) {
     return sb == kMxNanScale ? 0u : q;
 }
 
+// Block b's scale byte of a tile, and after the last one the bytes that pad the
+// tile.
+__device__ inline void put_scale(const MxTiles& g, uint8_t* tile, uint32_t b, int sb) {
+    const int64_t blocks = g.rows * g.blocks;
+    tile[blocks * 16 + b] = uint8_t(sb);
+    if (b == uint32_t(blocks) - 1)
+        for (int64_t i = blocks * 17; i < g.bytes; i++) tile[i] = 0;
+}
+
 // ---- any layout: a thread per block, its values found one by one (134 M bf16
 // values whose contracted labels are not side by side 380 us to quantise and 650
 // to read back; the kernels below take 67 and 53)
@@ -112,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxTiles g, const T* __
     uint8_t* out = dst + t * g.bytes;
     const uint32_t at_block = mx_block_of(uint32_t(g.rows), g.group, uint32_t(r), uint32_t(x - r * g.blocks));
     *reinterpret_cast<uint4*>(out + int64_t(at_block) * 16) = make_uint4(q[0], q[1], q[2], q[3]);
-    out[per * 16 + at_block] = uint8_t(sb);
+    put_scale(g, out, at_block, sb);
 }
 
 template <typename T>
@@ -289,7 +298,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize_rows(MxTiles g, const 
         uint8_t* out = dst + p.t * g.bytes;
         const uint32_t b = mx_block_of(rows, g.group, p.r, p.e / 4);
         *reinterpret_cast<uint32_t*>(out + int64_t(b) * 16 + (p.e & 3) * 4) = v[i].codes(sb);
-        if ((p.e & 3) == 0) out[g.rows * g.blocks * 16 + b] = uint8_t(sb);
+        if ((p.e & 3) == 0) put_scale(g, out, b, sb);
     }
 }
 
@@ -387,7 +396,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize_cols(MxTiles g, const 
 #pragma unroll
     for (int i = 0; i < kMxBlock; i++) v[i] = i < left ? v[i] : 0u;
     uint8_t* out = dst + p.t * g.bytes;
-    const int64_t b0 = mx_block_of(uint32_t(g.rows), g.group, p.r, p.kb), scales = g.rows * g.blocks * 16;
+    const int64_t b0 = mx_block_of(uint32_t(g.rows), g.group, p.r, p.kb);
     if constexpr (R == 1) {
         uint32_t m = 0;
         float f[kMxBlock];
@@ -399,7 +408,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize_cols(MxTiles g, const 
         const int sb = scale_byte(m);
         *reinterpret_cast<uint4*>(out + b0 * 16) =
             make_uint4(codes8(f, sb), codes8(f + 8, sb), codes8(f + 16, sb), codes8(f + 24, sb));
-        out[scales + b0] = uint8_t(sb);
+        put_scale(g, out, uint32_t(b0), sb);
     } else {
         u16x2 m = {0, 0};
 #pragma unroll
@@ -417,7 +426,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize_cols(MxTiles g, const 
                 q[i] = e.codes(sb);
             }
             *reinterpret_cast<uint4*>(out + (b0 + h * g.group) * 16) = make_uint4(q[0], q[1], q[2], q[3]);
-            out[scales + b0 + h * g.group] = uint8_t(sb);
+            put_scale(g, out, uint32_t(b0 + h * g.group), sb);
         }
     }
 }

@@ -495,3 +495,24 @@ def test_count_of_tiles_on_the_device():
         assert counts.tolist() == [here, here, 0, 0]
         assert torch.equal(wt[:here], want[:here]) and torch.equal(wk[:here], uk[:here])
         assert torch.all(wt[here:] == -3.0) and torch.all(wk[here:] == -9)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("einsum", ["ik,jk->ij", "ki,jk->ij", "kil,jlk->ij"])
+@pytest.mark.parametrize("rows,k", [(1, 1), (3, 32), (5, 20), (7, 64), (3, 70), (9, 300), (16, 32)])
+def test_padding_of_tiles_is_written(einsum, dtype, rows, k):
+    """Every byte of a 4-bit tile follows from its values, the ones behind its last
+    scale too (zero)."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    sizes = {"i": rows, "k": k, "l": 2, "j": 3}
+    plan = tre.Plan(einsum, "", {c: sizes[c] for c in einsum if c.isalpha()}, {}, "mxfp4")
+    n, kk = 3, k * (2 if "l" in einsum else 1)
+    x = torch.randn((n, plan.tile_elems[0]), device="cuda").to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    a, b = (torch.full((n, plan.tile_bytes[0]), fill, dtype=torch.uint8, device="cuda") for fill in (0xA5, 0x3C))
+    tre.mx_quantize(plan, "u", x, out=a)
+    tre.mx_quantize(plan, "u", x, out=b)
+    assert torch.equal(a, b)
+    assert not bool(a[:, 17 * rows * mx.row_blocks(kk):].any())
