@@ -471,6 +471,14 @@ class _Here:
     def buffer(self, make, result=True):
         return _buffer(self.stream, self.device, make, result)
 
+    def uses(self, *tensors):
+        """The caller's tensors: given back while a caller's stream still has the
+        call queued, their memory stays theirs until it is done."""
+        if self.stream is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+
 
 def _operand(plan, operand, where):
     if plan.dtype != "mxfp4":
@@ -496,6 +504,7 @@ def mx_quantize(plan: Plan, operand: str, tiles, out=None, stream=None):
             out = here.buffer(lambda: torch.empty((n, plan.tile_bytes[o]), dtype=torch.uint8, device=tiles.device))
         else:
             _want(out, w, "out", (n, plan.tile_bytes[o]), torch.uint8, tiles.device)
+        here.uses(tiles, out)
         _check(lib().tre_mx_quantize(plan.handle, o, _ptr(tiles), dt, n, _ptr(out), here.ptr), "tre_mx_quantize")
     return out
 
@@ -517,6 +526,7 @@ def mx_dequantize(plan: Plan, operand: str, mx_tiles, dtype=None, out=None, stre
                                                   device=mx_tiles.device))
         else:
             _want(out, w, "out", (n, plan.tile_elems[o]), dtype, mx_tiles.device)
+        here.uses(mx_tiles, out)
         _check(lib().tre_mx_dequantize(plan.handle, o, _ptr(mx_tiles), n, _ptr(out), dt, here.ptr), "tre_mx_dequantize")
     return out
 
@@ -578,6 +588,7 @@ def lookup(table, ids, scale: float = 1.0, dtype=None, out=None, plan: Plan | No
             out = here.buffer(lambda: torch.empty(shape, dtype=dtype, device=table.device))
         else:
             _want(out, w, "out", shape, dtype, table.device)
+        here.uses(table, ids, out, status)
         _check(lib().tre_lookup(_ptr(table), tdt, n_rows, elems, tile_rows, _ptr(ids), ids.element_size(), ids.numel(),
                                 float(scale), _ptr(out), odt, _ptr(status), here.ptr), "tre_lookup")
     return out
@@ -618,6 +629,7 @@ def lookup_grad(grad, ids, n_rows: int, scale: float = 1.0, dtype=None, out=None
                              result=False)
         else:
             _want(ws, w, "ws", device=grad.device)
+        here.uses(grad, ids, out, status, ws)
         _check(lib().tre_lookup_grad(_ptr(grad), gdt, _ptr(ids), ids.element_size(), n, float(scale), _ptr(out), odt, n_rows,
                                      elems, int(accumulate), _ptr(status), _ptr(ws), ws.numel() * ws.element_size(),
                                      here.ptr), "tre_lookup_grad")

@@ -548,3 +548,36 @@ def test_values_of_no_token_do_not_count(n, gdt):
     table = table.to(types()[gdt]).cuda()
     rows = tre.lookup(table, ids.cuda(), dtype=torch.float32).cpu()
     assert torch.equal(rows, torch.where(ok, 2.0, 0.0)[:, None].expand(n, d))
+
+
+def test_inputs_given_back_before_a_callers_stream_is_done():
+    """Inputs of a call queued on a busy stream, given back at once: their memory
+    is not handed out before the call has read them."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    n, vocab, d = 2048, 4096, 1024
+    table = torch.randn((vocab, d), device="cuda")
+    ids = torch.randint(0, vocab, (n,), device="cuda")
+    g = torch.randn((n, d), device="cuda")
+    plan = tre.Plan("vd,nd->nv", "v", {"v": vocab, "n": 4, "d": d}, {"v": 64}, "mxfp4")
+    tiles = table.view(vocab // 64, -1)
+    q = tre.mx_quantize(plan, "u", tiles)
+    side = torch.cuda.Stream()
+    busy = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    for name, call, args in (("lookup", lambda t, i, **kw: tre.lookup(t, i, scale=2.0, **kw), (table, ids)),
+                             ("lookup_grad", lambda t, i, **kw: tre.lookup_grad(t, i, vocab, **kw), (g, ids)),
+                             ("mx_quantize", lambda t, **kw: tre.mx_quantize(plan, "u", t, **kw), (tiles,)),
+                             ("mx_dequantize", lambda t, **kw: tre.mx_dequantize(plan, "u", t, **kw), (q,))):
+        want = call(*args)
+        copies = [a.clone() for a in args]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(100):
+                busy.fill_(1)
+        got = call(*copies, stream=side)
+        del copies
+        others = [torch.zeros_like(a) for a in args for _ in range(2)]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and len(others) == 2 * len(args), name
