@@ -736,9 +736,9 @@ __global__ __launch_bounds__(kThreads) void k_mx(MxArgs g) {
 //   all reads of a stage on their way before its first product     377
 //   four sums to a store                                           340
 //   no unit table                                                  325
-// The kernel is then at 299 to 308 us, 3.57 to 3.68 PFLOP/s, on two cards (348
-// on one whose clock had come down; a stage 0.99 us for two workgroups, their
-// starts and ends 12 us each).  With no copies in the loop
+// The kernel is then at 299 to 308 us, 3.57 to 3.68 PFLOP/s, at a clock of 1.86
+// GHz (in traces whose launches follow each other up to 348 in the median; a
+// stage 0.99 us for two workgroups, their starts and ends 12 us each).  With no copies in the loop
 // 16 x 16 tiles took 240; registers alone do 6.6 PFLOP/s of random codes (power;
 // 8.7 of zeros), so the wavefronts' waits for LDS and each other bound it.  A
 // raised priority around the products, the copies issued after the reads, and
