@@ -547,6 +547,63 @@ tre_status tre_lookup_grad(const void *grad, int32_t grad_dtype, const void *ids
                            float scale, void *table_grad, int32_t out_dtype, int64_t n_rows, int64_t row_elems,
                            int32_t accumulate, int64_t *status, void *ws, size_t ws_bytes, void *stream);
 
+/* --- probabilities of scores ---------------------------------------------- */
+
+/* Scores x[i, v] of n tokens i over `vocab` words v, scale times which is what
+ * the softmax is taken of: rows, or the tiles that a score EinSum writes when its
+ * relation is keyed by the word's tile ("vd,nd->nv" with v promoted in tiles of
+ * `cols`: w_tiles [vocab / cols][n][cols], all of them).  In both x[i, v] is
+ *     x + (v / cols) tile_stride + i row_stride + v % cols
+ * elements (rows: cols = vocab).  fp32 or bf16 (dtype), aligned to an element.
+ *
+ * tre_log_probs, with m = max_v x[i, v] and d_v = scale (x[i, v] - m):
+ *   stats     : device [n x 2]: m and log sum_v e^d_v, which tre_log_probs_grad
+ *               takes.
+ *   lse       : device [n]: log sum_v e^(scale x[i, v]).
+ *   ids       : device [n] int32 or int64 (id_bytes 4 or 8), or NULL: a word of
+ *               each token.  A negative one stands for no word; one of vocab or
+ *               more reads nothing either and sets `status`.
+ *   log_prob  : device [n] (with ids): scale x[i, ids[i]] - lse[i]; 0 for no word.
+ *   entropy   : device [n] or NULL: - sum_v p_v log p_v.
+ *   top       : 0, or up to 64 and vocab: so many words of the highest scores,
+ *               equal ones in the order of words, highest first:
+ *   top_ids, top_log_probs: device [n x top].
+ *   status    : device int64 or NULL; set to TRE_E_KEYRANGE where an id is vocab
+ *               or more, else left as it is.
+ * Maxima, sums and results are fp32.  Scores of -inf are words that cannot come.
+ * A row of nothing else has lse, log_prob and top_log_probs of -inf and entropy 0.
+ * A NaN or +inf makes its row's results NaN (top_ids: a NaN ranks as -inf).
+ *   ws        : device, 256-byte aligned, tre_log_probs_workspace_bytes(...)
+ *               bytes; NULL where that is 0 (sizes the call refuses: 0 too).  Holds
+ *               nothing between calls.  Calls that overlap need one each.
+ * Fewer than 2^31 - 1 tokens, up to 2^30 words, cols a divisor of vocab, scale
+ * positive.  Asynchronous on the stream; may be captured into a graph. */
+size_t tre_log_probs_workspace_bytes(int64_t n, int64_t vocab, int64_t cols, int32_t dtype, int32_t top);
+tre_status tre_log_probs(const void *x, int32_t dtype, int64_t n, int64_t vocab, int64_t cols, int64_t row_stride,
+                         int64_t tile_stride, const void *ids, int32_t id_bytes, float scale, float *log_prob,
+                         float *lse, float *stats, float *entropy, int32_t top, int32_t *top_ids,
+                         float *top_log_probs, int64_t *status, void *ws, size_t ws_bytes, void *stream);
+
+/* tre_log_probs_grad -- the gradient by the scores of a loss whose gradients by
+ * log_prob, lse and entropy are given (device [n] fp32, or NULL; one of them at
+ * least): with p_v = e^(log p_v),
+ *   grad[i, v] = scale (g_i [v = ids[i]] + p_v (gl_i - g_i - gh_i (log p_v + entropy_i))),
+ * computed in fp32 and rounded to out_dtype.
+ *   stats, entropy: as tre_log_probs gave them for these scores and this scale
+ *               (entropy with by_entropy only).
+ *   ids       : as there, needed with by_log_prob; no word has no g_i.
+ *   grad      : fp32 or bf16, laid out as the scores with strides of its own, its
+ *               rows apart.  May be x itself (with x's type and strides); else
+ *               disjoint from the inputs.
+ * A row of no possible word has a gradient of 0, as has one with g, gl and gh of
+ * 0, whose scores are not read.  Top words' log probabilities pass no gradient.
+ * Asynchronous on the stream; no workspace, so it may be captured into a graph. */
+tre_status tre_log_probs_grad(const void *x, int32_t dtype, int64_t n, int64_t vocab, int64_t cols,
+                              int64_t row_stride, int64_t tile_stride, const float *stats, const void *ids,
+                              int32_t id_bytes, float scale, const float *by_log_prob, const float *by_lse,
+                              const float *by_entropy, const float *entropy, void *grad, int32_t out_dtype,
+                              int64_t out_row_stride, int64_t out_tile_stride, int64_t *status, void *stream);
+
 /* --- errors -------------------------------------------------------------- */
 const char *tre_status_str(tre_status s);
 const char *tre_last_error(void);

@@ -772,6 +772,153 @@ tre_status tre_lookup_grad(const void* grad, int32_t grad_dtype, const void* ids
     return e == hipSuccess ? TRE_OK : dev_fail(e, "lookup_grad");
 }
 
+namespace {
+
+// Offsets into scores stay within 62 bits.
+bool scores_ok(const ScoreLayout& l) {
+    if (l.n < 0 || l.n >= INT32_MAX || l.vocab < 1 || l.vocab > (int64_t(1) << 30) || l.cols < 1 || l.cols > l.vocab ||
+        l.vocab % l.cols)
+        return false;
+    const int64_t most = int64_t(1) << 60;
+    return l.row_stride >= 0 && l.tile_stride >= 0 && l.row_stride <= most / std::max<int64_t>(l.n, 1) &&
+           l.tile_stride <= most / (l.vocab / l.cols);
+}
+// Whether no two elements of the layout share a place.
+bool scores_apart(const ScoreLayout& l) {
+    int64_t size[2] = {l.n, l.vocab / l.cols}, stride[2] = {l.row_stride, l.tile_stride};
+    if (stride[0] > stride[1]) {
+        std::swap(size[0], size[1]);
+        std::swap(stride[0], stride[1]);
+    }
+    int64_t reach = l.cols;
+    for (int d = 0; d < 2; d++) {
+        if (size[d] <= 1) continue;
+        if (stride[d] < reach) return false;
+        reach += stride[d] * (size[d] - 1);
+    }
+    return true;
+}
+tre_status scores_args(const char* where, const ScoreLayout& l, const void* x, int32_t dtype, const void* ids, int32_t id_bytes,
+                       float scale, const int64_t* status) {
+    const std::string w(where);
+    if (dtype != TRE_F32 && dtype != TRE_BF16) {
+        set_error(w + ": scores must be TRE_F32 or TRE_BF16");
+        return TRE_E_DTYPE;
+    }
+    if (!scores_ok(l)) {
+        set_error(w + ": size or stride out of range, or cols does not divide vocab");
+        return TRE_E_SHAPE;
+    }
+    const float scale2 = scale * 1.4426950408889634f;
+    if (!(scale2 > 0.f) || !std::isfinite(scale2)) {
+        set_error(w + ": scale must be positive and finite");
+        return TRE_E_ARG;
+    }
+    if (l.n > 0 && !x) {
+        set_error(w + ": null scores");
+        return TRE_E_ARG;
+    }
+    if (ids && id_bytes != 4 && id_bytes != 8) {
+        set_error(w + ": ids of neither 4 nor 8 bytes");
+        return TRE_E_ARG;
+    }
+    if (reinterpret_cast<uintptr_t>(x) % (dtype == TRE_BF16 ? 2 : 4) || (ids && reinterpret_cast<uintptr_t>(ids) % size_t(id_bytes)) ||
+        reinterpret_cast<uintptr_t>(status) % 8) {
+        set_error(w + ": scores, ids and status must be aligned to their size");
+        return TRE_E_ARG;
+    }
+    return TRE_OK;
+}
+bool floats_aligned(std::initializer_list<const void*> ps) {
+    for (const void* p : ps)
+        if (reinterpret_cast<uintptr_t>(p) % 4) return false;
+    return true;
+}
+
+}  // namespace
+
+size_t tre_log_probs_workspace_bytes(int64_t n, int64_t vocab, int64_t cols, int32_t dtype, int32_t top) {
+    const ScoreLayout l{n, vocab, cols, 0, 0};
+    if (!scores_ok(l) || (dtype != TRE_F32 && dtype != TRE_BF16) || top < 0 || top > 64) return 0;
+    return n == 0 ? 0 : log_probs_ws_bytes(l, dtype == TRE_BF16 ? 2 : 4, top);
+}
+
+tre_status tre_log_probs(const void* x, int32_t dtype, int64_t n, int64_t vocab, int64_t cols, int64_t row_stride,
+                         int64_t tile_stride, const void* ids, int32_t id_bytes, float scale, float* log_prob, float* lse,
+                         float* stats, float* entropy, int32_t top, int32_t* top_ids, float* top_log_probs, int64_t* status,
+                         void* ws, size_t ws_bytes, void* stream) {
+    const ScoreLayout l{n, vocab, cols, row_stride, tile_stride};
+    const tre_status st = scores_args("tre_log_probs", l, x, dtype, ids, id_bytes, scale, status);
+    if (st != TRE_OK) return st;
+    if (top < 0 || top > 64 || top > vocab) {
+        set_error("tre_log_probs: top must be 0 to 64, at most vocab");
+        return TRE_E_SHAPE;
+    }
+    if (n == 0) return TRE_OK;
+    if (!lse || !stats || (ids && !log_prob) || (!ids && log_prob) || (top > 0 && (!top_ids || !top_log_probs))) {
+        set_error("tre_log_probs: null array, or log_prob without ids");
+        return TRE_E_ARG;
+    }
+    if (!floats_aligned({log_prob, lse, stats, entropy, top_ids, top_log_probs})) {
+        set_error("tre_log_probs: results must be aligned to their size");
+        return TRE_E_ARG;
+    }
+    const size_t need = log_probs_ws_bytes(l, dtype == TRE_BF16 ? 2 : 4, top);
+    if (need > 0) {
+        if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) {
+            set_error("tre_log_probs: workspace null or not 256-byte aligned");
+            return TRE_E_ARG;
+        }
+        if (ws_bytes < need) {
+            set_error("tre_log_probs: workspace smaller than tre_log_probs_workspace_bytes");
+            return TRE_E_WORKSPACE;
+        }
+    }
+    const hipError_t e = launch_log_probs(l, x, dtype, ids, id_bytes, scale, top, log_prob, lse, stats, entropy, top_ids,
+                                          top_log_probs, status, static_cast<char*>(ws), reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TRE_OK : dev_fail(e, "log_probs");
+}
+
+tre_status tre_log_probs_grad(const void* x, int32_t dtype, int64_t n, int64_t vocab, int64_t cols, int64_t row_stride,
+                              int64_t tile_stride, const float* stats, const void* ids, int32_t id_bytes, float scale,
+                              const float* by_log_prob, const float* by_lse, const float* by_entropy, const float* entropy,
+                              void* grad, int32_t out_dtype, int64_t out_row_stride, int64_t out_tile_stride, int64_t* status,
+                              void* stream) {
+    const ScoreLayout l{n, vocab, cols, row_stride, tile_stride}, o{n, vocab, cols, out_row_stride, out_tile_stride};
+    if (out_dtype != TRE_F32 && out_dtype != TRE_BF16) {
+        set_error("tre_log_probs_grad: out_dtype must be TRE_F32 or TRE_BF16");
+        return TRE_E_DTYPE;
+    }
+    const tre_status st = scores_args("tre_log_probs_grad", l, x, dtype, ids, id_bytes, scale, status);
+    if (st != TRE_OK) return st;
+    if (!scores_ok(o) || !scores_apart(o)) {
+        set_error("tre_log_probs_grad: strides of the gradient out of range, or rows that overlap");
+        return TRE_E_SHAPE;
+    }
+    if (n == 0) return TRE_OK;
+    if ((!by_log_prob && !by_lse && !by_entropy) || (by_log_prob && !ids) || (by_entropy && !entropy)) {
+        set_error("tre_log_probs_grad: no gradient given, by_log_prob without ids or by_entropy without entropy");
+        return TRE_E_ARG;
+    }
+    if (!stats || !grad) {
+        set_error("tre_log_probs_grad: null array");
+        return TRE_E_ARG;
+    }
+    if (reinterpret_cast<uintptr_t>(grad) % (out_dtype == TRE_BF16 ? 2 : 4) ||
+        !floats_aligned({stats, by_log_prob, by_lse, by_entropy, entropy})) {
+        set_error("tre_log_probs_grad: arrays must be aligned to their elements");
+        return TRE_E_ARG;
+    }
+    if (grad == x && (out_dtype != dtype || out_row_stride != row_stride || out_tile_stride != tile_stride)) {
+        set_error("tre_log_probs_grad: in place the gradient has the scores' type and strides");
+        return TRE_E_ARG;
+    }
+    const hipError_t e = launch_log_probs_grad(l, x, dtype, stats, ids, id_bytes, scale, by_log_prob, by_lse, by_entropy, entropy,
+                                               grad, out_dtype, out_row_stride, out_tile_stride, status,
+                                               reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TRE_OK : dev_fail(e, "log_probs_grad");
+}
+
 size_t tre_stack_workspace_bytes(int64_t n) { return n < 0 ? 0 : stack_ws_bytes(n); }
 
 tre_status tre_stack_rows(const int32_t* keys, int64_t n, const void* tiles, int64_t row_elems, int32_t group,

@@ -341,6 +341,20 @@ hipError_t launch_lookup_grad(const void* grad, int grad_dtype, const void* ids,
                               void* out, int out_dtype, int64_t n_rows, int64_t elems, bool accumulate, int64_t* status,
                               char* ws, hipStream_t s);
 
+// probs.hip
+struct ScoreLayout {
+    int64_t n, vocab, cols, row_stride, tile_stride;  // element (i, v) at (v / cols) tile_stride + i row_stride + v % cols
+};
+// (0: the call needs none)
+size_t log_probs_ws_bytes(const ScoreLayout& l, int elem_bytes, int top);
+hipError_t launch_log_probs(const ScoreLayout& l, const void* x, int dtype, const void* ids, int id_bytes, float scale, int top,
+                            float* log_prob, float* lse, float* stats, float* entropy, int32_t* top_ids, float* top_log_probs,
+                            int64_t* status, char* ws, hipStream_t s);
+hipError_t launch_log_probs_grad(const ScoreLayout& l, const void* x, int dtype, const float* stats, const void* ids, int id_bytes,
+                                 float scale, const float* by_log_prob, const float* by_lse, const float* by_entropy,
+                                 const float* entropy, void* out, int out_dtype, int64_t out_row_stride, int64_t out_tile_stride,
+                                 int64_t* status, hipStream_t s);
+
 // glue.hip
 hipError_t launch_cast_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t s);
 hipError_t launch_scale(const float* x, float* y, int64_t n, float sc, hipStream_t s);

@@ -35,7 +35,7 @@ EXPORTS = [
     "tre_repartition_workspace_bytes", "tre_repartition", "tre_execute3_workspace_bytes", "tre_execute3",
     "tre_noalloc_scratch_bytes", "tre_execute_noalloc", "tre_output_bounds", "tre_execute_async",
     "tre_tile_bytes", "tre_mx_quantize", "tre_mx_dequantize", "tre_lookup", "tre_lookup_grad_workspace_bytes",
-    "tre_lookup_grad",
+    "tre_lookup_grad", "tre_log_probs_workspace_bytes", "tre_log_probs", "tre_log_probs_grad",
 ]
 
 
@@ -141,6 +141,11 @@ def lib():
         L.tre_lookup_grad_workspace_bytes.argtypes = [i64, i64, i64]
         L.tre_lookup_grad_workspace_bytes.restype = sz
         L.tre_lookup_grad.argtypes = [P, i32, P, i32, i64, ctypes.c_float, P, i32, i64, i64, i32, P, P, sz, P]
+        f32 = ctypes.c_float
+        L.tre_log_probs_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+        L.tre_log_probs_workspace_bytes.restype = sz
+        L.tre_log_probs.argtypes = [P, i32, i64, i64, i64, i64, i64, P, i32, f32, P, P, P, P, i32, P, P, P, P, sz, P]
+        L.tre_log_probs_grad.argtypes = [P, i32, i64, i64, i64, i64, i64, P, P, i32, f32, P, P, P, P, P, i32, i64, i64, P, P]
         L.tre_status_str.restype = ctypes.c_char_p
         L.tre_last_error.restype = ctypes.c_char_p
         L.tre_version.restype = ctypes.c_char_p
@@ -633,6 +638,121 @@ def lookup_grad(grad, ids, n_rows: int, scale: float = 1.0, dtype=None, out=None
         _check(lib().tre_lookup_grad(_ptr(grad), gdt, _ptr(ids), ids.element_size(), n, float(scale), _ptr(out), odt, n_rows,
                                      elems, int(accumulate), _ptr(status), _ptr(ws), ws.numel() * ws.element_size(),
                                      here.ptr), "tre_lookup_grad")
+    return out
+
+
+# ------------------------------------------------- probabilities of scores
+
+def _scores(x, where, what):
+    """(n, vocab, cols, row stride, tile stride) of scores [n, vocab] or in tiles
+    [tiles, n, cols], whose last dimension is contiguous."""
+    if x.dim() not in (2, 3) or x.shape[-1] < 1 or (x.dim() == 3 and x.shape[0] < 1):
+        raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"{what}: [n, vocab] or tiles [tiles, n, cols] wanted, got {tuple(x.shape)}")
+    if not x.is_cuda:
+        raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"{what}: on {x.device}, wanted on a GPU")
+    shape, stride = x.shape, x.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"{what}: a last stride of 1 wanted, got strides {stride}")
+    if len(shape) == 2:
+        return shape[0], shape[1], shape[1], stride[0], 0
+    return shape[1], shape[0] * shape[2], shape[2], stride[1], stride[0]
+
+
+@dataclass
+class LogProbs:
+    """What `log_probs` gives, in float32: of each token..."""
+    log_prob: object        # [n]: its given word's, or None
+    lse: object             # [n]: log of the sum of e^(scale x)
+    stats: object           # [n, 2]: what log_probs_grad takes
+    entropy: object         # [n], or None
+    top_ids: object         # int32 [n, top], or None
+    top_log_probs: object   # [n, top], or None
+
+
+def log_probs_workspace_bytes(n: int, vocab: int, cols: int | None = None, dtype=None, top: int = 0) -> int:
+    """For scores [n, vocab], or in tiles of ``cols`` words, of ``dtype`` (float32)."""
+    import torch
+
+    dt = _value_type(dtype or torch.float32, "tre.log_probs_workspace_bytes", "dtype")
+    return int(lib().tre_log_probs_workspace_bytes(int(n), int(vocab), int(cols or vocab), dt, int(top)))
+
+
+def log_probs(scores, ids=None, scale: float = 1.0, top: int = 0, entropy: bool = False, status=None, ws=None,
+              stream=None) -> LogProbs:
+    """Log probabilities out of scores (see tre_log_probs): softmax of scale *
+    scores, [n, vocab] or in the tiles [tiles, n, cols] that a score EinSum gives,
+    float32 or bfloat16, rows and tiles at any stride.  Of each token the given
+    word's (``ids`` [n], int32 or int64; 0 where negative), the log of the sum, the
+    entropy and the ``top`` (up to 64) best words, where asked for.  ``status``
+    (int64 [1]) is set to TRE_E_KEYRANGE where an id is vocab or more."""
+    import torch
+
+    w = "tre.log_probs"
+    dt = _value_type(scores, w, "scores")
+    layout = _scores(scores, w, "scores")
+    n, vocab, cols = layout[:3]
+    dev = scores.device
+    if ids is not None:
+        _ids(ids, w, dev)
+        if ids.shape != (n,):
+            raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"ids: [{n}] wanted, got {tuple(ids.shape)}")
+    _status(status, w, dev)
+    top = int(top)
+    if not 0 <= top <= min(64, vocab):
+        raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"top: 0 to {min(64, vocab)} wanted, got {top}")
+    with _Here(dev, stream, w) as here:
+        def make(*shape, dtype=torch.float32):
+            return here.buffer(lambda: torch.empty(shape, dtype=dtype, device=dev))
+
+        r = LogProbs(make(n) if ids is not None else None, make(n), make(n, 2), make(n) if entropy else None,
+                     make(n, top, dtype=torch.int32) if top else None, make(n, top) if top else None)
+        need = int(lib().tre_log_probs_workspace_bytes(n, vocab, cols, dt, top))
+        if ws is not None:
+            _want(ws, w, "ws", device=dev)
+        elif need:
+            ws = here.buffer(lambda: alloc_workspace(need, dev), result=False)
+        here.uses(scores, ids, status, ws)
+        _check(lib().tre_log_probs(_ptr(scores), dt, *layout, _ptr(ids), ids.element_size() if ids is not None else 0,
+                                   float(scale), _ptr(r.log_prob), _ptr(r.lse), _ptr(r.stats), _ptr(r.entropy), top,
+                                   _ptr(r.top_ids), _ptr(r.top_log_probs), _ptr(status), _ptr(ws),
+                                   ws.numel() * ws.element_size() if ws is not None else 0, here.ptr), "tre_log_probs")
+    return r
+
+
+def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, grad_entropy=None, entropy=None,
+                   scale: float = 1.0, dtype=None, out=None, status=None, stream=None):
+    """The gradient by the scores of a loss whose gradients by `log_probs`'s
+    log_prob, lse and entropy are given (see tre_log_probs_grad): ``stats`` and
+    ``entropy`` are those that it gave.  In the scores' layout and ``dtype`` (the
+    scores'); ``out`` may have strides of its own, and be ``scores``."""
+    import torch
+
+    w = "tre.log_probs_grad"
+    dt = _value_type(scores, w, "scores")
+    layout = _scores(scores, w, "scores")
+    n, dev = layout[0], scores.device
+    _want(stats, w, "stats", (n, 2), torch.float32, dev)
+    if ids is not None:
+        _ids(ids, w, dev)
+        if ids.shape != (n,):
+            raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"ids: [{n}] wanted, got {tuple(ids.shape)}")
+    for t, what in ((grad_log_prob, "grad_log_prob"), (grad_lse, "grad_lse"), (grad_entropy, "grad_entropy"), (entropy, "entropy")):
+        if t is not None:
+            _want(t, w, what, (n,), torch.float32, dev)
+    _status(status, w, dev)
+    dtype = dtype or (out.dtype if out is not None else scores.dtype)
+    odt = _value_type(dtype, w, "out")
+    with _Here(dev, stream, w) as here:
+        if out is None:
+            out = here.buffer(lambda: torch.empty(scores.shape, dtype=dtype, device=dev))
+        elif out.shape != scores.shape or out.device != dev or out.dtype != dtype:
+            raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"out: {dtype} {tuple(scores.shape)} on {dev} wanted, got {out.dtype} "
+                                                          f"{tuple(out.shape)} on {out.device}")
+        here.uses(scores, stats, ids, grad_log_prob, grad_lse, grad_entropy, entropy, out, status)
+        _check(lib().tre_log_probs_grad(_ptr(scores), dt, *layout, _ptr(stats), _ptr(ids),
+                                        ids.element_size() if ids is not None else 0, float(scale), _ptr(grad_log_prob),
+                                        _ptr(grad_lse), _ptr(grad_entropy), _ptr(entropy), _ptr(out), odt,
+                                        *_scores(out, w, "out")[3:], _ptr(status), here.ptr), "tre_log_probs_grad")
     return out
 
 
