@@ -604,6 +604,81 @@ tre_status tre_log_probs_grad(const void *x, int32_t dtype, int64_t n, int64_t v
                               const float *by_entropy, const float *entropy, void *grad, int32_t out_dtype,
                               int64_t out_row_stride, int64_t out_tile_stride, int64_t *status, void *stream);
 
+/* --- a training step of many tensors --------------------------------------- */
+
+/* tre_grad_norm -- the norm of n_tensors tensors taken together, and the factor
+ * that brings it to max_norm at most:
+ *   out : device fp32 [2]: sqrt(sum of all squares); min(1, max_norm / (norm +
+ *         1e-6)), or 1 with max_norm < 0 (no bound).  A norm that is not finite in
+ *         fp32 gives the factor NaN, with which tre_adamw takes no step.
+ *   tensors, types, sizes: host [n_tensors]: device arrays of fp32 or bf16 (a
+ *         tre_dtype each), aligned to an element, and their elements (0 too).
+ *   ws, ws_bytes: device workspace, 256-byte aligned, at least
+ *         tre_grad_norm_workspace_bytes(...) (0 on bad arguments); holds nothing
+ *         between calls.  Calls that overlap need one each.
+ * Squares are summed in 64 bits in an order that the sizes alone determine.  At
+ * most 2^42 elements in all (TRE_E_SHAPE).  Asynchronous on the stream; may be
+ * captured into a graph, which then holds the arrays' addresses. */
+size_t tre_grad_norm_workspace_bytes(int32_t n_tensors, const int64_t *sizes);
+tre_status tre_grad_norm(int32_t n_tensors, const void *const *tensors, const int32_t *types, const int64_t *sizes,
+                         float max_norm, float *out, void *ws, size_t ws_bytes, void *stream);
+
+/* tre_adamw -- one AdamW step t of many tensors, in place:
+ *   g' = grad_scale g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
+ *   params, param_types, grads, grad_types, sizes: host [n_tensors]: device arrays
+ *             of fp32 or bf16 (in any mixture), aligned to an element, and their
+ *             elements (0 too).  Parameters overlap neither each other nor a gradient
+ *             (TRE_E_ARG).
+ *   state   : device, 16-byte aligned, tre_adamw_state_bytes(...) bytes: the
+ *             moments, zeros before the first step.  Each tensor's begin at a
+ *             multiple of 32 elements, in the order of the tensors; with T elements
+ *             in all so counted,
+ *               32 bits: m fp32 [T], v fp32 [T];
+ *                8 bits: codes of m [T] and of v [T], a byte each, then a byte b
+ *                        for each 32 elements of m [T / 32] and of v [T / 32].
+ *             8 bits: 32 elements share 2^(b - 127), which brings the largest
+ *             magnitude into [128, 256) (b = 0: 2^-127 and small values); times it,
+ *             with E and f the upper and lower bits of the code c (f the lowest 3),
+ *             m is (-1)^s (1 + f / 8) 2^(E - 7), s bit 7 and E bits 3 to 6, and v
+ *             (1 + f / 8) 2^(E - 23), E bits 3 to 7; with E = 0 f / 8 2^-6 and
+ *             f / 8 2^-22.  b = 255: all NaN (a moment was not finite).  Weights
+ *             take their step from the moments before these are rounded.  A v that
+ *             is not zero takes code 1 at least.
+ *   opt     : host.  `lr_dev`, `step_dev` (t, at least 1) and `grad_scale_dev`
+ *             are device values or NULL, read when the step runs, in the place of
+ *             the host's: what a captured step that is replayed needs.  A
+ *             grad_scale_dev of NaN leaves everything as it is.
+ *             `stochastic`: 8-bit moments and bf16 weights are rounded up with the
+ *             probability that their place between two neighbours has, by a hash of
+ *             (seed, t, element); else to the nearest, ties to even.
+ * Computed in fp32.  At most 2^42 elements in all (TRE_E_SHAPE); TRE_E_ARG unless
+ * 0 <= beta < 1, eps > 0, lr >= 0, weight_decay >= 0, all finite, t >= 1 and bits
+ * 8 or 32.  Asynchronous on the stream; may be captured into a graph, which then
+ * holds the arrays' addresses. */
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay, grad_scale;
+    int64_t step;
+    const float *lr_dev;
+    const int64_t *step_dev;
+    const float *grad_scale_dev;
+    uint64_t seed;
+    int32_t stochastic;
+    int32_t bits;           /* of the moments: 32 or 8 */
+    int32_t reserved[2];
+} tre_adamw_options;
+
+/* (0 on bad arguments) */
+size_t tre_adamw_state_bytes(int32_t n_tensors, const int64_t *sizes, int32_t bits);
+tre_status tre_adamw(int32_t n_tensors, void *const *params, const int32_t *param_types, const void *const *grads,
+                     const int32_t *grad_types, const int64_t *sizes, void *state, const tre_adamw_options *opt,
+                     void *stream);
+
+/* tre_adamw_moments -- the values of 8-bit moments: m and v, device [total] of
+ * dtype TRE_F32 or TRE_BF16 (exact in both from 2^-126 up), 16-byte aligned, with
+ * total the state's elements of each, a multiple of 32.  Asynchronous. */
+tre_status tre_adamw_moments(const void *state, int64_t total, void *m, void *v, int32_t dtype, void *stream);
+
 /* --- errors -------------------------------------------------------------- */
 const char *tre_status_str(tre_status s);
 const char *tre_last_error(void);

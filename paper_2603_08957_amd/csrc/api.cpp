@@ -3,6 +3,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <memory>
+#include <new>
 
 #include "tre_internal.h"
 
@@ -917,6 +919,155 @@ tre_status tre_log_probs_grad(const void* x, int32_t dtype, int64_t n, int64_t v
                                                grad, out_dtype, out_row_stride, out_tile_stride, status,
                                                reinterpret_cast<hipStream_t>(stream));
     return e == hipSuccess ? TRE_OK : dev_fail(e, "log_probs_grad");
+}
+
+namespace {
+
+bool sizes_ok(int32_t n, const int64_t* sizes) {
+    if (n < 0 || (n > 0 && !sizes)) return false;
+    int64_t total = 0;
+    for (int32_t i = 0; i < n; i++) {
+        if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 42)) return false;
+        total += sizes[i];
+        if (total > (int64_t(1) << 42)) return false;
+    }
+    return true;
+}
+int elem_size(int32_t type) { return type == TRE_BF16 ? 2 : 4; }
+
+// Arrays of fp32 or bf16 of these sizes.
+tre_status arrays_args(const std::string& where, int32_t n, const void* const* arrays, const int32_t* types, const int64_t* sizes) {
+    if (n > 0 && (!arrays || !types)) {
+        set_error(where + ": null argument");
+        return TRE_E_ARG;
+    }
+    for (int32_t i = 0; i < n; i++) {
+        if (types[i] != TRE_F32 && types[i] != TRE_BF16) {
+            set_error(where + ": arrays must be TRE_F32 or TRE_BF16");
+            return TRE_E_DTYPE;
+        }
+        if (sizes[i] > 0 && (!arrays[i] || reinterpret_cast<uintptr_t>(arrays[i]) % size_t(elem_size(types[i])))) {
+            set_error(where + ": array null or not aligned to its elements");
+            return TRE_E_ARG;
+        }
+    }
+    return TRE_OK;
+}
+struct Span {
+    uintptr_t begin, end;
+};
+
+}  // namespace
+
+size_t tre_grad_norm_workspace_bytes(int32_t n_tensors, const int64_t* sizes) {
+    return sizes_ok(n_tensors, sizes) ? grad_norm_ws_bytes(n_tensors, sizes) : 0;
+}
+
+tre_status tre_grad_norm(int32_t n_tensors, const void* const* tensors, const int32_t* types, const int64_t* sizes, float max_norm,
+                         float* out, void* ws, size_t ws_bytes, void* stream) {
+    if (!sizes_ok(n_tensors, sizes)) {
+        set_error("tre_grad_norm: sizes out of range");
+        return TRE_E_SHAPE;
+    }
+    const tre_status st = arrays_args("tre_grad_norm", n_tensors, tensors, types, sizes);
+    if (st != TRE_OK) return st;
+    if (max_norm != max_norm || !out || reinterpret_cast<uintptr_t>(out) % 4 || !ws || reinterpret_cast<uintptr_t>(ws) % 256) {
+        set_error("tre_grad_norm: max_norm is NaN, or out or workspace null or misaligned");
+        return TRE_E_ARG;
+    }
+    if (ws_bytes < grad_norm_ws_bytes(n_tensors, sizes)) {
+        set_error("tre_grad_norm: workspace smaller than tre_grad_norm_workspace_bytes");
+        return TRE_E_WORKSPACE;
+    }
+    const hipError_t e = launch_grad_norm(n_tensors, tensors, types, sizes, max_norm, out, static_cast<char*>(ws),
+                                          reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TRE_OK : dev_fail(e, "grad_norm");
+}
+
+size_t tre_adamw_state_bytes(int32_t n_tensors, const int64_t* sizes, int32_t bits) {
+    if (!sizes_ok(n_tensors, sizes) || (bits != 8 && bits != 32)) return 0;
+    const size_t total = size_t(adamw_room(n_tensors, sizes));
+    return bits == 32 ? 8 * total : 2 * total + total / 16;
+}
+
+tre_status tre_adamw(int32_t n_tensors, void* const* params, const int32_t* param_types, const void* const* grads,
+                     const int32_t* grad_types, const int64_t* sizes, void* state, const tre_adamw_options* opt, void* stream) {
+    if (!sizes_ok(n_tensors, sizes)) {
+        set_error("tre_adamw: sizes out of range");
+        return TRE_E_SHAPE;
+    }
+    tre_status st = arrays_args("tre_adamw (parameters)", n_tensors, params, param_types, sizes);
+    if (st == TRE_OK) st = arrays_args("tre_adamw (gradients)", n_tensors, grads, grad_types, sizes);
+    if (st != TRE_OK) return st;
+    if (!opt) {
+        set_error("tre_adamw: null options");
+        return TRE_E_ARG;
+    }
+    auto rate = [](double x) { return x >= 0. && std::isfinite(float(x)); };
+    auto beta = [](double x) { return x >= 0. && x < 1.; };
+    if ((opt->bits != 8 && opt->bits != 32) || !beta(opt->beta1) || !beta(opt->beta2) || !rate(opt->eps) || !(float(opt->eps) > 0.f) ||
+        !rate(opt->weight_decay) || (!opt->lr_dev && !rate(opt->lr)) || (!opt->step_dev && opt->step < 1) ||
+        (!opt->grad_scale_dev && !std::isfinite(float(opt->grad_scale)))) {
+        set_error("tre_adamw: an option is out of range");
+        return TRE_E_ARG;
+    }
+    if (reinterpret_cast<uintptr_t>(opt->lr_dev) % 4 || reinterpret_cast<uintptr_t>(opt->grad_scale_dev) % 4 ||
+        reinterpret_cast<uintptr_t>(opt->step_dev) % 8 || reinterpret_cast<uintptr_t>(state) % 16) {
+        set_error("tre_adamw: device values must be aligned to their size, the state to 16 bytes");
+        return TRE_E_ARG;
+    }
+    if (adamw_room(n_tensors, sizes) == 0) return TRE_OK;
+    if (!state) {
+        set_error("tre_adamw: null state");
+        return TRE_E_ARG;
+    }
+    // a parameter twice, or two that overlap, would be stepped twice at once
+    std::unique_ptr<Span[]> spans(new (std::nothrow) Span[size_t(n_tensors)]);
+    if (!spans) {
+        set_error("tre_adamw: out of host memory");
+        return TRE_E_ARG;
+    }
+    auto span = [&](const void* at, int32_t type, int64_t size) {
+        const uintptr_t b = reinterpret_cast<uintptr_t>(at);
+        return Span{b, b + uintptr_t(size) * uintptr_t(elem_size(type))};
+    };
+    int32_t live = 0;
+    for (int32_t i = 0; i < n_tensors; i++)
+        if (sizes[i] > 0) spans[live++] = span(params[i], param_types[i], sizes[i]);
+    std::sort(spans.get(), spans.get() + live, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+    bool apart = true;
+    for (int32_t i = 1; i < live; i++) apart = apart && spans[i].begin >= spans[i - 1].end;
+    for (int32_t i = 0; i < n_tensors && apart; i++) {
+        if (sizes[i] == 0) continue;
+        const Span g = span(grads[i], grad_types[i], sizes[i]);
+        const Span* after = std::lower_bound(spans.get(), spans.get() + live, g, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+        apart = (after == spans.get() + live || after->begin >= g.end) && (after == spans.get() || after[-1].end <= g.begin);
+    }
+    if (!apart) {
+        set_error("tre_adamw: parameters overlap, or a gradient one");
+        return TRE_E_ARG;
+    }
+    const hipError_t e = launch_adamw(n_tensors, params, param_types, grads, grad_types, sizes, state, *opt,
+                                      reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TRE_OK : dev_fail(e, "adamw");
+}
+
+tre_status tre_adamw_moments(const void* state, int64_t total, void* m, void* v, int32_t dtype, void* stream) {
+    if (dtype != TRE_F32 && dtype != TRE_BF16) {
+        set_error("tre_adamw_moments: dtype must be TRE_F32 or TRE_BF16");
+        return TRE_E_DTYPE;
+    }
+    if (total < 0 || total % 32 || total > (int64_t(1) << 43)) {
+        set_error("tre_adamw_moments: total must be a multiple of 32");
+        return TRE_E_SHAPE;
+    }
+    if (total == 0) return TRE_OK;
+    if (!state || !m || !v || (reinterpret_cast<uintptr_t>(state) | reinterpret_cast<uintptr_t>(m) | reinterpret_cast<uintptr_t>(v)) & 15) {
+        set_error("tre_adamw_moments: array null or not 16-byte aligned");
+        return TRE_E_ARG;
+    }
+    const hipError_t e = launch_adamw_moments(state, total, m, v, dtype, reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TRE_OK : dev_fail(e, "adamw_moments");
 }
 
 size_t tre_stack_workspace_bytes(int64_t n) { return n < 0 ? 0 : stack_ws_bytes(n); }

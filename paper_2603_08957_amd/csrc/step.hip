@@ -1,0 +1,484 @@
+// What many tensors do together at the end of a training step: the norm of their
+// gradients, and an AdamW step of their weights with moments in 32 or 8 bits.
+//
+// Tensors of all sizes share a launch: its arguments hold their places and the
+// number of the first workgroup of each, so that nothing is kept on the device
+// between calls and a captured call holds what it was given.  Memory bounds both.
+#include "tre_internal.h"
+#include "values.h"
+
+#include <cmath>
+
+namespace tre {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+// Tensors of a launch: its arguments stay below 4 KB.
+constexpr int kMany = 96;
+
+struct Many {
+    const void* a[kMany];   // (weights)
+    const void* b[kMany];   // (gradients)
+    int64_t size[kMany];
+    int64_t at[kMany];      // first element's place in the moments
+    uint32_t first[kMany];  // workgroup
+    uint8_t kind[kMany];    // 1: a in bf16, 2: b in bf16
+    int32_t count;
+};
+
+// The tensor of a workgroup: the last that begins at it or before.
+__device__ inline int tensor_of(const Many& t, uint32_t block) {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kMany; i += 64) n += __popcll(__ballot(i + lane < t.count && t.first[min(i + lane, kMany - 1)] <= block));
+    return __builtin_amdgcn_readfirstlane(n - 1);
+}
+
+// ----------------------------------------------------------------- norm
+
+constexpr int kNormRuns = 8;
+
+struct NormArgs {
+    Many t;
+    double* part;       // of the launch's workgroups
+    int64_t per;        // elements of a workgroup
+};
+
+template <typename T>
+__device__ inline double squares(const T* x, int64_t n) {
+    constexpr int E = 16 / sizeof(T);
+    constexpr int64_t kStep = int64_t(kThreads) * E;
+    double s[2] = {0., 0.};
+    int64_t b = 0;
+    for (; b + kNormRuns * kStep <= n; b += kNormRuns * kStep) {
+        float v[kNormRuns][E];
+#pragma unroll
+        for (int j = 0; j < kNormRuns; j++) load_all(x + b + j * kStep + threadIdx.x * E, v[j]);
+#pragma unroll
+        for (int j = 0; j < kNormRuns; j++)
+#pragma unroll
+            for (int i = 0; i < E; i++) s[i & 1] = __builtin_fma(double(v[j][i]), double(v[j][i]), s[i & 1]);
+    }
+    for (b += threadIdx.x * E; b < n; b += kStep) {
+        float v[E];
+        load_run(x, b, n, v);
+#pragma unroll
+        for (int i = 0; i < E; i++) s[i & 1] = __builtin_fma(double(v[i]), double(v[i]), s[i & 1]);
+    }
+    return s[0] + s[1];
+}
+
+// The sum over a workgroup of one value each, in thread 0.
+__device__ inline double sum_all(double s) {
+    __shared__ double part[16];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.;
+    for (int w = 0; w < int(blockDim.x) >> 6; w++) s += part[w];
+    return s;
+}
+
+// Squares are summed in 64 bits: no fp32 value's overflows, and the sum's error
+// does not grow with the model.  Memory is still what bounds it: an element takes
+// a conversion and one fused product.
+__global__ __launch_bounds__(kThreads) void k_squares(NormArgs a) {
+    const uint32_t block = uint32_t(block_index());
+    const int i = tensor_of(a.t, block);
+    const int64_t at = int64_t(block - a.t.first[i]) * a.per, n = min(a.per, a.t.size[i] - at);
+    if (n <= 0) return;  // (a workgroup that only the grid's shape has)
+    const double s = sum_all(a.t.kind[i] & 1 ? squares(static_cast<const uint16_t*>(a.t.a[i]) + at, n)
+                                             : squares(static_cast<const float*>(a.t.a[i]) + at, n));
+    if (threadIdx.x == 0) a.part[block] = s;
+}
+
+constexpr int kFinishThreads = 1024;
+
+__global__ __launch_bounds__(kFinishThreads) void k_norm(const double* __restrict__ part, int64_t n, float max_norm,
+                                                         float* __restrict__ out) {
+    double s = 0.;
+    for (int64_t i = threadIdx.x; i < n; i += kFinishThreads) s += part[i];
+    s = sum_all(s);
+    if (threadIdx.x) return;
+    const double norm = sqrt(s);
+    const bool finite = norm <= double(__FLT_MAX__);
+    out[0] = float(norm);
+    out[1] = !finite ? __builtin_nanf("") : max_norm < 0.f ? 1.f : float(fmin(double(max_norm) / (norm + 1e-6), 1.));
+}
+
+// Elements of a workgroup: few workgroups' sums are left to add.
+constexpr int64_t kNormParts = 8192, kNormLeast = 4096;
+int64_t norm_per(int n, const int64_t* sizes) {
+    int64_t total = 0, per = kNormLeast;
+    for (int i = 0; i < n; i++) total += sizes[i];
+    while (per * kNormParts < total) per *= 2;
+    return per;
+}
+
+// ---------------------------------------------------------------- AdamW
+//
+//   m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2,
+//   p = p (1 - lr decay) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
+//
+// Moments in 8 bits.  32 consecutive elements share a power of two, the one that
+// brings the largest magnitude into [128, 256); times it a value is a small
+// floating point number: a first moment's a sign, 4 bits of exponent (bias 7) and
+// 3 of fraction, a second moment's 5 (bias 23) and 3.  A power of two loses
+// nothing where values have exponents of their own, and scaling by it is exact.
+// The second moment's range is twice the first's as exponents go, which the root
+// halves again.  One that is not zero takes the least code at least: a zero would
+// leave a first moment that is not zero over eps alone.
+//
+// Rounding to nearest loses steps that are below half a code's: a second moment
+// with b2 = 0.999 moves by a thousandth where codes are an eighth apart.  So with
+// a seed it is by chance, up with the probability that a value's place between two
+// codes has, which is right on average; weights in bf16 then too.
+
+struct AdamArgs {
+    Many t;
+    void* state;
+    int64_t total;
+    const float *lr_dev, *scale_dev;
+    const int64_t* step_dev;
+    double beta1, beta2;
+    float b1, nb1, b2, nb2, c1, c2, lr, decay, weight_decay, eps, scale;
+    uint32_t seed0, seed1, step;
+};
+
+static_assert(sizeof(AdamArgs) <= 4096, "a launch's arguments");
+
+struct Rates {
+    float c1, c2, lr, decay, scale;
+    uint32_t k0;
+};
+
+__device__ inline double power(double b, int64_t t) {
+    double r = 1.;
+    for (; t; t >>= 1, b *= b)
+        if (t & 1) r *= b;
+    return r;
+}
+
+__device__ inline Rates rates_of(const AdamArgs& a) {
+    Rates r{a.c1, a.c2, a.lr, a.decay, a.scale, 0};
+    uint32_t step = a.step;
+    if (a.scale_dev) r.scale = *a.scale_dev;
+    if (a.lr_dev) {
+        r.lr = *a.lr_dev;
+        r.decay = 1.f - r.lr * a.weight_decay;
+    }
+    if (a.step_dev) {
+        const int64_t t = max(*a.step_dev, int64_t(1));
+        r.c1 = float(1. / (1. - power(a.beta1, t)));
+        r.c2 = float(1. / (1. - power(a.beta2, t)));
+        step = uint32_t(t);
+    }
+    r.k0 = a.seed0 + step * 0x9E3779B1u;
+    return r;
+}
+
+// Random bits of an element: a hash of (seed, step, element) by shifts and products
+// with the leading bits of the golden ratio and of the roots of 2, 3 and 5.
+struct Chance {
+    uint32_t h, y;
+    __device__ uint32_t first() const { return h >> 12; }                 // 20 bits each
+    __device__ uint32_t second() const { return y >> 12; }
+    __device__ uint32_t weight() const { return (h ^ (y << 4)) & 0xffffu; }  // 16
+};
+__device__ inline Chance chance_of(int64_t i, uint32_t k0, uint32_t k1) {
+    uint32_t h = (uint32_t(i) ^ k0) * 0x6A09E667u;
+    h ^= h >> 15;
+    h = (h + k1 + uint32_t(i >> 32) * 0xBB67AE85u) * 0xBB67AE85u;
+    h ^= h >> 13;
+    uint32_t y = h * 0x3C6EF373u;
+    y ^= y >> 16;
+    return {h, y};
+}
+
+constexpr int kBias1 = 7, kBias2 = 23;
+
+template <int BIAS>
+__device__ inline float decode(uint32_t code, uint32_t byte) {  // of a magnitude
+    // (as the upper bits of a float, exponents below 1 a denormal's, the code is 2^(BIAS - 127) of its value)
+    const float v = ldexpf(__uint_as_float(code << 20), int(byte) - BIAS);
+    return byte == 255u ? __builtin_nanf("") : v;
+}
+
+// The code of a magnitude y < 256.5.  r: 20 random bits.
+template <int BIAS, bool CHANCE>
+__device__ inline uint32_t encode(float y, uint32_t r) {
+    const uint32_t u = __float_as_uint(y);
+    const uint32_t high = ((u + (CHANCE ? r : 0x7ffffu + (u >> 20 & 1))) >> 20) - ((127 - BIAS) << 3);
+    uint32_t low;
+    constexpr float kUnits = float(1u << (BIAS + 2));  // of codes below 8
+    if constexpr (CHANCE) low = (uint32_t(y * (kUnits * float(1u << 20))) + r) >> 20;
+    else low = uint32_t(rintf(y * kUnits));
+    return y >= 1.f / float(1u << (BIAS - 1)) ? high : low;
+}
+
+// The byte of a block's power of two, from its largest magnitude's bits; 8 lanes to
+// a block.  255: a NaN or an infinity.
+__device__ inline uint32_t block_byte(uint32_t bits) {
+    bits = max(bits, uint32_t(__builtin_amdgcn_update_dpp(0, bits, 0xB1, 0xf, 0xf, true)));
+    bits = max(bits, uint32_t(__builtin_amdgcn_update_dpp(0, bits, 0x4E, 0xf, 0xf, true)));
+    bits = max(bits, uint32_t(__builtin_amdgcn_update_dpp(0, bits, 0x141, 0xf, 0xf, true)));
+    const uint32_t e = bits >> 23;
+    return e == 255u ? 255u : e > 7u ? e - 7u : 0u;
+}
+
+// A lane's run is 4 elements (16 bytes in fp32), so many of them in flight together.
+constexpr int kRun = 4, kAdamRuns = 4;
+constexpr int64_t kAdamStep = int64_t(64) * kRun * kAdamRuns;       // elements of a wavefront at once
+constexpr int64_t kAdamBlock = kAdamStep * kWaves;
+
+template <int BITS, bool CHANCE, typename TP, typename TG, bool WHOLE>
+__device__ inline void adam_runs(const AdamArgs& a, const Rates& r, TP* p, const TG* g, int64_t at, int64_t e0, int64_t n) {
+    const int lane = threadIdx.x & 63;
+    float pv[kAdamRuns][kRun], gv[kAdamRuns][kRun], mv[kAdamRuns][kRun], vv[kAdamRuns][kRun];
+    uint32_t mc[kAdamRuns], vc[kAdamRuns], mb[kAdamRuns], vb[kAdamRuns];
+    float* m32 = static_cast<float*>(a.state) + at;
+    float* v32 = m32 + a.total;
+    uint8_t* m8 = static_cast<uint8_t*>(a.state) + at;
+    uint8_t* v8 = m8 + a.total;
+    uint8_t* mb8 = static_cast<uint8_t*>(a.state) + 2 * a.total + at / 32;
+    uint8_t* vb8 = mb8 + a.total / 32;
+#pragma unroll
+    for (int j = 0; j < kAdamRuns; j++) {
+        const int64_t e = e0 + (j * 64 + lane) * kRun;
+        if (!WHOLE && e / 32 * 32 >= n) break;  // (the moments have whole blocks)
+        if constexpr (WHOLE) {
+            load_all(p + e, pv[j]);
+            load_all(g + e, gv[j]);
+        } else {
+            load_run(p, e, n, pv[j]);
+            load_run(g, e, n, gv[j]);
+        }
+        if constexpr (BITS == 32) {
+            load_all(m32 + e, mv[j]);
+            load_all(v32 + e, vv[j]);
+        } else {
+            mc[j] = *reinterpret_cast<const uint32_t*>(m8 + e);
+            vc[j] = *reinterpret_cast<const uint32_t*>(v8 + e);
+            mb[j] = mb8[e / 32];
+            vb[j] = vb8[e / 32];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kAdamRuns; j++) {
+        const int64_t e = e0 + (j * 64 + lane) * kRun;
+        if (!WHOLE && e / 32 * 32 >= n) break;
+        Chance c[kRun];
+        uint32_t m_top = 0, v_top = 0;
+#pragma unroll
+        for (int i = 0; i < kRun; i++) {
+            if constexpr (BITS == 8) {
+                const uint32_t mi = mc[j] >> (8 * i) & 255u;
+                mv[j][i] = copysignf(decode<kBias1>(mi & 127u, mb[j]), __uint_as_float(mi << 24));
+                vv[j][i] = decode<kBias2>(vc[j] >> (8 * i) & 255u, vb[j]);
+            }
+            if constexpr (CHANCE) c[i] = chance_of(at + e + i, r.k0, a.seed1);
+            {
+                // (each product and sum rounded for itself, so that a moment next to a border between two codes is the same
+                // whoever computes it)
+#pragma clang fp contract(off)
+                const float gi = gv[j][i] * r.scale;
+                mv[j][i] = mv[j][i] * a.b1 + gi * a.nb1;
+                vv[j][i] = vv[j][i] * a.b2 + gi * gi * a.nb2;
+            }
+            const float root = __builtin_amdgcn_sqrtf(vv[j][i] * r.c2) + a.eps;
+            pv[j][i] = pv[j][i] * r.decay - r.lr * (mv[j][i] * r.c1) * __builtin_amdgcn_rcpf(root);
+            if constexpr (CHANCE && sizeof(TP) == 2) {
+                const uint32_t u = __float_as_uint(pv[j][i]);
+                if ((u & 0x7f800000u) != 0x7f800000u) pv[j][i] = __uint_as_float((u + c[i].weight()) & 0xffff0000u);
+            }
+            if constexpr (BITS == 8) {
+                m_top = max(m_top, __float_as_uint(mv[j][i]) & 0x7fffffffu);
+                v_top = max(v_top, __float_as_uint(vv[j][i]) & 0x7fffffffu);
+            }
+        }
+        if constexpr (WHOLE) store_all<true>(p + e, pv[j]);
+        else store_run<true>(p, e, n, pv[j]);
+        if constexpr (BITS == 32) {
+            store_all<true>(m32 + e, mv[j]);
+            store_all<true>(v32 + e, vv[j]);
+        } else {
+            const uint32_t bm = block_byte(m_top), bv = block_byte(v_top);
+            // 2^(127 - byte), at most 2^127
+            const float sm = __uint_as_float((254u - min(bm, 253u)) << 23), sv = __uint_as_float((254u - min(bv, 253u)) << 23);
+            uint32_t mq = 0, vq = 0;
+#pragma unroll
+            for (int i = 0; i < kRun; i++) {
+                const uint32_t q = encode<kBias1, CHANCE>(fabsf(mv[j][i]) * sm, c[i].first());
+                mq |= (q | (__float_as_uint(mv[j][i]) >> 31 << 7)) << (8 * i);
+                const uint32_t w = encode<kBias2, CHANCE>(vv[j][i] * sv, c[i].second());
+                vq |= (w == 0 && vv[j][i] > 0.f ? 1u : w) << (8 * i);
+            }
+            *reinterpret_cast<uint32_t*>(m8 + e) = bm == 255u ? 0u : mq;
+            *reinterpret_cast<uint32_t*>(v8 + e) = bv == 255u ? 0u : vq;
+            if ((lane & 7) == 0) {
+                mb8[e / 32] = uint8_t(bm);
+                vb8[e / 32] = uint8_t(bv);
+            }
+        }
+    }
+}
+
+template <int BITS, bool CHANCE, typename TP, typename TG>
+__device__ inline void adam_block(const AdamArgs& a, const Rates& r, int i, int64_t e0) {
+    TP* p = static_cast<TP*>(const_cast<void*>(a.t.a[i]));
+    const TG* g = static_cast<const TG*>(a.t.b[i]);
+    const int64_t n = a.t.size[i], at = a.t.at[i];
+    if (e0 + kAdamStep <= n) adam_runs<BITS, CHANCE, TP, TG, true>(a, r, p, g, at, e0, n);
+    else if (e0 < n) adam_runs<BITS, CHANCE, TP, TG, false>(a, r, p, g, at, e0, n);
+}
+
+template <int BITS, bool CHANCE>
+__global__ __launch_bounds__(kThreads) void k_adam(AdamArgs a) {
+    const uint32_t block = uint32_t(block_index());
+    const int i = tensor_of(a.t, block);
+    const Rates r = rates_of(a);
+    if (r.scale != r.scale) return;  // (a norm that is not finite: no step)
+    const int64_t e0 = int64_t(block - a.t.first[i]) * kAdamBlock + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kAdamStep;
+    switch (a.t.kind[i]) {
+        case 0: adam_block<BITS, CHANCE, float, float>(a, r, i, e0); break;
+        case 1: adam_block<BITS, CHANCE, uint16_t, float>(a, r, i, e0); break;
+        case 2: adam_block<BITS, CHANCE, float, uint16_t>(a, r, i, e0); break;
+        default: adam_block<BITS, CHANCE, uint16_t, uint16_t>(a, r, i, e0); break;
+    }
+}
+
+// 8-bit moments read back.
+template <typename TO>
+__global__ __launch_bounds__(kThreads) void k_moments(const uint8_t* __restrict__ state, int64_t total, TO* __restrict__ m,
+                                                      TO* __restrict__ v) {
+    const int64_t e = (block_index() * kThreads + threadIdx.x) * 8;
+    if (e >= total) return;
+    const uint2 mc = *reinterpret_cast<const uint2*>(state + e), vc = *reinterpret_cast<const uint2*>(state + total + e);
+    const uint32_t mb = state[2 * total + e / 32], vb = state[2 * total + total / 32 + e / 32];
+    float mv[8], vv[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const uint32_t mi = (i < 4 ? mc.x : mc.y) >> (8 * (i & 3)) & 255u;
+        mv[i] = copysignf(decode<kBias1>(mi & 127u, mb), __uint_as_float(mi << 24));
+        vv[i] = decode<kBias2>((i < 4 ? vc.x : vc.y) >> (8 * (i & 3)) & 255u, vb);
+    }
+    store_all<true>(m + e, mv);
+    store_all<true>(v + e, vv);
+}
+
+int64_t room_of(int64_t n) { return (n + 31) / 32 * 32; }
+
+template <int BITS>
+hipError_t adam(const AdamArgs& a, bool chance, int64_t blocks, hipStream_t s) {
+    if (chance) k_adam<BITS, true><<<grid_of(blocks), kThreads, 0, s>>>(a);
+    else k_adam<BITS, false><<<grid_of(blocks), kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t grad_norm_ws_bytes(int n, const int64_t* sizes) {
+    const int64_t per = norm_per(n, sizes);
+    int64_t parts = 1;
+    for (int i = 0; i < n; i++) parts += (sizes[i] + per - 1) / per;
+    return (size_t(parts) * 8 + 255) / 256 * 256;
+}
+
+hipError_t launch_grad_norm(int n, const void* const* tensors, const int32_t* types, const int64_t* sizes, float max_norm,
+                            float* out, char* ws, hipStream_t s) {
+    NormArgs a{};
+    a.per = norm_per(n, sizes);
+    a.part = reinterpret_cast<double*>(ws);
+    int64_t parts = 0, blocks = 0;
+    for (int i = 0; i < n; i++) {
+        if (sizes[i] > 0) {
+            const int k = a.t.count++;
+            a.t.a[k] = tensors[i];
+            a.t.size[k] = sizes[i];
+            a.t.first[k] = uint32_t(blocks);
+            a.t.kind[k] = types[i] == TRE_BF16;
+            blocks += (sizes[i] + a.per - 1) / a.per;
+        }
+        if (a.t.count == kMany || (i == n - 1 && a.t.count)) {
+            k_squares<<<grid_of(blocks), kThreads, 0, s>>>(a);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            a.part += blocks;
+            parts += blocks;
+            blocks = 0;
+            a.t.count = 0;
+        }
+    }
+    k_norm<<<1, kFinishThreads, 0, s>>>(reinterpret_cast<const double*>(ws), parts, max_norm, out);
+    return hipGetLastError();
+}
+
+int64_t adamw_room(int n, const int64_t* sizes) {
+    int64_t total = 0;
+    for (int i = 0; i < n; i++) total += room_of(sizes[i]);
+    return total;
+}
+
+hipError_t launch_adamw(int n, void* const* params, const int32_t* param_types, const void* const* grads,
+                        const int32_t* grad_types, const int64_t* sizes, void* state, const tre_adamw_options& o, hipStream_t s) {
+    AdamArgs a{};
+    a.state = state;
+    a.total = adamw_room(n, sizes);
+    a.lr_dev = o.lr_dev;
+    a.scale_dev = o.grad_scale_dev;
+    a.step_dev = o.step_dev;
+    a.beta1 = o.beta1;
+    a.beta2 = o.beta2;
+    a.b1 = float(o.beta1);
+    a.nb1 = float(1. - o.beta1);
+    a.b2 = float(o.beta2);
+    a.nb2 = float(1. - o.beta2);
+    if (!o.step_dev) {
+        a.c1 = float(1. / (1. - std::pow(o.beta1, double(o.step))));
+        a.c2 = float(1. / (1. - std::pow(o.beta2, double(o.step))));
+        a.step = uint32_t(o.step);
+    }
+    a.lr = float(o.lr);
+    a.decay = float(1. - o.lr * o.weight_decay);
+    a.weight_decay = float(o.weight_decay);
+    a.eps = float(o.eps);
+    a.scale = float(o.grad_scale);
+    a.seed0 = uint32_t(o.seed);
+    a.seed1 = uint32_t(o.seed >> 32);
+    int64_t blocks = 0, at = 0;
+    for (int i = 0; i < n; i++) {
+        if (sizes[i] > 0) {
+            const int k = a.t.count++;
+            a.t.a[k] = params[i];
+            a.t.b[k] = grads[i];
+            a.t.size[k] = sizes[i];
+            a.t.at[k] = at;
+            a.t.first[k] = uint32_t(blocks);
+            a.t.kind[k] = uint8_t((param_types[i] == TRE_BF16) | (grad_types[i] == TRE_BF16) << 1);
+            blocks += (sizes[i] + kAdamBlock - 1) / kAdamBlock;
+            at += room_of(sizes[i]);
+        }
+        if (a.t.count == kMany || (i == n - 1 && a.t.count)) {
+            const hipError_t e = o.bits == 8 ? adam<8>(a, o.stochastic != 0, blocks, s) : adam<32>(a, o.stochastic != 0, blocks, s);
+            if (e != hipSuccess) return e;
+            blocks = 0;
+            a.t.count = 0;
+        }
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_adamw_moments(const void* state, int64_t total, void* m, void* v, int dtype, hipStream_t s) {
+    const dim3 grid = grid_of((total / 8 + kThreads - 1) / kThreads);
+    const uint8_t* x = static_cast<const uint8_t*>(state);
+    if (dtype == TRE_BF16) k_moments<<<grid, kThreads, 0, s>>>(x, total, static_cast<uint16_t*>(m), static_cast<uint16_t*>(v));
+    else k_moments<<<grid, kThreads, 0, s>>>(x, total, static_cast<float*>(m), static_cast<float*>(v));
+    return hipGetLastError();
+}
+
+}  // namespace tre

@@ -355,6 +355,15 @@ hipError_t launch_log_probs_grad(const ScoreLayout& l, const void* x, int dtype,
                                  const float* entropy, void* out, int out_dtype, int64_t out_row_stride, int64_t out_tile_stride,
                                  int64_t* status, hipStream_t s);
 
+// step.hip
+size_t grad_norm_ws_bytes(int n, const int64_t* sizes);
+hipError_t launch_grad_norm(int n, const void* const* tensors, const int32_t* types, const int64_t* sizes, float max_norm,
+                            float* out, char* ws, hipStream_t s);
+int64_t adamw_room(int n, const int64_t* sizes);  // elements of a moment of all tensors, each in whole blocks of 32
+hipError_t launch_adamw(int n, void* const* params, const int32_t* param_types, const void* const* grads,
+                        const int32_t* grad_types, const int64_t* sizes, void* state, const tre_adamw_options& o, hipStream_t s);
+hipError_t launch_adamw_moments(const void* state, int64_t total, void* m, void* v, int dtype, hipStream_t s);
+
 // glue.hip
 hipError_t launch_cast_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t s);
 hipError_t launch_scale(const float* x, float* y, int64_t n, float sc, hipStream_t s);

@@ -8,7 +8,9 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from dataclasses import dataclass
+from operator import attrgetter
 
 import numpy as np
 
@@ -36,6 +38,7 @@ EXPORTS = [
     "tre_noalloc_scratch_bytes", "tre_execute_noalloc", "tre_output_bounds", "tre_execute_async",
     "tre_tile_bytes", "tre_mx_quantize", "tre_mx_dequantize", "tre_lookup", "tre_lookup_grad_workspace_bytes",
     "tre_lookup_grad", "tre_log_probs_workspace_bytes", "tre_log_probs", "tre_log_probs_grad",
+    "tre_grad_norm_workspace_bytes", "tre_grad_norm", "tre_adamw_state_bytes", "tre_adamw", "tre_adamw_moments",
 ]
 
 
@@ -64,6 +67,14 @@ class PlanInfo(ctypes.Structure):
 class JoinResult(ctypes.Structure):
     _fields_ = [("n_u", ctypes.c_int64), ("n_v", ctypes.c_int64), ("n_pairs", ctypes.c_int64), ("n_w", ctypes.c_int64),
                 ("internal", ctypes.c_uint64 * 16)]
+
+
+class AdamwOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64),
+                ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p), ("grad_scale_dev", ctypes.c_void_p),
+                ("seed", ctypes.c_uint64), ("stochastic", ctypes.c_int32), ("bits", ctypes.c_int32),
+                ("reserved", ctypes.c_int32 * 2)]
 
 
 class Timing(ctypes.Structure):
@@ -146,6 +157,13 @@ def lib():
         L.tre_log_probs_workspace_bytes.restype = sz
         L.tre_log_probs.argtypes = [P, i32, i64, i64, i64, i64, i64, P, i32, f32, P, P, P, P, i32, P, P, P, P, sz, P]
         L.tre_log_probs_grad.argtypes = [P, i32, i64, i64, i64, i64, i64, P, P, i32, f32, P, P, P, P, P, i32, i64, i64, P, P]
+        L.tre_grad_norm_workspace_bytes.argtypes = [i32, P]
+        L.tre_grad_norm_workspace_bytes.restype = sz
+        L.tre_grad_norm.argtypes = [i32, P, P, P, f32, P, P, sz, P]
+        L.tre_adamw_state_bytes.argtypes = [i32, P, i32]
+        L.tre_adamw_state_bytes.restype = sz
+        L.tre_adamw.argtypes = [i32, P, P, P, P, P, P, P, P]
+        L.tre_adamw_moments.argtypes = [P, i64, P, P, i32, P]
         L.tre_status_str.restype = ctypes.c_char_p
         L.tre_last_error.restype = ctypes.c_char_p
         L.tre_version.restype = ctypes.c_char_p
@@ -754,6 +772,163 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
                                         _ptr(grad_lse), _ptr(grad_entropy), _ptr(entropy), _ptr(out), odt,
                                         *_scores(out, w, "out")[3:], _ptr(status), here.ptr), "tre_log_probs_grad")
     return out
+
+
+# ------------------------------------------- a training step of many tensors
+
+class _Many:
+    """Host arrays of contiguous GPU tensors' addresses, types and elements, all
+    on one device, as the calls over many tensors take them."""
+
+    def __init__(self, tensors, where, what):
+        import torch
+
+        T = torch.Tensor
+        tensors = list(tensors)
+        try:
+            places = set(map(T.get_device, tensors))
+            kinds = list(map(attrgetter("dtype"), tensors))
+            self.numels = list(map(T.numel, tensors))
+            addresses = array("q", map(T.data_ptr, tensors))
+            contiguous = all(map(T.is_contiguous, tensors))
+        except TypeError:
+            raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"{what}: a list of tensors wanted") from None
+        if len(places) > 1 or -1 in places:
+            raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"{what}: wanted on one GPU")
+        if not contiguous:
+            raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"{what}: contiguous tensors wanted")
+        code = {torch.float32: 0, torch.bfloat16: 1}
+        try:
+            types = array("i", map(code.__getitem__, kinds))
+        except KeyError as e:
+            raise TreError(STATUS_CODE["TRE_E_DTYPE"], where, f"{what}: float32 or bfloat16 wanted, got {e.args[0]}") from None
+        sizes = array("q", self.numels)
+        self.tensors, self.n = tensors, len(tensors)
+        self.device = torch.device("cuda", places.pop()) if places else None
+        self._arrays = addresses, types, sizes
+        self.addresses, self.types, self.sizes = (ctypes.c_void_p(a.buffer_info()[0]) for a in self._arrays)
+
+
+def grad_norm_workspace_bytes(sizes) -> int:
+    """For tensors of these numbers of elements."""
+    sizes = array("q", sizes)
+    return int(lib().tre_grad_norm_workspace_bytes(len(sizes), ctypes.c_void_p(sizes.buffer_info()[0])))
+
+
+def grad_norm(tensors, max_norm: float | None = None, out=None, ws=None, stream=None):
+    """The norm of a list of tensors (float32 or bfloat16, contiguous, on one GPU)
+    taken together, and the factor that brings it to ``max_norm`` at most (1
+    without), float32 [2] on their device (see tre_grad_norm).  The factor,
+    ``out[1:]``, is what `adamw` takes as ``grad_scale``; it is NaN where the norm
+    is not finite, and then `adamw` takes no step."""
+    import torch
+
+    w = "tre.grad_norm"
+    many = _Many(tensors, w, "tensors")
+    if many.device is None:
+        raise TreError(STATUS_CODE["TRE_E_ARG"], w, "tensors: none")
+    max_norm = -1.0 if max_norm is None else float(max_norm)
+    with _Here(many.device, stream, w) as here:
+        if out is None:
+            out = here.buffer(lambda: torch.empty(2, dtype=torch.float32, device=many.device))
+        else:
+            _want(out, w, "out", (2,), torch.float32, many.device)
+        if ws is None:
+            need = int(lib().tre_grad_norm_workspace_bytes(many.n, many.sizes))
+            ws = here.buffer(lambda: alloc_workspace(need, many.device), result=False)
+        else:
+            _want(ws, w, "ws", device=many.device)
+        here.uses(*many.tensors, out, ws)
+        _check(lib().tre_grad_norm(many.n, many.addresses, many.types, many.sizes, max_norm, _ptr(out), _ptr(ws),
+                                   ws.numel() * ws.element_size(), here.ptr), "tre_grad_norm")
+    return out
+
+
+def adamw_state(params, bits: int = 32, stream=None):
+    """Moments of no step yet for a list of tensors (see tre_adamw): zeros,
+    float32 [2 T] for 32 bits, uint8 [2 T + T / 16] for 8."""
+    import torch
+
+    w = "tre.adamw_state"
+    many = _Many(params, w, "params")
+    if bits not in (8, 32) or many.device is None:
+        raise TreError(STATUS_CODE["TRE_E_ARG"], w, f"tensors and 8 or 32 bits wanted, got {many.n} and {bits}")
+    need = int(lib().tre_adamw_state_bytes(many.n, many.sizes, bits))
+    with _Here(many.device, stream, w) as here:
+        return here.buffer(lambda: torch.zeros(need // 4 if bits == 32 else need, device=many.device,
+                                               dtype=torch.float32 if bits == 32 else torch.uint8))
+
+
+def _device_value(x, where, what, dtype, device):
+    """(host value, tensor) of a number or a device tensor of one."""
+    import torch
+
+    if not isinstance(x, torch.Tensor):
+        return x, None
+    if x.numel() != 1:
+        raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"{what}: one value wanted, got {tuple(x.shape)}")
+    return 0, _want(x, where, what, dtype=dtype, device=device)
+
+
+def adamw(params, grads, state, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+          weight_decay: float = 0.0, grad_scale=1.0, seed: int | None = None, stream=None):
+    """One AdamW step of a list of tensors, in place (see tre_adamw): ``params``
+    and ``grads`` of the same shapes, float32 or bfloat16, contiguous, on one GPU;
+    ``state`` from `adamw_state`, whose type says how many bits the moments have.
+    ``step`` (the first is 1), ``lr`` and ``grad_scale`` are numbers or tensors of
+    one value (int64, float32, float32) on the device, read when the step runs.
+    With a ``seed`` 8-bit moments and bfloat16 weights are rounded by chance, by
+    (seed, step, element); else to the nearest."""
+    import torch
+
+    w = "tre.adamw"
+    p, g = _Many(params, w, "params"), _Many(grads, w, "grads")
+    if p.device != g.device or p.device is None:
+        raise TreError(STATUS_CODE["TRE_E_ARG"], w, f"params and grads wanted on one GPU, got {p.device} and {g.device}")
+    if p.numels != g.numels or list(map(attrgetter("shape"), p.tensors)) != list(map(attrgetter("shape"), g.tensors)):
+        raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, "grads: params' shapes wanted")
+    if state.dtype not in (torch.float32, torch.uint8):
+        raise TreError(STATUS_CODE["TRE_E_DTYPE"], w, f"state: float32 or uint8 wanted, got {state.dtype}")
+    bits = 32 if state.dtype == torch.float32 else 8
+    need = int(lib().tre_adamw_state_bytes(p.n, p.sizes, bits)) // (4 if bits == 32 else 1)
+    _want(state, w, "state", (need,), device=p.device)
+    step, step_dev = _device_value(step, w, "step", torch.int64, p.device)
+    lr, lr_dev = _device_value(lr, w, "lr", torch.float32, p.device)
+    scale, scale_dev = _device_value(grad_scale, w, "grad_scale", torch.float32, p.device)
+    opt = AdamwOptions(float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), float(scale), int(step),
+                       _ptr(lr_dev), _ptr(step_dev), _ptr(scale_dev), (seed or 0) & (1 << 64) - 1, int(seed is not None), bits)
+    with _Here(p.device, stream, w) as here:
+        here.uses(*p.tensors, *g.tensors, state, step_dev, lr_dev, scale_dev)
+        _check(lib().tre_adamw(p.n, p.addresses, p.types, g.addresses, g.types, p.sizes, _ptr(state), ctypes.byref(opt),
+                               here.ptr), "tre_adamw")
+
+
+def adamw_moments(state, dtype=None, stream=None):
+    """The moments m and v that a state of `adamw` holds, [T] each: views of a
+    float32 state's; of an 8-bit state's the values (see tre_adamw_moments), in
+    ``dtype`` (float32, the default, or bfloat16).  Tensor i's begin at the sum of
+    the elements before it, each tensor's taken up to a multiple of 32."""
+    import torch
+
+    w = "tre.adamw_moments"
+    if state.dtype not in (torch.float32, torch.uint8):
+        raise TreError(STATUS_CODE["TRE_E_DTYPE"], w, f"state: float32 or uint8 wanted, got {state.dtype}")
+    if state.dtype == torch.float32:
+        _want(state, w, "state")
+        if dtype not in (None, torch.float32) or state.numel() % 64:
+            raise TreError(STATUS_CODE["TRE_E_DTYPE"], w, "32-bit moments are float32, 64 k of them")
+        return state.view(2, -1).unbind()
+    _want(state, w, "state")
+    total = state.numel() * 16 // 33
+    if state.numel() % 66 or total % 32:
+        raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"state: a state of 8 bits wanted, got {state.numel()} bytes")
+    dtype = dtype or torch.float32
+    dt = _value_type(dtype, w, "moments")
+    with _Here(state.device, stream, w) as here:
+        m, v = (here.buffer(lambda: torch.empty(total, dtype=dtype, device=state.device)) for _ in range(2))
+        here.uses(state)
+        _check(lib().tre_adamw_moments(_ptr(state), total, _ptr(m), _ptr(v), dt, here.ptr), "tre_adamw_moments")
+    return m, v
 
 
 def cast_f32_bf16(x, out=None, stream=None):

@@ -1,0 +1,185 @@
+"""The 8-bit moments' oracle pinned, and refusals of the calls over many tensors and over scores, on the CPU."""
+import ctypes
+import math
+from array import array
+
+import numpy as np
+import pytest
+
+from oracle import moments
+
+
+@pytest.fixture(scope="module")
+def tre():
+    import paper_2603_08957_amd as t
+
+    t.lib()
+    return t
+
+
+def test_table():
+    m, v = moments.table(7), moments.table(23)
+    assert len(m) == 128 and len(v) == 256
+    assert m[[0, 1, 7, 8, 9, 16, 120]].tolist() == [0, 2.0 ** -9, 7 * 2.0 ** -9, 2.0 ** -6, 9 * 2.0 ** -9, 2.0 ** -5, 256]
+    assert v[[0, 1, 8, 248]].tolist() == [0, 2.0 ** -25, 2.0 ** -22, 256]
+    assert (np.diff(m) > 0).all() and (np.diff(v) > 0).all()
+
+
+def test_rounding_to_the_nearest():
+    x = np.zeros(32, np.float32)
+    x[:7] = [128, 136, 137, 144, 255, 248, 2.0 ** -10]  # 128 to 256 in steps of 16; ties to the even code; half of the least code
+    code, b = moments.encode(x, 7)
+    assert b.tolist() == [127]
+    assert moments.table(7)[code[:7]].tolist() == [128, 128, 144, 144, 256, 256, 0]
+    x[:3] = [-0.0, 200, 1e-30]
+    code, b = moments.encode(np.abs(x), 23)
+    assert code[2] == 1 and code[0] == 0
+
+
+@pytest.mark.parametrize("top", [1.0, 2.0 ** 100, 3.4e38, 2.0 ** -126, 1e-44, 127.99999, 2.0 ** -119, 2.0 ** -120])
+def test_block_byte(top):
+    x = np.full(32, top, np.float32)
+    b = moments.block_bytes(x)[0]
+    y = float(x[0]) * 2.0 ** (127 - b)
+    assert 128 <= y < 256 or (b == 0 and y < 128)
+
+
+def test_round_trip():
+    rng = np.random.default_rng(1)
+    m = (rng.standard_normal(32 * 100) * np.exp(3 * rng.standard_normal(32 * 100))).astype(np.float32)
+    v = np.float32(m) ** 2
+    m[32:64] = 0
+    m[70], v[100] = np.nan, np.inf
+    back_m, back_v = moments.unpack(moments.pack(m, v))
+    assert np.isnan(back_m[64:96]).all() and np.isnan(back_v[96:128]).all() and (back_m[32:64] == 0).all()
+    assert np.array_equal(moments.pack(np.nan_to_num(back_m).astype(np.float32), np.nan_to_num(back_v).astype(np.float32))[:64],
+                          moments.pack(m, v)[:64])
+    ok = np.isfinite(back_m)
+    unit = np.repeat(2.0 ** (moments.block_bytes(m).astype(float) - 127), 32)
+    assert np.all(np.abs(back_m - m)[ok] <= np.maximum(np.abs(m) * 2.0 ** -4, unit * 2.0 ** -10)[ok])
+    ok = np.isfinite(back_v) & (v > 0)
+    assert np.all(back_v[ok] > 0)
+
+
+def test_chance_is_even():
+    """Of 2^16 draws each bit is 1 half the time: off by 5 of the mean's standard deviations, 2^-9 (of 1/2 / 2^8), at most."""
+    for seed, step in ((0, 1), (5, 1), (1 << 40, 7)):
+        a, b, c = moments.chance(1 << 16, seed, step)
+        for x, bits in ((a, 20), (b, 20), (c, 16)):
+            ones = [(x >> k & 1).mean() for k in range(bits)]
+            assert max(abs(np.array(ones) - 0.5)) < 5 * 2.0 ** -9
+            assert abs(np.corrcoef(x[:-1], x[1:])[0, 1]) < 5 * 2.0 ** -8
+        assert abs(np.corrcoef(a, b)[0, 1]) < 5 * 2.0 ** -8
+
+
+# ---------------------------------------------------------------- refusals
+
+A = 1 << 20  # an address that nothing reads
+
+
+def arrays(*values, code="q"):
+    a = array(code, values)
+    return a, ctypes.c_void_p(a.buffer_info()[0])
+
+
+def test_grad_norm_refuses(tre):
+    L, S = tre.lib(), tre.tre.STATUS
+
+    def call(ptrs=(A, 2 * A), types=(0, 1), sizes=(5, 6), most=1.0, out=A, ws=A, wb=1 << 20):
+        p, t, s = arrays(*ptrs), arrays(*types, code="i"), arrays(*sizes)
+        return S[L.tre_grad_norm(len(sizes), p[1], t[1], s[1], most, out, ws, wb, None)]
+
+    assert call(types=(0, 2)) == "TRE_E_DTYPE"
+    assert call(sizes=(5, -1)) == call(sizes=(1 << 42, 1)) == call(sizes=(1 << 62, 1 << 62)) == "TRE_E_SHAPE"
+    assert call(ptrs=(0, A)) == call(ptrs=(A + 2, A)) == call(ptrs=(A, A + 1)) == call(most=math.nan) == "TRE_E_ARG"
+    assert call(out=None) == call(out=A + 2) == call(ws=None) == call(ws=A + 16) == "TRE_E_ARG"
+    assert call(wb=8) == "TRE_E_WORKSPACE"
+    assert tre.grad_norm_workspace_bytes([]) > 0 and tre.grad_norm_workspace_bytes([-1]) == 0
+    assert tre.grad_norm_workspace_bytes([1 << 30, 5]) >= tre.grad_norm_workspace_bytes([5])
+
+
+def test_adamw_refuses(tre):
+    L, S = tre.lib(), tre.tre.STATUS
+
+    def call(params=(A, 2 * A), ptypes=(0, 1), grads=(3 * A, 4 * A), gtypes=(1, 0), sizes=(5, 6), state=A * 8, opt=None, **kw):
+        o = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.1, grad_scale=1.0, step=1, bits=32)
+        o.update(kw)
+        o = tre.tre.AdamwOptions(**o)
+        a = [arrays(*params), arrays(*ptypes, code="i"), arrays(*grads), arrays(*gtypes, code="i"), arrays(*sizes)]
+        return S[L.tre_adamw(len(sizes), *(x[1] for x in a), state, None if opt is False else ctypes.byref(o), None)]
+
+    for bad in (dict(lr=-1), dict(lr=math.nan), dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(eps=0.0),
+                dict(eps=1e-60), dict(eps=math.inf), dict(weight_decay=-1), dict(grad_scale=math.nan), dict(step=0), dict(bits=16),
+                dict(state=None), dict(state=A + 8), dict(opt=False), dict(lr_dev=A + 2), dict(step_dev=A + 4),
+                dict(grad_scale_dev=A + 1), dict(params=(A, A)), dict(params=(A, A + 16)), dict(params=(0, A)), dict(grads=(0, A)),
+                dict(params=(A + 2, 2 * A)), dict(grads=(A, 4 * A)), dict(grads=(3 * A, A + 16)), dict(grads=(A - 4, 4 * A))):
+        assert call(**bad) == "TRE_E_ARG", bad
+    assert call(ptypes=(0, 3)) == call(gtypes=(-1, 0)) == "TRE_E_DTYPE"
+    assert call(sizes=(1, -5)) == call(sizes=(1 << 42, 1 << 42)) == "TRE_E_SHAPE"
+    assert call(sizes=(0, 0)) == "TRE_OK"
+    s = arrays(5, 64, 65, 0)
+    assert L.tre_adamw_state_bytes(4, s[1], 32) == 8 * (32 + 64 + 96)
+    assert L.tre_adamw_state_bytes(4, s[1], 8) == (2 * 192 + 12)
+    assert L.tre_adamw_state_bytes(4, s[1], 16) == 0
+    assert S[L.tre_adamw_moments(A, 32, A, A, 2, None)] == "TRE_E_DTYPE"
+    assert S[L.tre_adamw_moments(A, 33, A, A, 0, None)] == S[L.tre_adamw_moments(A, -32, A, A, 0, None)] == "TRE_E_SHAPE"
+    assert S[L.tre_adamw_moments(A, 32, None, A, 0, None)] == S[L.tre_adamw_moments(A, 32, A, A + 8, 0, None)] == "TRE_E_ARG"
+
+
+def test_log_probs_refuses(tre):
+    L, S = tre.lib(), tre.tre.STATUS
+    need = L.tre_log_probs_workspace_bytes(1, 1 << 20, 1 << 20, 0, 4)
+    assert need > 0 and L.tre_log_probs_workspace_bytes(1 << 20, 1 << 20, 1 << 20, 0, 4) == 0
+    assert L.tre_log_probs_workspace_bytes(1, 100, 7, 0, 0) == L.tre_log_probs_workspace_bytes(1, 100, 100, 2, 0) == 0
+
+    def call(x=A, dt=0, n=1, vocab=1 << 20, cols=1 << 20, rs=1 << 20, ts=0, ids=A, ib=8, scale=1.0, lp=A, lse=A, stats=A, ent=None, top=0,
+             ti=None, tl=None, status=None, ws=A, wb=1 << 30):
+        return S[L.tre_log_probs(x, dt, n, vocab, cols, rs, ts, ids, ib, scale, lp, lse, stats, ent, top, ti, tl, status, ws, wb, None)]
+
+    assert call(dt=2) == call(dt=-1) == "TRE_E_DTYPE"
+    for bad in (dict(n=-1), dict(n=2 ** 31 - 1), dict(vocab=0), dict(vocab=2 ** 31), dict(cols=7), dict(cols=0), dict(cols=2 ** 21),
+                dict(rs=-1), dict(ts=-1), dict(rs=2 ** 61), dict(top=-1), dict(top=65), dict(vocab=3, cols=3, top=4)):
+        assert call(**bad) == "TRE_E_SHAPE", bad
+    for bad in (dict(x=None), dict(x=A + 2), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(scale=3e38),
+                dict(ids=A + 4), dict(ib=2), dict(lp=None), dict(ids=None), dict(lse=None), dict(stats=None), dict(stats=A + 1),
+                dict(top=1), dict(top=1, ti=A), dict(top=1, ti=A, tl=A + 2), dict(status=A + 4), dict(ws=None), dict(ws=A + 8)):
+        assert call(**bad) == "TRE_E_ARG", bad
+    assert call(wb=0) == "TRE_E_WORKSPACE"
+    assert call(n=0, x=None, ids=None, lp=None) == "TRE_OK"
+
+    def grad(x=A, dt=0, n=4, vocab=100, cols=100, rs=100, ts=0, stats=A, ids=A, ib=8, scale=1.0, g=A, gl=None, gh=None, ent=None, out=8 * A,
+             odt=0, ors=100, ots=0, status=None):
+        return S[L.tre_log_probs_grad(x, dt, n, vocab, cols, rs, ts, stats, ids, ib, scale, g, gl, gh, ent, out, odt, ors, ots, status,
+                                      None)]
+
+    assert grad(dt=2) == grad(odt=2) == "TRE_E_DTYPE"
+    for bad in (dict(n=-1), dict(cols=7), dict(ors=99), dict(ors=0), dict(cols=50, ors=50, ots=150), dict(cols=50, ots=50, ors=99),
+                dict(cols=50, ors=50, ots=0), dict(ors=2 ** 60)):
+        assert grad(**bad) == "TRE_E_SHAPE", bad
+    for bad in (dict(g=None), dict(ids=None), dict(gh=A), dict(stats=None), dict(out=None), dict(out=A + 2), dict(g=A + 2), dict(scale=0),
+                dict(out=A, ors=200), dict(out=A, odt=1)):
+        assert grad(**bad) == "TRE_E_ARG", bad
+    assert grad(n=0, x=None, g=None, ids=None) == "TRE_OK"
+
+
+def test_binding_refuses(tre):
+    import torch
+
+    def refused(status, f, *a, **kw):
+        with pytest.raises(tre.TreError) as e:
+            f(*a, **kw)
+        assert e.value.status == status
+
+    x = torch.zeros(3, 8)
+    refused("TRE_E_ARG", tre.log_probs, x)
+    refused("TRE_E_DTYPE", tre.log_probs, x.double())
+    refused("TRE_E_SHAPE", tre.log_probs, x[0])
+    refused("TRE_E_SHAPE", tre.log_probs, torch.zeros(3, 0))
+    refused("TRE_E_ARG", tre.log_probs_grad, x, torch.zeros(3, 2))
+    refused("TRE_E_ARG", tre.grad_norm, [x])
+    refused("TRE_E_ARG", tre.grad_norm, [])
+    refused("TRE_E_ARG", tre.grad_norm, [None])
+    refused("TRE_E_ARG", tre.adamw_state, [x])
+    refused("TRE_E_ARG", tre.adamw, [x], [x], torch.zeros(64), 1, 1e-3)
+    refused("TRE_E_ARG", tre.adamw_moments, torch.zeros(64))
+    refused("TRE_E_DTYPE", tre.adamw_moments, torch.zeros(64, dtype=torch.int32))
