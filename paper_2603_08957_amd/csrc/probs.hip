@@ -19,6 +19,8 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
+// Runs of a lane in flight together.
+constexpr int kRuns = 4;
 
 // Scores as rows (one tile) or as the tiles of a relation keyed by the word's
 // tile: x[i, v] at (v / cols) tile_stride + i row_stride + v % cols.  A row is
@@ -56,23 +58,83 @@ __device__ inline Place place_of(const Scores& g, uint32_t q) {
     return {tile, q - tile * g.runs};
 }
 
-// The E elements of a run, what lies behind a tile's row -inf.
-template <int E, bool RAGGED, typename T>
-__device__ inline void load_scores(const Scores& g, const T* row, Place p, float (&v)[E]) {
-    const T* at = row + p.tile * g.tile_stride + int64_t(p.at) * E;
-    if (!RAGGED || (p.at + 1) * E <= g.cols) {
-        load_all(at, v);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < E; i++) v[i] = p.at * E + i < g.cols ? load1(at + i) : -kInf;
+// How runs lie on a tile's row: it is made of whole ones, its last one is taken
+// from the row's end (and overlaps the one before), or the row is shorter than one.
+enum Fit { kWhole, kOverlap, kShort };
+Fit fit_of(const Scores& g, int elems) {
+    return g.cols % elems == 0 ? kWhole : int(g.cols) >= elems ? kOverlap : kShort;
 }
+
+typedef uint32_t u32x4_1 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_1 __attribute__((ext_vector_type(2), aligned(2)));
+
+// E elements of one access, as they come: what is done with them waits, the loads do not.
+template <typename T, int E>
+struct Raw {
+    uint32_t w[E * sizeof(T) / 4];
+    __device__ void load(const T* at) {
+        if constexpr (sizeof(w) == 16) {
+            const u32x4_1 x = *reinterpret_cast<const u32x4_1*>(at);
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = x[i];
+        } else {
+            const u32x2_1 x = *reinterpret_cast<const u32x2_1*>(at);
+            w[0] = x[0];
+            w[1] = x[1];
+        }
+    }
+    __device__ void load_some(const T* at, int n) {  // of at least one
+#pragma unroll
+        for (int i = 0; i < int(sizeof(w) / 4); i++) w[i] = 0;
+#pragma unroll
+        for (int i = 0; i < E; i++) {
+            if (i >= n) break;
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(at[i]);
+            else w[i / 2] |= uint32_t(at[i]) << (16 * (i & 1));
+        }
+    }
+    __device__ float value(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+};
+
+// A run of a row and where it lies.
+template <typename T, int E, int FIT>
+struct Run {
+    Raw<T, E> raw;
+    uint32_t tile, start, own;  // columns from `start` on, its own from `own` on
+    __device__ void find(const Scores& g, uint32_t q) {
+        const Place p = place_of(g, q);
+        tile = p.tile;
+        own = start = p.at * E;
+        if constexpr (FIT == kOverlap) start = min(own, g.cols - E);
+    }
+    __device__ void load(const Scores& g, const T* row, uint32_t q) {
+        find(g, q);
+        const T* at = row + tile * g.tile_stride + start;
+        if constexpr (FIT == kShort) raw.load_some(at, int(g.cols));
+        else raw.load(at);
+    }
+    // Its scores, -inf for columns that are not its own.
+    __device__ void values(const Scores& g, float (&v)[E]) const {
+#pragma unroll
+        for (int i = 0; i < E; i++) {
+            v[i] = raw.value(i);
+            if constexpr (FIT == kOverlap) v[i] = start + i >= own ? v[i] : -kInf;
+            if constexpr (FIT == kShort) v[i] = i < int(g.cols) ? v[i] : -kInf;
+        }
+    }
+    __device__ bool whole() const { return FIT == kWhole || (FIT == kOverlap && start == own); }
+    __device__ bool has(const Scores& g, int i) const { return FIT == kShort ? i < int(g.cols) : start + i >= own; }
+};
 
 // ------------------------------------------------------------ top words
 //
 // The best words of a wavefront lie in its lanes, the best first, as keys of 64
 // bits: the score in an order of whole numbers, then the word, lower words
-// first.  0: none.  A NaN is taken as -inf.
+// first.  0: none.  Words that cannot come (-inf; a NaN is taken as that) have no
+// place in it: where a row has too few others they are found at the end.
 
 __device__ inline uint32_t order_of(float x) {
     x = x != x ? -kInf : x + 0.f;  // (-0 is 0)
@@ -83,16 +145,38 @@ __device__ inline float of_order(uint32_t o) {
     return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 constexpr uint32_t kOrderLowest = 0x007fffffu;  // order_of(-inf)
+// The highest order, less its lower 16 bits, that at least k lanes reach; that of -inf if fewer have another.
+__device__ inline uint32_t reached(uint32_t order, int k) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int b = 31; b >= 16; b--) {
+        const uint32_t c = t | 1u << b;
+        if (__popcll(__ballot(order >= c)) >= k) t = c;
+    }
+    return max(t, kOrderLowest);
+}
 
 __device__ inline uint64_t key_of(float x, uint32_t word) { return uint64_t(order_of(x)) << 32 | uint32_t(~word); }
 
+// The value of the lane whose number differs by MASK: no LDS.
 template <int MASK>
 __device__ inline uint32_t swap_lanes(uint32_t x) {
     if constexpr (MASK == 1) return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, true);
     else if constexpr (MASK == 2) return __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, true);
+    else if constexpr (MASK == 4)  // eight lanes turned round, then each four
+        return __builtin_amdgcn_update_dpp(0, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, true), 0x1B, 0xf, 0xf, true);
     else if constexpr (MASK == 8) return __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, true);
-    else if constexpr (MASK < 32) return __builtin_amdgcn_ds_swizzle(x, MASK << 10 | 0x1f);
-    else return __shfl_xor(x, MASK);
+    else if constexpr (MASK == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
+}
+template <int MASK>
+__device__ inline float swap_lanes(float x) {
+    return __uint_as_float(swap_lanes<MASK>(__float_as_uint(x)));
 }
 template <int MASK>
 __device__ inline uint64_t swap_keys(uint64_t k) {
@@ -173,6 +257,12 @@ __device__ inline Sums join(Sums a, Sums b, float scale2) {
     return {m, fa * a.s + fb * b.s, fa * (a.t + a.s * da) + fb * (b.t + b.s * db)};
 }
 
+template <int MASK, bool ENT>
+__device__ inline void join_lanes(Sums& u, float scale2) {
+    u = join(u, {swap_lanes<MASK>(u.m), swap_lanes<MASK>(u.s), ENT ? swap_lanes<MASK>(u.t) : 0.f}, scale2);
+    if constexpr (MASK < 32) join_lanes<MASK * 2, ENT>(u, scale2);
+}
+
 struct ProbArgs {
     Scores g;
     const void* x;
@@ -189,8 +279,30 @@ struct ProbArgs {
 };
 
 template <typename T>
-__device__ inline void put_row(const ProbArgs& a, int64_t row, Sums u, const Top& top) {
+__device__ inline const T* score_at(const ProbArgs& a, int64_t row, int64_t word) {
+    const int64_t tile = word / a.g.cols;
+    return static_cast<const T*>(a.x) + tile * a.g.tile_stride + row * a.g.row_stride + (word - tile * a.g.cols);
+}
+
+// The first words that cannot come, behind those that can.
+template <typename T>
+__device__ inline void fill_top(const ProbArgs& a, int64_t row, Top& top) {
     const int lane = threadIdx.x & 63;
+    int have = __popcll(__ballot(top.key != 0));
+    for (int64_t w = lane; have < a.top && w - lane < a.g.vocab; w += 64) {
+        bool dead = false;
+        if (w < a.g.vocab) dead = !(load1(score_at<T>(a, row, w)) > -kInf);
+        for (uint64_t m = __ballot(dead); m && have < a.top; m &= m - 1, have++) {
+            const uint32_t word = uint32_t(w - lane) + uint32_t(__ffsll((unsigned long long)m)) - 1;
+            if (lane == have) top.key = uint64_t(kOrderLowest) << 32 | uint32_t(~word);
+        }
+    }
+}
+
+template <typename T>
+__device__ inline void put_row(const ProbArgs& a, int64_t row, Sums u, Top& top) {
+    const int lane = threadIdx.x & 63;
+    if (a.top_ids && top.last == 0) fill_top<T>(a, row, top);
     const bool empty = u.s == 0.f;
     const float m = empty ? -kInf : u.m, logs = logf(u.s);
     if (a.top_ids && lane < a.top) {
@@ -210,8 +322,7 @@ __device__ inline void put_row(const ProbArgs& a, int64_t row, Sums u, const Top
         const int64_t id = token(a.ids, a.id_bytes, row);
         float lp = 0.f;
         if (id >= 0 && id < a.g.vocab) {
-            const int64_t tile = id / a.g.cols;
-            const float v = load1(static_cast<const T*>(a.x) + tile * a.g.tile_stride + row * a.g.row_stride + (id - tile * a.g.cols));
+            const float v = load1(score_at<T>(a, row, id));
             lp = empty ? -kInf : (v - m) * a.scale - logs;
         } else if (id >= 0 && a.status) {
             *a.status = TRE_E_KEYRANGE;
@@ -220,11 +331,8 @@ __device__ inline void put_row(const ProbArgs& a, int64_t row, Sums u, const Top
     }
 }
 
-// Runs of a lane in flight together.
-constexpr int kRuns = 4;
-
 // W wavefronts to a row, or to a part of it.
-template <typename T, bool RAGGED, bool TOP, bool ENT, int W>
+template <typename T, int FIT, bool TOP, bool ENT, int W>
 __global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
     constexpr int E = 16 / sizeof(T);
     constexpr uint32_t kStep = 64 * kRuns;
@@ -248,43 +356,43 @@ __global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
         }
     }
     for (uint32_t b = q0 + (W > 1 ? wave : 0) * kStep; b < q1; b += W * kStep) {
-        float v[kRuns][E];
-        Place p[kRuns];
+        Run<T, E, FIT> r[kRuns];
+#pragma unroll
+        for (int j = 0; j < kRuns; j++) r[j].load(a.g, x, min(b + j * 64 + lane, q1 - 1));
+        float v[kRuns][E], most[kRuns];
 #pragma unroll
         for (int j = 0; j < kRuns; j++) {
-            const uint32_t q = b + j * 64 + lane;
-            p[j] = place_of(a.g, q);
-            if (q < q1) {
-                load_scores<E, RAGGED>(a.g, x, p[j], v[j]);
-            } else {
+            r[j].values(a.g, v[j]);
+            if (b + kStep > q1) {
 #pragma unroll
-                for (int i = 0; i < E; i++) v[j][i] = -kInf;
+                for (int i = 0; i < E; i++) v[j][i] = b + j * 64 + lane < q1 ? v[j][i] : -kInf;
             }
+            most[j] = -FLT_MAX;
+#pragma unroll
+            for (int i = 0; i < E; i++) most[j] = fmaxf(most[j], v[j][i]);
         }
-        float most = -FLT_MAX;
+        float all = most[0];
 #pragma unroll
-        for (int j = 0; j < kRuns; j++)
-#pragma unroll
-            for (int i = 0; i < E; i++) most = fmaxf(most, v[j][i]);
+        for (int j = 1; j < kRuns; j++) all = fmaxf(all, most[j]);
         if constexpr (TOP) {
-            // what the other wavefronts have bars lower scores here too, but not equal ones, whose words may come first
+            // A score has a place if it is higher than this wavefront's last, whose words come before, and not lower than what
+            // the other wavefronts have.  At first so many lanes' highest scores bar all that is lower.
+            uint32_t least = max(uint32_t(top.last >> 32), kOrderLowest) + 1;
             uint32_t others = 0;
-            if constexpr (W > 1) others = *static_cast<volatile uint32_t*>(&bar);
-            others = __builtin_amdgcn_readfirstlane(others);
-            const bool full = top.last != 0, barred = others > kOrderLowest;
-            float limit = full ? of_order(uint32_t(top.last >> 32)) : -kInf;
-            if (barred) limit = fmaxf(limit, of_order(others == 0x80000000u ? others - 2 : others - 1));  // (0 and -0 are equal)
-            const bool any = !full && !barred;
-            if (any || __ballot(most > limit)) {
+            if constexpr (W > 1) others = __builtin_amdgcn_readfirstlane(*static_cast<volatile uint32_t*>(&bar));
+            least = max(least, others);
+            if (top.last == 0) least = max(least, reached(order_of(all), a.top));
+            float limit = of_order(least);
+            if (__ballot(all >= limit)) {
 #pragma unroll
                 for (int j = 0; j < kRuns; j++) {
-                    const uint32_t q = b + j * 64 + lane;
+                    if (!__ballot(most[j] >= limit)) continue;
 #pragma unroll
                     for (int i = 0; i < E; i++) {
-                        bool in = v[j][i] > limit;
-                        if (any) in = q < q1 && p[j].at * E + i < a.g.cols;
-                        const uint64_t from = __ballot(in);
-                        if (from) top.take(key_of(v[j][i], p[j].tile * a.g.cols + p[j].at * E + i), from);
+                        const uint64_t from = __ballot(v[j][i] >= limit);
+                        if (!from) continue;
+                        top.take(key_of(v[j][i], r[j].tile * a.g.cols + r[j].start + i), from);
+                        limit = fmaxf(limit, of_order(max(uint32_t(top.last >> 32), kOrderLowest + 1)));
                     }
                 }
                 if constexpr (W > 1) {
@@ -292,7 +400,7 @@ __global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
                 }
             }
         }
-        const float m = fmaxf(u.m, most), d = fmaxf((u.m - m) * a.scale2, -2000.f), f = __builtin_amdgcn_exp2f(d);
+        const float m = fmaxf(u.m, all), d = fmaxf((u.m - m) * a.scale2, -2000.f), f = __builtin_amdgcn_exp2f(d);
         if constexpr (ENT) u.t = f * (u.t + u.s * d);
         u.s *= f;
         u.m = m;
@@ -305,11 +413,7 @@ __global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
                 if constexpr (ENT) u.t += e * fmaxf(z, -2000.f);  // (no 0 * inf)
             }
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const Sums v{__shfl_xor(u.m, o), __shfl_xor(u.s, o), ENT ? __shfl_xor(u.t, o) : 0.f};
-        u = join(u, v, a.scale2);
-    }
+    join_lanes<1, ENT>(u, a.scale2);
     if constexpr (W > 1) {
         if (lane == 0) sums[wave] = u;
         if constexpr (TOP) keys[wave][lane] = lane < a.top ? top.key : 0;
@@ -329,21 +433,27 @@ __global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
     }
 }
 
-// The parts of a row joined: a wavefront to a row.
+// The parts of a row joined: a wavefront to a row, so many lists of top words in flight together.
+constexpr int kLists = 8;
+
 template <typename T>
 __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
     const int lane = threadIdx.x;
     const int64_t row = block_index();
     if (row >= a.g.n) return;
     Sums u = lane < int(a.splits) ? a.part[row * a.splits + lane] : Sums{-FLT_MAX, 0.f, 0.f};
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) u = join(u, {__shfl_xor(u.m, o), __shfl_xor(u.s, o), __shfl_xor(u.t, o)}, a.scale2);
+    join_lanes<1, true>(u, a.scale2);
     Top top;
     top.init(a.top_ids ? a.top : 1);
     if (a.top_ids) {
-        for (uint32_t i = 0; i < a.splits; i++) {
-            const int from = 63 - lane;
-            top.merge(from < a.top ? a.part_keys[(row * a.splits + i) * a.top + from] : 0);
+        const int from = 63 - lane;
+        const uint64_t* lists = a.part_keys + row * a.splits * a.top + from;
+        for (uint32_t b = 0; b < a.splits; b += kLists) {
+            uint64_t k[kLists];
+#pragma unroll
+            for (int i = 0; i < kLists; i++) k[i] = from < a.top && b + i < a.splits ? lists[(b + i) * a.top] : 0;
+#pragma unroll
+            for (int i = 0; i < kLists; i++) top.merge(k[i]);
         }
     }
     put_row<T>(a, row, u, top);
@@ -369,23 +479,27 @@ Cut cut_of(const Scores& g) {
     return c;
 }
 
-template <typename T, bool RAGGED, bool TOP, bool ENT>
+template <typename T, int FIT, bool TOP, bool ENT>
 hipError_t probs3(ProbArgs a, Cut c, hipStream_t s) {
-    if (c.wave) k_probs<T, RAGGED, TOP, ENT, 1><<<grid_of((a.g.n + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
-    else k_probs<T, RAGGED, TOP, ENT, kWaves><<<grid_of(a.g.n * c.splits), kThreads, 0, s>>>(a);
+    if (c.wave) k_probs<T, FIT, TOP, ENT, 1><<<grid_of((a.g.n + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
+    else k_probs<T, FIT, TOP, ENT, kWaves><<<grid_of(a.g.n * c.splits), kThreads, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.splits == 1) return e;
     k_probs_join<T><<<grid_of(a.g.n), 64, 0, s>>>(a);
     return hipGetLastError();
 }
-template <typename T, bool RAGGED>
+template <typename T, int FIT>
 hipError_t probs2(const ProbArgs& a, Cut c, hipStream_t s) {
-    if (a.top_ids) return a.entropy ? probs3<T, RAGGED, true, true>(a, c, s) : probs3<T, RAGGED, true, false>(a, c, s);
-    return a.entropy ? probs3<T, RAGGED, false, true>(a, c, s) : probs3<T, RAGGED, false, false>(a, c, s);
+    if (a.top_ids) return a.entropy ? probs3<T, FIT, true, true>(a, c, s) : probs3<T, FIT, true, false>(a, c, s);
+    return a.entropy ? probs3<T, FIT, false, true>(a, c, s) : probs3<T, FIT, false, false>(a, c, s);
 }
 template <typename T>
 hipError_t probs1(ProbArgs a, Cut c, hipStream_t s) {
-    return a.g.cols % (16 / sizeof(T)) ? probs2<T, true>(a, c, s) : probs2<T, false>(a, c, s);
+    switch (fit_of(a.g, 16 / sizeof(T))) {
+        case kWhole: return probs2<T, kWhole>(a, c, s);
+        case kOverlap: return probs2<T, kOverlap>(a, c, s);
+        default: return probs2<T, kShort>(a, c, s);
+    }
 }
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
@@ -407,7 +521,7 @@ struct ProbGradArgs {
     int32_t id_bytes;
 };
 
-template <typename TI, typename TO, bool RAGGED, bool ENT>
+template <typename TI, typename TO, int FIT, bool ENT>
 __global__ __launch_bounds__(kThreads) void k_probs_grad(ProbGradArgs a) {
     constexpr int E = lane_elems<TI, TO>();
     const int lane = threadIdx.x & 63;
@@ -433,54 +547,57 @@ __global__ __launch_bounds__(kThreads) void k_probs_grad(ProbGradArgs a) {
     one *= a.scale;
     if (m == -kInf) one = c0 = c1 = 0.f;  // a row of no words
     const bool zero = c0 == 0.f && c1 == 0.f && one == 0.f;
-    const int64_t id_tile = id >= 0 ? id / a.g.cols : -1, id_at = id >= 0 ? id - id_tile * a.g.cols : -1;
+    const uint32_t id_tile = id >= 0 ? uint32_t(id) / a.g.cols : ~0u, id_at = uint32_t(id) - id_tile * a.g.cols;
     const TI* x = static_cast<const TI*>(a.x) + row * a.g.row_stride;
     TO* out = static_cast<TO*>(a.out) + row * a.out_row_stride;
-    float v[kRuns][E];
-    Place p[kRuns];
+    Run<TI, E, FIT> r[kRuns];
+    if (!zero) {
 #pragma unroll
-    for (int j = 0; j < kRuns; j++) {
-        const uint32_t q = (part * kRuns + j) * 64 + lane;
-        p[j] = place_of(a.g, q);
-        if (!zero && q < a.g.total) load_scores<E, RAGGED>(a.g, x, p[j], v[j]);
+        for (int j = 0; j < kRuns; j++) r[j].load(a.g, x, min((part * kRuns + j) * 64 + lane, a.g.total - 1));
     }
 #pragma unroll
     for (int j = 0; j < kRuns; j++) {
         const uint32_t q = (part * kRuns + j) * 64 + lane;
         if (q >= a.g.total) break;
         float y[E];
+        if (zero) {
+            r[j].find(a.g, q);
 #pragma unroll
-        for (int i = 0; i < E; i++) {
-            y[i] = 0.f;
-            if (!zero) {
-                const float z = (v[j][i] - m) * a.scale2 - logs2, e = __builtin_amdgcn_exp2f(z);
+            for (int i = 0; i < E; i++) y[i] = 0.f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; i++) {
+                const float z = (r[j].raw.value(i) - m) * a.scale2 - logs2, e = __builtin_amdgcn_exp2f(z);
                 y[i] = e * (ENT ? c0 + c1 * fmaxf(z, -2000.f) : c0);
-                if (p[j].tile == id_tile && p[j].at * E + i == id_at) y[i] += one;
+                if (r[j].tile == id_tile && r[j].start + i == id_at) y[i] += one;
             }
         }
-        TO* at = out + p[j].tile * a.out_tile_stride + int64_t(p[j].at) * E;
-        if (!RAGGED || (p[j].at + 1) * E <= a.g.cols) {
+        TO* at = out + r[j].tile * a.out_tile_stride + r[j].start;
+        if (r[j].whole()) {
             store_all<true>(at, y);
         } else {
 #pragma unroll
             for (int i = 0; i < E; i++)
-                if (p[j].at * E + i < a.g.cols) store1(at + i, y[i]);
+                if (r[j].has(a.g, i)) store1(at + i, y[i]);
         }
     }
 }
 
+template <typename TI, typename TO, int FIT>
+void k_probs_grad_of(const ProbGradArgs& a, dim3 grid, hipStream_t s) {
+    if (a.by_entropy) k_probs_grad<TI, TO, FIT, true><<<grid, kThreads, 0, s>>>(a);
+    else k_probs_grad<TI, TO, FIT, false><<<grid, kThreads, 0, s>>>(a);
+}
 template <typename TI, typename TO>
 hipError_t probs_grad(ProbGradArgs a, const ScoreLayout& l, hipStream_t s) {
     constexpr int E = lane_elems<TI, TO>();
     a.g = scores_of(l, E);
     a.parts = (a.g.total + 64 * kRuns - 1) / (64 * kRuns);
     const dim3 grid = grid_of((l.n * a.parts + kWaves - 1) / kWaves);
-    if (l.cols % E) {
-        if (a.by_entropy) k_probs_grad<TI, TO, true, true><<<grid, kThreads, 0, s>>>(a);
-        else k_probs_grad<TI, TO, true, false><<<grid, kThreads, 0, s>>>(a);
-    } else {
-        if (a.by_entropy) k_probs_grad<TI, TO, false, true><<<grid, kThreads, 0, s>>>(a);
-        else k_probs_grad<TI, TO, false, false><<<grid, kThreads, 0, s>>>(a);
+    switch (fit_of(a.g, E)) {
+        case kWhole: k_probs_grad_of<TI, TO, kWhole>(a, grid, s); break;
+        case kOverlap: k_probs_grad_of<TI, TO, kOverlap>(a, grid, s); break;
+        default: k_probs_grad_of<TI, TO, kShort>(a, grid, s); break;
     }
     return hipGetLastError();
 }
