@@ -236,6 +236,7 @@ struct Top {
             merge(k);
             return;
         }
+#pragma unroll 1
         for (; from; from &= from - 1) {
             const int lane = __ffsll((unsigned long long)from) - 1;
             insert(uint64_t(uint32_t(__builtin_amdgcn_readlane(int(mine >> 32), lane))) << 32 |
@@ -331,14 +332,30 @@ __device__ inline void put_row(const ProbArgs& a, int64_t row, Sums u, Top& top)
     }
 }
 
-// W wavefronts to a row, or to a part of it.
+// Element `at` < N of a lane's runs, from FROM on.
+template <int N, int E, int FROM = 0>
+__device__ inline float pick(const float (&v)[kRuns][E], uint32_t at) {
+    if constexpr (N == 1) return v[FROM / E][FROM % E];
+    else {
+        const float low = pick<N / 2, E, FROM>(v, at), high = pick<N / 2, E, FROM + N / 2>(v, at);
+        return at & (N / 2) ? high : low;
+    }
+}
+
+// W wavefronts to a row, or to a part of it; with one, a workgroup has kWaves rows.
+//
+// Top words.  A score has a place in a wavefront's list if it is higher than the
+// list's last, whose words come before, and not lower than what the row's other
+// wavefronts have (`bar`).  Lists that fill from nothing would take hundreds of
+// scores in: so at first a score that top / W lanes of every wavefront reach, or
+// top lanes of one, bars all that is lower.
 template <typename T, int FIT, bool TOP, bool ENT, int W>
-__global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
+__global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a) {
     constexpr int E = 16 / sizeof(T);
     constexpr uint32_t kStep = 64 * kRuns;
-    __shared__ Sums sums[kWaves];
+    __shared__ Sums sums[W];
     __shared__ uint64_t keys[TOP && W > 1 ? W : 1][64];
-    __shared__ uint32_t bar;
+    __shared__ uint32_t bar, reach[W];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t task = W > 1 ? block_index() : block_index() * kWaves + wave;
     const int64_t row = a.splits > 1 ? task / a.splits : task;
@@ -348,6 +365,7 @@ __global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
     const T* x = static_cast<const T*>(a.x) + row * a.g.row_stride;
     Sums u{-FLT_MAX, 0.f, 0.f};
     Top top;
+    uint32_t known = 0;
     if constexpr (TOP) {
         top.init(a.top);
         if constexpr (W > 1) {
@@ -355,7 +373,10 @@ __global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
             __syncthreads();
         }
     }
-    for (uint32_t b = q0 + (W > 1 ? wave : 0) * kStep; b < q1; b += W * kStep) {
+#pragma unroll 1
+    for (uint32_t b0 = q0; b0 < q1; b0 += W * kStep) {
+        const uint32_t b = b0 + (W > 1 ? wave : 0) * kStep;
+        if (b >= q1 && !(TOP && W > 1 && b0 == q0)) break;  // (all come to the first barrier)
         Run<T, E, FIT> r[kRuns];
 #pragma unroll
         for (int j = 0; j < kRuns; j++) r[j].load(a.g, x, min(b + j * 64 + lane, q1 - 1));
@@ -375,28 +396,40 @@ __global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
 #pragma unroll
         for (int j = 1; j < kRuns; j++) all = fmaxf(all, most[j]);
         if constexpr (TOP) {
-            // A score has a place if it is higher than this wavefront's last, whose words come before, and not lower than what
-            // the other wavefronts have.  At first so many lanes' highest scores bar all that is lower.
-            uint32_t least = max(uint32_t(top.last >> 32), kOrderLowest) + 1;
-            uint32_t others = 0;
-            if constexpr (W > 1) others = __builtin_amdgcn_readfirstlane(*static_cast<volatile uint32_t*>(&bar));
-            least = max(least, others);
-            if (top.last == 0) least = max(least, reached(order_of(all), a.top));
+            if (W > 1 && b0 == q0) {
+                const uint32_t own = reached(order_of(all), (a.top + W - 1) / W);
+                if (lane == 0) reach[wave] = own;
+                __syncthreads();
+                known = reach[0];
+#pragma unroll
+                for (int w = 1; w < W; w++) known = min(known, reach[w]);
+            } else if (W > 1) {
+                known = max(known, *static_cast<volatile uint32_t*>(&bar));
+            }
+            known = __builtin_amdgcn_readfirstlane(known);
+            uint32_t least = max(max(uint32_t(top.last >> 32), kOrderLowest) + 1, known);
+            if (top.last == 0 && known <= kOrderLowest) least = max(least, reached(order_of(all), a.top));
             float limit = of_order(least);
             if (__ballot(all >= limit)) {
+                // a bit for each of a lane's scores that may have a place; then one of each lane at a time
+                uint32_t mine = 0;
 #pragma unroll
-                for (int j = 0; j < kRuns; j++) {
-                    if (!__ballot(most[j] >= limit)) continue;
+                for (int j = 0; j < kRuns; j++)
 #pragma unroll
-                    for (int i = 0; i < E; i++) {
-                        const uint64_t from = __ballot(v[j][i] >= limit);
-                        if (!from) continue;
-                        top.take(key_of(v[j][i], r[j].tile * a.g.cols + r[j].start + i), from);
-                        limit = fmaxf(limit, of_order(max(uint32_t(top.last >> 32), kOrderLowest + 1)));
-                    }
+                    for (int i = 0; i < E; i++) mine |= v[j][i] >= limit ? 1u << (j * E + i) : 0u;
+#pragma unroll 1
+                while (__ballot(mine != 0)) {
+                    const int at = mine ? __ffs(mine) - 1 : 0;
+                    const float y = pick<kRuns * E, E>(v, uint32_t(at));
+                    Run<T, E, FIT> run;
+                    run.find(a.g, b + uint32_t(at) / E * 64 + lane);
+                    const uint64_t from = __ballot(mine != 0 && y >= limit);
+                    if (from) top.take(key_of(y, run.tile * a.g.cols + run.start + uint32_t(at) % E), from);
+                    mine &= mine - 1;
+                    limit = fmaxf(limit, of_order(max(uint32_t(top.last >> 32), kOrderLowest + 1)));
                 }
                 if constexpr (W > 1) {
-                    if (lane == 0 && uint32_t(top.last >> 32) > others) atomicMax(&bar, uint32_t(top.last >> 32));
+                    if (lane == 0 && uint32_t(top.last >> 32) > known) atomicMax(&bar, uint32_t(top.last >> 32));
                 }
             }
         }
@@ -416,14 +449,20 @@ __global__ __launch_bounds__(kThreads) void k_probs(ProbArgs a) {
     join_lanes<1, ENT>(u, a.scale2);
     if constexpr (W > 1) {
         if (lane == 0) sums[wave] = u;
-        if constexpr (TOP) keys[wave][lane] = lane < a.top ? top.key : 0;
-        __syncthreads();
+        if constexpr (TOP) {
+            // lists in pairs: those of the upper half go to the lower one
+#pragma unroll 1
+            for (int h = W / 2; h > 0; h /= 2) {
+                if (wave >= h && wave < 2 * h) keys[wave][lane] = lane < a.top ? top.key : 0;
+                __syncthreads();
+                if (wave < h) top.merge(keys[wave + h][63 - lane]);
+            }
+        } else {
+            __syncthreads();
+        }
         if (wave) return;
 #pragma unroll
-        for (int w = 1; w < W; w++) {
-            u = join(u, sums[w], a.scale2);
-            if constexpr (TOP) top.merge(keys[w][63 - lane]);
-        }
+        for (int w = 1; w < W; w++) u = join(u, sums[w], a.scale2);
     }
     if (a.splits > 1) {
         if (lane == 0) a.part[task] = u;
@@ -453,27 +492,32 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
 #pragma unroll
             for (int i = 0; i < kLists; i++) k[i] = from < a.top && b + i < a.splits ? lists[(b + i) * a.top] : 0;
 #pragma unroll
-            for (int i = 0; i < kLists; i++) top.merge(k[i]);
+            for (int i = 0; i < kLists; i++)
+                if (b + i < a.splits) top.merge(k[i]);
         }
     }
     put_row<T>(a, row, u, top);
 }
 
-// A row of few scores is one wavefront's, and few rows are cut so that there are
-// workgroups for the chip.
-constexpr int64_t kWaveRuns = 4 * 64 * kRuns;   // up to so many runs
-constexpr int64_t kFill = 512;                  // workgroups
+// A row of few scores is one wavefront's, one of many four wavefronts'.  Few rows
+// have sixteen wavefronts each, which is one launch where a row cut into parts is
+// two, and are cut where that still leaves long rows to few workgroups.
+constexpr int64_t kWaveRuns = 4 * 64 * kRuns;    // up to so many runs
+constexpr int64_t kFewRows = 512;
+constexpr int kMostWaves = 16;
+constexpr int64_t kLongRuns = 4 * kMostWaves * 64 * kRuns;
+constexpr int64_t kFill = 256;                   // workgroups
 constexpr uint32_t kMaxSplits = 32;
 
 struct Cut {
-    bool wave;
+    int waves;
     uint32_t splits, per;
 };
 Cut cut_of(const Scores& g) {
-    Cut c{int64_t(g.total) <= kWaveRuns, 1, g.total};
-    if (c.wave) return c;
-    const uint32_t step = kWaves * 64 * kRuns, steps = (g.total + step - 1) / step;
-    uint32_t s = uint32_t(std::min<int64_t>(std::min<int64_t>(steps, kMaxSplits), std::max<int64_t>(1, kFill / std::max<int64_t>(g.n, 1))));
+    Cut c{int64_t(g.total) <= kWaveRuns ? 1 : g.n > kFewRows ? kWaves : kMostWaves, 1, g.total};
+    if (c.waves < kMostWaves || int64_t(g.total) <= kLongRuns || g.n > kFill / 2) return c;
+    const uint32_t step = kMostWaves * 64 * kRuns, steps = (g.total + step - 1) / step;
+    const uint32_t s = uint32_t(std::min<int64_t>(std::min<int64_t>(steps, kMaxSplits), kFill / std::max<int64_t>(g.n, 1)));
     c.per = (steps + s - 1) / s * step;
     c.splits = (g.total + c.per - 1) / c.per;
     return c;
@@ -481,8 +525,9 @@ Cut cut_of(const Scores& g) {
 
 template <typename T, int FIT, bool TOP, bool ENT>
 hipError_t probs3(ProbArgs a, Cut c, hipStream_t s) {
-    if (c.wave) k_probs<T, FIT, TOP, ENT, 1><<<grid_of((a.g.n + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
-    else k_probs<T, FIT, TOP, ENT, kWaves><<<grid_of(a.g.n * c.splits), kThreads, 0, s>>>(a);
+    if (c.waves == 1) k_probs<T, FIT, TOP, ENT, 1><<<grid_of((a.g.n + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
+    else if (c.waves == kWaves) k_probs<T, FIT, TOP, ENT, kWaves><<<grid_of(a.g.n), kThreads, 0, s>>>(a);
+    else k_probs<T, FIT, TOP, ENT, kMostWaves><<<grid_of(a.g.n * c.splits), kMostWaves * 64, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.splits == 1) return e;
     k_probs_join<T><<<grid_of(a.g.n), 64, 0, s>>>(a);
