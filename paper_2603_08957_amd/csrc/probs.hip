@@ -212,6 +212,8 @@ struct Top {
                uint32_t(__builtin_amdgcn_readlane(int(key), lane));
     }
     __device__ void settle() { last = lane_key(k - 1); }
+    // Whether any of these keys has a place.
+    __device__ bool beaten(uint64_t k) const { return __ballot(k > last) != 0; }
     // 64 keys, smallest first
     __device__ void merge(uint64_t sorted) {
         key = key > sorted ? key : sorted;
@@ -300,8 +302,24 @@ __device__ inline void fill_top(const ProbArgs& a, int64_t row, Top& top) {
     }
 }
 
+// A token's given word: its score is loaded before a row's pass, which hides it.
+struct Given {
+    float x;
+    bool is;
+};
 template <typename T>
-__device__ inline void put_row(const ProbArgs& a, int64_t row, Sums u, Top& top) {
+__device__ inline Given given_of(const ProbArgs& a, int64_t row) {
+    Given g{0.f, false};
+    if (!a.log_prob) return g;
+    const int64_t id = token(a.ids, a.id_bytes, row);
+    g.is = id >= 0 && id < a.g.vocab;
+    if (g.is) g.x = load1(score_at<T>(a, row, id));
+    else if (id >= 0 && a.status) *a.status = TRE_E_KEYRANGE;
+    return g;
+}
+
+template <typename T>
+__device__ inline void put_row(const ProbArgs& a, int64_t row, Sums u, Top& top, Given given) {
     const int lane = threadIdx.x & 63;
     if (a.top_ids && top.last == 0) fill_top<T>(a, row, top);
     const bool empty = u.s == 0.f;
@@ -319,17 +337,7 @@ __device__ inline void put_row(const ProbArgs& a, int64_t row, Sums u, Top& top)
         const float h = logs - kLn2 * u.t / u.s;
         a.entropy[row] = empty || h < 0.f ? 0.f : h;  // (a sum that rounding took below zero)
     }
-    if (a.log_prob) {
-        const int64_t id = token(a.ids, a.id_bytes, row);
-        float lp = 0.f;
-        if (id >= 0 && id < a.g.vocab) {
-            const float v = load1(score_at<T>(a, row, id));
-            lp = empty ? -kInf : (v - m) * a.scale - logs;
-        } else if (id >= 0 && a.status) {
-            *a.status = TRE_E_KEYRANGE;
-        }
-        a.log_prob[row] = lp;
-    }
+    if (a.log_prob) a.log_prob[row] = !given.is ? 0.f : empty ? -kInf : (given.x - m) * a.scale - logs;
 }
 
 // Element `at` < N of a lane's runs, from FROM on.
@@ -363,6 +371,8 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
     const uint32_t split = uint32_t(task - row * a.splits);
     const uint32_t q0 = split * a.per, q1 = min(q0 + a.per, a.g.total);
     const T* x = static_cast<const T*>(a.x) + row * a.g.row_stride;
+    Given given{0.f, false};
+    if ((W == 1 || wave == 0) && a.splits == 1) given = given_of<T>(a, row);
     Sums u{-FLT_MAX, 0.f, 0.f};
     Top top;
     uint32_t known = 0;
@@ -455,7 +465,10 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
             for (int h = W / 2; h > 0; h /= 2) {
                 if (wave >= h && wave < 2 * h) keys[wave][lane] = lane < a.top ? top.key : 0;
                 __syncthreads();
-                if (wave < h) top.merge(keys[wave + h][63 - lane]);
+                if (wave < h) {
+                    const uint64_t k = keys[wave + h][63 - lane];
+                    if (top.beaten(k)) top.merge(k);
+                }
             }
         } else {
             __syncthreads();
@@ -468,7 +481,7 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
         if (lane == 0) a.part[task] = u;
         if (TOP && lane < a.top) a.part_keys[task * a.top + lane] = top.key;
     } else {
-        put_row<T>(a, row, u, top);
+        put_row<T>(a, row, u, top, given);
     }
 }
 
@@ -480,6 +493,7 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
     const int lane = threadIdx.x;
     const int64_t row = block_index();
     if (row >= a.g.n) return;
+    const Given given = given_of<T>(a, row);
     Sums u = lane < int(a.splits) ? a.part[row * a.splits + lane] : Sums{-FLT_MAX, 0.f, 0.f};
     join_lanes<1, true>(u, a.scale2);
     Top top;
@@ -493,10 +507,10 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
             for (int i = 0; i < kLists; i++) k[i] = from < a.top && b + i < a.splits ? lists[(b + i) * a.top] : 0;
 #pragma unroll
             for (int i = 0; i < kLists; i++)
-                if (b + i < a.splits) top.merge(k[i]);
+                if (top.beaten(k[i])) top.merge(k[i]);
         }
     }
-    put_row<T>(a, row, u, top);
+    put_row<T>(a, row, u, top, given);
 }
 
 // A row of few scores is one wavefront's, one of many four wavefronts'.  Few rows

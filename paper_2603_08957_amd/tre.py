@@ -183,6 +183,11 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
+def _at(t):
+    """The same as a number, which costs a small call less."""
+    return None if t is None else t.data_ptr()
+
+
 def _stream(stream=None, device=None):
     """The hipStream_t of a torch stream, or of the (current) device's current
     one, whose handle torch gives without making a stream object (3 us less)."""
@@ -678,7 +683,7 @@ def _scores(x, where, what):
 
 @dataclass
 class LogProbs:
-    """What `log_probs` gives, in float32: of each token..."""
+    """What `log_probs` gives, in float32: of each token..."""  # (views of one allocation)
     log_prob: object        # [n]: its given word's, or None
     lse: object             # [n]: log of the sum of e^(scale x)
     stats: object           # [n, 2]: what log_probs_grad takes
@@ -719,22 +724,33 @@ def log_probs(scores, ids=None, scale: float = 1.0, top: int = 0, entropy: bool 
     if not 0 <= top <= min(64, vocab):
         raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"top: 0 to {min(64, vocab)} wanted, got {top}")
     with _Here(dev, stream, w) as here:
-        def make(*shape, dtype=torch.float32):
-            return here.buffer(lambda: torch.empty(shape, dtype=dtype, device=dev))
-
-        r = LogProbs(make(n) if ids is not None else None, make(n), make(n, 2), make(n) if entropy else None,
-                     make(n, top, dtype=torch.int32) if top else None, make(n, top) if top else None)
-        need = int(lib().tre_log_probs_workspace_bytes(n, vocab, cols, dt, top))
+        # views of one allocation: what several take is most of a small call
+        flat = here.buffer(lambda: torch.empty(n * (3 + (ids is not None) + bool(entropy) + top), dtype=torch.float32, device=dev))
+        column, rest = (n,), 3 * n
+        stats, lse = flat.as_strided((n, 2), (2, 1), 0), flat.as_strided(column, (1,), 2 * n)
+        log_prob = h = top_ids = top_log_probs = None
+        if ids is not None:
+            log_prob = flat.as_strided(column, (1,), rest)
+            rest += n
+        if entropy:
+            h = flat.as_strided(column, (1,), rest)
+            rest += n
+        if top:
+            top_log_probs = flat.as_strided((n, top), (top, 1), rest)
+            top_ids = here.buffer(lambda: torch.empty((n, top), dtype=torch.int32, device=dev))
+        need = 0
         if ws is not None:
             _want(ws, w, "ws", device=dev)
-        elif need:
-            ws = here.buffer(lambda: alloc_workspace(need, dev), result=False)
+            need = ws.numel() * ws.element_size()
+        else:
+            need = int(lib().tre_log_probs_workspace_bytes(n, vocab, cols, dt, top))
+            if need:
+                ws = here.buffer(lambda: alloc_workspace(need, dev), result=False)
         here.uses(scores, ids, status, ws)
-        _check(lib().tre_log_probs(_ptr(scores), dt, *layout, _ptr(ids), ids.element_size() if ids is not None else 0,
-                                   float(scale), _ptr(r.log_prob), _ptr(r.lse), _ptr(r.stats), _ptr(r.entropy), top,
-                                   _ptr(r.top_ids), _ptr(r.top_log_probs), _ptr(status), _ptr(ws),
-                                   ws.numel() * ws.element_size() if ws is not None else 0, here.ptr), "tre_log_probs")
-    return r
+        _check(lib().tre_log_probs(scores.data_ptr(), dt, *layout, _at(ids), ids.element_size() if ids is not None else 0,
+                                   float(scale), _at(log_prob), lse.data_ptr(), stats.data_ptr(), _at(h), top, _at(top_ids),
+                                   _at(top_log_probs), _at(status), _at(ws), need, here.ptr), "tre_log_probs")
+    return LogProbs(log_prob, lse, stats, h, top_ids, top_log_probs)
 
 
 def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, grad_entropy=None, entropy=None,
@@ -749,6 +765,8 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
     dt = _value_type(scores, w, "scores")
     layout = _scores(scores, w, "scores")
     n, dev = layout[0], scores.device
+    if grad_log_prob is None and grad_lse is None and grad_entropy is None:
+        raise TreError(STATUS_CODE["TRE_E_ARG"], w, "no gradient given")
     _want(stats, w, "stats", (n, 2), torch.float32, dev)
     if ids is not None:
         _ids(ids, w, dev)
@@ -766,11 +784,12 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
         elif out.shape != scores.shape or out.device != dev or out.dtype != dtype:
             raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"out: {dtype} {tuple(scores.shape)} on {dev} wanted, got {out.dtype} "
                                                           f"{tuple(out.shape)} on {out.device}")
+        out_layout = _scores(out, w, "out")[3:]
         here.uses(scores, stats, ids, grad_log_prob, grad_lse, grad_entropy, entropy, out, status)
-        _check(lib().tre_log_probs_grad(_ptr(scores), dt, *layout, _ptr(stats), _ptr(ids),
-                                        ids.element_size() if ids is not None else 0, float(scale), _ptr(grad_log_prob),
-                                        _ptr(grad_lse), _ptr(grad_entropy), _ptr(entropy), _ptr(out), odt,
-                                        *_scores(out, w, "out")[3:], _ptr(status), here.ptr), "tre_log_probs_grad")
+        _check(lib().tre_log_probs_grad(scores.data_ptr(), dt, *layout, stats.data_ptr(), _at(ids),
+                                        ids.element_size() if ids is not None else 0, float(scale), _at(grad_log_prob),
+                                        _at(grad_lse), _at(grad_entropy), _at(entropy), out.data_ptr(), odt, *out_layout,
+                                        _at(status), here.ptr), "tre_log_probs_grad")
     return out
 
 

@@ -175,7 +175,7 @@ def test_binding_refuses(tre):
     refused("TRE_E_DTYPE", tre.log_probs, x.double())
     refused("TRE_E_SHAPE", tre.log_probs, x[0])
     refused("TRE_E_SHAPE", tre.log_probs, torch.zeros(3, 0))
-    refused("TRE_E_ARG", tre.log_probs_grad, x, torch.zeros(3, 2))
+    refused("TRE_E_ARG", tre.log_probs_grad, x, torch.zeros(3, 2), grad_lse=torch.zeros(3))
     refused("TRE_E_ARG", tre.grad_norm, [x])
     refused("TRE_E_ARG", tre.grad_norm, [])
     refused("TRE_E_ARG", tre.grad_norm, [None])
