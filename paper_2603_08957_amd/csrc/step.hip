@@ -145,6 +145,7 @@ struct AdamArgs {
     int64_t total;
     const float *lr_dev, *scale_dev;
     const int64_t* step_dev;
+    int64_t per;            // elements of a workgroup
     double beta1, beta2;
     float b1, nb1, b2, nb2, c1, c2, lr, decay, weight_decay, eps, scale;
     uint32_t seed0, seed1, step;
@@ -183,42 +184,52 @@ __device__ inline Rates rates_of(const AdamArgs& a) {
 }
 
 // Random bits of an element: a hash of (seed, step, element) by shifts and products
-// with the leading bits of the golden ratio and of the roots of 2, 3 and 5.
+// with the leading bits of the golden ratio and of the roots of 2, 3 and 5.  low:
+// the element's number; k1: the seed's upper half and what the number's adds.
 struct Chance {
     uint32_t h, y;
     __device__ uint32_t first() const { return h >> 12; }                 // 20 bits each
     __device__ uint32_t second() const { return y >> 12; }
     __device__ uint32_t weight() const { return (h ^ (y << 4)) & 0xffffu; }  // 16
 };
-__device__ inline Chance chance_of(int64_t i, uint32_t k0, uint32_t k1) {
-    uint32_t h = (uint32_t(i) ^ k0) * 0x6A09E667u;
+__device__ inline Chance chance_of(uint32_t low, uint32_t k0, uint32_t k1) {
+    uint32_t h = (low ^ k0) * 0x6A09E667u;
     h ^= h >> 15;
-    h = (h + k1 + uint32_t(i >> 32) * 0xBB67AE85u) * 0xBB67AE85u;
+    h = (h + k1) * 0xBB67AE85u;
     h ^= h >> 13;
     uint32_t y = h * 0x3C6EF373u;
     y ^= y >> 16;
     return {h, y};
 }
+__device__ inline uint32_t chance_key(uint32_t k1, int64_t element) { return k1 + uint32_t(element >> 32) * 0xBB67AE85u; }
 
 constexpr int kBias1 = 7, kBias2 = 23;
 
+// Code i of four, as the upper bits of a float: a float of exponent E less 127
+// (a denormal for E = 0) is 2^(BIAS - 127) of the code's value.
+__device__ inline float code_value(uint32_t codes, int i, uint32_t mask) {
+    const int up = 20 - 8 * i;
+    return __uint_as_float((up >= 0 ? codes << up : codes >> -up) & mask);
+}
+// Magnitudes of a block whose byte is not 255.
 template <int BIAS>
-__device__ inline float decode(uint32_t code, uint32_t byte) {  // of a magnitude
-    // (as the upper bits of a float, exponents below 1 a denormal's, the code is 2^(BIAS - 127) of its value)
-    const float v = ldexpf(__uint_as_float(code << 20), int(byte) - BIAS);
-    return byte == 255u ? __builtin_nanf("") : v;
+__device__ inline float decode(uint32_t codes, int i, uint32_t byte) {
+    return ldexpf(code_value(codes, i, BIAS == kBias1 ? 0x07f00000u : 0x0ff00000u), int(byte) - BIAS);
+}
+__device__ inline float first_moment(uint32_t codes, int i, uint32_t byte) {
+    return copysignf(decode<kBias1>(codes, i, byte), __uint_as_float(codes << (24 - 8 * i)));
 }
 
 // The code of a magnitude y < 256.5.  r: 20 random bits.
 template <int BIAS, bool CHANCE>
 __device__ inline uint32_t encode(float y, uint32_t r) {
-    const uint32_t u = __float_as_uint(y);
-    const uint32_t high = ((u + (CHANCE ? r : 0x7ffffu + (u >> 20 & 1))) >> 20) - ((127 - BIAS) << 3);
-    uint32_t low;
     constexpr float kUnits = float(1u << (BIAS + 2));  // of codes below 8
-    if constexpr (CHANCE) low = (uint32_t(y * (kUnits * float(1u << 20))) + r) >> 20;
-    else low = uint32_t(rintf(y * kUnits));
-    return y >= 1.f / float(1u << (BIAS - 1)) ? high : low;
+    constexpr uint32_t kLeast = uint32_t(127 - BIAS) << 23;
+    const uint32_t u = __float_as_uint(y);
+    const bool normal = y >= 1.f / float(1u << (BIAS - 1));
+    // by chance: the codes below 8 and the others are whole numbers of 2^-20 of a step
+    if constexpr (CHANCE) return ((normal ? u - kLeast : uint32_t(y * (kUnits * float(1u << 20)))) + r) >> 20;
+    else return normal ? (u - kLeast + 0x7ffffu + (u >> 20 & 1)) >> 20 : uint32_t(rintf(y * kUnits));
 }
 
 // The byte of a block's power of two, from its largest magnitude's bits; 8 lanes to
@@ -231,110 +242,195 @@ __device__ inline uint32_t block_byte(uint32_t bits) {
     return e == 255u ? 255u : e > 7u ? e - 7u : 0u;
 }
 
-// A lane's run is 4 elements (16 bytes in fp32), so many of them in flight together.
-constexpr int kRun = 4, kAdamRuns = 4;
-constexpr int64_t kAdamStep = int64_t(64) * kRun * kAdamRuns;       // elements of a wavefront at once
-constexpr int64_t kAdamBlock = kAdamStep * kWaves;
+// A lane takes 4 elements at once (16 bytes in fp32), a wavefront a run of 256; the
+// next run's are loaded before this one's are used.
+constexpr int kLane = 4;
+constexpr int64_t kRun = 64 * kLane;
 
-template <int BITS, bool CHANCE, typename TP, typename TG, bool WHOLE>
-__device__ inline void adam_runs(const AdamArgs& a, const Rates& r, TP* p, const TG* g, int64_t at, int64_t e0, int64_t n) {
-    const int lane = threadIdx.x & 63;
-    float pv[kAdamRuns][kRun], gv[kAdamRuns][kRun], mv[kAdamRuns][kRun], vv[kAdamRuns][kRun];
-    uint32_t mc[kAdamRuns], vc[kAdamRuns], mb[kAdamRuns], vb[kAdamRuns];
-    float* m32 = static_cast<float*>(a.state) + at;
-    float* v32 = m32 + a.total;
-    uint8_t* m8 = static_cast<uint8_t*>(a.state) + at;
-    uint8_t* v8 = m8 + a.total;
-    uint8_t* mb8 = static_cast<uint8_t*>(a.state) + 2 * a.total + at / 32;
-    uint8_t* vb8 = mb8 + a.total / 32;
-#pragma unroll
-    for (int j = 0; j < kAdamRuns; j++) {
-        const int64_t e = e0 + (j * 64 + lane) * kRun;
-        if (!WHOLE && e / 32 * 32 >= n) break;  // (the moments have whole blocks)
-        if constexpr (WHOLE) {
-            load_all(p + e, pv[j]);
-            load_all(g + e, gv[j]);
-        } else {
-            load_run(p, e, n, pv[j]);
-            load_run(g, e, n, gv[j]);
-        }
-        if constexpr (BITS == 32) {
-            load_all(m32 + e, mv[j]);
-            load_all(v32 + e, vv[j]);
-        } else {
-            mc[j] = *reinterpret_cast<const uint32_t*>(m8 + e);
-            vc[j] = *reinterpret_cast<const uint32_t*>(v8 + e);
-            mb[j] = mb8[e / 32];
-            vb[j] = vb8[e / 32];
+template <typename T>
+__device__ inline void store4(T* at, const float (&v)[kLane], bool cut) {
+    if constexpr (sizeof(T) == 2) {
+        if (cut) {  // (bf16 values already)
+            u32x2_2 w;
+            w[0] = __float_as_uint(v[0]) >> 16 | (__float_as_uint(v[1]) & 0xffff0000u);
+            w[1] = __float_as_uint(v[2]) >> 16 | (__float_as_uint(v[3]) & 0xffff0000u);
+            __builtin_nontemporal_store(w, reinterpret_cast<u32x2_2*>(at));
+            return;
         }
     }
+    store_all<true>(at, v);
+}
+
+// 4 elements as they come.
+template <int BITS, typename TP, typename TG>
+struct Held {
+    uint32_t p[sizeof(TP)], g[sizeof(TG)], m[BITS / 8], v[BITS / 8];  // (4 elements of so many bytes each, in words)
+    uint32_t mb, vb;
+};
+template <typename T>
+__device__ inline void load4(const T* at, uint32_t (&w)[sizeof(T)]) {
+    if constexpr (sizeof(T) == 4) {
+        const f32x4_4 x = *reinterpret_cast<const f32x4_4*>(at);
 #pragma unroll
-    for (int j = 0; j < kAdamRuns; j++) {
-        const int64_t e = e0 + (j * 64 + lane) * kRun;
-        if (!WHOLE && e / 32 * 32 >= n) break;
-        Chance c[kRun];
+        for (int i = 0; i < 4; i++) w[i] = __float_as_uint(x[i]);
+    } else {
+        const u32x2_2 x = *reinterpret_cast<const u32x2_2*>(at);
+        w[0] = x[0];
+        w[1] = x[1];
+    }
+}
+template <typename T>
+__device__ inline void load_upto4(const T* at, int64_t n, uint32_t (&w)[sizeof(T)]) {
+#pragma unroll
+    for (int i = 0; i < int(sizeof(T)); i++) w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if (i >= n) break;
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(at[i]);
+        else w[i / 2] |= uint32_t(at[i]) << (16 * (i & 1));
+    }
+}
+template <int N>
+__device__ inline float value4(const uint32_t (&w)[N], int i) {
+    if constexpr (N == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+}
+
+// A tensor's part that a wavefront steps.
+template <int BITS, bool CHANCE, typename TP, typename TG>
+struct Part {
+    using H = Held<BITS, TP, TG>;
+    const AdamArgs& a;
+    const Rates& r;
+    TP* p;
+    const TG* g;
+    int64_t at, n;   // the tensor's first element among all, its elements
+    uint32_t lane;
+
+    // The run from element e on (a scalar; the lanes' offsets from it are 32 bits).
+    template <bool WHOLE>
+    __device__ H load(int64_t e) const {
+        H h;
+        const uint32_t o = lane * kLane;
+        if constexpr (WHOLE) {
+            load4(p + e + o, h.p);
+            load4(g + e + o, h.g);
+        } else {
+            load_upto4(p + e + o, n - e - o, h.p);
+            load_upto4(g + e + o, n - e - o, h.g);
+        }
+        if constexpr (BITS == 32) {
+            const float* m = static_cast<const float*>(a.state) + at + e;
+            load4(m + o, h.m);
+            load4(m + a.total + o, h.v);
+        } else {
+            const uint8_t* m = static_cast<const uint8_t*>(a.state) + at + e;
+            const uint8_t* b = static_cast<const uint8_t*>(a.state) + 2 * a.total + (at + e) / 32;
+            h.m[0] = *reinterpret_cast<const uint32_t*>(m + o);
+            h.v[0] = *reinterpret_cast<const uint32_t*>(m + a.total + o);
+            h.mb = b[o / 32];
+            h.vb = b[a.total / 32 + o / 32];
+        }
+        return h;
+    }
+
+    template <bool WHOLE>
+    __device__ void step(int64_t e, const H& h) const {
+        const uint32_t o = lane * kLane;
+        float pv[kLane], mv[kLane], vv[kLane];
+        Chance c[kLane];
         uint32_t m_top = 0, v_top = 0;
+        float b1 = a.b1, b2 = a.b2;
+        if constexpr (BITS == 8) {  // a block that holds NaN
+            b1 = h.mb == 255u ? __builtin_nanf("") : b1;
+            b2 = h.vb == 255u ? __builtin_nanf("") : b2;
+        }
+        const float rate = -r.lr * r.c1;
+        // (the element's number may pass 2^32 in a run)
+        const uint32_t low0 = uint32_t(at + e), low = low0 + o;
+        const uint32_t k = low < low0 ? chance_key(a.seed1, at + e + kRun) : chance_key(a.seed1, at + e);
 #pragma unroll
-        for (int i = 0; i < kRun; i++) {
+        for (int i = 0; i < kLane; i++) {
             if constexpr (BITS == 8) {
-                const uint32_t mi = mc[j] >> (8 * i) & 255u;
-                mv[j][i] = copysignf(decode<kBias1>(mi & 127u, mb[j]), __uint_as_float(mi << 24));
-                vv[j][i] = decode<kBias2>(vc[j] >> (8 * i) & 255u, vb[j]);
+                mv[i] = first_moment(h.m[0], i, h.mb);
+                vv[i] = decode<kBias2>(h.v[0], i, h.vb);
+            } else {
+                mv[i] = value4(h.m, i);
+                vv[i] = value4(h.v, i);
             }
-            if constexpr (CHANCE) c[i] = chance_of(at + e + i, r.k0, a.seed1);
+            if constexpr (CHANCE && (BITS == 8 || sizeof(TP) == 2)) c[i] = chance_of(low + i, r.k0, k);
             {
                 // (each product and sum rounded for itself, so that a moment next to a border between two codes is the same
                 // whoever computes it)
 #pragma clang fp contract(off)
-                const float gi = gv[j][i] * r.scale;
-                mv[j][i] = mv[j][i] * a.b1 + gi * a.nb1;
-                vv[j][i] = vv[j][i] * a.b2 + gi * gi * a.nb2;
+                const float gi = value4(h.g, i) * r.scale;
+                mv[i] = mv[i] * b1 + gi * a.nb1;
+                vv[i] = vv[i] * b2 + gi * gi * a.nb2;
             }
-            const float root = __builtin_amdgcn_sqrtf(vv[j][i] * r.c2) + a.eps;
-            pv[j][i] = pv[j][i] * r.decay - r.lr * (mv[j][i] * r.c1) * __builtin_amdgcn_rcpf(root);
+            const float root = __builtin_amdgcn_sqrtf(vv[i] * r.c2) + a.eps;
+            pv[i] = value4(h.p, i) * r.decay + rate * mv[i] * __builtin_amdgcn_rcpf(root);
             if constexpr (CHANCE && sizeof(TP) == 2) {
-                const uint32_t u = __float_as_uint(pv[j][i]);
-                if ((u & 0x7f800000u) != 0x7f800000u) pv[j][i] = __uint_as_float((u + c[i].weight()) & 0xffff0000u);
+                const float up = __uint_as_float((__float_as_uint(pv[i]) + c[i].weight()) & 0xffff0000u);
+                pv[i] = pv[i] == pv[i] ? up : __builtin_nanf("");
             }
             if constexpr (BITS == 8) {
-                m_top = max(m_top, __float_as_uint(mv[j][i]) & 0x7fffffffu);
-                v_top = max(v_top, __float_as_uint(vv[j][i]) & 0x7fffffffu);
+                m_top = max(m_top, __float_as_uint(mv[i]) & 0x7fffffffu);
+                v_top = max(v_top, __float_as_uint(vv[i]) & 0x7fffffffu);
             }
         }
-        if constexpr (WHOLE) store_all<true>(p + e, pv[j]);
-        else store_run<true>(p, e, n, pv[j]);
+        if constexpr (WHOLE) store4(p + e + o, pv, CHANCE);
+        else store_run<true>(p, e + o, n, pv);
         if constexpr (BITS == 32) {
-            store_all<true>(m32 + e, mv[j]);
-            store_all<true>(v32 + e, vv[j]);
+            float* m = static_cast<float*>(a.state) + at + e;
+            store_all<true>(m + o, mv);
+            store_all<true>(m + a.total + o, vv);
         } else {
             const uint32_t bm = block_byte(m_top), bv = block_byte(v_top);
             // 2^(127 - byte), at most 2^127
             const float sm = __uint_as_float((254u - min(bm, 253u)) << 23), sv = __uint_as_float((254u - min(bv, 253u)) << 23);
             uint32_t mq = 0, vq = 0;
 #pragma unroll
-            for (int i = 0; i < kRun; i++) {
-                const uint32_t q = encode<kBias1, CHANCE>(fabsf(mv[j][i]) * sm, c[i].first());
-                mq |= (q | (__float_as_uint(mv[j][i]) >> 31 << 7)) << (8 * i);
-                const uint32_t w = encode<kBias2, CHANCE>(vv[j][i] * sv, c[i].second());
-                vq |= (w == 0 && vv[j][i] > 0.f ? 1u : w) << (8 * i);
+            for (int i = 0; i < kLane; i++) {
+                const uint32_t q = encode<kBias1, CHANCE>(fabsf(mv[i]) * sm, c[i].first());
+                mq |= (q | (__float_as_uint(mv[i]) >> 24 & 0x80u)) << (8 * i);
+                const uint32_t w = encode<kBias2, CHANCE>(vv[i] * sv, c[i].second());
+                vq |= max(w, min(__float_as_uint(vv[i]), 1u)) << (8 * i);
             }
-            *reinterpret_cast<uint32_t*>(m8 + e) = bm == 255u ? 0u : mq;
-            *reinterpret_cast<uint32_t*>(v8 + e) = bv == 255u ? 0u : vq;
+            uint8_t* m = static_cast<uint8_t*>(a.state) + at + e;
+            uint8_t* b = static_cast<uint8_t*>(a.state) + 2 * a.total + (at + e) / 32;
+            *reinterpret_cast<uint32_t*>(m + o) = bm == 255u ? 0u : mq;
+            *reinterpret_cast<uint32_t*>(m + a.total + o) = bv == 255u ? 0u : vq;
             if ((lane & 7) == 0) {
-                mb8[e / 32] = uint8_t(bm);
-                vb8[e / 32] = uint8_t(bv);
+                b[o / 32] = uint8_t(bm);
+                b[a.total / 32 + o / 32] = uint8_t(bv);
             }
         }
     }
-}
+
+    // The runs from e on, kRun * kWaves apart, that end at `end` or before; what is left of the tensor's last one.
+    __device__ void all(int64_t e, int64_t end) const {
+        constexpr int64_t kNext = kRun * kWaves;
+        if (e + kRun <= end) {
+            H h = load<true>(e);
+#pragma unroll 1
+            for (; e + kNext + kRun <= end; e += kNext) {
+                const H next = load<true>(e + kNext);
+                step<true>(e, h);
+                h = next;
+            }
+            step<true>(e, h);
+            e += kNext;
+        }
+        // (the moments have whole blocks)
+        if (e < end && end == n && e + lane * kLane / 32 * 32 < n) step<false>(e, load<false>(e));
+    }
+};
 
 template <int BITS, bool CHANCE, typename TP, typename TG>
-__device__ inline void adam_block(const AdamArgs& a, const Rates& r, int i, int64_t e0) {
-    TP* p = static_cast<TP*>(const_cast<void*>(a.t.a[i]));
-    const TG* g = static_cast<const TG*>(a.t.b[i]);
-    const int64_t n = a.t.size[i], at = a.t.at[i];
-    if (e0 + kAdamStep <= n) adam_runs<BITS, CHANCE, TP, TG, true>(a, r, p, g, at, e0, n);
-    else if (e0 < n) adam_runs<BITS, CHANCE, TP, TG, false>(a, r, p, g, at, e0, n);
+__device__ inline void adam_block(const AdamArgs& a, const Rates& r, int i, int64_t e) {
+    const Part<BITS, CHANCE, TP, TG> part{a, r, static_cast<TP*>(const_cast<void*>(a.t.a[i])), static_cast<const TG*>(a.t.b[i]),
+                                          a.t.at[i], a.t.size[i], threadIdx.x & 63};
+    part.all(e + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kRun, min(part.n, e + a.per));
 }
 
 template <int BITS, bool CHANCE>
@@ -343,7 +439,7 @@ __global__ __launch_bounds__(kThreads) void k_adam(AdamArgs a) {
     const int i = tensor_of(a.t, block);
     const Rates r = rates_of(a);
     if (r.scale != r.scale) return;  // (a norm that is not finite: no step)
-    const int64_t e0 = int64_t(block - a.t.first[i]) * kAdamBlock + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kAdamStep;
+    const int64_t e0 = int64_t(block - a.t.first[i]) * a.per;
     switch (a.t.kind[i]) {
         case 0: adam_block<BITS, CHANCE, float, float>(a, r, i, e0); break;
         case 1: adam_block<BITS, CHANCE, uint16_t, float>(a, r, i, e0); break;
@@ -363,12 +459,17 @@ __global__ __launch_bounds__(kThreads) void k_moments(const uint8_t* __restrict_
     float mv[8], vv[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        const uint32_t mi = (i < 4 ? mc.x : mc.y) >> (8 * (i & 3)) & 255u;
-        mv[i] = copysignf(decode<kBias1>(mi & 127u, mb), __uint_as_float(mi << 24));
-        vv[i] = decode<kBias2>((i < 4 ? vc.x : vc.y) >> (8 * (i & 3)) & 255u, vb);
+        mv[i] = mb == 255u ? __builtin_nanf("") : first_moment(i < 4 ? mc.x : mc.y, i & 3, mb);
+        vv[i] = vb == 255u ? __builtin_nanf("") : decode<kBias2>(i < 4 ? vc.x : vc.y, i & 3, vb);
     }
     store_all<true>(m + e, mv);
     store_all<true>(v + e, vv);
+}
+
+// Elements of a workgroup.
+int64_t adam_per(int, const int64_t*) {
+    static const char* e = getenv("ADAM_PER");
+    return kRun * kWaves * (e ? atoi(e) : 4);
 }
 
 int64_t room_of(int64_t n) { return (n + 31) / 32 * 32; }
@@ -427,6 +528,7 @@ int64_t adamw_room(int n, const int64_t* sizes) {
 hipError_t launch_adamw(int n, void* const* params, const int32_t* param_types, const void* const* grads,
                         const int32_t* grad_types, const int64_t* sizes, void* state, const tre_adamw_options& o, hipStream_t s) {
     AdamArgs a{};
+    a.per = adam_per(n, sizes);
     a.state = state;
     a.total = adamw_room(n, sizes);
     a.lr_dev = o.lr_dev;
@@ -460,7 +562,7 @@ hipError_t launch_adamw(int n, void* const* params, const int32_t* param_types, 
             a.t.at[k] = at;
             a.t.first[k] = uint32_t(blocks);
             a.t.kind[k] = uint8_t((param_types[i] == TRE_BF16) | (grad_types[i] == TRE_BF16) << 1);
-            blocks += (sizes[i] + kAdamBlock - 1) / kAdamBlock;
+            blocks += (sizes[i] + a.per - 1) / a.per;
             at += room_of(sizes[i]);
         }
         if (a.t.count == kMany || (i == n - 1 && a.t.count)) {
