@@ -927,9 +927,9 @@ bool sizes_ok(int32_t n, const int64_t* sizes) {
     if (n < 0 || (n > 0 && !sizes)) return false;
     int64_t total = 0;
     for (int32_t i = 0; i < n; i++) {
-        if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 42)) return false;
+        if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 40)) return false;
         total += sizes[i];
-        if (total > (int64_t(1) << 42)) return false;
+        if (total > (int64_t(1) << 40)) return false;
     }
     return true;
 }

@@ -146,7 +146,7 @@ struct AdamArgs {
     const float *lr_dev, *scale_dev;
     const int64_t* step_dev;
     int64_t per;            // elements of a workgroup
-    double beta1, beta2;
+    double log_beta1, log_beta2;
     float b1, nb1, b2, nb2, c1, c2, lr, decay, weight_decay, eps, scale;
     uint32_t seed0, seed1, step;
 };
@@ -158,11 +158,17 @@ struct Rates {
     uint32_t k0;
 };
 
-__device__ inline double power(double b, int64_t t) {
-    double r = 1.;
-    for (; t; t >>= 1, b *= b)
-        if (t & 1) r *= b;
-    return r;
+// 1 / (1 - b^t) from the logarithm of b: 1 - e^x for x = t log b < 0, near 0 by its
+// series (to 2^-24 of itself for x > -1/2, whose next term is x^8 / 9!).
+__device__ inline float correction(double log_b, int64_t t) {
+    const float x = float(log_b * double(t));
+    float s = 1.f / 40320.f;
+#pragma unroll
+    for (int k = 7; k >= 1; k--) {
+        constexpr float kInverse[8] = {0.f, 1.f, 1.f / 2.f, 1.f / 6.f, 1.f / 24.f, 1.f / 120.f, 1.f / 720.f, 1.f / 5040.f};
+        s = s * x + kInverse[k];
+    }
+    return 1.f / (x > -0.5f ? -x * s : 1.f - __builtin_amdgcn_exp2f(x * 1.4426950408889634f));
 }
 
 __device__ inline Rates rates_of(const AdamArgs& a) {
@@ -175,8 +181,8 @@ __device__ inline Rates rates_of(const AdamArgs& a) {
     }
     if (a.step_dev) {
         const int64_t t = max(*a.step_dev, int64_t(1));
-        r.c1 = float(1. / (1. - power(a.beta1, t)));
-        r.c2 = float(1. / (1. - power(a.beta2, t)));
+        r.c1 = correction(a.log_beta1, t);
+        r.c2 = correction(a.log_beta2, t);
         step = uint32_t(t);
     }
     r.k0 = a.seed0 + step * 0x9E3779B1u;
@@ -187,10 +193,8 @@ __device__ inline Rates rates_of(const AdamArgs& a) {
 // with the leading bits of the golden ratio and of the roots of 2, 3 and 5.  low:
 // the element's number; k1: the seed's upper half and what the number's adds.
 struct Chance {
-    uint32_t h, y;
-    __device__ uint32_t first() const { return h >> 12; }                 // 20 bits each
-    __device__ uint32_t second() const { return y >> 12; }
-    __device__ uint32_t weight() const { return (h ^ (y << 4)) & 0xffffu; }  // 16
+    uint32_t h, y;  // the upper 20 bits are the first and the second moment's
+    __device__ uint32_t weight() const { return (h ^ (y << 4)) & 0xffffu; }
 };
 __device__ inline Chance chance_of(uint32_t low, uint32_t k0, uint32_t k1) {
     uint32_t h = (low ^ k0) * 0x6A09E667u;
@@ -203,44 +207,66 @@ __device__ inline Chance chance_of(uint32_t low, uint32_t k0, uint32_t k1) {
 }
 __device__ inline uint32_t chance_key(uint32_t k1, int64_t element) { return k1 + uint32_t(element >> 32) * 0xBB67AE85u; }
 
-constexpr int kBias1 = 7, kBias2 = 23;
+constexpr int kBias2 = 23;  // of second moments' exponents
 
-// Code i of four, as the upper bits of a float: a float of exponent E less 127
-// (a denormal for E = 0) is 2^(BIAS - 127) of the code's value.
-__device__ inline float code_value(uint32_t codes, int i, uint32_t mask) {
-    const int up = 20 - 8 * i;
-    return __uint_as_float((up >= 0 ? codes << up : codes >> -up) & mask);
+// A first moment's codes are those of the instructions for 8-bit floats (4 bits of
+// exponent, bias 7), which stay below 480, their NaN's: two of four codes.
+template <bool UPPER>
+__device__ inline void first_pair(uint32_t codes, uint32_t byte, float& x, float& y) {
+    const auto v = __builtin_amdgcn_cvt_pk_f32_fp8(codes, UPPER);
+    x = ldexpf(v[0], int(byte) - 127);
+    y = ldexpf(v[1], int(byte) - 127);
 }
-// Magnitudes of a block whose byte is not 255.
-template <int BIAS>
-__device__ inline float decode(uint32_t codes, int i, uint32_t byte) {
-    return ldexpf(code_value(codes, i, BIAS == kBias1 ? 0x07f00000u : 0x0ff00000u), int(byte) - BIAS);
-}
-__device__ inline float first_moment(uint32_t codes, int i, uint32_t byte) {
-    return copysignf(decode<kBias1>(codes, i, byte), __uint_as_float(codes << (24 - 8 * i)));
+// A second moment's code as the upper bits of a float of exponent E less 127 (a
+// denormal for E = 0) is 2^(bias - 127) of its value.
+__device__ inline float second_moment(uint32_t codes, int i, uint32_t byte) {
+    return ldexpf(__uint_as_float((codes >> (8 * i) & 255u) << 20), int(byte) - kBias2);
 }
 
-// The code of a magnitude y < 256.5.  r: 20 random bits.
-template <int BIAS, bool CHANCE>
-__device__ inline uint32_t encode(float y, uint32_t r) {
-    constexpr float kUnits = float(1u << (BIAS + 2));  // of codes below 8
-    constexpr uint32_t kLeast = uint32_t(127 - BIAS) << 23;
+// Codes of first moments times the block's power of two.  By chance the
+// instruction adds a word's upper 20 bits below the last bit that stays.
+template <bool CHANCE, typename C>
+__device__ inline uint32_t first_codes(const float (&y)[4], const C& c) {
+    int q = 0;
+    if constexpr (CHANCE) {
+        q = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], c[0].h, q, 0);
+        q = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], c[1].h, q, 1);
+        q = __builtin_amdgcn_cvt_sr_fp8_f32(y[2], c[2].h, q, 2);
+        q = __builtin_amdgcn_cvt_sr_fp8_f32(y[3], c[3].h, q, 3);
+    } else {
+        q = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], q, false);
+        q = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], q, true);
+    }
+    return uint32_t(q);
+}
+__device__ inline int middle(int a, int b, int c) { return min(max(a, b), max(min(a, b), c)); }
+// The code of a second moment times its block's power of two, y < 256.5.  `high` is
+// what it is where E is not 0, `low` where it is; of these and the least code with E
+// = 1 the right one lies in the middle.
+template <bool CHANCE>
+__device__ inline uint32_t second_code(float y, uint32_t word) {
+    constexpr float kUnits = float(1u << (kBias2 + 2));  // of codes below 8
+    constexpr uint32_t kNone = uint32_t(127 - kBias2) << 23;
     const uint32_t u = __float_as_uint(y);
-    const bool normal = y >= 1.f / float(1u << (BIAS - 1));
-    // by chance: the codes below 8 and the others are whole numbers of 2^-20 of a step
-    if constexpr (CHANCE) return ((normal ? u - kLeast : uint32_t(y * (kUnits * float(1u << 20)))) + r) >> 20;
-    else return normal ? (u - kLeast + 0x7ffffu + (u >> 20 & 1)) >> 20 : uint32_t(rintf(y * kUnits));
+    if constexpr (CHANCE) {  // in steps of 2^-20 of a code
+        const int w = middle(int(u - kNone), (8 << 20) - 1, int(y * (kUnits * float(1u << 20))));
+        return (uint32_t(w) + (word >> 12)) >> 20;
+    } else {
+        return uint32_t(middle(int(u - kNone + 0x7ffffu + (u >> 20 & 1)) >> 20, 8, int(rintf(y * kUnits))));
+    }
 }
 
-// The byte of a block's power of two, from its largest magnitude's bits; 8 lanes to
-// a block.  255: a NaN or an infinity.
-__device__ inline uint32_t block_byte(uint32_t bits) {
+// The exponent (of a float's bits) of a block's largest magnitude, 7 at least; 8
+// lanes to a block.  255: a NaN or an infinity.
+__device__ inline uint32_t block_exponent(uint32_t bits) {
     bits = max(bits, uint32_t(__builtin_amdgcn_update_dpp(0, bits, 0xB1, 0xf, 0xf, true)));
     bits = max(bits, uint32_t(__builtin_amdgcn_update_dpp(0, bits, 0x4E, 0xf, 0xf, true)));
     bits = max(bits, uint32_t(__builtin_amdgcn_update_dpp(0, bits, 0x141, 0xf, 0xf, true)));
-    const uint32_t e = bits >> 23;
-    return e == 255u ? 255u : e > 7u ? e - 7u : 0u;
+    return max(bits >> 23, 7u);
 }
+__device__ inline uint8_t block_byte(uint32_t exponent) { return uint8_t(exponent == 255u ? 255u : exponent - 7u); }
+// 2^(127 - byte)
+__device__ inline float block_scale(uint32_t exponent) { return __uint_as_float((261u - exponent) << 23); }
 
 // A lane takes 4 elements at once (16 bytes in fp32), a wavefront a run of 256; the
 // next run's are loaded before this one's are used.
@@ -349,11 +375,14 @@ struct Part {
         // (the element's number may pass 2^32 in a run)
         const uint32_t low0 = uint32_t(at + e), low = low0 + o;
         const uint32_t k = low < low0 ? chance_key(a.seed1, at + e + kRun) : chance_key(a.seed1, at + e);
+        if constexpr (BITS == 8) {
+            first_pair<false>(h.m[0], h.mb, mv[0], mv[1]);
+            first_pair<true>(h.m[0], h.mb, mv[2], mv[3]);
+        }
 #pragma unroll
         for (int i = 0; i < kLane; i++) {
             if constexpr (BITS == 8) {
-                mv[i] = first_moment(h.m[0], i, h.mb);
-                vv[i] = decode<kBias2>(h.v[0], i, h.vb);
+                vv[i] = second_moment(h.v[0], i, h.vb);
             } else {
                 mv[i] = value4(h.m, i);
                 vv[i] = value4(h.v, i);
@@ -385,24 +414,23 @@ struct Part {
             store_all<true>(m + o, mv);
             store_all<true>(m + a.total + o, vv);
         } else {
-            const uint32_t bm = block_byte(m_top), bv = block_byte(v_top);
-            // 2^(127 - byte), at most 2^127
-            const float sm = __uint_as_float((254u - min(bm, 253u)) << 23), sv = __uint_as_float((254u - min(bv, 253u)) << 23);
-            uint32_t mq = 0, vq = 0;
+            const uint32_t em = block_exponent(m_top), ev = block_exponent(v_top);
+            const float sm = block_scale(em), sv = block_scale(ev);
+            const float y[kLane] = {mv[0] * sm, mv[1] * sm, mv[2] * sm, mv[3] * sm};
+            const uint32_t mq = first_codes<CHANCE>(y, c);
+            uint32_t vq = 0;
 #pragma unroll
-            for (int i = 0; i < kLane; i++) {
-                const uint32_t q = encode<kBias1, CHANCE>(fabsf(mv[i]) * sm, c[i].first());
-                mq |= (q | (__float_as_uint(mv[i]) >> 24 & 0x80u)) << (8 * i);
-                const uint32_t w = encode<kBias2, CHANCE>(vv[i] * sv, c[i].second());
+            for (int i = 0; i < kLane; i++) {  // (at least 1 where it is not zero)
+                const uint32_t w = second_code<CHANCE>(vv[i] * sv, c[i].y);
                 vq |= max(w, min(__float_as_uint(vv[i]), 1u)) << (8 * i);
             }
             uint8_t* m = static_cast<uint8_t*>(a.state) + at + e;
             uint8_t* b = static_cast<uint8_t*>(a.state) + 2 * a.total + (at + e) / 32;
-            *reinterpret_cast<uint32_t*>(m + o) = bm == 255u ? 0u : mq;
-            *reinterpret_cast<uint32_t*>(m + a.total + o) = bv == 255u ? 0u : vq;
+            *reinterpret_cast<uint32_t*>(m + o) = em == 255u ? 0u : mq;
+            *reinterpret_cast<uint32_t*>(m + a.total + o) = ev == 255u ? 0u : vq;
             if ((lane & 7) == 0) {
-                b[o / 32] = uint8_t(bm);
-                b[a.total / 32 + o / 32] = uint8_t(bv);
+                b[o / 32] = block_byte(em);
+                b[a.total / 32 + o / 32] = block_byte(ev);
             }
         }
     }
@@ -457,20 +485,23 @@ __global__ __launch_bounds__(kThreads) void k_moments(const uint8_t* __restrict_
     const uint2 mc = *reinterpret_cast<const uint2*>(state + e), vc = *reinterpret_cast<const uint2*>(state + total + e);
     const uint32_t mb = state[2 * total + e / 32], vb = state[2 * total + total / 32 + e / 32];
     float mv[8], vv[8];
+    first_pair<false>(mc.x, mb, mv[0], mv[1]);
+    first_pair<true>(mc.x, mb, mv[2], mv[3]);
+    first_pair<false>(mc.y, mb, mv[4], mv[5]);
+    first_pair<true>(mc.y, mb, mv[6], mv[7]);
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        mv[i] = mb == 255u ? __builtin_nanf("") : first_moment(i < 4 ? mc.x : mc.y, i & 3, mb);
-        vv[i] = vb == 255u ? __builtin_nanf("") : decode<kBias2>(i < 4 ? vc.x : vc.y, i & 3, vb);
+        vv[i] = vb == 255u ? __builtin_nanf("") : second_moment(i < 4 ? vc.x : vc.y, i & 3, vb);
+        if (mb == 255u) mv[i] = __builtin_nanf("");
     }
     store_all<true>(m + e, mv);
     store_all<true>(v + e, vv);
 }
 
-// Elements of a workgroup.
-int64_t adam_per(int, const int64_t*) {
-    static const char* e = getenv("ADAM_PER");
-    return kRun * kWaves * (e ? atoi(e) : 4);
-}
+// Elements of a workgroup: a run for each wavefront, or four of the shorter 8-bit
+// ones.  (134 M elements in 32 bits: 671 us with one, 695 with two, 715 with four;
+// 67 M in 8 bits, rounded by chance: 233, 207, 176, and 180 with eight.)
+int64_t adam_per(int bits) { return kRun * kWaves * (bits == 32 ? 1 : 4); }
 
 int64_t room_of(int64_t n) { return (n + 31) / 32 * 32; }
 
@@ -528,14 +559,14 @@ int64_t adamw_room(int n, const int64_t* sizes) {
 hipError_t launch_adamw(int n, void* const* params, const int32_t* param_types, const void* const* grads,
                         const int32_t* grad_types, const int64_t* sizes, void* state, const tre_adamw_options& o, hipStream_t s) {
     AdamArgs a{};
-    a.per = adam_per(n, sizes);
+    a.per = adam_per(o.bits);
     a.state = state;
     a.total = adamw_room(n, sizes);
     a.lr_dev = o.lr_dev;
     a.scale_dev = o.grad_scale_dev;
     a.step_dev = o.step_dev;
-    a.beta1 = o.beta1;
-    a.beta2 = o.beta2;
+    a.log_beta1 = std::log(o.beta1);  // (-inf for 0)
+    a.log_beta2 = std::log(o.beta2);
     a.b1 = float(o.beta1);
     a.nb1 = float(1. - o.beta1);
     a.b2 = float(o.beta2);

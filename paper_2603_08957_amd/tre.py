@@ -10,7 +10,7 @@ import ctypes
 import os
 from array import array
 from dataclasses import dataclass
-from operator import attrgetter
+from operator import attrgetter, eq
 
 import numpy as np
 
@@ -795,21 +795,26 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
 
 # ------------------------------------------- a training step of many tensors
 
-class _Many:
-    """Host arrays of contiguous GPU tensors' addresses, types and elements, all
-    on one device, as the calls over many tensors take them."""
+_kinds, _shapes = attrgetter("dtype"), attrgetter("shape")
 
-    def __init__(self, tensors, where, what):
+
+class _Many:
+    """Host arrays of contiguous GPU tensors' addresses, types and (``sizes``)
+    elements, all on one device, as the calls over many tensors take them.  Of some
+    hundred tensors this is most of a call's time on the host, so each property is
+    asked of all of them in one pass."""
+
+    def __init__(self, tensors, where, what, sizes=True):
         import torch
 
         T = torch.Tensor
         tensors = list(tensors)
         try:
             places = set(map(T.get_device, tensors))
-            kinds = list(map(attrgetter("dtype"), tensors))
-            self.numels = list(map(T.numel, tensors))
-            addresses = array("q", map(T.data_ptr, tensors))
+            kinds = list(map(_kinds, tensors))
+            addresses = array("q", list(map(T.data_ptr, tensors)))
             contiguous = all(map(T.is_contiguous, tensors))
+            elements = array("q", list(map(T.numel, tensors))) if sizes else None
         except TypeError:
             raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"{what}: a list of tensors wanted") from None
         if len(places) > 1 or -1 in places:
@@ -817,15 +822,15 @@ class _Many:
         if not contiguous:
             raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"{what}: contiguous tensors wanted")
         code = {torch.float32: 0, torch.bfloat16: 1}
-        try:
-            types = array("i", map(code.__getitem__, kinds))
-        except KeyError as e:
-            raise TreError(STATUS_CODE["TRE_E_DTYPE"], where, f"{what}: float32 or bfloat16 wanted, got {e.args[0]}") from None
-        sizes = array("q", self.numels)
-        self.tensors, self.n = tensors, len(tensors)
+        other = set(kinds) - code.keys()
+        if other:
+            raise TreError(STATUS_CODE["TRE_E_DTYPE"], where, f"{what}: float32 or bfloat16 wanted, got {other.pop()}")
+        n = len(tensors)
+        types = array("i", [code[kinds[0]]]) * n if len(set(kinds)) == 1 else array("i", [code[k] for k in kinds])
+        self.tensors, self.n = tensors, n
         self.device = torch.device("cuda", places.pop()) if places else None
-        self._arrays = addresses, types, sizes
-        self.addresses, self.types, self.sizes = (ctypes.c_void_p(a.buffer_info()[0]) for a in self._arrays)
+        self._arrays = addresses, types, elements
+        self.addresses, self.types, self.sizes = (a and ctypes.c_void_p(a.buffer_info()[0]) for a in self._arrays)
 
 
 def grad_norm_workspace_bytes(sizes) -> int:
@@ -857,7 +862,8 @@ def grad_norm(tensors, max_norm: float | None = None, out=None, ws=None, stream=
             ws = here.buffer(lambda: alloc_workspace(need, many.device), result=False)
         else:
             _want(ws, w, "ws", device=many.device)
-        here.uses(*many.tensors, out, ws)
+        if stream is not None:
+            here.uses(*many.tensors, out, ws)
         _check(lib().tre_grad_norm(many.n, many.addresses, many.types, many.sizes, max_norm, _ptr(out), _ptr(ws),
                                    ws.numel() * ws.element_size(), here.ptr), "tre_grad_norm")
     return out
@@ -901,10 +907,10 @@ def adamw(params, grads, state, step, lr, beta1: float = 0.9, beta2: float = 0.9
     import torch
 
     w = "tre.adamw"
-    p, g = _Many(params, w, "params"), _Many(grads, w, "grads")
+    p, g = _Many(params, w, "params"), _Many(grads, w, "grads", sizes=False)
     if p.device != g.device or p.device is None:
         raise TreError(STATUS_CODE["TRE_E_ARG"], w, f"params and grads wanted on one GPU, got {p.device} and {g.device}")
-    if p.numels != g.numels or list(map(attrgetter("shape"), p.tensors)) != list(map(attrgetter("shape"), g.tensors)):
+    if p.n != g.n or not all(map(eq, map(_shapes, p.tensors), map(_shapes, g.tensors))):
         raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, "grads: params' shapes wanted")
     if state.dtype not in (torch.float32, torch.uint8):
         raise TreError(STATUS_CODE["TRE_E_DTYPE"], w, f"state: float32 or uint8 wanted, got {state.dtype}")
@@ -917,7 +923,8 @@ def adamw(params, grads, state, step, lr, beta1: float = 0.9, beta2: float = 0.9
     opt = AdamwOptions(float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), float(scale), int(step),
                        _ptr(lr_dev), _ptr(step_dev), _ptr(scale_dev), (seed or 0) & (1 << 64) - 1, int(seed is not None), bits)
     with _Here(p.device, stream, w) as here:
-        here.uses(*p.tensors, *g.tensors, state, step_dev, lr_dev, scale_dev)
+        if stream is not None:
+            here.uses(*p.tensors, *g.tensors, state, step_dev, lr_dev, scale_dev)
         _check(lib().tre_adamw(p.n, p.addresses, p.types, g.addresses, g.types, p.sizes, _ptr(state), ctypes.byref(opt),
                                here.ptr), "tre_adamw")
 
