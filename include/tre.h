@@ -617,7 +617,7 @@ tre_status tre_log_probs_grad(const void *x, int32_t dtype, int64_t n, int64_t v
  *         tre_grad_norm_workspace_bytes(...) (0 on bad arguments); holds nothing
  *         between calls.  Calls that overlap need one each.
  * Squares are summed in 64 bits in an order that the sizes alone determine.  At
- * most 2^40 elements in all (TRE_E_SHAPE).  Asynchronous on the stream; may be
+ * most 2^37 elements in all (TRE_E_SHAPE).  Asynchronous on the stream; may be
  * captured into a graph, which then holds the arrays' addresses. */
 size_t tre_grad_norm_workspace_bytes(int32_t n_tensors, const int64_t *sizes);
 tre_status tre_grad_norm(int32_t n_tensors, const void *const *tensors, const int32_t *types, const int64_t *sizes,
@@ -652,7 +652,7 @@ tre_status tre_grad_norm(int32_t n_tensors, const void *const *tensors, const in
  *             `stochastic`: 8-bit moments and bf16 weights are rounded up with the
  *             probability that their place between two neighbours has, by a hash of
  *             (seed, t, element); else to the nearest, ties to even.
- * Computed in fp32.  At most 2^40 elements in all (TRE_E_SHAPE); TRE_E_ARG unless
+ * Computed in fp32.  At most 2^37 elements in all (TRE_E_SHAPE); TRE_E_ARG unless
  * 0 <= beta < 1, eps > 0, lr >= 0, weight_decay >= 0, all finite, t >= 1 and bits
  * 8 or 32.  Asynchronous on the stream; may be captured into a graph, which then
  * holds the arrays' addresses. */

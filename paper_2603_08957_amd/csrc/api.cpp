@@ -441,7 +441,7 @@ AsyncBounds async_bounds(const Plan& p, int64_t n_u, int64_t n_v, int64_t max_pa
         b.pairs = b.keys = n_u;
     } else {
         int64_t w_space = 1;
-        for (int c = 0; c < p.nk[2] && w_space <= (int64_t(1) << 40); c++) w_space *= p.radix[2][c];
+        for (int c = 0; c < p.nk[2] && w_space <= (int64_t(1) << 37); c++) w_space *= p.radix[2][c];
         b.pairs = (n_u > 0 && n_v > 0) ? std::max<int64_t>(0, std::min(max_pairs, pair_bound(p, n_u, n_v))) : 0;
         b.keys = std::min(b.pairs, w_space);
     }
@@ -927,9 +927,9 @@ bool sizes_ok(int32_t n, const int64_t* sizes) {
     if (n < 0 || (n > 0 && !sizes)) return false;
     int64_t total = 0;
     for (int32_t i = 0; i < n; i++) {
-        if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 40)) return false;
+        if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 37)) return false;
         total += sizes[i];
-        if (total > (int64_t(1) << 40)) return false;
+        if (total > (int64_t(1) << 37)) return false;
     }
     return true;
 }

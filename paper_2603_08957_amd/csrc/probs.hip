@@ -48,16 +48,6 @@ Scores scores_of(const ScoreLayout& l, int elems) {
     return g;
 }
 
-struct Place {
-    uint32_t tile, at;  // run `at` of the tile's row
-};
-__device__ inline Place place_of(const Scores& g, uint32_t q) {
-    if (g.total == g.runs) return {0, q};
-    if (g.runs == 1) return {q, 0};
-    const uint32_t tile = __umulhi(q, g.mul) >> g.shift;
-    return {tile, q - tile * g.runs};
-}
-
 // How runs lie on a tile's row: it is made of whole ones, its last one is taken
 // from the row's end (and overlaps the one before), or the row is shorter than one.
 enum Fit { kWhole, kOverlap, kShort };
@@ -105,14 +95,22 @@ struct Run {
     Raw<T, E> raw;
     uint32_t tile, start, own;  // columns from `start` on, its own from `own` on
     __device__ void find(const Scores& g, uint32_t q) {
-        const Place p = place_of(g, q);
-        tile = p.tile;
-        own = start = p.at * E;
+        tile = 0;
+        if (g.total != g.runs) tile = g.runs == 1 ? q : __umulhi(q, g.mul) >> g.shift;
+        own = start = (q - tile * g.runs) * E;
         if constexpr (FIT == kOverlap) start = min(own, g.cols - E);
     }
     __device__ void load(const Scores& g, const T* row, uint32_t q) {
-        find(g, q);
-        const T* at = row + tile * g.tile_stride + start;
+        const T* at;
+        if (g.total == g.runs) {  // (one tile: 8 operations fewer)
+            tile = 0;
+            own = start = q * E;
+            if constexpr (FIT == kOverlap) start = min(own, g.cols - E);
+            at = row + start;
+        } else {
+            find(g, q);
+            at = row + tile * g.tile_stride + start;
+        }
         if constexpr (FIT == kShort) raw.load_some(at, int(g.cols));
         else raw.load(at);
     }
@@ -424,9 +422,11 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
                 // a bit for each of a lane's scores that may have a place; then one of each lane at a time
                 uint32_t mine = 0;
 #pragma unroll
-                for (int j = 0; j < kRuns; j++)
+                for (int j = 0; j < kRuns; j++) {
+                    if (!__ballot(most[j] >= limit)) continue;
 #pragma unroll
                     for (int i = 0; i < E; i++) mine |= v[j][i] >= limit ? 1u << (j * E + i) : 0u;
+                }
 #pragma unroll 1
                 while (__ballot(mine != 0)) {
                     const int at = mine ? __ffs(mine) - 1 : 0;
@@ -626,9 +626,13 @@ __global__ __launch_bounds__(kThreads) void k_probs_grad(ProbGradArgs a) {
         } else {
 #pragma unroll
             for (int i = 0; i < E; i++) {
-                const float z = (r[j].raw.value(i) - m) * a.scale2 - logs2, e = __builtin_amdgcn_exp2f(z);
+                const float v = r[j].raw.value(i);
+                const float z = (v - m) * a.scale2 - logs2, e = __builtin_amdgcn_exp2f(z);
                 y[i] = e * (ENT ? c0 + c1 * fmaxf(z, -2000.f) : c0);
-                if (r[j].tile == id_tile && r[j].start + i == id_at) y[i] += one;
+            }
+            if (r[j].tile == id_tile && id_at - r[j].start < uint32_t(E)) {
+#pragma unroll
+                for (int i = 0; i < E; i++) y[i] += r[j].start + i == id_at ? one : 0.f;
             }
         }
         TO* at = out + r[j].tile * a.out_tile_stride + r[j].start;

@@ -16,25 +16,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
-// Tensors of a launch: its arguments stay below 4 KB.
-constexpr int kMany = 96;
-
-struct Many {
-    const void* a[kMany];   // (weights)
-    const void* b[kMany];   // (gradients)
-    int64_t size[kMany];
-    int64_t at[kMany];      // first element's place in the moments
-    uint32_t first[kMany];  // workgroup
-    uint8_t kind[kMany];    // 1: a in bf16, 2: b in bf16
-    int32_t count;
-};
-
-// The tensor of a workgroup: the last that begins at it or before.
-__device__ inline int tensor_of(const Many& t, uint32_t block) {
+// The tensor of a workgroup: the last whose first workgroup is it or one before.
+template <int N>
+__device__ inline int tensor_of(const uint32_t (&first)[N], int count, uint32_t block) {
     const int lane = threadIdx.x & 63;
     int n = 0;
 #pragma unroll
-    for (int i = 0; i < kMany; i += 64) n += __popcll(__ballot(i + lane < t.count && t.first[min(i + lane, kMany - 1)] <= block));
+    for (int i = 0; i < N; i += 64) n += __popcll(__ballot(i + lane < count && first[min(i + lane, N - 1)] <= block));
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
@@ -42,11 +30,19 @@ __device__ inline int tensor_of(const Many& t, uint32_t block) {
 
 constexpr int kNormRuns = 8;
 
+// Tensors of a launch, whose arguments stay below 4 KB.
+constexpr int kNormMany = 190;
+
 struct NormArgs {
-    Many t;
+    const void* x[kNormMany];
+    int64_t size[kNormMany];
+    uint32_t first[kNormMany];  // workgroup
+    uint8_t half[kNormMany];    // whether in bf16
+    int32_t count;
     double* part;       // of the launch's workgroups
     int64_t per;        // elements of a workgroup
 };
+static_assert(sizeof(NormArgs) <= 4096, "a launch's arguments");
 
 template <typename T>
 __device__ inline double squares(const T* x, int64_t n) {
@@ -89,11 +85,11 @@ __device__ inline double sum_all(double s) {
 // a conversion and one fused product.
 __global__ __launch_bounds__(kThreads) void k_squares(NormArgs a) {
     const uint32_t block = uint32_t(block_index());
-    const int i = tensor_of(a.t, block);
-    const int64_t at = int64_t(block - a.t.first[i]) * a.per, n = min(a.per, a.t.size[i] - at);
+    const int i = tensor_of(a.first, a.count, block);
+    const int64_t at = int64_t(block - a.first[i]) * a.per, n = min(a.per, a.size[i] - at);
     if (n <= 0) return;  // (a workgroup that only the grid's shape has)
-    const double s = sum_all(a.t.kind[i] & 1 ? squares(static_cast<const uint16_t*>(a.t.a[i]) + at, n)
-                                             : squares(static_cast<const float*>(a.t.a[i]) + at, n));
+    const double s = sum_all(a.half[i] ? squares(static_cast<const uint16_t*>(a.x[i]) + at, n)
+                                       : squares(static_cast<const float*>(a.x[i]) + at, n));
     if (threadIdx.x == 0) a.part[block] = s;
 }
 
@@ -111,7 +107,9 @@ __global__ __launch_bounds__(kFinishThreads) void k_norm(const double* __restric
     out[1] = !finite ? __builtin_nanf("") : max_norm < 0.f ? 1.f : float(fmin(double(max_norm) / (norm + 1e-6), 1.));
 }
 
-// Elements of a workgroup: few workgroups' sums are left to add.
+// Elements of a workgroup, so that some thousand workgroups' sums are left to one
+// workgroup: 400 M bf16 elements take 137 us (5.8 TB/s) and 4.5 for the sums, with
+// twice as many parts 137 and 6.4, with half 143 and 4.
 constexpr int64_t kNormParts = 8192, kNormLeast = 4096;
 int64_t norm_per(int n, const int64_t* sizes) {
     int64_t total = 0, per = kNormLeast;
@@ -139,8 +137,17 @@ int64_t norm_per(int n, const int64_t* sizes) {
 // a seed it is by chance, up with the probability that a value's place between two
 // codes has, which is right on average; weights in bf16 then too.
 
+// Tensors of a launch, whose arguments stay below 4 KB: weights, gradients, elements
+// (the upper bits in `kind`), where the moments begin (in blocks of 32) and the first
+// workgroup.
+constexpr int kAdamMany = 134;
+
 struct AdamArgs {
-    Many t;
+    void* p[kAdamMany];
+    const void* g[kAdamMany];
+    uint32_t size[kAdamMany], at32[kAdamMany], first[kAdamMany];
+    uint8_t kind[kAdamMany];  // 1: weights in bf16, 2: gradients in bf16; the rest: size >> 32
+    int32_t count;
     void* state;
     int64_t total;
     const float *lr_dev, *scale_dev;
@@ -456,19 +463,19 @@ struct Part {
 
 template <int BITS, bool CHANCE, typename TP, typename TG>
 __device__ inline void adam_block(const AdamArgs& a, const Rates& r, int i, int64_t e) {
-    const Part<BITS, CHANCE, TP, TG> part{a, r, static_cast<TP*>(const_cast<void*>(a.t.a[i])), static_cast<const TG*>(a.t.b[i]),
-                                          a.t.at[i], a.t.size[i], threadIdx.x & 63};
+    const Part<BITS, CHANCE, TP, TG> part{a, r, static_cast<TP*>(a.p[i]), static_cast<const TG*>(a.g[i]), int64_t(a.at32[i]) * 32,
+                                          int64_t(a.kind[i] >> 2) << 32 | a.size[i], threadIdx.x & 63};
     part.all(e + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kRun, min(part.n, e + a.per));
 }
 
 template <int BITS, bool CHANCE>
 __global__ __launch_bounds__(kThreads) void k_adam(AdamArgs a) {
     const uint32_t block = uint32_t(block_index());
-    const int i = tensor_of(a.t, block);
+    const int i = tensor_of(a.first, a.count, block);
     const Rates r = rates_of(a);
     if (r.scale != r.scale) return;  // (a norm that is not finite: no step)
-    const int64_t e0 = int64_t(block - a.t.first[i]) * a.per;
-    switch (a.t.kind[i]) {
+    const int64_t e0 = int64_t(block - a.first[i]) * a.per;
+    switch (a.kind[i] & 3) {
         case 0: adam_block<BITS, CHANCE, float, float>(a, r, i, e0); break;
         case 1: adam_block<BITS, CHANCE, uint16_t, float>(a, r, i, e0); break;
         case 2: adam_block<BITS, CHANCE, float, uint16_t>(a, r, i, e0); break;
@@ -529,21 +536,21 @@ hipError_t launch_grad_norm(int n, const void* const* tensors, const int32_t* ty
     int64_t parts = 0, blocks = 0;
     for (int i = 0; i < n; i++) {
         if (sizes[i] > 0) {
-            const int k = a.t.count++;
-            a.t.a[k] = tensors[i];
-            a.t.size[k] = sizes[i];
-            a.t.first[k] = uint32_t(blocks);
-            a.t.kind[k] = types[i] == TRE_BF16;
+            const int k = a.count++;
+            a.x[k] = tensors[i];
+            a.size[k] = sizes[i];
+            a.first[k] = uint32_t(blocks);
+            a.half[k] = types[i] == TRE_BF16;
             blocks += (sizes[i] + a.per - 1) / a.per;
         }
-        if (a.t.count == kMany || (i == n - 1 && a.t.count)) {
+        if (a.count == kNormMany || (i == n - 1 && a.count)) {
             k_squares<<<grid_of(blocks), kThreads, 0, s>>>(a);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             a.part += blocks;
             parts += blocks;
             blocks = 0;
-            a.t.count = 0;
+            a.count = 0;
         }
     }
     k_norm<<<1, kFinishThreads, 0, s>>>(reinterpret_cast<const double*>(ws), parts, max_norm, out);
@@ -586,21 +593,21 @@ hipError_t launch_adamw(int n, void* const* params, const int32_t* param_types, 
     int64_t blocks = 0, at = 0;
     for (int i = 0; i < n; i++) {
         if (sizes[i] > 0) {
-            const int k = a.t.count++;
-            a.t.a[k] = params[i];
-            a.t.b[k] = grads[i];
-            a.t.size[k] = sizes[i];
-            a.t.at[k] = at;
-            a.t.first[k] = uint32_t(blocks);
-            a.t.kind[k] = uint8_t((param_types[i] == TRE_BF16) | (grad_types[i] == TRE_BF16) << 1);
+            const int k = a.count++;
+            a.p[k] = params[i];
+            a.g[k] = grads[i];
+            a.size[k] = uint32_t(sizes[i]);
+            a.at32[k] = uint32_t(at / 32);
+            a.first[k] = uint32_t(blocks);
+            a.kind[k] = uint8_t((param_types[i] == TRE_BF16) | (grad_types[i] == TRE_BF16) << 1 | (sizes[i] >> 32) << 2);
             blocks += (sizes[i] + a.per - 1) / a.per;
             at += room_of(sizes[i]);
         }
-        if (a.t.count == kMany || (i == n - 1 && a.t.count)) {
+        if (a.count == kAdamMany || (i == n - 1 && a.count)) {
             const hipError_t e = o.bits == 8 ? adam<8>(a, o.stochastic != 0, blocks, s) : adam<32>(a, o.stochastic != 0, blocks, s);
             if (e != hipSuccess) return e;
             blocks = 0;
-            a.t.count = 0;
+            a.count = 0;
         }
     }
     return hipSuccess;
