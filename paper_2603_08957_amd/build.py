@@ -1,4 +1,5 @@
-"""Build the HIP library ``libtre.so`` for gfx950 with hipcc (in-tree)."""
+"""Build the HIP library ``libtre.so`` for gfx950 with hipcc, and the binding's
+``_tensors.so`` (in-tree)."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -39,10 +40,35 @@ def _compile(src: str) -> str:
     return obj
 
 
+TENSORS = os.path.join(HERE, "_tensors.so")
+
+
+def build_tensors() -> str:
+    """Build ``_tensors.so``, the binding's reader of lists of torch tensors: host
+    code against torch's headers, the only part that knows them."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+
+    dirs = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]
+    libs = cpp_extension.library_paths()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w", *(f"-I{d}" for d in dirs),
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", os.path.join(HERE, "pysrc", "tensors.cpp"),
+           "-o", TENSORS + ".tmp", *(f"-L{d}" for d in libs), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stderr}")
+    os.replace(TENSORS + ".tmp", TENSORS)
+    return TENSORS
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:
+        binding = ex.submit(build_tensors)
         objs = list(ex.map(_compile, sources()))
+        binding.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -1,4 +1,5 @@
-"""ctypes binding of ``libtre.so`` (the C ABI declared in ``include/tre.h``).
+"""ctypes binding of ``libtre.so`` (the C ABI declared in ``include/tre.h``); lists
+of tensors are read by ``_tensors.so``.
 
 Argument marshalling only: torch supplies device memory and the stream, and
 every step of the path runs in the library's HIP kernels.  There is no CPU
@@ -10,7 +11,6 @@ import ctypes
 import os
 from array import array
 from dataclasses import dataclass
-from operator import attrgetter, eq
 
 import numpy as np
 
@@ -795,48 +795,47 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
 
 # ------------------------------------------- a training step of many tensors
 
-_kinds, _shapes = attrgetter("dtype"), attrgetter("shape")
+_tensors = None
+
+
+def _reader():
+    """The reader of lists of tensors, _tensors.so (no other path)."""
+    global _tensors
+    if _tensors is None:
+        import torch  # noqa: F401  (whose libraries it uses)
+
+        try:
+            from . import _tensors as t
+        except ImportError as e:
+            raise RuntimeError(f"_tensors.so is missing: build it with `python -m paper_2603_08957_amd.build` ({e})") from None
+        _tensors = t
+    return _tensors
 
 
 class _Many:
-    """Host arrays of contiguous GPU tensors' addresses, types and (``sizes``)
-    elements, all on one device, as the calls over many tensors take them.  Of some
-    hundred tensors this is most of a call's time on the host, so each property is
-    asked of all of them in one pass."""
+    """Host arrays of contiguous GPU tensors' addresses, types and elements, all
+    on one device, as the calls over many tensors take them."""
 
-    def __init__(self, tensors, where, what, sizes=True):
+    _WHY = {1: ("TRE_E_ARG", "a list of tensors wanted"), 2: ("TRE_E_ARG", "wanted on one GPU"),
+            3: ("TRE_E_SHAPE", "contiguous tensors wanted"), 4: ("TRE_E_DTYPE", "float32 or bfloat16 wanted")}
+
+    def __init__(self, tensors, where, what):
         import torch
 
-        T = torch.Tensor
-        tensors = list(tensors)
-        try:
-            places = set(map(T.get_device, tensors))
-            kinds = list(map(_kinds, tensors))
-            addresses = array("q", list(map(T.data_ptr, tensors)))
-            contiguous = all(map(T.is_contiguous, tensors))
-            elements = array("q", list(map(T.numel, tensors))) if sizes else None
-        except TypeError:
-            raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"{what}: a list of tensors wanted") from None
-        if len(places) > 1 or -1 in places:
-            raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"{what}: wanted on one GPU")
-        if not contiguous:
-            raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"{what}: contiguous tensors wanted")
-        code = {torch.float32: 0, torch.bfloat16: 1}
-        other = set(kinds) - code.keys()
-        if other:
-            raise TreError(STATUS_CODE["TRE_E_DTYPE"], where, f"{what}: float32 or bfloat16 wanted, got {other.pop()}")
-        n = len(tensors)
-        types = array("i", [code[kinds[0]]]) * n if len(set(kinds)) == 1 else array("i", [code[k] for k in kinds])
-        self.tensors, self.n = tensors, n
-        self.device = torch.device("cuda", places.pop()) if places else None
-        self._arrays = addresses, types, elements
-        self.addresses, self.types, self.sizes = (a and ctypes.c_void_p(a.buffer_info()[0]) for a in self._arrays)
+        self.tensors = tensors = tensors if isinstance(tensors, (list, tuple)) else list(tensors)
+        why, *got = _reader().gather(tensors)
+        if why:
+            status, text = self._WHY[why]
+            raise TreError(STATUS_CODE[status], where, f"{what}[{got[0]}]: {text}")
+        device, self.addresses, self.types, self.sizes = got
+        self.n = len(tensors)
+        self.device = torch.device("cuda", device) if device >= 0 else None
 
 
 def grad_norm_workspace_bytes(sizes) -> int:
     """For tensors of these numbers of elements."""
     sizes = array("q", sizes)
-    return int(lib().tre_grad_norm_workspace_bytes(len(sizes), ctypes.c_void_p(sizes.buffer_info()[0])))
+    return int(lib().tre_grad_norm_workspace_bytes(len(sizes), sizes.tobytes()))
 
 
 def grad_norm(tensors, max_norm: float | None = None, out=None, ws=None, stream=None):
@@ -907,10 +906,10 @@ def adamw(params, grads, state, step, lr, beta1: float = 0.9, beta2: float = 0.9
     import torch
 
     w = "tre.adamw"
-    p, g = _Many(params, w, "params"), _Many(grads, w, "grads", sizes=False)
+    p, g = _Many(params, w, "params"), _Many(grads, w, "grads")
     if p.device != g.device or p.device is None:
         raise TreError(STATUS_CODE["TRE_E_ARG"], w, f"params and grads wanted on one GPU, got {p.device} and {g.device}")
-    if p.n != g.n or not all(map(eq, map(_shapes, p.tensors), map(_shapes, g.tensors))):
+    if not _reader().same_shapes(p.tensors, g.tensors):
         raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, "grads: params' shapes wanted")
     if state.dtype not in (torch.float32, torch.uint8):
         raise TreError(STATUS_CODE["TRE_E_DTYPE"], w, f"state: float32 or uint8 wanted, got {state.dtype}")
