@@ -69,10 +69,10 @@ def unpack(state):
     return np.where(c > 127, -m, m), decode(cv, bv, 23)
 
 
-def chance(n, seed, step):
-    """20, 20 and 16 random bits of each of n elements."""
+def chance(n, seed, step, start=0):
+    """20, 20 and 16 random bits of each of n elements from element `start` on."""
     one = np.uint64(0xFFFFFFFF)
-    i = np.arange(n, dtype=np.uint64)
+    i = np.arange(start, start + n, dtype=np.uint64)
 
     def times(x, k):
         return x * np.uint64(k) & one

@@ -416,7 +416,8 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
             }
             known = __builtin_amdgcn_readfirstlane(known);
             uint32_t least = max(max(uint32_t(top.last >> 32), kOrderLowest) + 1, known);
-            if (top.last == 0 && known <= kOrderLowest) least = max(least, reached(order_of(all), a.top));
+            // (a wavefront of few words that can come bars nothing for the others)
+            if (top.last == 0 && known <= kOrderLowest + 1) least = max(least, reached(order_of(all), a.top));
             float limit = of_order(least);
             if (__ballot(all >= limit)) {
                 // a bit for each of a lane's scores that may have a place; then one of each lane at a time
@@ -576,6 +577,7 @@ struct ProbGradArgs {
     int64_t* status;
     int64_t out_row_stride, out_tile_stride;
     uint32_t parts;      // wavefronts of a row
+    bool apart;          // the output is not the scores' memory: what two runs have in common may be written twice
     float scale, scale2;
     int32_t id_bytes;
 };
@@ -636,8 +638,8 @@ __global__ __launch_bounds__(kThreads) void k_probs_grad(ProbGradArgs a) {
             }
         }
         TO* at = out + r[j].tile * a.out_tile_stride + r[j].start;
-        if (r[j].whole()) {
-            store_all<true>(at, y);
+        if (r[j].whole() || (FIT == kOverlap && a.apart)) {
+            store_all<FIT == kWhole>(at, y);
         } else {
 #pragma unroll
             for (int i = 0; i < E; i++)
@@ -717,6 +719,7 @@ hipError_t launch_log_probs_grad(const ScoreLayout& l, const void* x, int dtype,
     a.by_entropy = by_entropy;
     a.out = out;
     a.status = status;
+    a.apart = out != x;
     a.out_row_stride = out_row_stride;
     a.out_tile_stride = out_tile_stride;
     a.scale = scale;

@@ -781,10 +781,12 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
     with _Here(dev, stream, w) as here:
         if out is None:
             out = here.buffer(lambda: torch.empty(scores.shape, dtype=dtype, device=dev))
+            out_layout = layout[2], n * layout[2]
         elif out.shape != scores.shape or out.device != dev or out.dtype != dtype:
             raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"out: {dtype} {tuple(scores.shape)} on {dev} wanted, got {out.dtype} "
                                                           f"{tuple(out.shape)} on {out.device}")
-        out_layout = _scores(out, w, "out")[3:]
+        else:
+            out_layout = _scores(out, w, "out")[3:]
         here.uses(scores, stats, ids, grad_log_prob, grad_lse, grad_entropy, entropy, out, status)
         _check(lib().tre_log_probs_grad(scores.data_ptr(), dt, *layout, stats.data_ptr(), _at(ids),
                                         ids.element_size() if ids is not None else 0, float(scale), _at(grad_log_prob),
@@ -822,6 +824,8 @@ class _Many:
     def __init__(self, tensors, where, what):
         import torch
 
+        if isinstance(tensors, torch.Tensor):
+            tensors = [tensors]
         self.tensors = tensors = tensors if isinstance(tensors, (list, tuple)) else list(tensors)
         why, *got = _reader().gather(tensors)
         if why:
