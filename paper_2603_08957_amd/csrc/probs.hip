@@ -577,6 +577,7 @@ struct ProbGradArgs {
     int64_t* status;
     int64_t out_row_stride, out_tile_stride;
     uint32_t parts;      // wavefronts of a row
+    bool rows_first;     // wavefronts that follow each other take a part of one row after the other
     bool apart;          // the output is not the scores' memory: what two runs have in common may be written twice
     float scale, scale2;
     int32_t id_bytes;
@@ -587,9 +588,10 @@ __global__ __launch_bounds__(kThreads) void k_probs_grad(ProbGradArgs a) {
     constexpr int E = lane_elems<TI, TO>();
     const int lane = threadIdx.x & 63;
     const int64_t w = block_index() * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t row = w / a.parts;
-    if (row >= a.g.n) return;
-    const uint32_t part = uint32_t(w - row * a.parts);
+    const int64_t by = a.rows_first ? a.g.n : int64_t(a.parts), q0 = w / by, q1 = w - q0 * by;
+    const int64_t row = a.rows_first ? q1 : q0;
+    const uint32_t part = uint32_t(a.rows_first ? q0 : q1);
+    if (row >= a.g.n || part >= a.parts) return;
     const float m = a.stats[2 * row], logs2 = a.stats[2 * row + 1] * kLog2e;
     int64_t id = a.ids ? token(a.ids, a.id_bytes, row) : -1;
     if (id >= a.g.vocab) {
@@ -658,6 +660,10 @@ hipError_t probs_grad(ProbGradArgs a, const ScoreLayout& l, hipStream_t s) {
     constexpr int E = lane_elems<TI, TO>();
     a.g = scores_of(l, E);
     a.parts = (a.g.total + 64 * kRuns - 1) / (64 * kRuns);
+    // Where a tile's rows do not end with lines of 128 bytes, those of neighbours are written at about the same time, and a
+    // line that two share once: 2458 x 23750 fp32 values in tiles of 250 take 93 us so, 114 row by row.  (Whole lines: 8192 x
+    // 32768 fp32 values in tiles of 128 433 and 405.)
+    a.rows_first = l.vocab > l.cols && l.cols * int64_t(sizeof(TO)) % 128 != 0;
     const dim3 grid = grid_of((l.n * a.parts + kWaves - 1) / kWaves);
     switch (fit_of(a.g, E)) {
         case kWhole: k_probs_grad_of<TI, TO, kWhole>(a, grid, s); break;
