@@ -928,7 +928,7 @@ bool sizes_ok(int32_t n, const int64_t* sizes) {
     int64_t total = 0;
     for (int32_t i = 0; i < n; i++) {
         if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 37)) return false;
-        total += sizes[i];
+        total += (sizes[i] + 31) / 32 * 32;
         if (total > (int64_t(1) << 37)) return false;
     }
     return true;

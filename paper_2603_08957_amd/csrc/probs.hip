@@ -602,7 +602,7 @@ __global__ __launch_bounds__(kThreads) void k_probs_grad(ProbGradArgs a) {
     float c0 = (a.by_lse ? a.by_lse[row] : 0.f) - one, c1 = 0.f;
     if constexpr (ENT) {
         c1 = -a.by_entropy[row];
-        c0 += c1 * a.entropy[row];
+        if (c1 != 0.f) c0 += c1 * a.entropy[row];  // (which may be NaN)
         c1 *= kLn2;
     }
     c0 *= a.scale;

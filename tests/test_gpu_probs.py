@@ -311,6 +311,11 @@ def test_rows_without_gradient_are_not_read():
     r = tre.log_probs(x, ids)
     dx = tre.log_probs_grad(x, r.stats, ids, torch.ones(4, device="cuda"))
     assert not dx[1:3].any() and dx[0].isfinite().all() and dx[0].any() and dx[3].any()
+    r = tre.log_probs(x, ids, entropy=True)
+    assert r.entropy[1].isnan()
+    gh = torch.tensor([1.0, 0, 0, 1], device="cuda")
+    dx = tre.log_probs_grad(x, r.stats, ids, torch.ones(4, device="cuda"), grad_entropy=gh, entropy=r.entropy)
+    assert not dx[1:3].any() and dx[0].isfinite().all() and dx[0].any() and dx[3].any()
 
 
 @pytest.mark.parametrize("n", [0, 1])
