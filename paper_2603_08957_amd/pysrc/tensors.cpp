@@ -1,6 +1,7 @@
-// Addresses, types and sizes of a list of torch tensors in one pass, for the calls
-// that take many: asked of each tensor from Python, five properties of some hundred
-// tensors cost more than the kernels that follow.
+// What the binding asks of torch tensors where asking from Python costs more than the
+// kernel that follows: lists of some hundred tensors, and the tensors of calls that
+// take microseconds.  Nothing is decided here but whether all is as it should be; what
+// is not, the binding looks into itself, for its error.
 #include <Python.h>
 
 #include <torch/csrc/autograd/python_variable.h>
@@ -84,7 +85,84 @@ PyObject* same_shapes(PyObject*, PyObject* args) {
     return PyBool_FromLong(same);
 }
 
-PyMethodDef methods[] = {{"gather", gather, METH_O, nullptr}, {"same_shapes", same_shapes, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+// The tensor of an object, or null: strided, with memory of its own.
+const at::Tensor* tensor_of(PyObject* x) {
+    if (!THPVariable_Check(x)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(x);
+    return t.layout() == at::kStrided && t.has_storage() ? &t : nullptr;
+}
+
+// scores(x) -> (type, n, vocab, cols, row stride, tile stride, address, device) of
+// scores on a GPU, [n, vocab] or in tiles [tiles, n, cols], whose last dimension is
+// contiguous; None of anything else.
+PyObject* scores(PyObject*, PyObject* x) try {
+    const at::Tensor* t = tensor_of(x);
+    if (!t || !t->is_cuda() || (t->dim() != 2 && t->dim() != 3) || (t->scalar_type() != at::kFloat && t->scalar_type() != at::kBFloat16))
+        Py_RETURN_NONE;
+    const bool tiles = t->dim() == 3;
+    const int64_t cols = t->size(-1), n = t->size(tiles ? 1 : 0);
+    if (cols < 1 || (cols > 1 && t->stride(-1) != 1) || (tiles && t->size(0) < 1)) Py_RETURN_NONE;
+    return Py_BuildValue("(iLLLLLLi)", int(t->scalar_type() == at::kBFloat16), (long long)n,
+                         (long long)(tiles ? t->size(0) * cols : cols), (long long)cols, (long long)t->stride(tiles ? 1 : 0),
+                         (long long)(tiles ? t->stride(0) : 0), (long long)reinterpret_cast<intptr_t>(t->data_ptr()),
+                         int(t->get_device()));
+} catch (const std::exception&) {
+    Py_RETURN_NONE;
+}
+
+// vector(x, kind, device, n, row) -> its address, of a contiguous tensor [n] (row 0) or
+// [n, row] on that GPU: kind 0 float32, 1 int32 or int64 (then negated for int32).  None
+// of anything else.
+PyObject* vector(PyObject*, PyObject* args) try {
+    PyObject* x;
+    int kind, device;
+    long long n, row;
+    if (!PyArg_ParseTuple(args, "OiiLL", &x, &kind, &device, &n, &row)) return nullptr;
+    const at::Tensor* t = tensor_of(x);
+    if (!t || !t->is_cuda() || t->get_device() != device || !t->is_contiguous() || t->dim() != (row ? 2 : 1) || t->size(0) != n ||
+        (row && t->size(1) != row))
+        Py_RETURN_NONE;
+    const at::ScalarType s = t->scalar_type();
+    if (kind == 0 ? s != at::kFloat : s != at::kInt && s != at::kLong) Py_RETURN_NONE;
+    const long long at = (long long)reinterpret_cast<intptr_t>(t->data_ptr());
+    return PyLong_FromLongLong(s == at::kInt ? -at : at);
+} catch (const std::exception&) {
+    Py_RETURN_NONE;
+}
+
+// views(flat, n, given, entropy, top) -> (stats [n, 2], lse [n], given: [n], entropy: [n],
+// top: [n, top] and int32 [n, top]), None for what is not asked for, one after the other
+// in the float32 tensor `flat`.
+PyObject* views(PyObject*, PyObject* args) try {
+    PyObject* x;
+    long long n, top;
+    int given, entropy;
+    if (!PyArg_ParseTuple(args, "OLppL", &x, &n, &given, &entropy, &top)) return nullptr;
+    const at::Tensor& flat = THPVariable_Unpack(x);
+    int64_t at = 0;
+    auto part = [&](int64_t row, bool wanted, bool whole = false) -> PyObject* {
+        if (!wanted) Py_RETURN_NONE;
+        at::Tensor t = row ? flat.as_strided({n, row}, {row, 1}, at) : flat.as_strided({n}, {1}, at);
+        at += n * (row ? row : 1);
+        return THPVariable_Wrap(whole ? t.view(at::kInt) : t);
+    };
+    PyObject* r = PyTuple_New(6);
+    if (!r) return nullptr;
+    PyTuple_SET_ITEM(r, 0, part(2, true));
+    PyTuple_SET_ITEM(r, 1, part(0, true));
+    PyTuple_SET_ITEM(r, 2, part(0, given));
+    PyTuple_SET_ITEM(r, 3, part(0, entropy));
+    PyTuple_SET_ITEM(r, 4, part(top, top > 0));
+    PyTuple_SET_ITEM(r, 5, part(top, top > 0, true));
+    return r;
+} catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+}
+
+PyMethodDef methods[] = {{"gather", gather, METH_O, nullptr},       {"same_shapes", same_shapes, METH_VARARGS, nullptr},
+                         {"scores", scores, METH_O, nullptr},       {"vector", vector, METH_VARARGS, nullptr},
+                         {"views", views, METH_VARARGS, nullptr},   {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -664,21 +664,60 @@ def lookup_grad(grad, ids, n_rows: int, scale: float = 1.0, dtype=None, out=None
     return out
 
 
+_tensors = None
+
+
+def _reader():
+    """The reader of tensors, _tensors.so (no other path)."""
+    global _tensors
+    if _tensors is None:
+        import torch  # noqa: F401  (whose libraries it uses)
+
+        try:
+            from . import _tensors as t
+        except ImportError as e:
+            raise RuntimeError(f"_tensors.so is missing: build it with `python -m paper_2603_08957_amd.build` ({e})") from None
+        _tensors = t
+    return _tensors
+
+
 # ------------------------------------------------- probabilities of scores
 
 def _scores(x, where, what):
-    """(n, vocab, cols, row stride, tile stride) of scores [n, vocab] or in tiles
-    [tiles, n, cols], whose last dimension is contiguous."""
-    if x.dim() not in (2, 3) or x.shape[-1] < 1 or (x.dim() == 3 and x.shape[0] < 1):
+    """(type, n, vocab, cols, row stride, tile stride, address, GPU) of scores
+    [n, vocab] or in tiles [tiles, n, cols], whose last dimension is contiguous."""
+    got = _reader().scores(x)
+    if got is not None:
+        return got
+    _value_type(x, where, what)
+    if x.dim() not in (2, 3) or 0 in (x.shape[-1], x.shape[0] if x.dim() == 3 else 1):
         raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"{what}: [n, vocab] or tiles [tiles, n, cols] wanted, got {tuple(x.shape)}")
     if not x.is_cuda:
         raise TreError(STATUS_CODE["TRE_E_ARG"], where, f"{what}: on {x.device}, wanted on a GPU")
-    shape, stride = x.shape, x.stride()
-    if stride[-1] != 1 and shape[-1] > 1:
-        raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"{what}: a last stride of 1 wanted, got strides {stride}")
-    if len(shape) == 2:
-        return shape[0], shape[1], shape[1], stride[0], 0
-    return shape[1], shape[0] * shape[2], shape[2], stride[1], stride[0]
+    raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"{what}: a last stride of 1 wanted, got strides {x.stride()}")
+
+
+def _words(ids, where, n, gpu, device):
+    """(address, bytes of one) of words [n], (None, 0) for none."""
+    if ids is None:
+        return None, 0
+    at = _reader().vector(ids, 1, gpu, n, 0)
+    if at is None:
+        _ids(ids, where, device)
+        raise TreError(STATUS_CODE["TRE_E_SHAPE"], where, f"ids: [{n}] wanted, got {tuple(ids.shape)}")
+    return (at, 8) if at > 0 or ids.element_size() == 8 else (-at, 4)
+
+
+def _floats(t, where, what, n, row, gpu, device):
+    """The address of a float32 tensor [n] or [n, row], None for none."""
+    import torch
+
+    if t is None:
+        return None
+    at = _reader().vector(t, 0, gpu, n, row)
+    if at is None:
+        _want(t, where, what, (n, row) if row else (n,), torch.float32, device)
+    return at
 
 
 @dataclass
@@ -711,45 +750,33 @@ def log_probs(scores, ids=None, scale: float = 1.0, top: int = 0, entropy: bool 
     import torch
 
     w = "tre.log_probs"
-    dt = _value_type(scores, w, "scores")
-    layout = _scores(scores, w, "scores")
-    n, vocab, cols = layout[:3]
+    dt, n, vocab, cols, rows, tiles, at, gpu = _scores(scores, w, "scores")
     dev = scores.device
-    if ids is not None:
-        _ids(ids, w, dev)
-        if ids.shape != (n,):
-            raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"ids: [{n}] wanted, got {tuple(ids.shape)}")
-    _status(status, w, dev)
+    ids_at, id_bytes = _words(ids, w, n, gpu, dev)
+    if status is not None:
+        _status(status, w, dev)
     top = int(top)
     if not 0 <= top <= min(64, vocab):
         raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"top: 0 to {min(64, vocab)} wanted, got {top}")
+    given, entropy = ids is not None, bool(entropy)
+    L = lib()
     with _Here(dev, stream, w) as here:
         # views of one allocation: what several take is most of a small call
-        flat = here.buffer(lambda: torch.empty(n * (3 + (ids is not None) + bool(entropy) + top), dtype=torch.float32, device=dev))
-        column, rest = (n,), 3 * n
-        stats, lse = flat.as_strided((n, 2), (2, 1), 0), flat.as_strided(column, (1,), 2 * n)
-        log_prob = h = top_ids = top_log_probs = None
-        if ids is not None:
-            log_prob = flat.as_strided(column, (1,), rest)
-            rest += n
-        if entropy:
-            h = flat.as_strided(column, (1,), rest)
-            rest += n
-        if top:
-            top_log_probs = flat.as_strided((n, top), (top, 1), rest)
-            top_ids = here.buffer(lambda: torch.empty((n, top), dtype=torch.int32, device=dev))
-        need = 0
+        flat = here.buffer(lambda: torch.empty(n * (3 + given + entropy + 2 * top), dtype=torch.float32, device=dev))
+        stats, lse, log_prob, h, top_log_probs, top_ids = _reader().views(flat, n, given, entropy, top)
         if ws is not None:
             _want(ws, w, "ws", device=dev)
             need = ws.numel() * ws.element_size()
         else:
-            need = int(lib().tre_log_probs_workspace_bytes(n, vocab, cols, dt, top))
+            need = L.tre_log_probs_workspace_bytes(n, vocab, cols, dt, top)
             if need:
                 ws = here.buffer(lambda: alloc_workspace(need, dev), result=False)
-        here.uses(scores, ids, status, ws)
-        _check(lib().tre_log_probs(scores.data_ptr(), dt, *layout, _at(ids), ids.element_size() if ids is not None else 0,
-                                   float(scale), _at(log_prob), lse.data_ptr(), stats.data_ptr(), _at(h), top, _at(top_ids),
-                                   _at(top_log_probs), _at(status), _at(ws), need, here.ptr), "tre_log_probs")
+        if stream is not None:
+            here.uses(scores, ids, status, ws)
+        base = flat.data_ptr()
+        _check(L.tre_log_probs(at, dt, n, vocab, cols, rows, tiles, ids_at, id_bytes, float(scale), _at(log_prob), base + 8 * n,
+                               base, _at(h), top, _at(top_ids), _at(top_log_probs), _at(status), _at(ws), need, here.ptr),
+               "tre_log_probs")
     return LogProbs(log_prob, lse, stats, h, top_ids, top_log_probs)
 
 
@@ -762,57 +789,35 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
     import torch
 
     w = "tre.log_probs_grad"
-    dt = _value_type(scores, w, "scores")
-    layout = _scores(scores, w, "scores")
-    n, dev = layout[0], scores.device
+    dt, n, vocab, cols, rows, tiles, at, gpu = _scores(scores, w, "scores")
     if grad_log_prob is None and grad_lse is None and grad_entropy is None:
         raise TreError(STATUS_CODE["TRE_E_ARG"], w, "no gradient given")
-    _want(stats, w, "stats", (n, 2), torch.float32, dev)
-    if ids is not None:
-        _ids(ids, w, dev)
-        if ids.shape != (n,):
-            raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"ids: [{n}] wanted, got {tuple(ids.shape)}")
-    for t, what in ((grad_log_prob, "grad_log_prob"), (grad_lse, "grad_lse"), (grad_entropy, "grad_entropy"), (entropy, "entropy")):
-        if t is not None:
-            _want(t, w, what, (n,), torch.float32, dev)
-    _status(status, w, dev)
+    dev = scores.device
+    stats_at = _floats(stats, w, "stats", n, 2, gpu, dev)
+    ids_at, id_bytes = _words(ids, w, n, gpu, dev)
+    g, gl, gh, h = (_floats(t, w, what, n, 0, gpu, dev) for t, what in (
+        (grad_log_prob, "grad_log_prob"), (grad_lse, "grad_lse"), (grad_entropy, "grad_entropy"), (entropy, "entropy")))
+    if status is not None:
+        _status(status, w, dev)
     dtype = dtype or (out.dtype if out is not None else scores.dtype)
     odt = _value_type(dtype, w, "out")
     with _Here(dev, stream, w) as here:
         if out is None:
             out = here.buffer(lambda: torch.empty(scores.shape, dtype=dtype, device=dev))
-            out_layout = layout[2], n * layout[2]
+            out_rows, out_tiles = cols, n * cols
         elif out.shape != scores.shape or out.device != dev or out.dtype != dtype:
             raise TreError(STATUS_CODE["TRE_E_SHAPE"], w, f"out: {dtype} {tuple(scores.shape)} on {dev} wanted, got {out.dtype} "
                                                           f"{tuple(out.shape)} on {out.device}")
         else:
-            out_layout = _scores(out, w, "out")[3:]
-        here.uses(scores, stats, ids, grad_log_prob, grad_lse, grad_entropy, entropy, out, status)
-        _check(lib().tre_log_probs_grad(scores.data_ptr(), dt, *layout, stats.data_ptr(), _at(ids),
-                                        ids.element_size() if ids is not None else 0, float(scale), _at(grad_log_prob),
-                                        _at(grad_lse), _at(grad_entropy), _at(entropy), out.data_ptr(), odt, *out_layout,
-                                        _at(status), here.ptr), "tre_log_probs_grad")
+            out_rows, out_tiles = _scores(out, w, "out")[4:6]
+        if stream is not None:
+            here.uses(scores, stats, ids, grad_log_prob, grad_lse, grad_entropy, entropy, out, status)
+        _check(lib().tre_log_probs_grad(at, dt, n, vocab, cols, rows, tiles, stats_at, ids_at, id_bytes, float(scale), g, gl, gh, h,
+                                        out.data_ptr(), odt, out_rows, out_tiles, _at(status), here.ptr), "tre_log_probs_grad")
     return out
 
 
 # ------------------------------------------- a training step of many tensors
-
-_tensors = None
-
-
-def _reader():
-    """The reader of lists of tensors, _tensors.so (no other path)."""
-    global _tensors
-    if _tensors is None:
-        import torch  # noqa: F401  (whose libraries it uses)
-
-        try:
-            from . import _tensors as t
-        except ImportError as e:
-            raise RuntimeError(f"_tensors.so is missing: build it with `python -m paper_2603_08957_amd.build` ({e})") from None
-        _tensors = t
-    return _tensors
-
 
 class _Many:
     """Host arrays of contiguous GPU tensors' addresses, types and elements, all
