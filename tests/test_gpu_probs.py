@@ -412,3 +412,73 @@ def test_tiles_of_a_score_einsum():
     gt = torch.zeros(vocab, d, dtype=torch.double).index_add_(0, ids[ids >= 0], gx[ids >= 0])
     ot = torch.zeros(vocab, d, dtype=torch.double).index_add_(0, ids[ids >= 0], off[ids >= 0] + 40 * U * gx[ids >= 0].abs())
     assert ((dt.cpu().double() - gt).abs() <= ot + 41 * U).all()
+
+
+def test_refusals():
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    def refused(wanted, f, *a, **kw):
+        with pytest.raises(tre.TreError) as e:
+            f(*a, **kw)
+        assert e.value.status == wanted
+
+    x = torch.randn(4, 60, device="cuda")
+    ids = torch.zeros(4, dtype=torch.int64, device="cuda")
+    refused("TRE_E_SHAPE", tre.log_probs, x.T)
+    refused("TRE_E_SHAPE", tre.log_probs, x[:, :0])
+    refused("TRE_E_SHAPE", tre.log_probs, x.view(2, 2, 3, 20))
+    refused("TRE_E_DTYPE", tre.log_probs, x.half())
+    refused("TRE_E_SHAPE", tre.log_probs, x, ids[:3])
+    refused("TRE_E_SHAPE", tre.log_probs, x.view(4, 3, 20), ids)  # (tiles of three tokens)
+    refused("TRE_E_SHAPE", tre.log_probs, x, ids.repeat(2)[::2])
+    refused("TRE_E_DTYPE", tre.log_probs, x, ids.float())
+    refused("TRE_E_ARG", tre.log_probs, x, ids.cpu())
+    refused("TRE_E_SHAPE", tre.log_probs, x, ids, top=61)
+    refused("TRE_E_SHAPE", tre.log_probs, torch.randn(4, 80, device="cuda"), ids, top=65)
+    refused("TRE_E_SHAPE", tre.log_probs, x, ids, top=-1)
+    for scale in (0.0, -1.0, math.nan, math.inf):
+        refused("TRE_E_ARG", tre.log_probs, x, ids, scale=scale)
+    refused("TRE_E_DTYPE", tre.log_probs, x, ids, status=torch.zeros(1, device="cuda"))
+    long = torch.randn(1, 1 << 20, device="cuda")
+    assert tre.log_probs_workspace_bytes(1, 1 << 20) > 0
+    refused("TRE_E_WORKSPACE", tre.log_probs, long, ws=torch.empty(256, dtype=torch.uint8, device="cuda")[:16])
+    refused("TRE_E_ARG", tre.log_probs, long, ws=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[8:])
+    ws = tre.alloc_workspace(tre.log_probs_workspace_bytes(1, 1 << 20, top=3))
+    assert torch.equal(tre.log_probs(long, top=3, ws=ws).top_ids, tre.log_probs(long, top=3).top_ids)
+
+    r = tre.log_probs(x, ids, entropy=True)
+    g = torch.ones(4, device="cuda")
+    refused("TRE_E_ARG", tre.log_probs_grad, x, r.stats, ids)
+    refused("TRE_E_ARG", tre.log_probs_grad, x, r.stats, None, g)
+    refused("TRE_E_ARG", tre.log_probs_grad, x, r.stats, ids, grad_entropy=g)
+    refused("TRE_E_SHAPE", tre.log_probs_grad, x, r.stats[:, 0], ids, g)
+    refused("TRE_E_DTYPE", tre.log_probs_grad, x, r.stats.double(), ids, g)
+    refused("TRE_E_SHAPE", tre.log_probs_grad, x, r.stats, ids, g.repeat(2)[::2])
+    refused("TRE_E_DTYPE", tre.log_probs_grad, x, r.stats, ids, g.double())
+    refused("TRE_E_ARG", tre.log_probs_grad, x, r.stats, ids, g.cpu())
+    refused("TRE_E_DTYPE", tre.log_probs_grad, x, r.stats, ids, g, dtype=torch.float16)
+    refused("TRE_E_SHAPE", tre.log_probs_grad, x, r.stats, ids, g, out=torch.empty(4, 61, device="cuda"))
+    refused("TRE_E_SHAPE", tre.log_probs_grad, x, r.stats, ids, g, dtype=torch.bfloat16, out=torch.empty(4, 60, device="cuda"))
+    refused("TRE_E_SHAPE", tre.log_probs_grad, x, r.stats, ids, g, out=torch.empty(1, 60, device="cuda").expand(4, 60))
+    refused("TRE_E_SHAPE", tre.log_probs_grad, x, r.stats, ids, g, out=torch.empty(60, 4, device="cuda").T)
+    # in place, but laid out otherwise
+    buf = torch.randn(4, 120, device="cuda")
+    refused("TRE_E_ARG", tre.log_probs_grad, buf[:, :60], r.stats, ids, g, out=buf.view(8, 60)[:4])
+
+
+def test_scores_that_all_tokens_share():
+    """Rows at a stride of zero are read as they are."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    x = torch.randn(1, 5000, device="cuda")
+    ids = torch.arange(6, device="cuda")
+    r = tre.log_probs(x.expand(6, 5000), ids, top=4)
+    want = tre.log_probs(x.repeat(6, 1), ids, top=4)
+    for a, b in zip(vars(r).values(), vars(want).values()):
+        assert a is None and b is None or torch.equal(a, b)
+    g = torch.ones(6, device="cuda")
+    assert torch.equal(tre.log_probs_grad(x.expand(6, 5000), r.stats, ids, g), tre.log_probs_grad(x.repeat(6, 1), r.stats, ids, g))
