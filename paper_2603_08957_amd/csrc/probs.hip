@@ -21,6 +21,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 // Runs of a lane in flight together.
 constexpr int kRuns = 4;
+constexpr int kMostWaves = 16;  // of a row
 
 // Scores as rows (one tile) or as the tiles of a relation keyed by the word's
 // tile: x[i, v] at (v / cols) tile_stride + i row_stride + v % cols.  A row is
@@ -197,51 +198,54 @@ __device__ inline void sort_lanes(uint64_t& k) {  // smallest first
     merge_lanes<SIZE / 2>(k, SIZE == 64 || !(threadIdx.x & SIZE));
 }
 
+// What a wavefront keeps of its scores: at first no more than the keys as they come
+// (`pending`, LDS); 64 of them are sorted and merged into a list of the best that the
+// lanes hold.  (Insertion one by one takes 300 cycles each, a wavefront's sort and
+// merge 2700.)
+constexpr int kPending = 128;
 struct Top {
-    uint64_t key;  // of a lane, largest first
-    uint64_t last; // the top-th
-    int k;
+    uint64_t key;   // of a lane, largest first; none before the first merge
+    uint64_t last;  // the top-th
+    int n, k;       // pending, below 64; top
     __device__ void init(int top) {
         key = last = 0;
+        n = 0;
         k = top;
     }
-    __device__ uint64_t lane_key(int lane) const {
-        return uint64_t(uint32_t(__builtin_amdgcn_readlane(int(key >> 32), lane))) << 32 |
-               uint32_t(__builtin_amdgcn_readlane(int(key), lane));
-    }
-    __device__ void settle() { last = lane_key(k - 1); }
-    // Whether any of these keys has a place.
-    __device__ bool beaten(uint64_t k) const { return __ballot(k > last) != 0; }
+    // Whether any of these keys has a place in the list.
+    __device__ bool beaten(uint64_t c) const { return __ballot(c > last) != 0; }
     // 64 keys, smallest first
     __device__ void merge(uint64_t sorted) {
         key = key > sorted ? key : sorted;
         merge_lanes<32>(key, false);
-        settle();
+        last = uint64_t(uint32_t(__builtin_amdgcn_readlane(int(key >> 32), k - 1))) << 32 |
+               uint32_t(__builtin_amdgcn_readlane(int(key), k - 1));
     }
-    __device__ void insert(uint64_t c) {  // (the same in all lanes)
-        if (c <= last) return;
+    __device__ void merge_pending(uint64_t (&pending)[kPending]) {  // the first 64 of them
         const int lane = threadIdx.x & 63;
-        const int at = __popcll(__ballot(key > c));
-        const uint32_t hi = __builtin_amdgcn_update_dpp(0, uint32_t(key >> 32), 0x138, 0xf, 0xf, true);  // the lane before
-        const uint32_t lo = __builtin_amdgcn_update_dpp(0, uint32_t(key), 0x138, 0xf, 0xf, true);
-        key = lane < at ? key : lane == at ? c : uint64_t(hi) << 32 | lo;
-        settle();
+        uint64_t c = lane < n ? pending[lane] : 0;
+        const uint64_t rest = lane + 64 < n ? pending[lane + 64] : 0;
+        sort_lanes<64>(c);
+        merge(c);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (lane + 64 < n) pending[lane] = rest;
+        n = max(n - 64, 0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    // Keys of the lanes of `from`.  More than a few are sorted and merged: that
-    // takes as long as some 12 insertions.
-    __device__ void take(uint64_t mine, uint64_t from) {
-        if (__popcll(from) > 12) {
-            uint64_t k = from >> (threadIdx.x & 63) & 1 ? mine : 0;
-            sort_lanes<64>(k);
-            merge(k);
-            return;
-        }
-#pragma unroll 1
-        for (; from; from &= from - 1) {
-            const int lane = __ffsll((unsigned long long)from) - 1;
-            insert(uint64_t(uint32_t(__builtin_amdgcn_readlane(int(mine >> 32), lane))) << 32 |
-                   uint32_t(__builtin_amdgcn_readlane(int(mine), lane)));
-        }
+    // Keys of the lanes of `from`.
+    __device__ void take(uint64_t (&pending)[kPending], uint64_t mine, uint64_t from) {
+        const int lane = threadIdx.x & 63;
+        if (from >> lane & 1) pending[n + __popcll(from & ((uint64_t(1) << lane) - 1))] = mine;
+        n += __popcll(from);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (other lanes read it)
+        if (n >= 64) merge_pending(pending);
+    }
+    // The wavefront's best, a key a lane: as they came, or the list.
+    __device__ uint64_t best(uint64_t (&pending)[kPending]) {
+        const int lane = threadIdx.x & 63;
+        if (last == 0) return lane < n ? pending[lane] : 0;
+        if (n > 0) merge_pending(pending);
+        return lane < k ? key : 0;
     }
 };
 
@@ -258,11 +262,14 @@ __device__ inline Sums join(Sums a, Sums b, float scale2) {
     return {m, fa * a.s + fb * b.s, fa * (a.t + a.s * da) + fb * (b.t + b.s * db)};
 }
 
-template <int MASK, bool ENT>
+__device__ inline float first_lane(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+// The sums of lanes 0 to 2 END - 1 in one, in each of them up to its last bits.
+template <int MASK, int END, bool ENT>
 __device__ inline void join_lanes(Sums& u, float scale2) {
     u = join(u, {swap_lanes<MASK>(u.m), swap_lanes<MASK>(u.s), ENT ? swap_lanes<MASK>(u.t) : 0.f}, scale2);
-    if constexpr (MASK < 32) join_lanes<MASK * 2, ENT>(u, scale2);
+    if constexpr (MASK < END) join_lanes<MASK * 2, END, ENT>(u, scale2);
 }
+__device__ inline Sums first_lane(Sums u) { return {first_lane(u.m), first_lane(u.s), first_lane(u.t)}; }
 
 struct ProbArgs {
     Scores g;
@@ -285,57 +292,67 @@ __device__ inline const T* score_at(const ProbArgs& a, int64_t row, int64_t word
     return static_cast<const T*>(a.x) + tile * a.g.tile_stride + row * a.g.row_stride + (word - tile * a.g.cols);
 }
 
-// The first words that cannot come, behind those that can.
+// A token's given word.
 template <typename T>
-__device__ inline void fill_top(const ProbArgs& a, int64_t row, Top& top) {
-    const int lane = threadIdx.x & 63;
-    int have = __popcll(__ballot(top.key != 0));
-    for (int64_t w = lane; have < a.top && w - lane < a.g.vocab; w += 64) {
-        bool dead = false;
-        if (w < a.g.vocab) dead = !(load1(score_at<T>(a, row, w)) > -kInf);
-        for (uint64_t m = __ballot(dead); m && have < a.top; m &= m - 1, have++) {
-            const uint32_t word = uint32_t(w - lane) + uint32_t(__ffsll((unsigned long long)m)) - 1;
-            if (lane == have) top.key = uint64_t(kOrderLowest) << 32 | uint32_t(~word);
-        }
-    }
+__device__ inline int64_t given_word(const ProbArgs& a, int64_t row) {
+    return a.log_prob ? token(a.ids, a.id_bytes, row) : -1;
 }
-
-// A token's given word: its score is loaded before a row's pass, which hides it.
+// Its score as it comes (no word's: any), so that nothing waits for it.
+template <typename T>
 struct Given {
-    float x;
+    T raw;
     bool is;
+    __device__ float x() const {
+        if constexpr (sizeof(T) == 4) return raw;
+        else return __uint_as_float(uint32_t(raw) << 16);
+    }
 };
 template <typename T>
-__device__ inline Given given_of(const ProbArgs& a, int64_t row) {
-    Given g{0.f, false};
-    if (!a.log_prob) return g;
-    const int64_t id = token(a.ids, a.id_bytes, row);
-    g.is = id >= 0 && id < a.g.vocab;
-    if (g.is) g.x = load1(score_at<T>(a, row, id));
-    else if (id >= 0 && a.status) *a.status = TRE_E_KEYRANGE;
-    return g;
+__device__ inline Given<T> given_of(const ProbArgs& a, int64_t row, int64_t id) {
+    const int64_t last = a.g.vocab - 1;
+    return {*score_at<T>(a, row, min(max(id, int64_t(0)), last)), id >= 0 && id <= last};
 }
 
+// What a row's sums say.
+struct Row {
+    float m, logs;
+    bool empty;
+    __device__ explicit Row(Sums u) : m(u.s == 0.f ? -kInf : u.m), logs(logf(u.s)), empty(u.s == 0.f) {}
+    __device__ float log_prob(float x, float scale) const { return empty ? -kInf : (x - m) * scale - logs; }
+};
+
+// (one thread)
 template <typename T>
-__device__ inline void put_row(const ProbArgs& a, int64_t row, Sums u, Top& top, Given given) {
-    const int lane = threadIdx.x & 63;
-    if (a.top_ids && top.last == 0) fill_top<T>(a, row, top);
-    const bool empty = u.s == 0.f;
-    const float m = empty ? -kInf : u.m, logs = logf(u.s);
-    if (a.top_ids && lane < a.top) {
-        const float v = of_order(uint32_t(top.key >> 32));
-        a.top_ids[row * a.top + lane] = int32_t(~uint32_t(top.key));
-        a.top_log_probs[row * a.top + lane] = empty ? -kInf : (v - m) * a.scale - logs;
-    }
-    if (lane) return;
-    a.stats[2 * row] = m;
-    a.stats[2 * row + 1] = logs;
-    a.lse[row] = a.scale * m + logs;
+__device__ inline void put_sums(const ProbArgs& a, int64_t row, Sums u, Row r, Given<T> given, int64_t word) {
+    a.stats[2 * row] = r.m;
+    a.stats[2 * row + 1] = r.logs;
+    a.lse[row] = a.scale * r.m + r.logs;
     if (a.entropy) {
-        const float h = logs - kLn2 * u.t / u.s;
-        a.entropy[row] = empty || h < 0.f ? 0.f : h;  // (a sum that rounding took below zero)
+        const float h = r.logs - kLn2 * u.t / u.s;
+        a.entropy[row] = r.empty || h < 0.f ? 0.f : h;  // (a sum that rounding took below zero)
     }
-    if (a.log_prob) a.log_prob[row] = !given.is ? 0.f : empty ? -kInf : (given.x - m) * a.scale - logs;
+    if (!a.log_prob) return;
+    a.log_prob[row] = given.is ? r.log_prob(given.x(), a.scale) : 0.f;
+    if (word >= a.g.vocab && a.status) *a.status = TRE_E_KEYRANGE;
+}
+// A word of rank `rank`, where that is one of the top ones.
+__device__ inline void put_top(const ProbArgs& a, int64_t row, Row r, uint64_t key, int rank) {
+    if (rank >= a.top) return;
+    a.top_ids[row * a.top + rank] = int32_t(~uint32_t(key));
+    a.top_log_probs[row * a.top + rank] = r.log_prob(of_order(uint32_t(key >> 32)), a.scale);
+}
+// The first words that cannot come, behind the `have` that can (a wavefront).
+template <typename T>
+__device__ inline void fill_top(const ProbArgs& a, int64_t row, Row r, int have) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t b = 0; have < a.top && b < a.g.vocab; b += 64) {
+        const int64_t w = b + lane;
+        bool dead = false;
+        if (w < a.g.vocab) dead = !(load1(score_at<T>(a, row, w)) > -kInf);
+        const uint64_t all = __ballot(dead);
+        if (dead) put_top(a, row, r, uint64_t(kOrderLowest) << 32 | uint32_t(~uint32_t(w)), have + __popcll(all & ((uint64_t(1) << lane) - 1)));
+        have += __popcll(all);
+    }
 }
 
 // Element `at` < N of a lane's runs, from FROM on.
@@ -350,18 +367,23 @@ __device__ inline float pick(const float (&v)[kRuns][E], uint32_t at) {
 
 // W wavefronts to a row, or to a part of it; with one, a workgroup has kWaves rows.
 //
-// Top words.  A score has a place in a wavefront's list if it is higher than the
-// list's last, whose words come before, and not lower than what the row's other
-// wavefronts have (`bar`).  Lists that fill from nothing would take hundreds of
-// scores in: so at first a score that top / W lanes of every wavefront reach, or
-// top lanes of one, bars all that is lower.
+// Top words.  A score may have a place if it is higher than the last of the
+// wavefront's list, whose words come before, and not lower than what as many scores
+// of the row as are wanted are known to reach (`known`): at first what top / W lanes
+// of every wavefront reach, or top lanes of one, later the last of any list (`bar`).
+// At the end what top / W keys of every wavefront reach leaves few; the rank of each
+// of these is the number of those that are larger, a part of which every wavefront
+// counts.  (Lists in order merged in pairs took 5 us of 12.5 for 20 of 32768.)
 template <typename T, int FIT, bool TOP, bool ENT, int W>
 __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a) {
     constexpr int E = 16 / sizeof(T);
     constexpr uint32_t kStep = 64 * kRuns;
     __shared__ Sums sums[W];
-    __shared__ uint64_t keys[TOP && W > 1 ? W : 1][64];
-    __shared__ uint32_t bar, reach[W];
+    __shared__ uint64_t pending[TOP ? (W > 1 ? W : kWaves) : 1][TOP ? kPending : 1];
+    __shared__ uint64_t pool[TOP && W > 1 ? W * 64 : 1];
+    __shared__ int rank[TOP && W > 1 ? W * 64 : 1];
+    __shared__ uint32_t bar, reach[W], reach_last[W];  // (a wavefront may be done while another still reads `reach`)
+    __shared__ int count;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t task = W > 1 ? block_index() : block_index() * kWaves + wave;
     const int64_t row = a.splits > 1 ? task / a.splits : task;
@@ -369,15 +391,19 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
     const uint32_t split = uint32_t(task - row * a.splits);
     const uint32_t q0 = split * a.per, q1 = min(q0 + a.per, a.g.total);
     const T* x = static_cast<const T*>(a.x) + row * a.g.row_stride;
-    Given given{0.f, false};
-    if ((W == 1 || wave == 0) && a.splits == 1) given = given_of<T>(a, row);
+    // the given word, and its score when the row's first loads are on their way
+    Given<T> given{};
+    const int64_t word = (W == 1 || wave == 0) && a.splits == 1 ? given_word<T>(a, row) : -1;
     Sums u{-FLT_MAX, 0.f, 0.f};
     Top top;
     uint32_t known = 0;
     if constexpr (TOP) {
         top.init(a.top);
         if constexpr (W > 1) {
-            if (threadIdx.x == 0) bar = 0;
+            if (threadIdx.x == 0) {
+                bar = 0;
+                count = 0;
+            }
             __syncthreads();
         }
     }
@@ -388,6 +414,7 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
         Run<T, E, FIT> r[kRuns];
 #pragma unroll
         for (int j = 0; j < kRuns; j++) r[j].load(a.g, x, min(b + j * 64 + lane, q1 - 1));
+        if (b0 == q0 && (W == 1 || wave == 0) && a.log_prob && a.splits == 1) given = given_of<T>(a, row, word);
         float v[kRuns][E], most[kRuns];
 #pragma unroll
         for (int j = 0; j < kRuns; j++) {
@@ -415,9 +442,9 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
                 known = max(known, *static_cast<volatile uint32_t*>(&bar));
             }
             known = __builtin_amdgcn_readfirstlane(known);
-            uint32_t least = max(max(uint32_t(top.last >> 32), kOrderLowest) + 1, known);
             // (a wavefront of few words that can come bars nothing for the others)
-            if (top.last == 0 && known <= kOrderLowest + 1) least = max(least, reached(order_of(all), a.top));
+            if (known <= kOrderLowest + 1 && top.last == 0) known = reached(order_of(all), a.top);
+            const uint32_t least = max(max(uint32_t(top.last >> 32), kOrderLowest) + 1, known);
             float limit = of_order(least);
             if (__ballot(all >= limit)) {
                 // a bit for each of a lane's scores that may have a place; then one of each lane at a time
@@ -435,7 +462,7 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
                     Run<T, E, FIT> run;
                     run.find(a.g, b + uint32_t(at) / E * 64 + lane);
                     const uint64_t from = __ballot(mine != 0 && y >= limit);
-                    if (from) top.take(key_of(y, run.tile * a.g.cols + run.start + uint32_t(at) % E), from);
+                    if (from) top.take(pending[wave], key_of(y, run.tile * a.g.cols + run.start + uint32_t(at) % E), from);
                     mine &= mine - 1;
                     limit = fmaxf(limit, of_order(max(uint32_t(top.last >> 32), kOrderLowest + 1)));
                 }
@@ -457,32 +484,76 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
                 if constexpr (ENT) u.t += e * fmaxf(z, -2000.f);  // (no 0 * inf)
             }
     }
-    join_lanes<1, ENT>(u, a.scale2);
-    if constexpr (W > 1) {
+    join_lanes<1, 32, ENT>(u, a.scale2);
+    uint64_t key = 0;
+    if constexpr (TOP) key = top.best(pending[wave]);
+    if constexpr (W == 1) {
+        const Row r(first_lane(u));
+        if constexpr (TOP) {
+            int at = lane, n = a.top;
+            if (top.last == 0) {
+                n = top.n;
+                at = 0;
+                for (int j = 0; j < n; j++) at += pending[wave][j] > key;
+            }
+            if (key) put_top(a, row, r, key, at);
+            if (n < a.top) fill_top<T>(a, row, r, n);  // (n: all that can come)
+        }
+        if (lane == 0) put_sums(a, row, u, r, given, word);
+    } else {
         if (lane == 0) sums[wave] = u;
         if constexpr (TOP) {
-            // lists in pairs: those of the upper half go to the lower one
-#pragma unroll 1
-            for (int h = W / 2; h > 0; h /= 2) {
-                if (wave >= h && wave < 2 * h) keys[wave][lane] = lane < a.top ? top.key : 0;
-                __syncthreads();
-                if (wave < h) {
-                    const uint64_t k = keys[wave + h][63 - lane];
-                    if (top.beaten(k)) top.merge(k);
-                }
-            }
-        } else {
+            rank[threadIdx.x] = 0;
+            const uint32_t own = reached(uint32_t(key >> 32), (a.top + W - 1) / W);
+            if (lane == 0) reach_last[wave] = own;
             __syncthreads();
-        }
-        if (wave) return;
+            uint32_t least = reach_last[0];
 #pragma unroll
-        for (int w = 1; w < W; w++) u = join(u, sums[w], a.scale2);
-    }
-    if (a.splits > 1) {
-        if (lane == 0) a.part[task] = u;
-        if (TOP && lane < a.top) a.part_keys[task * a.top + lane] = top.key;
-    } else {
-        put_row<T>(a, row, u, top, given);
+            for (int w = 1; w < W; w++) least = min(least, reach_last[w]);
+            least = max(least, max(known, bar));
+            const bool in = key && uint32_t(key >> 32) >= least;
+            const uint64_t from = __ballot(in);
+            int at = 0;
+            if (lane == 0 && from) at = atomicAdd(&count, __popcll(from));
+            at = __builtin_amdgcn_readfirstlane(at);
+            if (in) pool[at + __popcll(from & ((uint64_t(1) << lane) - 1))] = key;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            if constexpr (W == kMostWaves) {
+                u = sums[lane & (W - 1)];
+                join_lanes<1, W / 2, ENT>(u, a.scale2);
+            } else {
+#pragma unroll
+                for (int w = 1; w < W; w++) u = join(u, sums[w], a.scale2);
+            }
+            if (TOP && lane == 0) sums[0] = u;  // (what the others take when all have counted)
+        }
+        if constexpr (TOP) {
+            const int n = count, j0 = wave * n / W, j1 = (wave + 1) * n / W;
+            for (int c = 0; c < n; c += 64) {
+                const uint64_t mine = c + lane < n ? pool[c + lane] : 0;
+                int larger = 0;
+                for (int j = j0; j < j1; j++) larger += pool[j] > mine;
+                if (larger) atomicAdd(&rank[c + lane], larger);
+            }
+            __syncthreads();
+            u = sums[0];
+        }
+        const Row r(u);
+        if constexpr (TOP) {
+            const int n = count, i = threadIdx.x;
+            if (a.splits > 1) {
+                if (i < n && rank[i] < a.top) a.part_keys[task * a.top + rank[i]] = pool[i];
+                if (i >= n && i < a.top) a.part_keys[task * a.top + i] = 0;
+            } else {
+                if (i < n) put_top(a, row, r, pool[i], rank[i]);
+                if (n < a.top && wave == 0) fill_top<T>(a, row, r, n);  // (n: all that can come)
+            }
+        }
+        if (threadIdx.x) return;  // (without top words the others' sums are their own)
+        if (a.splits > 1) a.part[task] = u;
+        else put_sums(a, row, u, r, given, word);
     }
 }
 
@@ -494,9 +565,10 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
     const int lane = threadIdx.x;
     const int64_t row = block_index();
     if (row >= a.g.n) return;
-    const Given given = given_of<T>(a, row);
+    const int64_t word = given_word<T>(a, row);
     Sums u = lane < int(a.splits) ? a.part[row * a.splits + lane] : Sums{-FLT_MAX, 0.f, 0.f};
-    join_lanes<1, true>(u, a.scale2);
+    join_lanes<1, 32, true>(u, a.scale2);
+    u = first_lane(u);
     Top top;
     top.init(a.top_ids ? a.top : 1);
     if (a.top_ids) {
@@ -511,7 +583,14 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
                 if (top.beaten(k[i])) top.merge(k[i]);
         }
     }
-    put_row<T>(a, row, u, top, given);
+    const Row r(u);
+    if (a.top_ids) {
+        if (top.key) put_top(a, row, r, top.key, lane);
+        if (top.last == 0) fill_top<T>(a, row, r, __popcll(__ballot(top.key != 0)));
+    }
+    Given<T> given{};
+    if (a.log_prob) given = given_of<T>(a, row, word);
+    if (lane == 0) put_sums(a, row, u, r, given, word);
 }
 
 // A row of few scores is one wavefront's, one of many four wavefronts'.  Few rows
@@ -519,7 +598,6 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
 // two, and are cut where that still leaves long rows to few workgroups.
 constexpr int64_t kWaveRuns = 4 * 64 * kRuns;    // up to so many runs
 constexpr int64_t kFewRows = 512;
-constexpr int kMostWaves = 16;
 constexpr int64_t kLongRuns = 4 * kMostWaves * 64 * kRuns;
 constexpr int64_t kFill = 256;                   // workgroups
 constexpr uint32_t kMaxSplits = 32;
