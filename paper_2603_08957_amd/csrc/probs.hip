@@ -5,7 +5,16 @@
 //   lse = scale m + log s,   log p_v = d_v - log s,   entropy = log s - t / s.
 // Every score is read once: lanes keep a maximum of their own and sums by it,
 // and only where these are joined are they brought to one maximum.  Exponentials
-// are taken to the base 2, with log2(e) in the scale.
+// are taken to the base 2, with log2(e) in the scale.  x - m comes before the
+// product with the scale, so that large scores lose nothing, and the maximum and
+// log s are kept apart for the gradient for the same reason: a probability out of
+// lse alone is off by 2^-24 |lse|.
+//
+// Memory bounds large calls: 8192 x 32768 bf16 scores with entropy take 101 us
+// (5.3 TB/s; 11 vector operations a score, 81 us of the vector units' time), their
+// gradient in bf16 194 us (5.3 TB/s read and written).  Of 2048 x 32768 with 8 top
+// words, 39 us, the words are 10.  A lane's four loads of 16 bytes are in flight
+// together: with each waited for the first took 113 us.
 #include "tre_internal.h"
 #include "values.h"
 
@@ -593,9 +602,11 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
     if (lane == 0) put_sums(a, row, u, r, given, word);
 }
 
-// A row of few scores is one wavefront's, one of many four wavefronts'.  Few rows
+// A row of few scores is one wavefront's, one of many four wavefronts' (one takes
+// 107 us for 8192 x 32768 bf16, four 103; with 8 top words 117 and 119).  Few rows
 // have sixteen wavefronts each, which is one launch where a row cut into parts is
-// two, and are cut where that still leaves long rows to few workgroups.
+// two (one row of 32768 with 20 top words 10.4 us, in 8 parts of four wavefronts
+// 13), and are cut where that still leaves long rows to few workgroups.
 constexpr int64_t kWaveRuns = 4 * 64 * kRuns;    // up to so many runs
 constexpr int64_t kFewRows = 512;
 constexpr int64_t kLongRuns = 4 * kMostWaves * 64 * kRuns;
