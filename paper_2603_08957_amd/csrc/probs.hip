@@ -10,10 +10,10 @@
 // log s are kept apart for the gradient for the same reason: a probability out of
 // lse alone is off by 2^-24 |lse|.
 //
-// Memory bounds large calls: 8192 x 32768 bf16 scores with entropy take 101 us
+// Memory bounds large calls: 8192 x 32768 bf16 scores with entropy take 102 us
 // (5.3 TB/s; 11 vector operations a score, 81 us of the vector units' time), their
 // gradient in bf16 194 us (5.3 TB/s read and written).  Of 2048 x 32768 with 8 top
-// words, 39 us, the words are 10.  A lane's four loads of 16 bytes are in flight
+// words, 35 us, the words are 11.  A lane's four loads of 16 bytes are in flight
 // together: with each waited for the first took 113 us.
 #include "tre_internal.h"
 #include "values.h"
@@ -602,12 +602,18 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
     if (lane == 0) put_sums(a, row, u, r, given, word);
 }
 
-// A row of few scores is one wavefront's, one of many four wavefronts' (one takes
-// 107 us for 8192 x 32768 bf16, four 103; with 8 top words 117 and 119).  Few rows
+// A row of few scores is one wavefront's, one of many four wavefronts'.  Many rows
+// fill the device with a wavefront each, and four that wait for each other at a
+// row's top words take longer: one and four take, for 20000 bf16 scores (2500 runs)
+// with 8 top words, 18 and 13 us for 600 rows, 25 and 27 for 2048, 69 and 94 for
+// 8192 (without top words 9, 7; 15, 16; 55, 57).  With 32768 (4096 runs) 36 and 34
+// us for 2048 rows, 113 and 115 for 8192.  Few rows
 // have sixteen wavefronts each, which is one launch where a row cut into parts is
 // two (one row of 32768 with 20 top words 10.4 us, in 8 parts of four wavefronts
 // 13), and are cut where that still leaves long rows to few workgroups.
 constexpr int64_t kWaveRuns = 4 * 64 * kRuns;    // up to so many runs
+constexpr int64_t kManyRows = 2048;              // from so many rows
+constexpr int64_t kManyRuns = 14 * 64 * kRuns;   // up to so many runs
 constexpr int64_t kFewRows = 512;
 constexpr int64_t kLongRuns = 4 * kMostWaves * 64 * kRuns;
 constexpr int64_t kFill = 256;                   // workgroups
@@ -618,7 +624,8 @@ struct Cut {
     uint32_t splits, per;
 };
 Cut cut_of(const Scores& g) {
-    Cut c{int64_t(g.total) <= kWaveRuns ? 1 : g.n > kFewRows ? kWaves : kMostWaves, 1, g.total};
+    const bool one = int64_t(g.total) <= (g.n < kManyRows ? kWaveRuns : kManyRuns);
+    Cut c{one ? 1 : g.n > kFewRows ? kWaves : kMostWaves, 1, g.total};
     if (c.waves < kMostWaves || int64_t(g.total) <= kLongRuns || g.n > kFill / 2) return c;
     const uint32_t step = kMostWaves * 64 * kRuns, steps = (g.total + step - 1) / step;
     const uint32_t s = uint32_t(std::min<int64_t>(std::min<int64_t>(steps, kMaxSplits), kFill / std::max<int64_t>(g.n, 1)));

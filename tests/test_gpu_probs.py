@@ -145,6 +145,26 @@ def test_log_probs(n, vocab, tile, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,tile", [(2047, 8250, 250), (2048, 8250, 250), (2051, 8193, 0)])
+def test_many_rows(n, vocab, tile, dtype):
+    """A wavefront to each of many rows, four to one of fewer."""
+    import torch
+
+    import paper_2603_08957_amd as tre
+
+    rng = np.random.default_rng(n + vocab)
+    x, rows = scores_of(rng, n, vocab, tile, dtype, strided=True)
+    ids = rng.integers(0, vocab, n)
+    want = Reference(rows, ids, 0.7)
+    for top, entropy in ((0, True), (9, True)):
+        r = tre.log_probs(x, torch.from_numpy(ids).cuda(), scale=0.7, top=top, entropy=entropy)
+        want.check(r, ids, top, entropy)
+    again = tre.log_probs(x, torch.from_numpy(ids).cuda(), scale=0.7, top=9, entropy=True)
+    for a, b in zip(vars(r).values(), vars(again).values()):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,vocab,tile", [(1, 300, 0), (12, 515, 103), (12, 9000, 0), (3, 33000, 250), (12, 40000, 0)])
 def test_rows_of_few_words(n, vocab, tile, dtype):
     """-inf: masked words, rows of one word and of none; all scores alike; scores of one sign of zero and the other."""
