@@ -5,7 +5,7 @@
 // number of the first workgroup of each, so that nothing is kept on the device
 // between calls and a captured call holds what it was given.  Memory bounds both:
 // 134 M fp32 weights, gradients and moments take 679 us (5.5 TB/s), 67 M weights in
-// fp32 with bf16 gradients and 8-bit moments 185 (5.1), the norm of 400 M bf16
+// fp32 with bf16 gradients and 8-bit moments 176 (5.4), the norm of 400 M bf16
 // gradients 141 (5.7).  Rounded by chance, 67 M weights in bf16 take 170 us, of
 // which the vector units work 120 (70 operations an element, 15 of them the hash).
 #include "tre_internal.h"
