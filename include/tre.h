@@ -653,7 +653,7 @@ tre_status tre_grad_norm(int32_t n_tensors, const void *const *tensors, const in
  *             probability that their place between two neighbours has, by a hash of
  *             (seed, t, element); else to the nearest, ties to even.
  * Computed in fp32.  At most 2^37 elements in all (TRE_E_SHAPE); TRE_E_ARG unless
- * 0 <= beta < 1, eps > 0, lr >= 0, weight_decay >= 0, all finite, t >= 1 and bits
+ * 0 <= beta < 1, eps >= 2^-126, lr >= 0, weight_decay >= 0, all finite, t >= 1 and bits
  * 8 or 32.  Asynchronous on the stream; may be captured into a graph, which then
  * holds the arrays' addresses. */
 typedef struct {

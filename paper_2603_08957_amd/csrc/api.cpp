@@ -1005,7 +1005,8 @@ tre_status tre_adamw(int32_t n_tensors, void* const* params, const int32_t* para
     }
     auto rate = [](double x) { return x >= 0. && std::isfinite(float(x)); };
     auto beta = [](double x) { return x >= 0. && x < 1.; };
-    if ((opt->bits != 8 && opt->bits != 32) || !beta(opt->beta1) || !beta(opt->beta2) || !rate(opt->eps) || !(float(opt->eps) > 0.f) ||
+    // (a reciprocal of less than 2^-126 is infinite: a weight without moments would become 0 * inf)
+    if ((opt->bits != 8 && opt->bits != 32) || !beta(opt->beta1) || !beta(opt->beta2) || !rate(opt->eps) || !(float(opt->eps) >= 0x1p-126f) ||
         !rate(opt->weight_decay) || (!opt->lr_dev && !rate(opt->lr)) || (!opt->step_dev && opt->step < 1) ||
         (!opt->grad_scale_dev && !std::isfinite(float(opt->grad_scale)))) {
         set_error("tre_adamw: an option is out of range");

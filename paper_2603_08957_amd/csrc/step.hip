@@ -158,6 +158,7 @@ struct AdamArgs {
     const int64_t* step_dev;
     int64_t per;            // elements of a workgroup
     double log_beta1, log_beta2;
+    bool small_roots;       // whether roots below 2^-63 count beside eps
     float b1, nb1, b2, nb2, c1, c2, lr, decay, weight_decay, eps, scale;
     uint32_t seed0, seed1, step;
 };
@@ -298,6 +299,16 @@ __device__ inline void store4(T* at, const float (&v)[kLane], bool cut) {
     store_all<true>(at, v);
 }
 
+// The square root of v c, c >= 1.  The instruction takes what is below 2^-126 for 0,
+// so small ones are brought up by 2^24 first: a root below 2^-63 would be lost, which
+// is less than half a unit of an eps of 2^-39 or more, and only below that is it
+// looked for (four operations more of an element's 72).
+__device__ inline float root_of(float v, float c, bool small) {
+    if (!small) return __builtin_amdgcn_sqrtf(v * c);
+    const bool low = v < 0x1p-100f;
+    return __builtin_amdgcn_sqrtf((low ? v * 0x1p24f : v) * c) * (low ? 0x1p-12f : 1.f);
+}
+
 // 4 elements as they come.
 template <int BITS, typename TP, typename TG>
 struct Held {
@@ -407,7 +418,7 @@ struct Part {
                 mv[i] = mv[i] * b1 + gi * a.nb1;
                 vv[i] = vv[i] * b2 + gi * gi * a.nb2;
             }
-            const float root = __builtin_amdgcn_sqrtf(vv[i] * r.c2) + a.eps;
+            const float root = root_of(vv[i], r.c2, a.small_roots) + a.eps;
             pv[i] = value4(h.p, i) * r.decay + rate * mv[i] * __builtin_amdgcn_rcpf(root);
             if constexpr (CHANCE && sizeof(TP) == 2) {
                 const float up = __uint_as_float((__float_as_uint(pv[i]) + c[i].weight()) & 0xffff0000u);
@@ -591,6 +602,7 @@ hipError_t launch_adamw(int n, void* const* params, const int32_t* param_types, 
     a.decay = float(1. - o.lr * o.weight_decay);
     a.weight_decay = float(o.weight_decay);
     a.eps = float(o.eps);
+    a.small_roots = a.eps < 0x1p-39f;
     a.scale = float(o.grad_scale);
     a.seed0 = uint32_t(o.seed);
     a.seed1 = uint32_t(o.seed >> 32);
