@@ -8,6 +8,7 @@
 // fp32 with bf16 gradients and 8-bit moments 176 (5.4), the norm of 400 M bf16
 // gradients 141 (5.7).  Rounded by chance, 67 M weights in bf16 take 170 us, of
 // which the vector units work 120 (70 operations an element, 15 of them the hash).
+#include "codes.h"
 #include "tre_internal.h"
 #include "values.h"
 
@@ -219,8 +220,6 @@ __device__ inline Chance chance_of(uint32_t low, uint32_t k0, uint32_t k1) {
 }
 __device__ inline uint32_t chance_key(uint32_t k1, int64_t element) { return k1 + uint32_t(element >> 32) * 0xBB67AE85u; }
 
-constexpr int kBias2 = 23;  // of second moments' exponents
-
 // A first moment's codes are those of the instructions for 8-bit floats (4 bits of
 // exponent, bias 7), which stay below 480, their NaN's: two of four codes.
 template <bool UPPER>
@@ -251,23 +250,6 @@ __device__ inline uint32_t first_codes(const float (&y)[4], const C& c) {
     }
     return uint32_t(q);
 }
-__device__ inline int middle(int a, int b, int c) { return min(max(a, b), max(min(a, b), c)); }
-// The code of a second moment times its block's power of two, y < 256.5.  `high` is
-// what it is where E is not 0, `low` where it is; of these and the least code with E
-// = 1 the right one lies in the middle.
-template <bool CHANCE>
-__device__ inline uint32_t second_code(float y, uint32_t word) {
-    constexpr float kUnits = float(1u << (kBias2 + 2));  // of codes below 8
-    constexpr uint32_t kNone = uint32_t(127 - kBias2) << 23;
-    const uint32_t u = __float_as_uint(y);
-    if constexpr (CHANCE) {  // in steps of 2^-20 of a code
-        const int w = middle(int(u - kNone), (8 << 20) - 1, int(y * (kUnits * float(1u << 20))));
-        return (uint32_t(w) + (word >> 12)) >> 20;
-    } else {
-        return uint32_t(middle(int(u - kNone + 0x7ffffu + (u >> 20 & 1)) >> 20, 8, int(rintf(y * kUnits))));
-    }
-}
-
 // The exponent (of a float's bits) of a block's largest magnitude, 7 at least; 8
 // lanes to a block.  255: a NaN or an infinity.
 __device__ inline uint32_t block_exponent(uint32_t bits) {
