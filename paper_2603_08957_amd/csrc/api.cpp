@@ -440,10 +440,8 @@ AsyncBounds async_bounds(const Plan& p, int64_t n_u, int64_t n_v, int64_t max_pa
     if (n_u > 0 && n_v == 1 && keyed_by_u(p)) {
         b.pairs = b.keys = n_u;
     } else {
-        int64_t w_space = 1;
-        for (int c = 0; c < p.nk[2] && w_space <= (int64_t(1) << 37); c++) w_space *= p.radix[2][c];
         b.pairs = (n_u > 0 && n_v > 0) ? std::max<int64_t>(0, std::min(max_pairs, pair_bound(p, n_u, n_v))) : 0;
-        b.keys = std::min(b.pairs, w_space);
+        b.keys = std::min(b.pairs, key_space(p));
     }
     if (b.pairs <= 0) {
         b.ok = true;

@@ -518,6 +518,12 @@ bool u_ranges_possible(const Plan& p) {
            p.opt.max_pairs_per_unit > 0;
 }
 
+int64_t key_space(const Plan& p) {
+    int64_t n = 1;
+    for (int c = 0; c < p.nk[2]; c++) n = n > INT64_MAX / p.radix[2][c] ? INT64_MAX : n * p.radix[2][c];
+    return n;
+}
+
 Layout make_layout(const Plan& p, int64_t n_u, int64_t n_v, int64_t max_pairs) {
     Layout L;
     L.n_u = n_u;
@@ -532,9 +538,7 @@ Layout make_layout(const Plan& p, int64_t n_u, int64_t n_v, int64_t max_pairs) {
     if (u_ranges_possible(p)) {
         // U-range mode: up to kMaxURanges partial tiles per output key, at
         // most 4 GiB of them
-        int64_t wspace = 1;
-        for (int c = 0; c < p.nk[2] && wspace < (int64_t(1) << 40); c++) wspace *= p.radix[2][c];
-        const int64_t n_w_max = std::min<int64_t>(P, wspace);
+        const int64_t n_w_max = std::min<int64_t>(P, key_space(p));
         const int64_t range_cap = std::min<int64_t>(kMaxURanges * n_w_max, (int64_t(4) << 30) / wtile_bytes);
         cap = std::max<int64_t>(cap, range_cap);
     }

@@ -204,6 +204,7 @@ struct Unit {
     int32_t slot;
 };
 
+int64_t key_space(const Plan& p);  // W's keys, INT64_MAX where they are more
 Layout make_layout(const Plan& p, int64_t n_u, int64_t n_v, int64_t max_pairs);
 bool u_ranges_possible(const Plan& p);
 
