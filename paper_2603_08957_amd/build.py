@@ -56,19 +56,24 @@ def build_tensors() -> str:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w", *(f"-I{d}" for d in dirs),
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", os.path.join(HERE, "pysrc", "tensors.cpp"),
            "-o", TENSORS + ".tmp", *(f"-L{d}" for d in libs), "-ltorch_python", "-ltorch_cpu", "-lc10"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+    except OSError as e:
+        raise RuntimeError(f"{os.path.basename(TENSORS)}: no C++ compiler: {e}") from None
     if r.returncode != 0:
         raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stderr}")
     os.replace(TENSORS + ".tmp", TENSORS)
     return TENSORS
 
 
-def build(verbose: bool = False) -> str:
+def build(verbose: bool = False, binding: bool = True) -> str:
+    """Build ``libtre.so``, for which hipcc is enough, and ``_tensors.so``, for
+    which torch, Python's headers and a C++ compiler are needed: the library is
+    linked also where that fails, and without torch only a note is left."""
     os.makedirs(OBJ, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:
-        binding = ex.submit(build_tensors)
+        reader = ex.submit(build_tensors) if binding else None
         objs = list(ex.map(_compile, sources()))
-        binding.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -77,6 +82,11 @@ def build(verbose: bool = False) -> str:
     os.replace(tmp, LIB)
     if verbose:
         print(f"built {LIB}")
+    try:
+        if reader:
+            reader.result()
+    except ImportError as e:
+        print(f"{os.path.basename(TENSORS)}, the Python binding's reader of tensors, is not built: {e}", file=sys.stderr)
     return LIB
 
 
@@ -125,5 +135,5 @@ if __name__ == "__main__":
     if "--host-sanitized" in sys.argv:
         build_host_sanitized(verbose=True)
     else:
-        build(verbose=True)
+        build(verbose=True, binding="--library" not in sys.argv)
     sys.exit(0)
