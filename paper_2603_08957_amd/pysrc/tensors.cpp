@@ -160,9 +160,38 @@ PyObject* views(PyObject*, PyObject* args) try {
     return nullptr;
 }
 
+// written(a, b, ...): counts a version of each tensor, or of those of a list (None: none),
+// as an operation in place does, so that a backward pass that saved one finds it changed.
+// Tensors of inference mode, which nothing saves, have no count.
+bool count_version(PyObject* x) {
+    if (x == Py_None) return true;
+    if (!THPVariable_Check(x)) return false;
+    const at::Tensor& t = THPVariable_Unpack(x);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    return true;
+}
+PyObject* written(PyObject*, PyObject* args) try {
+    bool all = true;
+    for (Py_ssize_t k = 0; k < PyTuple_GET_SIZE(args); k++) {
+        PyObject* x = PyTuple_GET_ITEM(args, k);
+        if (!PyList_Check(x) && !PyTuple_Check(x)) {
+            all = count_version(x) && all;
+            continue;
+        }
+        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(x); i++) all = count_version(PySequence_Fast_GET_ITEM(x, i)) && all;
+    }
+    if (all) Py_RETURN_NONE;
+    PyErr_SetString(PyExc_TypeError, "tensors wanted");
+    return nullptr;
+} catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+}
+
 PyMethodDef methods[] = {{"gather", gather, METH_O, nullptr},       {"same_shapes", same_shapes, METH_VARARGS, nullptr},
                          {"scores", scores, METH_O, nullptr},       {"vector", vector, METH_VARARGS, nullptr},
-                         {"views", views, METH_VARARGS, nullptr},   {nullptr, nullptr, 0, nullptr}};
+                         {"views", views, METH_VARARGS, nullptr},   {"written", written, METH_VARARGS, nullptr},
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

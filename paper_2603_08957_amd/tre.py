@@ -785,7 +785,8 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
     """The gradient by the scores of a loss whose gradients by `log_probs`'s
     log_prob, lse and entropy are given (see tre_log_probs_grad): ``stats`` and
     ``entropy`` are those that it gave.  In the scores' layout and ``dtype`` (the
-    scores'); ``out`` may have strides of its own, and be ``scores``."""
+    scores'); ``out`` may have strides of its own, and be ``scores``.  torch counts
+    the write into ``out`` as one in place."""
     import torch
 
     w = "tre.log_probs_grad"
@@ -801,8 +802,9 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
         _status(status, w, dev)
     dtype = dtype or (out.dtype if out is not None else scores.dtype)
     odt = _value_type(dtype, w, "out")
+    given = out is not None
     with _Here(dev, stream, w) as here:
-        if out is None:
+        if not given:
             out = here.buffer(lambda: torch.empty(scores.shape, dtype=dtype, device=dev))
             out_rows, out_tiles = cols, n * cols
         elif out.shape != scores.shape or out.device != dev or out.dtype != dtype:
@@ -814,6 +816,8 @@ def log_probs_grad(scores, stats, ids=None, grad_log_prob=None, grad_lse=None, g
             here.uses(scores, stats, ids, grad_log_prob, grad_lse, grad_entropy, entropy, out, status)
         _check(lib().tre_log_probs_grad(at, dt, n, vocab, cols, rows, tiles, stats_at, ids_at, id_bytes, float(scale), g, gl, gh, h,
                                         out.data_ptr(), odt, out_rows, out_tiles, _at(status), here.ptr), "tre_log_probs_grad")
+        if given:
+            _reader().written(out)
     return out
 
 
@@ -860,8 +864,9 @@ def grad_norm(tensors, max_norm: float | None = None, out=None, ws=None, stream=
     if many.device is None:
         raise TreError(STATUS_CODE["TRE_E_ARG"], w, "tensors: none")
     max_norm = -1.0 if max_norm is None else float(max_norm)
+    given = out is not None
     with _Here(many.device, stream, w) as here:
-        if out is None:
+        if not given:
             out = here.buffer(lambda: torch.empty(2, dtype=torch.float32, device=many.device))
         else:
             _want(out, w, "out", (2,), torch.float32, many.device)
@@ -874,6 +879,8 @@ def grad_norm(tensors, max_norm: float | None = None, out=None, ws=None, stream=
             here.uses(*many.tensors, out, ws)
         _check(lib().tre_grad_norm(many.n, many.addresses, many.types, many.sizes, max_norm, _ptr(out), _ptr(ws),
                                    ws.numel() * ws.element_size(), here.ptr), "tre_grad_norm")
+        if given:
+            _reader().written(out)
     return out
 
 
@@ -894,6 +901,8 @@ def adamw_state(params, bits: int = 32, stream=None):
 
 def _device_value(x, where, what, dtype, device):
     """(host value, tensor) of a number or a device tensor of one."""
+    if isinstance(x, (int, float)):
+        return x, None
     import torch
 
     if not isinstance(x, torch.Tensor):
@@ -911,7 +920,9 @@ def adamw(params, grads, state, step, lr, beta1: float = 0.9, beta2: float = 0.9
     ``step`` (the first is 1), ``lr`` and ``grad_scale`` are numbers or tensors of
     one value (int64, float32, float32) on the device, read when the step runs.
     With a ``seed`` 8-bit moments and bfloat16 weights are rounded by chance, by
-    (seed, step, element); else to the nearest."""
+    (seed, step, element); else to the nearest.  torch counts the step as one in
+    place of ``params`` and ``state``: a backward pass that saved a weight before
+    it is an error."""
     import torch
 
     w = "tre.adamw"
@@ -935,6 +946,7 @@ def adamw(params, grads, state, step, lr, beta1: float = 0.9, beta2: float = 0.9
             here.uses(*p.tensors, *g.tensors, state, step_dev, lr_dev, scale_dev)
         _check(lib().tre_adamw(p.n, p.addresses, p.types, g.addresses, g.types, p.sizes, _ptr(state), ctypes.byref(opt),
                                here.ptr), "tre_adamw")
+    _reader().written(p.tensors, state)
 
 
 def adamw_moments(state, dtype=None, stream=None):
