@@ -594,7 +594,8 @@ tre_status tre_log_probs(const void *x, int32_t dtype, int64_t n, int64_t vocab,
  *   ids       : as there, needed with by_log_prob; no word has no g_i.
  *   grad      : fp32 or bf16, laid out as the scores with strides of its own, its
  *               rows apart.  May be x itself (with x's type and strides); else
- *               disjoint from the inputs.
+ *               disjoint from the inputs (TRE_E_ARG where an overlap is seen: with
+ *               what is [n], with scores without gaps or in the same strides).
  * A row of no possible word has a gradient of 0, as has one with g, gl and gh of
  * 0, whose scores are not read.  Top words' log probabilities pass no gradient.
  * Asynchronous on the stream; no workspace, so it may be captured into a graph. */

@@ -798,6 +798,61 @@ bool scores_apart(const ScoreLayout& l) {
     }
     return true;
 }
+// Whether [begin, end) meets an element (of so many bytes) of a layout at `at` that scores_apart holds for: its runs of
+// `cols` elements come one after the other, so the last one that begins before `end` reaches farthest.
+bool meets(uintptr_t begin, uintptr_t end, uintptr_t at, const ScoreLayout& l, int bytes) {
+    if (begin >= end || end <= at) return false;
+    int64_t size[2] = {l.n, l.vocab / l.cols}, stride[2] = {l.row_stride * bytes, l.tile_stride * bytes};
+    if (size[1] > 1 && (size[0] <= 1 || stride[1] > stride[0])) {
+        std::swap(size[0], size[1]);
+        std::swap(stride[0], stride[1]);
+    }
+    int64_t left = int64_t(end - 1 - at), run = 0;
+    for (int d = 0; d < 2; d++) {
+        if (size[d] <= 1) continue;
+        const int64_t k = std::min(left / stride[d], size[d] - 1);
+        left -= k * stride[d];
+        run += k * stride[d];
+    }
+    return at + uintptr_t(run) + uintptr_t(l.cols * bytes) > begin;
+}
+// Whether the gradient `o` at `out` surely meets the scores `l` at `x`: where the scores lie without gaps, or both in the
+// same strides.  (Layouts of other kinds that lie between each other are the caller's to keep apart.)
+bool meet(const ScoreLayout& l, uintptr_t x, int x_bytes, const ScoreLayout& o, uintptr_t out, int out_bytes) {
+    int64_t size[2] = {l.n, l.vocab / l.cols}, stride[2] = {l.row_stride * x_bytes, l.tile_stride * x_bytes};
+    const int64_t out_stride[2] = {o.row_stride * out_bytes, o.tile_stride * out_bytes};
+    bool same = true;
+    for (int d = 0; d < 2; d++) same = same && (size[d] <= 1 || stride[d] == out_stride[d]);
+    if (stride[0] > stride[1]) {
+        std::swap(size[0], size[1]);
+        std::swap(stride[0], stride[1]);
+    }
+    int64_t reach = l.cols * x_bytes;
+    bool whole = true;
+    for (int d = 0; d < 2; d++) {
+        if (size[d] <= 1) continue;
+        whole = whole && stride[d] <= reach;
+        reach += stride[d] * (size[d] - 1);
+    }
+    if (whole) return meets(x, x + uintptr_t(reach), out, o, out_bytes);
+    if (!same) return false;
+    // in the same strides a run of the one meets some run of the other if it meets one of those that a whole number of
+    // strides apart lie nearest: the difference of the places, less strides of the larger and then of the smaller
+    const int64_t apart = int64_t(x - out), len_x = l.cols * x_bytes, len_out = l.cols * out_bytes;
+    const int big = size[1] > 1 ? 1 : 0, small = 1 - big;
+    for (int64_t i = -3; i <= 3; i++) {
+        const int64_t a = size[big] > 1 ? apart / stride[big] + i : 0;
+        if (std::abs(a) >= size[big]) continue;
+        const int64_t rest = apart - a * (size[big] > 1 ? stride[big] : 0);
+        for (int64_t j = -3; j <= 3; j++) {
+            const int64_t b = size[small] > 1 ? rest / stride[small] + j : 0;
+            if (std::abs(b) >= size[small]) continue;
+            const int64_t d = rest - b * (size[small] > 1 ? stride[small] : 0);
+            if (d < len_out && d + len_x > 0) return true;
+        }
+    }
+    return false;
+}
 tre_status scores_args(const char* where, const ScoreLayout& l, const void* x, int32_t dtype, const void* ids, int32_t id_bytes,
                        float scale, const int64_t* status) {
     const std::string w(where);
@@ -911,6 +966,19 @@ tre_status tre_log_probs_grad(const void* x, int32_t dtype, int64_t n, int64_t v
     }
     if (grad == x && (out_dtype != dtype || out_row_stride != row_stride || out_tile_stride != tile_stride)) {
         set_error("tre_log_probs_grad: in place the gradient has the scores' type and strides");
+        return TRE_E_ARG;
+    }
+    const uintptr_t to = reinterpret_cast<uintptr_t>(grad);
+    const int out_bytes = out_dtype == TRE_BF16 ? 2 : 4;
+    auto meets_row = [&](const void* p, int64_t bytes) {  // (values of every token)
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        return p && meets(at, at + uintptr_t(n * bytes), to, o, out_bytes);
+    };
+    if ((grad != x && meet(l, reinterpret_cast<uintptr_t>(x), dtype == TRE_BF16 ? 2 : 4, o, to, out_bytes)) || meets_row(stats, 8) ||
+        meets_row(ids, id_bytes) || meets_row(by_log_prob, 4) || meets_row(by_lse, 4) || meets_row(by_entropy, 4) ||
+        (by_entropy && meets_row(entropy, 4)) ||
+        (status && meets(reinterpret_cast<uintptr_t>(status), reinterpret_cast<uintptr_t>(status) + 8, to, o, out_bytes))) {
+        set_error("tre_log_probs_grad: the gradient overlaps an input");
         return TRE_E_ARG;
     }
     const hipError_t e = launch_log_probs_grad(l, x, dtype, stats, ids, id_bytes, scale, by_log_prob, by_lse, by_entropy, entropy,
