@@ -138,22 +138,32 @@ PyObject* views(PyObject*, PyObject* args) try {
     long long n, top;
     int given, entropy;
     if (!PyArg_ParseTuple(args, "OLppL", &x, &n, &given, &entropy, &top)) return nullptr;
+    if (!THPVariable_Check(x)) {
+        PyErr_SetString(PyExc_TypeError, "a tensor wanted");
+        return nullptr;
+    }
     const at::Tensor& flat = THPVariable_Unpack(x);
+    at::Tensor t[6];
     int64_t at = 0;
-    auto part = [&](int64_t row, bool wanted, bool whole = false) -> PyObject* {
-        if (!wanted) Py_RETURN_NONE;
-        at::Tensor t = row ? flat.as_strided({n, row}, {row, 1}, at) : flat.as_strided({n}, {1}, at);
+    auto part = [&](at::Tensor& t, int64_t row) {
+        t = row ? flat.as_strided({n, row}, {row, 1}, at) : flat.as_strided({n}, {1}, at);
         at += n * (row ? row : 1);
-        return THPVariable_Wrap(whole ? t.view(at::kInt) : t);
     };
-    PyObject* r = PyTuple_New(6);
-    if (!r) return nullptr;
-    PyTuple_SET_ITEM(r, 0, part(2, true));
-    PyTuple_SET_ITEM(r, 1, part(0, true));
-    PyTuple_SET_ITEM(r, 2, part(0, given));
-    PyTuple_SET_ITEM(r, 3, part(0, entropy));
-    PyTuple_SET_ITEM(r, 4, part(top, top > 0));
-    PyTuple_SET_ITEM(r, 5, part(top, top > 0, true));
+    part(t[0], 2);
+    part(t[1], 0);
+    if (given) part(t[2], 0);
+    if (entropy) part(t[3], 0);
+    if (top > 0) {
+        part(t[4], top);
+        part(t[5], top);
+        t[5] = t[5].view(at::kInt);
+    }
+    PyObject* r = PyTuple_New(6);  // (None for a tensor that is not there)
+    for (int i = 0; r && i < 6; i++) {
+        PyObject* v = THPVariable_Wrap(t[i]);
+        if (v) PyTuple_SET_ITEM(r, i, v);
+        else Py_CLEAR(r);
+    }
     return r;
 } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
