@@ -281,14 +281,21 @@ __device__ inline void store4(T* at, const float (&v)[kLane], bool cut) {
     store_all<true>(at, v);
 }
 
-// The square root of v c, c >= 1.  The instruction takes what is below 2^-126 for 0,
+// The square roots of v c, c >= 1.  The instruction takes what is below 2^-126 for 0,
 // so small ones are brought up by 2^24 first: a root below 2^-63 would be lost, which
 // is less than half a unit of an eps of 2^-39 or more, and only below that is it
 // looked for (four operations more of an element's 72).
-__device__ inline float root_of(float v, float c, bool small) {
-    if (!small) return __builtin_amdgcn_sqrtf(v * c);
-    const bool low = v < 0x1p-100f;
-    return __builtin_amdgcn_sqrtf((low ? v * 0x1p24f : v) * c) * (low ? 0x1p-12f : 1.f);
+__device__ inline void roots_of(const float (&v)[kLane], float c, bool small, float (&root)[kLane]) {
+    if (!small) {
+#pragma unroll
+        for (int i = 0; i < kLane; i++) root[i] = __builtin_amdgcn_sqrtf(v[i] * c);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kLane; i++) {
+        const bool low = v[i] < 0x1p-100f;
+        root[i] = __builtin_amdgcn_sqrtf((low ? v[i] * 0x1p24f : v[i]) * c) * (low ? 0x1p-12f : 1.f);
+    }
 }
 
 // 4 elements as they come.
@@ -400,8 +407,12 @@ struct Part {
                 mv[i] = mv[i] * b1 + gi * a.nb1;
                 vv[i] = vv[i] * b2 + gi * gi * a.nb2;
             }
-            const float root = root_of(vv[i], r.c2, a.small_roots) + a.eps;
-            pv[i] = value4(h.p, i) * r.decay + rate * mv[i] * __builtin_amdgcn_rcpf(root);
+        }
+        float root[kLane];
+        roots_of(vv, r.c2, a.small_roots, root);
+#pragma unroll
+        for (int i = 0; i < kLane; i++) {
+            pv[i] = value4(h.p, i) * r.decay + rate * mv[i] * __builtin_amdgcn_rcpf(root[i] + a.eps);
             if constexpr (CHANCE && sizeof(TP) == 2) {
                 const float up = __uint_as_float((__float_as_uint(pv[i]) + c[i].weight()) & 0xffff0000u);
                 pv[i] = pv[i] == pv[i] ? up : __builtin_nanf("");
