@@ -10,11 +10,12 @@
 // log s are kept apart for the gradient for the same reason: a probability out of
 // lse alone is off by 2^-24 |lse|.
 //
-// Memory bounds large calls: 8192 x 32768 bf16 scores with entropy take 102 us
-// (5.3 TB/s; 11 vector operations a score, 81 us of the vector units' time), their
-// gradient in bf16 194 us (5.3 TB/s read and written).  Of 2048 x 32768 with 8 top
-// words, 35 us, the words are 11.  A lane's four loads of 16 bytes are in flight
-// together: with each waited for the first took 113 us.
+// Memory bounds large calls: 8192 x 32768 bf16 scores with entropy take 98 us
+// (5.5 TB/s; 10 vector operations a score, 77 us of the vector units' time), their
+// gradient in bf16 196 us (5.2 TB/s read and written; 17 operations).  2048 x 32768
+// take 24 us, with 8 top words 38 (17 operations, 31 us of the units' time).  A
+// lane's four loads of 16 bytes are in flight together: with each waited for the
+// first took 113 us.
 #include "tre_internal.h"
 #include "values.h"
 
@@ -302,7 +303,6 @@ __device__ inline const T* score_at(const ProbArgs& a, int64_t row, int64_t word
 }
 
 // A token's given word.
-template <typename T>
 __device__ inline int64_t given_word(const ProbArgs& a, int64_t row) {
     return a.log_prob ? token(a.ids, a.id_bytes, row) : -1;
 }
@@ -402,7 +402,7 @@ __global__ __launch_bounds__(W > 1 ? W * 64 : kThreads) void k_probs(ProbArgs a)
     const T* x = static_cast<const T*>(a.x) + row * a.g.row_stride;
     // the given word, and its score when the row's first loads are on their way
     Given<T> given{};
-    const int64_t word = (W == 1 || wave == 0) && a.splits == 1 ? given_word<T>(a, row) : -1;
+    const int64_t word = (W == 1 || wave == 0) && a.splits == 1 ? given_word(a, row) : -1;
     Sums u{-FLT_MAX, 0.f, 0.f};
     Top top;
     uint32_t known = 0;
@@ -574,7 +574,7 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
     const int lane = threadIdx.x;
     const int64_t row = block_index();
     if (row >= a.g.n) return;
-    const int64_t word = given_word<T>(a, row);
+    const int64_t word = given_word(a, row);
     Sums u = lane < int(a.splits) ? a.part[row * a.splits + lane] : Sums{-FLT_MAX, 0.f, 0.f};
     join_lanes<1, 32, true>(u, a.scale2);
     u = first_lane(u);
@@ -604,13 +604,27 @@ __global__ __launch_bounds__(64) void k_probs_join(ProbArgs a) {
 
 // A row of few scores is one wavefront's, one of many four wavefronts'.  Many rows
 // fill the device with a wavefront each, and four that wait for each other at a
-// row's top words take longer: one and four take, for 20000 bf16 scores (2500 runs)
-// with 8 top words, 18 and 13 us for 600 rows, 25 and 27 for 2048, 69 and 94 for
-// 8192 (without top words 9, 7; 15, 16; 55, 57).  With 32768 (4096 runs) 36 and 34
-// us for 2048 rows, 113 and 115 for 8192.  Few rows
-// have sixteen wavefronts each, which is one launch where a row cut into parts is
-// two (one row of 32768 with 20 top words 10.4 us, in 8 parts of four wavefronts
-// 13), and are cut where that still leaves long rows to few workgroups.
+// row's top words take longer: one and four take, a call in a graph, for 20000 bf16
+// scores (2500 runs) with 8 top words, 20 and 14 us for 600 rows, 25 and 26 for 2048,
+// 69 and 88 for 8192 (without top words 11, 8; 15, 16; 59, 58).  With 32768 (4096
+// runs) 36 and 33 us for 2048 rows, 108 and 115 for 8192.
+//
+// Few rows have sixteen wavefronts each: with them and with four, 128 rows of 8192
+// fp32 runs take 11 and 16 us with 8 top words, 5.3 and 6.4 without, 256 rows 13 and
+// 18, 8.0 and 8.4.  From one row to a unit on four do better: 400 rows take 21 and 18,
+// 11.0 and 10.2, 512 rows 22 and 20, 12.6 and 12.2 (of 4096 runs 18 and 13, 8.3 and
+// 7.8), 513 rows 26 and 20, 13.9 and 12.3.
+//
+// One launch is less than the two of a row cut into parts, so these are cut only
+// where that leaves long rows to few workgroups.  13 rows uncut and cut, with 8 top
+// words and without: 12664 runs 12.2, 12.3 and 5.8, 6.1 us in fp32, 15.5, 13.1 and
+// 8.2, 6.8 in bf16, whose runs have twice the scores; 16384 runs 13.5, 12.1 and 6.4,
+// 6.2, in bf16 17.6, 13.2 and 9.3, 7.0; 65536 runs 35, 15 and 17, 6.5, in bf16 50, 17
+// and 29, 8.4.  Up to 256 parts in all: 32 rows of 65536 runs take 17.5 us in 8 parts
+// each, 24 in 16 and 20 in 4, 128 rows 31 in 2, 36 in 4 and 37 uncut (without top
+// words 24 in 2 and 22 uncut), 200 rows 56 in 2 and 44 uncut.  Up to 32 a row: one of
+// 131072 runs takes 15.3 us in 32, 15.0 in 16 and 17.8 in 8, without top words 5.7,
+// 6.6 and 8.4.
 constexpr int64_t kWaveRuns = 4 * 64 * kRuns;    // up to so many runs
 constexpr int64_t kManyRows = 2048;              // from so many rows
 constexpr int64_t kManyRuns = 14 * 64 * kRuns;   // up to so many runs

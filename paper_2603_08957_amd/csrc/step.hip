@@ -4,10 +4,10 @@
 // Tensors of all sizes share a launch: its arguments hold their places and the
 // number of the first workgroup of each, so that nothing is kept on the device
 // between calls and a captured call holds what it was given.  Memory bounds both:
-// 134 M fp32 weights, gradients and moments take 679 us (5.5 TB/s), 67 M weights in
-// fp32 with bf16 gradients and 8-bit moments 176 (5.4), the norm of 400 M bf16
-// gradients 141 (5.7).  Rounded by chance, 67 M weights in bf16 take 170 us, of
-// which the vector units work 120 (70 operations an element, 15 of them the hash).
+// 134 M fp32 weights, gradients and moments take 675 us (5.6 TB/s), 67 M weights in
+// fp32 with bf16 gradients and 8-bit moments 182 (5.2), the norm of 400 M bf16
+// gradients 143 (5.6).  Rounded by chance, 67 M weights in bf16 take 174 us and more,
+// of which the vector units work 130 (73 operations an element, 15 of them the hash).
 #include "codes.h"
 #include "tre_internal.h"
 #include "values.h"
@@ -284,7 +284,7 @@ __device__ inline void store4(T* at, const float (&v)[kLane], bool cut) {
 // The square roots of v c, c >= 1.  The instruction takes what is below 2^-126 for 0,
 // so small ones are brought up by 2^24 first: a root below 2^-63 would be lost, which
 // is less than half a unit of an eps of 2^-39 or more, and only below that is it
-// looked for (four operations more of an element's 72).
+// looked for (four operations more of an element's 73).
 __device__ inline void roots_of(const float (&v)[kLane], float c, bool small, float (&root)[kLane]) {
     if (!small) {
 #pragma unroll

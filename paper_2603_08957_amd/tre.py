@@ -722,7 +722,9 @@ def _floats(t, where, what, n, row, gpu, device):
 
 @dataclass
 class LogProbs:
-    """What `log_probs` gives, in float32: of each token..."""  # (views of one allocation)
+    """What `log_probs` gives of each token, in float32: views of one allocation.
+    They share its memory, which one that is kept keeps whole, and torch's count of
+    writes, so that writing one counts for all: clone what is kept long or written."""
     log_prob: object        # [n]: its given word's, or None
     lse: object             # [n]: log of the sum of e^(scale x)
     stats: object           # [n, 2]: what log_probs_grad takes
